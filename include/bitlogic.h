@@ -425,6 +425,97 @@ int bitlogic_network_forward_noalloc(const bitlogic_network *net, const uint8_t 
                                      int64_t n_samples, int32_t *out, int32_t *argmax,
                                      void *stream);
 
+/* ---- Rows of class scores or logits -------------------------------------
+ * What follows the head: a network's int32 scores, or logits of a trained head
+ * or another model, [n_rows][n_classes] with row_stride elements from row to row
+ * (>= 0; 0 reads one row for all).  Element types:                             */
+enum {
+    BITLOGIC_LOGITS_I32 = 0,   /* int32 scores; the lowest integer is masked      */
+    BITLOGIC_LOGITS_F32 = 1,   /* float types: -inf is masked                     */
+    BITLOGIC_LOGITS_F16 = 2,
+    BITLOGIC_LOGITS_BF16 = 3
+};
+/* A row's order is descending logit, then ascending class.  Softmax statistics,
+ * sums and losses are held in 32 bits whatever the type; results do not depend on
+ * how a launch is scheduled.  Buffers need their elements' natural alignment only.
+ * Limits: 1 <= n_classes <= 2^30, 0 <= n_rows < 2^31 (0 enqueues nothing, with any
+ * pointers), 1 <= k <= BITLOGIC_TOP_MAX, temperatures positive and finite
+ * (BITLOGIC_ERR_SHAPE; an unknown type or a larger k: BITLOGIC_ERR_UNSUPPORTED). */
+#define BITLOGIC_TOP_MAX 1024
+
+/* The k largest logits of every row and the row's log-normalizer: what a teacher
+ * hands on for bitlogic_distill.
+ *   values    [n_rows][k] of the logits' type, in the row's order
+ *   indices   int32 [n_rows][k], their classes
+ *   log_norm  float [n_rows] or NULL: log sum_i e^(l_i / temperature)
+ * Masked classes and NaNs have no place in the order and no mass; places past the
+ * others get class -1 and the masked value, and a row without any class log_norm
+ * -inf (with a +inf logit: +inf). */
+int bitlogic_top_logits(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
+                        int64_t row_stride, int32_t k, float temperature, void *values,
+                        int32_t *indices, float *log_norm, void *stream);
+
+/* Distillation loss of every row against a teacher's top logits, and its gradient.
+ * The teacher's list J of row s: top_values [n_rows][k] (of top_type) at the classes
+ * top_indices [n_rows][k], distinct within a row; an index outside [0, n_classes)
+ * marks an empty place.  With z the row's logits, p = softmax(z / temperature),
+ * q_j = exp(top_values_j / top_temperature - norm) and w = row_weight[s] (NULL: 1):
+ *   loss[s]  = w * (sum_J q_j (log q_j - log p_j) + q_r (log q_r - log p_r))
+ *   grad     = d loss[s] / d z
+ * top_log_norm float [n_rows] is the teacher's log-normalizer at top_temperature
+ * (bitlogic_top_logits' log_norm): norm = top_log_norm[s], and the rest of the
+ * classes counts as one, q_r = max(0, 1 - sum_J q_j) against the student's mass p_r
+ * outside J.  NULL: norm is J's own log-normalizer and q_r = 0.
+ *   loss  float [n_rows] or NULL;  grad of `type`, grad_stride >= n_classes elements
+ *   from row to row, or NULL (not both NULL); with int32 scores grad must be NULL
+ *   (BITLOGIC_ERR_UNSUPPORTED)
+ * grad may not overlap logits.  The loss alone is the forward pass; the gradient
+ * alone, with row_weight the gradient of a sum over the losses, the backward pass;
+ * both together read the logits once.  A row of weight 0 is not read and gets zeros,
+ * a row whose list is empty loss and gradient 0; a row whose logits are all -inf,
+ * or that holds a NaN, NaNs.  Classes with p = 0 get gradient 0 outside J. */
+int bitlogic_distill(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
+                     int64_t row_stride, float temperature, const void *top_values,
+                     int32_t top_type, const int32_t *top_indices, int32_t k,
+                     const float *top_log_norm, float top_temperature,
+                     const float *row_weight, float *loss, void *grad, int64_t grad_stride,
+                     void *stream);
+
+/* How bitlogic_sample draws.  Each parameter is one value for all rows or, where its
+ * array (device memory) is not NULL, a value per row. */
+typedef struct bitlogic_sampling {
+    float temperature;              /* T; 0: greedy, the first class of the order   */
+    int32_t top_k;                  /* the first k classes; 0: all                   */
+    float top_p;                    /* 1: all                                        */
+    float min_p;                    /* 0: all                                        */
+    const float *temperatures;      /* [n_rows] or NULL; values <= 0 are greedy      */
+    const int32_t *top_ks;          /* [n_rows] or NULL; values <= 0 keep all        */
+    const float *top_ps;            /* [n_rows] or NULL                              */
+    const float *min_ps;            /* [n_rows] or NULL                              */
+} bitlogic_sampling;
+
+/* A class per row, drawn with given random numbers.  With m the row's largest logit,
+ * x_i = (l_i - m) * (1 / T) (0 where l_i = m) and w_i = e^x_i, in 32-bit arithmetic:
+ *   top-k  keeps the first k classes of the row's order;
+ *   top-p  of those, the ones before which the sum of w is below top_p times the
+ *          sum over them all (top_p >= 1: every one; the first one always);
+ *   min-p  of those, the ones with x_i >= log(min_p) (the first one always);
+ * and token[s] is the kept class with the largest x_i + noise[s][i], the lowest one
+ * of equals; where no sum is above -inf, the first of the order.  With independent
+ * standard Gumbel numbers -log(-log u), u uniform in (0, 1), class i is drawn with
+ * probability w_i over the sum of the kept w.
+ *   noise     float [n_rows][n_classes], noise_stride >= 0 elements from row to row;
+ *             NULL only if every row is greedy (temperatures NULL, temperature 0).
+ *             Numbers of classes that are not kept need not be finite.
+ *   token     int32 [n_rows]; -1 for a row whose classes are all masked or NaN
+ *   log_prob  float [n_rows] or NULL: x_token - log of the sum of the kept w (0 for
+ *             a greedy row, -inf for token -1)
+ * Masked classes and NaNs are never kept. */
+int bitlogic_sample(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
+                    int64_t row_stride, const float *noise, int64_t noise_stride,
+                    const bitlogic_sampling *sampling, int32_t *token, float *log_prob,
+                    void *stream);
+
 /* ---- Peak probes (measurement, not part of the inference path) ---------- */
 
 /* Integer VALU probe: `blocks` blocks of 256 lanes.  Lane l (global index)
@@ -523,8 +614,9 @@ const char *bitlogic_last_error(void);
  * fused_network member (the whole-network kernel was removed), and the
  * instruction-rate and gather probes; 0.7.0 bitlogic_forward_info.jump_layers
  * and the node-per-wave layer kernel, whose per-node records enlarge the
- * forward workspace of networks that use it; 0.8.0 bitlogic_network_path). */
-#define BITLOGIC_VERSION 800
+ * forward workspace of networks that use it; 0.8.0 bitlogic_network_path; 0.9.0
+ * bitlogic_top_logits, bitlogic_distill and bitlogic_sample). */
+#define BITLOGIC_VERSION 900
 int bitlogic_version(void);
 
 #ifdef __cplusplus

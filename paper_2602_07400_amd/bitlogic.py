@@ -26,6 +26,7 @@ __all__ = [
     "bitlogic_encode_binary", "bitlogic_fit_quantile_thresholds", "bitlogic_network_forward",
     "bitlogic_network_forward_noalloc", "NOALLOC_SCRATCH_BYTES",
     "bitlogic_groupsum_head_workspace_bytes", "bitlogic_status_string", "bitlogic_version",
+    "bitlogic_top_logits", "bitlogic_distill", "bitlogic_distill_loss", "bitlogic_sample",
     "BitlogicModel", "bitlogic_specialize_layer", "bitlogic_specialize_network", "library_path",
     "load_library", "words",
 ]
@@ -66,6 +67,13 @@ class _Network(ctypes.Structure):
                 ("head_weights", ctypes.c_void_p), ("pass_fanin", ctypes.c_void_p)]
 
 
+class _Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p),
+                ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p)]
+
+
 _PATHS = ("slab", "columns", "block")      # BITLOGIC_PATH_*
 MAX_FANIN = 6
 SPECIALIZE_PASS = 32          # nodes per entry of a specialized layer's fan-in array
@@ -86,6 +94,7 @@ def load_library():
             "(hipcc --offload-arch=gfx950); there is no fallback path")
     lib = ctypes.CDLL(_LIB_PATH)
     P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    f32 = ctypes.c_float
     sig = {
         "bitlogic_encode": ([P, i64, i32, P, i32, P, P], ctypes.c_int),
         "bitlogic_lut_layer": ([P, i32, i64, P, P, i32, i32, P, P], ctypes.c_int),
@@ -110,6 +119,10 @@ def load_library():
         "bitlogic_specialize_layer": ([P, P, i32, i32, i32, P, P, P], ctypes.c_int),
         "bitlogic_specialize_network": ([i32, P, P, P, P, i32, i32, ctypes.c_double, P, P, P,
                                          P, P, P], ctypes.c_int),
+        "bitlogic_top_logits": ([P, i32, i64, i32, i64, i32, f32, P, P, P, P], ctypes.c_int),
+        "bitlogic_distill": ([P, i32, i64, i32, i64, f32, P, i32, P, i32, P, f32, P, P, P, i64,
+                              P], ctypes.c_int),
+        "bitlogic_sample": ([P, i32, i64, i32, i64, P, i64, P, P, P, P], ctypes.c_int),
         "bitlogic_probe_valu": ([P, i32, i32, ctypes.c_uint32, P], ctypes.c_int),
         "bitlogic_probe_hbm": ([i32, P, P, i64, i32, i32, P], ctypes.c_int),
         "bitlogic_probe_valu_op": ([i32, P, i32, i32, ctypes.c_uint32, P], ctypes.c_int),
@@ -666,6 +679,179 @@ def bitlogic_network_forward_noalloc(model: BitlogicModel, x: torch.Tensor, out:
         _dev(out, "out", _I32) if out is not None else None,
         _dev(argmax, "argmax", _I32) if argmax is not None else None, _stream(stream, x.device)))
     return out, argmax
+
+
+# ------------------------------------------- rows of class scores or logits
+
+TOP_MAX = 1024                        # BITLOGIC_TOP_MAX
+_F32 = (torch.float32,)
+_LOGITS = {torch.int32: 0, torch.float32: 1, torch.float16: 2, torch.bfloat16: 3}
+
+
+def _rows(t: torch.Tensor, name: str, dtypes=_LOGITS) -> Tuple[int, int]:
+    """Address and row stride of a 2-D tensor on the GPU whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {tuple(dtypes)}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D")
+    stride, step = t.stride()
+    if step != 1 and t.shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), stride if t.shape[0] > 1 else t.shape[1]
+
+
+def _like(t: torch.Tensor, name: str, dtypes, shape, device) -> int:
+    """Address of a contiguous tensor of the given shape on the given device."""
+    p = _dev(t, name, dtypes)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    return p
+
+
+def bitlogic_top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0,
+                        values: Optional[torch.Tensor] = None,
+                        indices: Optional[torch.Tensor] = None,
+                        log_norm: Optional[torch.Tensor] = None, stream=None,
+                        want_log_norm: bool = True):
+    """The k largest logits of every row of logits [N][c] (int32, float32, float16 or
+    bfloat16; rows may be strided): (values [N][k], indices int32 [N][k], log_norm
+    float32 [N] or None), in descending order, equal logits by class; log_norm is
+    log sum exp(logits / temperature)."""
+    ptr, stride = _rows(logits, "logits")
+    n, c = logits.shape
+    dev, dtype = logits.device, logits.dtype
+    if values is None:
+        values = _empty((n, k), dtype, dev, stream)
+    if indices is None:
+        indices = _empty((n, k), torch.int32, dev, stream)
+    if log_norm is None and want_log_norm:
+        log_norm = _empty((n,), torch.float32, dev, stream)
+    _check(load_library().bitlogic_top_logits(
+        ptr, _LOGITS[dtype], n, c, stride, k, temperature,
+        _like(values, "values", (dtype,), (n, k), dev),
+        _like(indices, "indices", _I32, (n, k), dev),
+        _like(log_norm, "log_norm", _F32, (n,), dev) if log_norm is not None else None,
+        _stream(stream, dev)))
+    return values, indices, log_norm
+
+
+def bitlogic_distill(logits: torch.Tensor, top_values: torch.Tensor, top_indices: torch.Tensor,
+                     top_log_norm: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                     top_temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None,
+                     loss: Optional[torch.Tensor] = None, grad: Optional[torch.Tensor] = None,
+                     stream=None, want_loss: bool = True, want_grad: bool = True):
+    """Distillation of a student's logits [N][c] against a teacher's top logits
+    (bitlogic_top_logits' values [N][k], indices [N][k] and, to count the mass outside
+    the list, log_norm [N]): (loss float32 [N] or None, grad [N][c] or None), both
+    times row_weight [N].  Int32 scores have a loss only (want_grad=False)."""
+    ptr, stride = _rows(logits, "logits")
+    n, c = logits.shape
+    dev, dtype = logits.device, logits.dtype
+    if top_values.dim() != 2:
+        raise ValueError("top_values must be [N][k]")
+    shape = (n, top_values.shape[1])
+    if loss is None and want_loss:
+        loss = _empty((n,), torch.float32, dev, stream)
+    if grad is None and want_grad:
+        grad = _empty((n, c), dtype, dev, stream)
+    grad_ptr, grad_stride = None, 0
+    if grad is not None:
+        grad_ptr, grad_stride = _rows(grad, "grad", (dtype,))
+        if grad.shape != logits.shape or grad.device != dev:
+            raise ValueError("grad must have the logits' shape and device")
+    _check(load_library().bitlogic_distill(
+        ptr, _LOGITS[dtype], n, c, stride, temperature,
+        _like(top_values, "top_values", _LOGITS, shape, dev), _LOGITS[top_values.dtype],
+        _like(top_indices, "top_indices", _I32, shape, dev), shape[1],
+        _like(top_log_norm, "top_log_norm", _F32, (n,), dev) if top_log_norm is not None
+        else None, top_temperature,
+        _like(row_weight, "row_weight", _F32, (n,), dev) if row_weight is not None else None,
+        _like(loss, "loss", _F32, (n,), dev) if loss is not None else None,
+        grad_ptr, grad_stride, _stream(stream, dev)))
+    return loss, grad
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, top_values, top_indices, top_log_norm, temperature,
+                top_temperature):
+        ctx.save_for_backward(logits, top_values, top_indices, top_log_norm)
+        ctx.temperatures = temperature, top_temperature
+        return bitlogic_distill(logits, top_values, top_indices, top_log_norm, temperature,
+                                top_temperature, want_grad=False)[0]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        logits, top_values, top_indices, top_log_norm = ctx.saved_tensors
+        grad = bitlogic_distill(logits, top_values, top_indices, top_log_norm,
+                                *ctx.temperatures, row_weight=grad_loss.contiguous(),
+                                want_loss=False)[1]
+        return grad, None, None, None, None, None
+
+
+def bitlogic_distill_loss(logits: torch.Tensor, top_values: torch.Tensor,
+                          top_indices: torch.Tensor,
+                          top_log_norm: Optional[torch.Tensor] = None,
+                          temperature: float = 1.0,
+                          top_temperature: float = 1.0) -> torch.Tensor:
+    """bitlogic_distill as a differentiable function: loss float32 [N] whose backward
+    pass gives the gradient with respect to logits (the teacher's side has none).  Both
+    passes run on the current stream."""
+    return _DistillLoss.apply(logits, top_values, top_indices, top_log_norm, temperature,
+                              top_temperature)
+
+
+def bitlogic_sample(logits: torch.Tensor, noise: Optional[torch.Tensor] = None,
+                    temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                    token: Optional[torch.Tensor] = None,
+                    log_prob: Optional[torch.Tensor] = None, stream=None,
+                    want_log_prob: bool = True):
+    """A class per row of logits [N][c], drawn with standard Gumbel numbers noise
+    float32 [N][c] (-log(-log u)): (token int32 [N], log_prob float32 [N] or None).
+    temperature (0: greedy, then noise may be None), top_k (0: all), top_p and min_p
+    are numbers or tensors [N] on the GPU (float32; top_k int32) with a value per row."""
+    ptr, stride = _rows(logits, "logits")
+    n, c = logits.shape
+    dev, dtype = logits.device, logits.dtype
+    sp = _Sampling(1.0, 0, 1.0, 0.0, None, None, None, None)
+    if isinstance(temperature, torch.Tensor):
+        sp.temperatures = _like(temperature, "temperature", _F32, (n,), dev)
+    else:
+        sp.temperature = temperature
+    if isinstance(top_k, torch.Tensor):
+        sp.top_ks = _like(top_k, "top_k", _I32, (n,), dev)
+    else:
+        sp.top_k = top_k
+    if isinstance(top_p, torch.Tensor):
+        sp.top_ps = _like(top_p, "top_p", _F32, (n,), dev)
+    else:
+        sp.top_p = top_p
+    if isinstance(min_p, torch.Tensor):
+        sp.min_ps = _like(min_p, "min_p", _F32, (n,), dev)
+    else:
+        sp.min_p = min_p
+    noise_ptr, noise_stride = None, 0
+    if noise is not None:
+        noise_ptr, noise_stride = _rows(noise, "noise", _F32)
+        if noise.shape != logits.shape or noise.device != dev:
+            raise ValueError("noise must have the logits' shape and device")
+    if token is None:
+        token = _empty((n,), torch.int32, dev, stream)
+    if log_prob is None and want_log_prob:
+        log_prob = _empty((n,), torch.float32, dev, stream)
+    _check(load_library().bitlogic_sample(
+        ptr, _LOGITS[dtype], n, c, stride, noise_ptr, noise_stride, ctypes.addressof(sp),
+        _like(token, "token", _I32, (n,), dev),
+        _like(log_prob, "log_prob", _F32, (n,), dev) if log_prob is not None else None,
+        _stream(stream, dev)))
+    return token, log_prob
 
 
 # ---------------------------------------------------------------- peak probes

@@ -1,6 +1,7 @@
 // C-ABI front end of libbitlogic: argument checks on the host, workspace
 // carving, launches.  Every check runs before any HIP runtime call, so a
 // rejected call enqueues nothing (and needs no GPU to be rejected).
+#include <float.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -11,6 +12,7 @@
 
 #include "bitlogic.h"
 #include "bl_internal.h"
+#include "logit_rows.h"
 
 // Scratch of bitlogic_network_forward_noalloc: one copy of this array per GPU
 // the library runs on, held until the process ends.  In host code `scratch`
@@ -102,6 +104,39 @@ int check_head(const uint64_t *bits, int32_t w, int64_t n, int32_t c, const int3
         return fail(BITLOGIC_ERR_SHAPE, "head: n_samples too large");
     if (!aligned(bits, 8) || (scores && !aligned(scores, 4)) || (argmax && !aligned(argmax, 4)))
         return fail(BITLOGIC_ERR_ALIGN, "head: misaligned buffer");
+    return BITLOGIC_OK;
+}
+
+// Rows of class scores or logits: type, sizes and stride.
+constexpr int64_t kMaxStride = 1 << 30;
+
+size_t logit_bytes(int32_t type)
+{
+    return type == BITLOGIC_LOGITS_I32 || type == BITLOGIC_LOGITS_F32 ? 4 : 2;
+}
+
+int check_rows(const char *who, int32_t type, int64_t n_rows, int32_t n_classes,
+               int64_t row_stride)
+{
+    if (type < BITLOGIC_LOGITS_I32 || type > BITLOGIC_LOGITS_BF16)
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "%s: unknown element type %d", who, type);
+    if (n_rows < 0 || n_rows > kMaxRows || n_classes < 1 || n_classes > bl::rows::kMaxClasses)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: need 0 <= n_rows < 2^31, 1 <= n_classes <= 2^30",
+                    who);
+    if (row_stride < 0 || row_stride > kMaxStride)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: need 0 <= row_stride <= 2^30", who);
+    return BITLOGIC_OK;
+}
+
+int check_list(const char *who, int32_t k, float temperature)
+{
+    if (k < 1)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: need k >= 1", who);
+    if (k > BITLOGIC_TOP_MAX)
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "%s: k=%d > %d", who, k, BITLOGIC_TOP_MAX);
+    if (!(temperature > 0.0f && temperature <= FLT_MAX))
+        return fail(BITLOGIC_ERR_SHAPE, "%s: temperature %g is not positive and finite", who,
+                    (double)temperature);
     return BITLOGIC_OK;
 }
 
@@ -897,6 +932,104 @@ const char *bitlogic_status_string(int status)
 const char *bitlogic_last_error(void) { return g_last_error; }
 
 int bitlogic_version(void) { return BITLOGIC_VERSION; }
+
+// ---- rows of class scores or logits ----
+
+static_assert(bl::rows::kI32 == BITLOGIC_LOGITS_I32 && bl::rows::kF32 == BITLOGIC_LOGITS_F32 &&
+              bl::rows::kF16 == BITLOGIC_LOGITS_F16 && bl::rows::kBf16 == BITLOGIC_LOGITS_BF16,
+              "the kernels' element types are the interface's");
+
+int bitlogic_top_logits(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
+                        int64_t row_stride, int32_t k, float temperature, void *values,
+                        int32_t *indices, float *log_norm, void *stream)
+{
+    if (int rc = check_rows("top_logits", type, n_rows, n_classes, row_stride))
+        return rc;
+    if (int rc = check_list("top_logits", k, temperature))
+        return rc;
+    if (n_rows == 0)
+        return ok();
+    if (!logits || !values || !indices)
+        return fail(BITLOGIC_ERR_NULL, "top_logits: NULL pointer");
+    if (!aligned(logits, logit_bytes(type)) || !aligned(values, logit_bytes(type)) ||
+        !aligned(indices, 4) || !aligned(log_norm, 4))
+        return fail(BITLOGIC_ERR_ALIGN, "top_logits: misaligned buffer");
+    return hip_status(bl::launch_top_logits(logits, type, n_rows, n_classes, row_stride, k,
+                                            1.0f / temperature, values, indices, log_norm,
+                                            (hipStream_t)stream),
+                      "top_logits launch");
+}
+
+int bitlogic_distill(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
+                     int64_t row_stride, float temperature, const void *top_values,
+                     int32_t top_type, const int32_t *top_indices, int32_t k,
+                     const float *top_log_norm, float top_temperature,
+                     const float *row_weight, float *loss, void *grad, int64_t grad_stride,
+                     void *stream)
+{
+    if (int rc = check_rows("distill", type, n_rows, n_classes, row_stride))
+        return rc;
+    if (int rc = check_rows("distill", top_type, n_rows, n_classes, 0))
+        return rc;
+    if (int rc = check_list("distill", k, temperature))
+        return rc;
+    if (int rc = check_list("distill", k, top_temperature))
+        return rc;
+    if (grad && type == BITLOGIC_LOGITS_I32)
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "distill: int32 scores have no gradient");
+    if (grad && (grad_stride < n_classes || grad_stride > kMaxStride))
+        return fail(BITLOGIC_ERR_SHAPE, "distill: need n_classes <= grad_stride <= 2^30");
+    if (n_rows == 0)
+        return ok();
+    if (!logits || !top_values || !top_indices || (!loss && !grad))
+        return fail(BITLOGIC_ERR_NULL, "distill: NULL input, or both outputs NULL");
+    if (!aligned(logits, logit_bytes(type)) || !aligned(grad, logit_bytes(type)) ||
+        !aligned(top_values, logit_bytes(top_type)) || !aligned(top_indices, 4) ||
+        !aligned(top_log_norm, 4) || !aligned(row_weight, 4) || !aligned(loss, 4))
+        return fail(BITLOGIC_ERR_ALIGN, "distill: misaligned buffer");
+    return hip_status(bl::launch_distill(logits, type, n_rows, n_classes, row_stride,
+                                         1.0f / temperature, top_values, top_type, top_indices,
+                                         k, top_log_norm, 1.0f / top_temperature, row_weight,
+                                         loss, grad, grad_stride, (hipStream_t)stream),
+                      "distill launch");
+}
+
+int bitlogic_sample(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
+                    int64_t row_stride, const float *noise, int64_t noise_stride,
+                    const bitlogic_sampling *sampling, int32_t *token, float *log_prob,
+                    void *stream)
+{
+    if (int rc = check_rows("sample", type, n_rows, n_classes, row_stride))
+        return rc;
+    if (!sampling)
+        return fail(BITLOGIC_ERR_NULL, "sample: NULL sampling parameters");
+    if (noise_stride < 0 || noise_stride > kMaxStride)
+        return fail(BITLOGIC_ERR_SHAPE, "sample: need 0 <= noise_stride <= 2^30");
+    const bitlogic_sampling &s = *sampling;
+    if (!s.temperatures && !(s.temperature >= 0.0f && s.temperature <= FLT_MAX))
+        return fail(BITLOGIC_ERR_SHAPE, "sample: temperature %g is not in [0, inf)",
+                    (double)s.temperature);
+    if (!s.top_ks && s.top_k < 0)
+        return fail(BITLOGIC_ERR_SHAPE, "sample: top_k %d < 0", s.top_k);
+    if (!s.top_ps && !(s.top_p >= 0.0f && s.top_p <= 1.0f))
+        return fail(BITLOGIC_ERR_SHAPE, "sample: top_p %g is not in [0, 1]", (double)s.top_p);
+    if (!s.min_ps && !(s.min_p >= 0.0f && s.min_p <= 1.0f))
+        return fail(BITLOGIC_ERR_SHAPE, "sample: min_p %g is not in [0, 1]", (double)s.min_p);
+    if (n_rows == 0)
+        return ok();
+    const bool greedy = !s.temperatures && s.temperature == 0.0f;
+    if (!logits || !token || (!noise && !greedy))
+        return fail(BITLOGIC_ERR_NULL, "sample: NULL pointer");
+    if (!aligned(logits, logit_bytes(type)) || !aligned(noise, 4) || !aligned(token, 4) ||
+        !aligned(log_prob, 4) || !aligned(s.temperatures, 4) || !aligned(s.top_ks, 4) ||
+        !aligned(s.top_ps, 4) || !aligned(s.min_ps, 4))
+        return fail(BITLOGIC_ERR_ALIGN, "sample: misaligned buffer");
+    const bl::SampleParams sp = {s.temperature, s.top_p, s.min_p, s.top_k,
+                                 s.temperatures, s.top_ps, s.min_ps, s.top_ks};
+    return hip_status(bl::launch_sample(logits, type, n_rows, n_classes, row_stride, noise,
+                                        noise_stride, sp, token, log_prob, (hipStream_t)stream),
+                      "sample launch");
+}
 
 int bitlogic_probe_valu(uint32_t *out, int32_t blocks, int32_t iters, uint32_t seed,
                         void *stream)

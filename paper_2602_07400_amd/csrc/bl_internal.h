@@ -242,6 +242,27 @@ hipError_t launch_column_head(const uint64_t *in, int32_t w_in, const int32_t *c
                               int64_t n, const ColumnHeadPlan &hp, int32_t *counts,
                               int32_t *argmax, const uint8_t *fanin, hipStream_t stream);
 
+// Rows of class scores or logits (logit_rows.h).  type: BITLOGIC_LOGITS_*; strides
+// in elements from row to row.
+hipError_t launch_top_logits(const void *logits, int32_t type, int64_t n_rows, int32_t n,
+                             int64_t row_stride, int32_t k, float inv_t, void *values,
+                             int32_t *indices, float *log_norm, hipStream_t stream);
+hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int32_t n,
+                          int64_t row_stride, float inv_t, const void *top_values,
+                          int32_t top_type, const int32_t *top_indices, int32_t k,
+                          const float *top_log_norm, float inv_top_t, const float *row_weight,
+                          float *loss, void *grad, int64_t grad_stride, hipStream_t stream);
+struct SampleParams {                  // a row's value where its array is given
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    const float *temperatures, *top_ps, *min_ps;
+    const int32_t *top_ks;
+};
+hipError_t launch_sample(const void *logits, int32_t type, int64_t n_rows, int32_t n,
+                         int64_t row_stride, const float *noise, int64_t noise_stride,
+                         const SampleParams &sp, int32_t *token, float *log_prob,
+                         hipStream_t stream);
+
 // Peak probes (probes.hip): kProbeThreads = 256 lanes a block.
 hipError_t launch_probe_valu(uint32_t *out, int32_t blocks, int32_t iters, uint32_t seed,
                              hipStream_t stream);

@@ -1,0 +1,270 @@
+// Distillation from a teacher's top logits, loss and gradient.
+//
+// A row has the student's logits z and a list J of distinct classes with the
+// teacher's logits t.  With p = softmax(z / Ts), q_j = e^(t_j / Tt - log_norm) and a
+// row weight w,
+//
+//   loss    = w [ sum_J q_j (log q_j - log p_j)  +  q_r (log q_r - log p_r) ]
+//   dl/dz_i = w / Ts [ (Q + q_r) p_i - q_i ]               i in J
+//           = w / Ts   (Q + q_r - q_r / p_r) p_i           elsewhere
+//
+// where Q = sum_J q_j.  With the teacher's log_norm given, the rest counts as one
+// more class: q_r = max(0, 1 - Q), p_r = the student's mass outside J, summed over
+// those classes themselves (1 - sum_J p_j would cancel).  Without it, log_norm is
+// that of the list and q_r = 0.
+//
+// The row is loaded once and stays in registers; the running maximum and sum of the
+// softmax are taken as it arrives.  The list lies in LDS, linked per owning lane: a
+// lane with entries masks them out of the sum over the rest and puts their gradient
+// in its registers before it stores, so each gradient is stored once.
+#include "logit_rows.h"
+
+namespace bl {
+namespace {
+
+using namespace rows;
+
+struct DistillArgs {
+    const char *logits;
+    int64_t stride;                     // bytes from row to row
+    int64_t n_rows;
+    int32_t n, k, top_type;
+    float inv_t, inv_top_t;
+    const char *top_values;             // [rows][k], top_type
+    const int32_t *top_indices;         // [rows][k]
+    const float *top_log_norm;          // [rows] or NULL
+    const float *row_weight;            // [rows] or NULL
+    float *loss;                        // [rows] or NULL
+    char *grad;                         // or NULL, the logits' type
+    int64_t grad_stride;                // bytes
+};
+
+template <int TYPE, int VEC>
+__device__ __forceinline__ void store_piece(char *row, int32_t i, int32_t n, const float (&v)[VEC])
+{
+    if constexpr (TYPE == kF32) {
+        float *o = reinterpret_cast<float *>(row) + i;
+        if (i + VEC <= n) {
+            __builtin_memcpy(o, v, sizeof v);
+        } else {
+#pragma unroll
+            for (int u = 0; u < VEC; ++u)
+                if (i + u < n)
+                    o[u] = v[u];
+        }
+    } else {
+        typedef typename std::conditional<TYPE == kF16, _Float16, __bf16>::type H;
+        H h[VEC];
+        if constexpr (VEC == 1) {
+            h[0] = (H)v[0];
+        } else {
+            typedef H H2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int u = 0; u < VEC; u += 2) {
+                const H2 two = __builtin_convertvector((f32x2){v[u], v[u + 1]}, H2);
+                h[u] = two[0];
+                h[u + 1] = two[1];
+            }
+        }
+        H *o = reinterpret_cast<H *>(row) + i;
+        if (i + VEC <= n) {
+            __builtin_memcpy(o, h, sizeof h);
+        } else {
+#pragma unroll
+            for (int u = 0; u < VEC; ++u)
+                if (i + u < n)
+                    o[u] = h[u];
+        }
+    }
+}
+
+// A teacher's entry in LDS.
+struct Entry {
+    int32_t cls, next;                  // class (-1: none); next entry of the owning lane
+    float t;                            // teacher logit / Tt; later the gradient
+    float z;                            // the student's logit
+};
+
+template <int TYPE, class L>
+__global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
+{
+    typedef Piece<TYPE, L::VEC> P;
+    extern __shared__ Entry entries[];                    // [rows of the block][k]
+    __shared__ Scratch scratch;
+    __shared__ int32_t heads[L::kBlock];                  // first entry of the lane's list
+    __shared__ uint32_t marks[L::kBlock];                 // bit j % 32: an entry in piece j
+    const int gi = threadIdx.x / L::G;
+    const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
+    if (r >= a.n_rows)
+        return;
+    Group<L::G> g(threadIdx.x % L::G, &scratch);
+    Entry *list = entries + (int64_t)gi * a.k;
+    int32_t *head = heads + gi * L::G;
+    uint32_t *mark = marks + gi * L::G;
+    const char *src = a.logits + r * a.stride;
+    char *dst = a.grad ? a.grad + r * a.grad_stride : nullptr;
+    const float w = a.row_weight ? a.row_weight[r] : 1.0f;
+
+    const Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, w == 0.0f ? 0 : a.n, g.t);
+    const bool rest = a.top_log_norm != nullptr;
+    float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f, from = 0.0f;
+    const float c = a.inv_t * kLog2e;
+    if (w != 0.0f) {
+        head[g.t] = -1;
+        mark[g.t] = 0;
+        g.barrier();
+        float tm = -__builtin_inff();
+        for (int e = g.t; e < a.k; e += L::G) {
+            const int32_t cls = a.top_indices[r * a.k + e];
+            Entry x = {-1, -1, -__builtin_inff(), 0.0f};
+            if (cls >= 0 && cls < a.n) {
+                x.cls = cls;
+                x.t = load_float(a.top_values, a.top_type, r * a.k + e) * a.inv_top_t;
+                x.z = Elem<TYPE>::to_float(load_one<TYPE>(src, cls));
+                const int piece = cls / L::VEC, owner = piece % L::G;
+                atomicOr(&mark[owner], 1u << (piece / L::G % 32));
+                x.next = atomicExch(&head[owner], e);
+                tm = fmaxf(tm, x.t);
+            }
+            list[e] = x;
+        }
+        // the teacher's normalizer: of the list, or given
+        float log_norm;
+        if (rest) {
+            log_norm = a.top_log_norm[r];
+        } else {
+            tm = g.reduce(tm, Max());
+            float sum = 0.0f;
+            for (int e = g.t; e < a.k; e += L::G)
+                if (list[e].cls >= 0)
+                    sum += exp_fast(list[e].t - tm);
+            log_norm = tm + logf(g.reduce(sum, Add()));
+        }
+        Softmax listed = {-__builtin_inff(), 0.0f};
+        for (int e = g.t; e < a.k; e += L::G)
+            if (list[e].cls >= 0) {
+                Q += exp_fast(list[e].t - log_norm);
+                listed.raise(list[e].z, c);
+                listed.s += __builtin_amdgcn_exp2f((list[e].z - listed.from()) * c);
+            }
+        Q = g.reduce(Q, Add());
+        const float q_rest = rest ? fmaxf(0.0f, 1.0f - Q) : 0.0f;
+
+        g.barrier();
+        const uint32_t marked = rest ? mark[g.t] : 0;
+        Softmax sm = {-__builtin_inff(), 0.0f};
+        row.each([&](int j, int32_t, const P &given) {
+            P p = given;
+            if (marked >> (j % 32) & 1)
+                for (int e = head[g.t]; e >= 0; e = list[e].next)
+                    if (list[e].cls / (L::G * L::VEC) == j)
+                        p.mask(list[e].cls % L::VEC);
+            float z[L::VEC], zm = -__builtin_inff();
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u) {
+                z[u] = Elem<TYPE>::to_float(p.get(u));
+                if (TYPE == kI32 && p.get(u) == Elem<TYPE>::lowest())
+                    z[u] = -__builtin_inff();
+                zm = fmaxf(zm, z[u]);
+            }
+            sm.raise(zm, c);
+            const float from = sm.from();
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u)
+                sm.s += __builtin_amdgcn_exp2f((z[u] - from) * c);
+        });
+        // everything relative to the row's maximum
+        const float m = g.reduce(fmaxf(sm.m, rest ? listed.m : sm.m), Max());
+        sm.raise(m, c);
+        listed.raise(m, c);
+        from = sm.from();
+        const float s_out = g.reduce(sm.s, Add());
+        S = s_out;
+        if (rest)
+            S += g.reduce(listed.s, Add());
+        const float log_s = __builtin_amdgcn_logf(S) * kLn2;
+        if (a.loss) {
+            float sum = 0.0f;
+            for (int e = g.t; e < a.k; e += L::G)
+                if (list[e].cls >= 0) {
+                    const float log_q = list[e].t - log_norm, q = exp_fast(log_q);
+                    const float log_p = (list[e].z - from) * a.inv_t - log_s;
+                    sum += q == 0.0f ? 0.0f : q * (log_q - log_p);
+                }
+            sum = g.reduce(sum, Add());
+            if (q_rest > 0.0f)
+                sum += q_rest * (logf(q_rest) - (__builtin_amdgcn_logf(s_out) * kLn2 - log_s));
+            if (g.t == 0)
+                a.loss[r] = w * sum;
+        }
+        scale = w * a.inv_t;
+        if (Q + q_rest == 0.0f)
+            scale = 0.0f;                                 // a teacher without classes
+        in_list = scale * (Q + q_rest) / S;
+        outside = in_list;
+        if (q_rest > 0.0f)
+            outside = s_out == 0.0f && S > 0.0f
+                          ? 0.0f : scale * ((Q + q_rest) / S - q_rest / s_out);
+        if (dst) {
+            for (int e = g.t; e < a.k; e += L::G)
+                if (list[e].cls >= 0)
+                    list[e].t = in_list * __builtin_amdgcn_exp2f((list[e].z - from) * c) -
+                                scale * exp_fast(list[e].t - log_norm);
+            g.barrier();
+        }
+    } else if (a.loss && g.t == 0) {
+        a.loss[r] = 0.0f;
+    }
+    if constexpr (TYPE != kI32) {
+        if (!dst)
+            return;
+        if (scale == 0.0f) {
+            const float zero[L::VEC] = {};
+            for (int32_t i = g.t * L::VEC; i < a.n; i += L::G * L::VEC)
+                store_piece<TYPE, L::VEC>(dst, i, a.n, zero);
+            return;
+        }
+        const uint32_t marked = mark[g.t];
+        row.each([&](int j, int32_t i, const P &p) {
+            float v[L::VEC];
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u)
+                v[u] = outside * __builtin_amdgcn_exp2f((p.get(u) - from) * c);
+            if (marked >> (j % 32) & 1)
+                for (int e = head[g.t]; e >= 0; e = list[e].next)
+                    if (list[e].cls / (L::G * L::VEC) == j) {
+#pragma unroll
+                        for (int u = 0; u < L::VEC; ++u)
+                            if (u == list[e].cls % L::VEC)
+                                v[u] = list[e].t;
+                    }
+            store_piece<TYPE, L::VEC>(dst, i, a.n, v);
+        });
+    }
+}
+
+}  // namespace
+
+hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int32_t n,
+                          int64_t row_stride, float inv_t, const void *top_values,
+                          int32_t top_type, const int32_t *top_indices, int32_t k,
+                          const float *top_log_norm, float inv_top_t, const float *row_weight,
+                          float *loss, void *grad, int64_t grad_stride, hipStream_t stream)
+{
+    return with_type(type, [&](auto ty) {
+        constexpr int TYPE = decltype(ty)::value;
+        const DistillArgs a = {static_cast<const char *>(logits),
+                               row_stride * Elem<TYPE>::kBytes, n_rows, n, k, top_type, inv_t,
+                               inv_top_t, static_cast<const char *>(top_values), top_indices,
+                               top_log_norm, row_weight, loss, static_cast<char *>(grad),
+                               grad_stride * Elem<TYPE>::kBytes};
+        return with_layout<TYPE>(n, k, [&](auto layout) {
+            typedef decltype(layout) L;
+            k_distill<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock,
+                                 (size_t)L::kGroups * k * sizeof(Entry), stream>>>(a);
+            return hipGetLastError();
+        });
+    });
+}
+
+}  // namespace bl

@@ -1,0 +1,439 @@
+// Rows of class scores or logits (internal): element types, a group of lanes that
+// holds a row, reductions over the group and the order of a row's classes.
+//
+// A row of n classes belongs to a group of G lanes: part of a wave, a wave, or a
+// block of several waves.  Lane t holds elements (j * G + t) * VEC + u, u < VEC,
+// j < NV, in registers: one element a load for short rows, 16 bytes a load for
+// long ones (at any alignment: rows of odd lengths start anywhere).  Rows longer
+// than the registers hold are read again for every pass.
+//
+// The order of a row is descending logit, then ascending class.  A NaN, a -inf or
+// (int32) the lowest integer is masked and has no place in it.  Selection works on
+// 32-bit keys that grow with the logit; -0 and +0 have one key.
+#pragma once
+
+#include <type_traits>
+
+#include "bl_internal.h"
+
+namespace bl {
+namespace rows {
+
+constexpr int32_t kMaxClasses = 1 << 30;
+
+enum : int { kI32 = 0, kF32 = 1, kF16 = 2, kBf16 = 3 };
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// ---- element types ----
+// Cmp: what elements are compared as; kShift: key bits below the type's own.
+template <int TYPE>
+struct Elem {
+    typedef float Cmp;
+    static constexpr int kBytes = TYPE == kF32 ? 4 : 2;
+    static constexpr int kShift = TYPE == kF32 ? 0 : TYPE == kF16 ? 13 : 16;
+    static __device__ __forceinline__ Cmp lowest() { return -__builtin_inff(); }
+    static __device__ __forceinline__ float to_float(Cmp v) { return v; }
+    static __device__ __forceinline__ uint32_t key(Cmp v)
+    {
+        const uint32_t b = __float_as_uint(v + 0.0f);
+        return (b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) >> kShift;
+    }
+    // the element whose key is k (for a key that no element has: one between its neighbours)
+    static __device__ __forceinline__ Cmp from_key(uint32_t k)
+    {
+        k <<= kShift;
+        if (!(k & 0x80000000u))
+            k |= (1u << kShift) - 1;
+        return __uint_as_float(k ^ ((k & 0x80000000u) ? 0x80000000u : 0xFFFFFFFFu));
+    }
+    static constexpr uint32_t kFirstKey = 0x00800000u >> kShift;   // of the lowest finite value
+};
+
+template <>
+struct Elem<kI32> {
+    typedef int32_t Cmp;
+    static constexpr int kBytes = 4;
+    static constexpr int kShift = 0;
+    static __device__ __forceinline__ Cmp lowest() { return INT32_MIN; }
+    static __device__ __forceinline__ float to_float(Cmp v) { return (float)v; }
+    static __device__ __forceinline__ uint32_t key(Cmp v) { return (uint32_t)v ^ 0x80000000u; }
+    static __device__ __forceinline__ Cmp from_key(uint32_t k)
+    {
+        return (int32_t)(k ^ 0x80000000u);
+    }
+    static constexpr uint32_t kFirstKey = 1;
+};
+
+// One element from memory, as it is compared.
+template <int TYPE>
+__device__ __forceinline__ typename Elem<TYPE>::Cmp load_one(const char *row, int64_t i)
+{
+    if constexpr (TYPE == kI32)
+        return reinterpret_cast<const int32_t *>(row)[i];
+    else if constexpr (TYPE == kF32)
+        return reinterpret_cast<const float *>(row)[i];
+    else if constexpr (TYPE == kF16)
+        return (float)reinterpret_cast<const _Float16 *>(row)[i];
+    else
+        return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(row)[i] << 16);
+}
+
+// An element of a type known at run time, as float (teacher lists).
+__device__ __forceinline__ float load_float(const char *p, int type, int64_t i)
+{
+    switch (type) {
+    case kI32: return (float)load_one<kI32>(p, i);
+    case kF32: return load_one<kF32>(p, i);
+    case kF16: return load_one<kF16>(p, i);
+    default: return load_one<kBf16>(p, i);
+    }
+}
+
+// ---- pieces: VEC elements in registers ----
+template <int TYPE, int VEC>
+struct Piece {
+    static constexpr int kWords = VEC * Elem<TYPE>::kBytes >= 4 ? VEC * Elem<TYPE>::kBytes / 4 : 1;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ typename Elem<TYPE>::Cmp get(int u) const
+    {
+        if constexpr (TYPE == kI32) {
+            return (int32_t)w[u];
+        } else if constexpr (TYPE == kF32) {
+            return __uint_as_float(w[u]);
+        } else if constexpr (TYPE == kBf16) {
+            return __uint_as_float(u & 1 ? w[u / 2] & 0xFFFF0000u : w[u / 2] << 16);
+        } else {
+            f16x2 h;
+            __builtin_memcpy(&h, &w[u / 2], 4);
+            return (float)(u & 1 ? h[1] : h[0]);
+        }
+    }
+    __device__ __forceinline__ void fill_masked()
+    {
+        constexpr uint32_t m = TYPE == kI32 ? 0x80000000u : TYPE == kF32 ? 0xFF800000u
+                               : TYPE == kF16 ? 0xFC00FC00u : 0xFF80FF80u;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            w[i] = m;
+    }
+    // elements [i, i + VEC) of a row of n; those past it are masked
+    __device__ __forceinline__ void load(const char *row, int32_t i, int32_t n)
+    {
+        const char *p = row + (int64_t)i * Elem<TYPE>::kBytes;
+        if (i + VEC <= n) {
+            if constexpr (VEC * Elem<TYPE>::kBytes >= 4) {
+                __builtin_memcpy(w, p, sizeof w);
+            } else {
+                w[0] = *reinterpret_cast<const uint16_t *>(p);
+            }
+            return;
+        }
+        fill_masked();
+        if constexpr (VEC > 1) {
+#pragma unroll
+            for (int u = 0; u < VEC - 1; ++u)
+                if (i + u < n) {
+                    if constexpr (Elem<TYPE>::kBytes == 4)
+                        w[u] = reinterpret_cast<const uint32_t *>(p)[u];
+                    else
+                        put16(u, reinterpret_cast<const uint16_t *>(p)[u]);
+                }
+        }
+    }
+    __device__ __forceinline__ void put16(int u, uint32_t v)
+    {
+        w[u / 2] = u & 1 ? (w[u / 2] & 0x0000FFFFu) | v << 16 : (w[u / 2] & 0xFFFF0000u) | v;
+    }
+    // element u (a run-time index) masked
+    __device__ __forceinline__ void mask(int at)
+    {
+#pragma unroll
+        for (int u = 0; u < VEC; ++u)
+            if (u == at) {
+                if constexpr (Elem<TYPE>::kBytes == 4)
+                    w[u] = TYPE == kI32 ? 0x80000000u : 0xFF800000u;
+                else
+                    put16(u, TYPE == kF16 ? 0xFC00u : 0xFF80u);
+            }
+    }
+};
+
+// ---- reductions over the lanes of a group ----
+// The value of the lane that holds the other half's result of a reduction over
+// 2 S lanes, once every S lanes hold theirs: within a row of 16 lanes by DPP.
+template <int S>
+__device__ __forceinline__ uint32_t other_half(uint32_t v)
+{
+    constexpr int ctrl = S == 1 ? 0xB1 : S == 2 ? 0x4E : S == 4 ? 0x141 : 0x140;
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xF, 0xF, true);
+}
+
+template <int S, class T, class Op>
+__device__ __forceinline__ T reduce_step(T v, Op op)
+{
+    static_assert(sizeof(T) == 4 || sizeof(T) == 8, "32- or 64-bit values");
+    constexpr int W = sizeof(T) / 4;
+    uint32_t a[W], x[W], y[W];
+    __builtin_memcpy(a, &v, sizeof v);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if constexpr (S <= 8) {
+            x[i] = a[i];
+            y[i] = other_half<S>(a[i]);
+        } else if constexpr (S == 16) {
+            const auto r = __builtin_amdgcn_permlane16_swap(a[i], a[i], false, false);
+            x[i] = r[0];
+            y[i] = r[1];
+        } else {
+            const auto r = __builtin_amdgcn_permlane32_swap(a[i], a[i], false, false);
+            x[i] = r[0];
+            y[i] = r[1];
+        }
+    }
+    T p, q;
+    __builtin_memcpy(&p, x, sizeof p);
+    __builtin_memcpy(&q, y, sizeof q);
+    return op(p, q);
+}
+
+// Over G <= 64 lanes of a wave; every lane gets the result.
+template <int G, class T, class Op>
+__device__ __forceinline__ T wave_reduce(T v, Op op)
+{
+    if constexpr (G > 1) v = reduce_step<1>(v, op);
+    if constexpr (G > 2) v = reduce_step<2>(v, op);
+    if constexpr (G > 4) v = reduce_step<4>(v, op);
+    if constexpr (G > 8) v = reduce_step<8>(v, op);
+    if constexpr (G > 16) v = reduce_step<16>(v, op);
+    if constexpr (G > 32) v = reduce_step<32>(v, op);
+    return v;
+}
+
+constexpr int kMaxWaves = 16;
+
+// LDS of one group's reductions and scans (only groups of several waves use it).
+struct Scratch {
+    uint64_t slot[2][kMaxWaves];
+};
+
+struct Max {
+    template <class T> __device__ T operator()(T a, T b) const { return a > b ? a : b; }
+    // the other one where one is a NaN
+    __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Add {
+    template <class T> __device__ T operator()(T a, T b) const { return a + b; }
+};
+
+// A group of G lanes; t is the lane's place in it.  Reductions of several waves
+// go through LDS, alternating between two sets of slots so that one barrier each
+// is enough.
+template <int G>
+struct Group {
+    int t;
+    Scratch *s;
+    int turn;
+
+    __device__ __forceinline__ Group(int place, Scratch *scratch) : t(place), s(scratch), turn(0) {}
+
+    __device__ __forceinline__ void barrier()
+    {
+        if constexpr (G > kWave) {
+            __syncthreads();
+        } else {
+            // one wave: LDS accesses run in order; keep the compiler's order too
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+
+    template <class T, class Op>
+    __device__ __forceinline__ T reduce(T v, Op op)
+    {
+        v = wave_reduce<(G < kWave ? G : kWave)>(v, op);
+        if constexpr (G > kWave) {
+            constexpr int W = G / kWave;
+            T *slot = reinterpret_cast<T *>(s->slot[turn]);
+            turn ^= 1;
+            if (t % kWave == 0)
+                slot[t / kWave] = v;
+            __syncthreads();
+            v = wave_reduce<W>(slot[t % W], op);
+        }
+        return v;
+    }
+
+    // the sum of v over the lanes before this one, and (total) over all
+    __device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t &total)
+    {
+        constexpr int L = G < kWave ? G : kWave;
+        uint32_t in = v;
+#pragma unroll
+        for (int d = 1; d < L; d *= 2) {
+            const uint32_t o = __shfl_up(in, d, L);
+            if (t % L >= d)
+                in += o;
+        }
+        total = __shfl(in, L - 1, L);
+        uint32_t before = in - v;
+        if constexpr (G > kWave) {
+            constexpr int W = G / kWave;
+            uint32_t *slot = reinterpret_cast<uint32_t *>(s->slot[turn]);
+            turn ^= 1;
+            if (t % kWave == 0)
+                slot[t / kWave] = total;
+            __syncthreads();
+            total = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const uint32_t c = slot[w];
+                if (w < t / kWave)
+                    before += c;
+                total += c;
+            }
+        }
+        return before;
+    }
+};
+
+// ---- a row in a group's registers, or in memory ----
+template <int TYPE, int G, int NV, int VEC, bool RESIDENT>
+struct Row {
+    typedef typename Elem<TYPE>::Cmp Cmp;
+    typedef Piece<TYPE, VEC> P;
+    static constexpr int kSpan = G * VEC;                 // elements of one piece per lane
+    static constexpr int kFlight = RESIDENT ? 1 : 4;      // pieces loaded together
+    const char *row;
+    int32_t n, t;
+    P piece[RESIDENT ? NV : 1];
+
+    __device__ __forceinline__ Row(const char *r, int32_t classes, int lane)
+        : row(r), n(classes), t(lane)
+    {
+        if constexpr (RESIDENT) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (j * kSpan < n)
+                    piece[j].load(row, j * kSpan + t * VEC, n);
+                else
+                    piece[j].fill_masked();
+            }
+        }
+    }
+
+    // f(j, its first element, piece j) in index order of the pieces
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        if constexpr (RESIDENT) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j * kSpan < n)
+                    f(j, j * kSpan + t * VEC, piece[j]);
+        } else {
+            for (int32_t i = 0; i < n; i += kFlight * kSpan) {
+                P p[kFlight];
+#pragma unroll
+                for (int j = 0; j < kFlight; ++j)
+                    p[j].load(row, i + j * kSpan + t * VEC, n);
+#pragma unroll
+                for (int j = 0; j < kFlight; ++j)
+                    f(i / kSpan + j, i + j * kSpan + t * VEC, p[j]);
+            }
+        }
+    }
+};
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// e^x, x <= 0, by the hardware's exponential of base 2: the product's rounding is
+// an error of |x| 2^-24 of the result.
+__device__ __forceinline__ float exp_fast(float x)
+{
+    return __builtin_amdgcn_exp2f(x * kLog2e);
+}
+
+// A running maximum m of z and the sum s of 2^(c (z - m)): with c = log2(e) / T the
+// exponentials of a softmax at temperature T.  The difference comes first: c z alone
+// overflows where z is its type's lowest value, which masks are made of.
+struct Softmax {
+    float m, s;
+    __device__ __forceinline__ float from() const { return m == -__builtin_inff() ? 0.0f : m; }
+    __device__ __forceinline__ void raise(float to, float c)
+    {
+        const float old = from();
+        m = fmaxf(m, to);
+        s *= __builtin_amdgcn_exp2f(s == 0.0f ? 0.0f : (old - from()) * c);
+    }
+    // log sum e^(z / T)
+    __device__ __forceinline__ float log_norm(float inv_t) const
+    {
+        return m == __builtin_inff() || m == -__builtin_inff()
+                   ? m : m * inv_t + __builtin_amdgcn_logf(s) * kLn2;
+    }
+};
+
+// Over a group: the maximum first, then the sums relative to it.
+template <class Grp>
+__device__ __forceinline__ Softmax combine(Grp &g, Softmax a, float c)
+{
+    a.raise(g.reduce(a.m, Max()), c);
+    a.s = g.reduce(a.s, Add());
+    return a;
+}
+
+// ---- which group holds rows of n classes ----
+template <int G_, int NV_, int VEC_, bool RESIDENT_>
+struct Layout {
+    static constexpr int G = G_, NV = NV_, VEC = VEC_;
+    static constexpr bool RESIDENT = RESIDENT_;
+    static constexpr int kBlock = G < 256 ? 256 : G;
+    static constexpr int kGroups = kBlock / G;            // rows of a block
+};
+
+// f(Layout) for rows of n classes of a type whose lists have up to k entries a row.
+template <int TYPE, class F>
+hipError_t with_layout(int32_t n, int32_t k, F f)
+{
+    constexpr int V = 16 / Elem<TYPE>::kBytes;            // elements of a 16-byte load
+    if (n <= 16 && k <= 16)
+        return f(Layout<8, 2, 1, true>());
+    if (n <= 64 && k <= 64)
+        return f(Layout<16, 4, 1, true>());
+    if (n <= 128 && k <= 128)
+        return f(Layout<32, 4, 1, true>());
+    if (n <= 512)
+        return f(Layout<64, 8, 1, true>());
+    if (n <= 1024)
+        return f(Layout<64, 16 / V, V, true>());
+    if (n <= 8192)
+        return f(Layout<256, 32 / V, V, true>());
+    if (n <= 32768)
+        return f(Layout<1024, 32 / V, V, true>());
+    if (n <= 65536)
+        return f(Layout<1024, 64 / V, V, true>());
+    if constexpr (V == 8) {
+        if (n <= 131072)
+            return f(Layout<1024, 16, V, true>());
+    }
+    return f(Layout<1024, 1, V, false>());
+}
+
+template <class F>
+hipError_t with_type(int32_t type, F f)
+{
+    switch (type) {
+    case kI32: return f(std::integral_constant<int, kI32>());
+    case kF32: return f(std::integral_constant<int, kF32>());
+    case kF16: return f(std::integral_constant<int, kF16>());
+    default: return f(std::integral_constant<int, kBf16>());
+    }
+}
+
+}  // namespace rows
+}  // namespace bl
