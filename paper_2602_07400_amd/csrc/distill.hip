@@ -105,7 +105,7 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
     char *dst = a.grad ? a.grad + r * a.grad_stride : nullptr;
     const float w = a.row_weight ? a.row_weight[r] : 1.0f;
 
-    const Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, w == 0.0f ? 0 : a.n, g.t);
+    Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, w == 0.0f ? 0 : a.n, g.t);
     const bool rest = a.top_log_norm != nullptr;
     float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f, from = 0.0f;
     const float c = a.inv_t * kLog2e;

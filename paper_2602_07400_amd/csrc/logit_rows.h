@@ -268,21 +268,24 @@ struct Group {
     }
 
     // the sum of v over the lanes before this one, and (total) over all
-    __device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t &total)
+    template <class T>
+    __device__ __forceinline__ T scan(T v, T &total)
     {
         constexpr int L = G < kWave ? G : kWave;
-        uint32_t in = v;
+        T in = v;
 #pragma unroll
         for (int d = 1; d < L; d *= 2) {
-            const uint32_t o = __shfl_up(in, d, L);
+            const T o = __shfl_up(in, d, L);
             if (t % L >= d)
                 in += o;
         }
         total = __shfl(in, L - 1, L);
-        uint32_t before = in - v;
+        T before = __shfl_up(in, 1, L);
+        if (t % L == 0)
+            before = 0;
         if constexpr (G > kWave) {
             constexpr int W = G / kWave;
-            uint32_t *slot = reinterpret_cast<uint32_t *>(s->slot[turn]);
+            T *slot = reinterpret_cast<T *>(s->slot[turn]);
             turn ^= 1;
             if (t % kWave == 0)
                 slot[t / kWave] = total;
@@ -290,7 +293,7 @@ struct Group {
             total = 0;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const uint32_t c = slot[w];
+                const T c = slot[w];
                 if (w < t / kWave)
                     before += c;
                 total += c;
@@ -327,13 +330,20 @@ struct Row {
 
     // f(j, its first element, piece j) in index order of the pieces
     template <class F>
-    __device__ __forceinline__ void each(F f) const
+    __device__ __forceinline__ void each(F f)
     {
         if constexpr (RESIDENT) {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                if (j * kSpan < n)
+                if (j * kSpan < n) {
+                    // every pass unpacks the elements again: kept unpacked from an
+                    // earlier one, they would take more registers than there are
+                    if constexpr (VEC > 1)
+#pragma unroll
+                        for (int i = 0; i < P::kWords; ++i)
+                            asm("" : "+v"(piece[j].w[i]));
                     f(j, j * kSpan + t * VEC, piece[j]);
+                }
         } else {
             for (int32_t i = 0; i < n; i += kFlight * kSpan) {
                 P p[kFlight];
@@ -387,6 +397,70 @@ __device__ __forceinline__ Softmax combine(Grp &g, Softmax a, float c)
     return a;
 }
 
+// ---- lists of candidates ----
+// An element with its place in the order: larger entries come first.
+__device__ __forceinline__ uint64_t entry(uint32_t key, int32_t cls)
+{
+    return (uint64_t)key << 32 | ~(uint32_t)cls;
+}
+__device__ __forceinline__ int32_t class_of(uint64_t e) { return (int32_t)~(uint32_t)e; }
+__device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
+
+// The largest key of which at least m lanes of a whole wave have as much (1 <= m <=
+// 64), or a little less where that ends the search early: never too much.
+__device__ __forceinline__ uint32_t wave_mth(uint32_t key, uint32_t m)
+{
+    uint32_t hi = wave_reduce<kWave>(key, Max()), lo = wave_reduce<kWave>(~key, Max());
+    lo = ~lo;                                             // every lane has it
+    if (m <= 1)
+        return hi;
+    while (hi - lo > 1) {                                 // count(>= lo) >= m > count(> hi)
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const uint32_t count = __popcll(__ballot(key >= mid));
+        if (count >= m)
+            lo = mid;
+        else
+            hi = mid;
+        if (count >= m && count <= m + m / 8)
+            break;
+    }
+    return lo;
+}
+
+// c entries in descending order, in place; room for the next power of two.
+template <int G>
+__device__ __forceinline__ void sort_entries(Group<G> &g, uint64_t *e, uint32_t c)
+{
+    uint32_t p = 2;
+    while (p < c)
+        p *= 2;
+    for (uint32_t i = c + g.t; i < p; i += G)
+        e[i] = 0;
+    for (uint32_t size = 2; size <= p; size *= 2)
+        for (uint32_t stride = size / 2; stride; stride /= 2) {
+            g.barrier();
+            for (uint32_t i = g.t; i < p / 2; i += G) {
+                const uint32_t a = 2 * i - (i & (stride - 1)), b = a + stride;
+                const uint64_t x = e[a], y = e[b];
+                if ((x < y) == !(a & size)) {
+                    e[a] = y;
+                    e[b] = x;
+                }
+            }
+        }
+    g.barrier();
+}
+
+// How many of c entries are larger than mine.
+__device__ __forceinline__ uint32_t place_of(uint64_t mine, const uint64_t *e, uint32_t c)
+{
+    uint32_t place = 0;
+#pragma unroll 8
+    for (uint32_t f = 0; f < c; ++f)
+        place += e[f] > mine;
+    return place;
+}
+
 // ---- which group holds rows of n classes ----
 template <int G_, int NV_, int VEC_, bool RESIDENT_>
 struct Layout {
@@ -394,6 +468,8 @@ struct Layout {
     static constexpr bool RESIDENT = RESIDENT_;
     static constexpr int kBlock = G < 256 ? 256 : G;
     static constexpr int kGroups = kBlock / G;            // rows of a block
+    // candidates of a row that LDS holds (a power of two; all n classes of a wave's row)
+    static constexpr int kList = G == 1024 ? 4096 : G == 256 ? 2048 : NV * VEC * G;
 };
 
 // f(Layout) for rows of n classes of a type whose lists have up to k entries a row.

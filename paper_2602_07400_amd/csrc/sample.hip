@@ -11,9 +11,12 @@
 // a comparison of elementary sums; one uniform number a row would make it depend on
 // the rounding of a prefix sum over all classes.)
 //
-// Every filter keeps a prefix of the order, so the kept set is (key > tau) and the
-// first classes of (key == tau).  tau comes from bisection on the key: on counts for
-// top-k, on sums of w for top-p.
+// Every filter keeps a prefix of the order.  Where it is short, its classes are among
+// those of a list in LDS, found from the lanes' largest logits as in top_logits.hip
+// and put in order: top-k is a place, top-p a prefix sum, and the kept classes' numbers
+// are all that is read of the noise.  Otherwise the kept set is (key > tau) and the
+// first classes of (key == tau), tau from bisection on the key: on counts for top-k,
+// on sums of w for top-p.
 #include "logit_rows.h"
 
 namespace bl {
@@ -36,64 +39,88 @@ struct SampleArgs {
     float *log_prob;                    // [rows] or NULL
 };
 
+// Places up to here come from counting the larger entries, more from a sort.
+constexpr uint32_t kCounted = 128;
+// Lanes of each wave whose largest logits bound the list of a top-p without a top-k.
+constexpr uint32_t kNucleusLanes = 16;
+
 template <int TYPE, class L>
 __global__ __launch_bounds__(L::kBlock) void k_sample(SampleArgs a)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
     typedef Piece<TYPE, L::VEC> P;
+    constexpr int G = L::G;
+    constexpr bool kLists = G >= kWave;
     __shared__ Scratch scratch;
-    const int64_t r = (int64_t)blockIdx.x * L::kGroups + threadIdx.x / L::G;
+    __shared__ uint64_t lists[kLists ? L::kGroups : 1][kLists ? L::kList : 1];
+    __shared__ uint64_t placed[kLists ? L::kGroups : 1][kCounted];
+    __shared__ uint32_t fills[L::kGroups];
+    const int gi = threadIdx.x / G;
+    const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
     if (r >= a.n_rows)
         return;
-    Group<L::G> g(threadIdx.x % L::G, &scratch);
+    Group<G> g(threadIdx.x % G, &scratch);
+    if (g.t == 0)
+        fills[gi] = 0;
     const char *src = a.logits + r * a.stride;
-    const Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
+    const float *noise = a.noise + r * a.noise_stride;
+    Row<TYPE, G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
     const float temperature = a.temperatures ? a.temperatures[r] : a.temperature;
     const float top_p = a.top_ps ? a.top_ps[r] : a.top_p;
     const float min_p = a.min_ps ? a.min_ps[r] : a.min_p;
-    const int32_t top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+    int32_t top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+    if (top_k <= 0 || top_k > a.n)
+        top_k = a.n;
+    const float inv_t = 1.0f / temperature;
 
-    // the first of the order: the lowest class among the largest logits
-    Cmp top = E::lowest();
-    row.each([&](int, int32_t, const P &p) {
+    // the lane's and its pieces' largest logits
+    Cmp mine = E::lowest(), most[L::NV];
+    row.each([&](int j, int32_t, const P &p) {
+        Cmp vm = E::lowest();
 #pragma unroll
         for (int u = 0; u < L::VEC; ++u) {
             const Cmp v = p.get(u);
-            top = v > top ? v : top;
+            vm = v > vm ? v : vm;
         }
+        mine = vm > mine ? vm : mine;
+        if constexpr (L::RESIDENT)
+            most[j] = vm;
     });
-    top = g.reduce(top, Max());
-    if (!(top > E::lowest())) {                           // nothing to draw from
-        if (g.t == 0) {
-            a.token[r] = -1;
-            if (a.log_prob)
-                a.log_prob[r] = -__builtin_inff();
-        }
-        return;
-    }
-    uint32_t first = 0;                                   // its ~class
-    row.each([&](int, int32_t i, const P &p) {
+    const Cmp top = g.reduce(mine, Max());
+    const auto first_class = [&]() __attribute__((always_inline)) {
+        uint32_t first = 0;                               // of the largest, ~class
+        if (mine == top)
+            row.each([&](int, int32_t i, const P &p) {
 #pragma unroll
-        for (int u = 0; u < L::VEC; ++u)
-            if (p.get(u) == top)
-                first = max(first, ~(uint32_t)(i + u));
-    });
-    first = ~g.reduce(first, Max());
-    if (!(temperature > 0.0f)) {                          // greedy
+                for (int u = 0; u < L::VEC; ++u)
+                    if (p.get(u) == top)
+                        first = max(first, ~(uint32_t)(i + u));
+            });
+        return (int32_t)~g.reduce(first, Max());
+    };
+    if (!(top > E::lowest()) || !(temperature > 0.0f)) {
+        const bool any = top > E::lowest();               // greedy, or nothing to draw from
+        const int32_t token = any ? first_class() : -1;
         if (g.t == 0) {
-            a.token[r] = (int32_t)first;
+            a.token[r] = token;
             if (a.log_prob)
-                a.log_prob[r] = 0.0f;
+                a.log_prob[r] = any ? 0.0f : -__builtin_inff();
         }
         return;
     }
 
-    const float inv_t = 1.0f / temperature, ftop = E::to_float(top);
-    const auto x_of = [&](Cmp v) __attribute__((always_inline)) { return v == top ? 0.0f : (E::to_float(v) - ftop) * inv_t; };
-    const auto mass_from = [&](Cmp at) __attribute__((always_inline)) {                  // sum of w over logits >= at
-        float sum = 0.0f;
-        row.each([&](int, int32_t, const P &p) {
+    const float ftop = E::to_float(top);
+    const float floor_x = min_p > 0.0f ? logf(min_p) : -__builtin_inff();
+    const auto x_of = [&](Cmp v) __attribute__((always_inline)) {
+        return v == top ? 0.0f : (E::to_float(v) - ftop) * inv_t;
+    };
+    const auto mass_from = [&](Cmp at) __attribute__((always_inline)) {
+        float sum = 0.0f;                                 // of w over logits >= at
+        row.each([&](int j, int32_t, const P &p) {
+            if constexpr (L::RESIDENT)
+                if (!(most[j] >= at))
+                    return;
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
                 const Cmp v = p.get(u);
@@ -104,18 +131,111 @@ __global__ __launch_bounds__(L::kBlock) void k_sample(SampleArgs a)
     };
     const auto count_from = [&](Cmp at) __attribute__((always_inline)) {
         uint32_t count = 0;
-        row.each([&](int, int32_t, const P &p) {
+        row.each([&](int j, int32_t, const P &p) {
+            if constexpr (L::RESIDENT)
+                if (!(most[j] >= at))
+                    return;
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
                 count += p.get(u) >= at;
         });
         return g.reduce(count, Add());
     };
+    float sum = 0.0f;                                     // of the kept w
+    uint64_t best = 0;                                    // (key of x + g, ~class)
+    const auto draw = [&](float x, int32_t cls, float number) __attribute__((always_inline)) {
+        const float score = x + number;
+        if (score > -__builtin_inff()) {
+            const uint64_t s = entry(Elem<kF32>::key(score), cls);
+            best = s > best ? s : best;
+        }
+    };
+    const auto finish = [&](auto first) __attribute__((always_inline)) {
+        best = g.reduce(best, Max());
+        sum = g.reduce(sum, Add());
+        const int32_t token = best ? class_of(best) : first();
+        if (g.t == 0) {
+            a.token[r] = token;
+            if (a.log_prob)
+                a.log_prob[r] = x_of(load_one<TYPE>(src, token)) - logf(sum);
+        }
+    };
+
+    const bool by_k = top_k < a.n, by_p = top_p < 1.0f;
+    const Cmp all = E::from_key(E::kFirstKey);
+    float row_mass = 0.0f;
+    if (by_p && !by_k)
+        row_mass = mass_from(all);
+
+    if constexpr (kLists) {
+        constexpr uint32_t W = G / kWave;
+        const uint32_t lanes = by_k ? (top_k + W - 1) / W : kNucleusLanes;
+        if ((by_k || by_p) && lanes <= kWave) {
+            uint64_t *list = lists[gi], *sorted = placed[gi];
+            uint32_t *fill = &fills[gi];
+            const uint32_t key = mine > E::lowest() ? E::key(mine) : 0;
+            const uint32_t lo = max((uint32_t)E::kFirstKey,
+                                    ~g.reduce(~wave_mth(key, lanes), Max()));
+            const Cmp at = E::from_key(lo);
+            row.each([&](int j, int32_t i, const P &p) {
+                if constexpr (L::RESIDENT)
+                    if (!(most[j] >= at))
+                        return;
+#pragma unroll
+                for (int u = 0; u < L::VEC; ++u) {
+                    const Cmp v = p.get(u);
+                    if (v >= at) {
+                        const uint32_t to = atomicAdd(fill, 1u);
+                        if (to < (uint32_t)L::kList)
+                            list[to] = entry(E::key(v), i + u);
+                    }
+                }
+            });
+            g.barrier();
+            const uint32_t found = *fill;
+            if (found <= (uint32_t)L::kList) {
+                if (found <= kCounted) {
+                    for (uint32_t e = g.t; e < found; e += G) {
+                        const uint64_t x = list[e];
+                        sorted[place_of(x, list, found)] = x;
+                    }
+                    g.barrier();
+                } else {
+                    sort_entries(g, list, found);
+                    sorted = list;
+                }
+                const uint32_t n = by_k ? min(found, (uint32_t)top_k) : found;
+                // sums of w before each entry: a run of entries a lane
+                const uint32_t run = (n + G - 1) / G, e0 = min(n, g.t * run),
+                               e1 = min(n, e0 + run);
+                float w = 0.0f, total;
+                for (uint32_t e = e0; e < e1; ++e)
+                    w += exp_fast(x_of(E::from_key(key_of(sorted[e]))));
+                float before = g.scan(w, total);
+                const float target = top_p * (by_k ? total : row_mass);
+                // the list reaches the target, or holds every class
+                if (!by_p || by_k || total >= target || lo == E::kFirstKey) {
+                    for (uint32_t e = e0; e < e1; ++e) {
+                        const float x = x_of(E::from_key(key_of(sorted[e])));
+                        const float we = exp_fast(x);
+                        if (e == 0 || ((!by_p || before < target) && x >= floor_x)) {
+                            const int32_t cls = class_of(sorted[e]);
+                            sum += we;
+                            draw(x, cls, noise[cls]);
+                        }
+                        before += we;
+                    }
+                    finish([&] { return class_of(sorted[0]); });
+                    return;
+                }
+            }
+        }
+    }
 
     // the kept prefix: keys above tau, and `ties` of those equal to it
     const uint32_t end = E::key(top) + 1;
     uint32_t tau = E::kFirstKey, ties = 0xFFFFFFFFu;
-    if (top_k > 0 && top_k < a.n && count_from(E::from_key(tau)) > (uint32_t)top_k) {
+    if (by_k && count_from(all) > (uint32_t)top_k) {
         uint32_t hi = end;                                // count(>= tau) >= k > count(>= hi)
         while (hi - tau > 1) {
             const uint32_t mid = tau + (hi - tau) / 2;
@@ -126,15 +246,17 @@ __global__ __launch_bounds__(L::kBlock) void k_sample(SampleArgs a)
         }
         ties = top_k - (hi == end ? 0 : count_from(E::from_key(hi)));
     }
-    if (top_p < 1.0f) {
-        const Cmp at = E::from_key(tau);
-        float target;
-        if (ties != 0xFFFFFFFFu) {
-            const float above = tau + 1 == end ? 0.0f : mass_from(E::from_key(tau + 1));
-            target = top_p * (above + (float)ties * exp_fast(x_of(at)));
-        } else {
-            target = top_p * mass_from(at);
+    if (by_p) {
+        float target = row_mass;
+        if (by_k) {
+            if (ties != 0xFFFFFFFFu) {
+                const float above = tau + 1 == end ? 0.0f : mass_from(E::from_key(tau + 1));
+                target = above + (float)ties * exp_fast(x_of(E::from_key(tau)));
+            } else {
+                target = mass_from(all);
+            }
         }
+        target *= top_p;
         uint32_t lo = tau, hi = end;                      // mass(>= lo) >= target > mass(>= hi)
         float above = 0.0f;                               // mass(>= hi)
         while (hi - lo > 1) {
@@ -159,7 +281,7 @@ __global__ __launch_bounds__(L::kBlock) void k_sample(SampleArgs a)
     int32_t last = INT32_MAX;
     if (ties != 0xFFFFFFFFu) {
         uint32_t seen = 0;
-        int32_t mine = -1;
+        int32_t equal = -1;
         row.each([&](int, int32_t i, const P &p) {
             if (seen >= ties)
                 return;
@@ -172,38 +294,25 @@ __global__ __launch_bounds__(L::kBlock) void k_sample(SampleArgs a)
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
                 if (p.get(u) == at && place++ < ties)
-                    mine = i + u;
+                    equal = i + u;
         });
-        last = g.reduce(mine, Max());
+        last = g.reduce(equal, Max());
     }
-    const float floor_x = min_p > 0.0f ? logf(min_p) : -__builtin_inff();
-
-    float sum = 0.0f;
-    uint64_t best = 0;
-    const float *noise = a.noise + r * a.noise_stride;
-    row.each([&](int, int32_t i, const P &p) {
+    row.each([&](int j, int32_t i, const P &p) {
+        if constexpr (L::RESIDENT)
+            if (!(most[j] >= at))
+                return;
 #pragma unroll
         for (int u = 0; u < L::VEC; ++u) {
             const Cmp v = p.get(u);
             const float x = x_of(v);
             if ((v > at || (v == at && i + u <= last)) && (x >= floor_x || v == top)) {
                 sum += exp_fast(x);
-                const float score = x + noise[i + u];
-                if (score > -__builtin_inff()) {
-                    const uint64_t s = (uint64_t)Elem<kF32>::key(score) << 32 | ~(uint32_t)(i + u);
-                    best = s > best ? s : best;
-                }
+                draw(x, i + u, noise[i + u]);
             }
         }
     });
-    best = g.reduce(best, Max());
-    sum = g.reduce(sum, Add());
-    if (g.t == 0) {
-        const int32_t token = best ? (int32_t)~(uint32_t)best : (int32_t)first;
-        a.token[r] = token;
-        if (a.log_prob)
-            a.log_prob[r] = x_of(load_one<TYPE>(src, token)) - logf(sum);
-    }
+    finish(first_class);
 }
 
 }  // namespace

@@ -1,11 +1,14 @@
 // Top logits: the k largest logits of every row with their classes, and the row's
 // log-normalizer log sum_i e^(l_i / T): what a teacher hands on to a student.
 //
-// One pass over the row takes the running maximum and sum of the softmax.  The k-th
-// largest key tau is then found by bisection on counts (key >= tau), the classes
-// above tau and the first classes equal to it fill a list in LDS, and each entry's
-// place is the number of entries before it.  Keys (key, class) are unique, so the
-// order in which the list fills does not matter.
+// One pass over the row, as it arrives, takes the running maximum and sum of the
+// softmax and every lane's largest logit.  If m lanes in each of a row's W waves have
+// a logit >= lo, W m >= k classes have: the classes >= lo, a few more than k, go to a
+// list in LDS that is put in order.  Where the bound does not hold so few (many equal
+// logits, or k far above the lanes), tau, the k-th largest key, is found by bisection
+// on counts (key >= tau), and the list gets the classes above tau and the first ones
+// equal to it.  Entries (key, class) are unique, so the order in which the list fills
+// does not matter.
 #include "logit_rows.h"
 
 namespace bl {
@@ -24,47 +27,56 @@ struct TopArgs {
     float *log_norm;           // [rows] or NULL
 };
 
+// Places up to here come from counting the larger entries, more from a sort: at 128
+// entries both take about a microsecond of a block.
+constexpr uint32_t kCounted = 128;
+
 template <int TYPE, class L>
 __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
-    extern __shared__ uint64_t lists[];                   // [rows of the block][min(k, n)]
+    typedef Piece<TYPE, L::VEC> P;
+    constexpr int G = L::G;
     __shared__ Scratch scratch;
+    __shared__ uint64_t lists[L::kGroups][L::kList];
     __shared__ uint32_t fills[L::kGroups];
-    const int gi = threadIdx.x / L::G;
+    const int gi = threadIdx.x / G;
     const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
     if (r >= a.n_rows)
         return;
-    Group<L::G> g(threadIdx.x % L::G, &scratch);
-    const int cap = min(a.k, a.n);
-    uint64_t *list = lists + (int64_t)gi * cap;
-    uint32_t *fill = fills + gi;
+    Group<G> g(threadIdx.x % G, &scratch);
+    uint64_t *list = lists[gi];
+    uint32_t *fill = &fills[gi];
     if (g.t == 0)
         *fill = 0;
     const char *src = a.logits + r * a.stride;
-    const Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
+    Row<TYPE, G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
 
     const float c = a.inv_t * kLog2e;
     Softmax sm = {-__builtin_inff(), 0.0f};
-    Cmp top = E::lowest();
+    Cmp top = E::lowest(), most[L::NV];                   // the lane's and its pieces' largest
     uint32_t valid = 0;
-    row.each([&](int, int32_t, const Piece<TYPE, L::VEC> &p) {
-        float z[L::VEC], zm = -__builtin_inff();
+    row.each([&](int j, int32_t, const P &p) {
+        Cmp vm = E::lowest();
 #pragma unroll
         for (int u = 0; u < L::VEC; ++u) {
             const Cmp v = p.get(u);
             const bool in = v > E::lowest();
             valid += in;
-            top = in && v > top ? v : top;
-            z[u] = in ? E::to_float(v) : -__builtin_inff();
-            zm = fmaxf(zm, z[u]);
+            vm = in && v > vm ? v : vm;
         }
-        sm.raise(zm, c);
+        sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
         const float from = sm.from();
 #pragma unroll
-        for (int u = 0; u < L::VEC; ++u)
-            sm.s += __builtin_amdgcn_exp2f((z[u] - from) * c);
+        for (int u = 0; u < L::VEC; ++u) {
+            const Cmp v = p.get(u);
+            const float z = v > E::lowest() ? E::to_float(v) : -__builtin_inff();
+            sm.s += __builtin_amdgcn_exp2f((z - from) * c);
+        }
+        top = vm > top ? vm : top;
+        if constexpr (L::RESIDENT)
+            most[j] = vm;
     });
     if (a.log_norm) {
         sm = combine(g, sm, c);
@@ -72,78 +84,118 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
             a.log_norm[r] = sm.log_norm(a.inv_t);
     }
     const uint32_t k = min((uint32_t)a.k, g.reduce(valid, Add()));
-    top = g.reduce(top, Max());
 
-    uint32_t lo = E::kFirstKey, hi = E::key(top) + 1;     // count(>= lo) >= k > count(>= hi)
-    while (k && hi - lo > 1) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const Cmp at = E::from_key(mid);
-        uint32_t count = 0;
-        row.each([&](int, int32_t, const Piece<TYPE, L::VEC> &p) {
-#pragma unroll
-            for (int u = 0; u < L::VEC; ++u)
-                count += p.get(u) >= at;
-        });
-        if (g.reduce(count, Add()) >= k)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    const Cmp tau = E::from_key(lo);
-    g.barrier();
-    if (k)
-        row.each([&](int, int32_t i, const Piece<TYPE, L::VEC> &p) {
+    // entries of logits >= at into the list, as many as it holds; their number
+    const auto collect = [&](Cmp at) __attribute__((always_inline)) {
+        row.each([&](int j, int32_t i, const P &p) {
+            if constexpr (L::RESIDENT)
+                if (!(most[j] >= at))
+                    return;
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
                 const Cmp v = p.get(u);
-                if (v > tau)
-                    list[atomicAdd(fill, 1u)] = (uint64_t)E::key(v) << 32 | ~(uint32_t)(i + u);
+                if (v >= at) {
+                    const uint32_t to = atomicAdd(fill, 1u);
+                    if (to < (uint32_t)L::kList)
+                        list[to] = entry(E::key(v), i + u);
+                }
             }
         });
-    g.barrier();
-    uint32_t taken = *fill;                               // then the equal ones, by class
-    g.barrier();
-    row.each([&](int, int32_t i, const Piece<TYPE, L::VEC> &p) {
-        if (taken >= k)
-            return;
-        uint32_t mine = 0, total;
-#pragma unroll
-        for (int u = 0; u < L::VEC; ++u)
-            mine += p.get(u) == tau;
-        uint32_t place = taken + g.scan(mine, total);
-        taken += total;
-#pragma unroll
-        for (int u = 0; u < L::VEC; ++u)
-            if (p.get(u) == tau) {
-                if (place < k)
-                    list[place] = (uint64_t)lo << 32 | ~(uint32_t)(i + u);
-                ++place;
-            }
-    });
-    g.barrier();
+        g.barrier();
+        return *fill;
+    };
 
+    uint32_t lo = E::kFirstKey, found = 0;
+    if (k) {
+        if constexpr (G >= kWave) {
+            // W waves of which m lanes each have a logit >= lo: W m >= k of them
+            constexpr uint32_t W = G / kWave;
+            const uint32_t m = (k + W - 1) / W;
+            if (m <= kWave) {
+                const uint32_t mine = top > E::lowest() ? E::key(top) : 0;
+                lo = max(lo, ~g.reduce(~wave_mth(mine, m), Max()));
+            }
+            found = collect(E::from_key(lo));
+        }
+        if (G < kWave || found > (uint32_t)L::kList) {
+            // exactly: count(>= lo) >= k > count(>= hi)
+            uint32_t hi = E::key(g.reduce(top, Max())) + 1;
+            while (hi - lo > 1) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                const Cmp at = E::from_key(mid);
+                uint32_t count = 0;
+                row.each([&](int, int32_t, const P &p) {
+#pragma unroll
+                    for (int u = 0; u < L::VEC; ++u)
+                        count += p.get(u) >= at;
+                });
+                if (g.reduce(count, Add()) >= k)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            // those above, then the first classes of the equal ones
+            const Cmp tau = E::from_key(lo);
+            if (g.t == 0)
+                *fill = 0;
+            g.barrier();
+            row.each([&](int, int32_t i, const P &p) {
+#pragma unroll
+                for (int u = 0; u < L::VEC; ++u) {
+                    const Cmp v = p.get(u);
+                    if (v > tau)
+                        list[atomicAdd(fill, 1u)] = entry(E::key(v), i + u);
+                }
+            });
+            g.barrier();
+            found = *fill;
+            row.each([&](int, int32_t i, const P &p) {
+                if (found >= k)
+                    return;
+                uint32_t mine = 0, total;
+#pragma unroll
+                for (int u = 0; u < L::VEC; ++u)
+                    mine += p.get(u) == tau;
+                uint32_t place = found + g.scan(mine, total);
+                found += total;
+#pragma unroll
+                for (int u = 0; u < L::VEC; ++u)
+                    if (p.get(u) == tau) {
+                        if (place < k)
+                            list[place] = entry(lo, i + u);
+                        ++place;
+                    }
+            });
+            found = k;
+            g.barrier();
+        }
+    }
+
+    // the list in order
+    const bool counted = found <= kCounted;
+    if (!counted)
+        sort_entries(g, list, found);
     char *values = a.values + r * a.k * E::kBytes;
     int32_t *indices = a.indices + r * a.k;
-    for (uint32_t e = g.t; e < (uint32_t)a.k; e += L::G) {
-        uint32_t to = e;
-        int32_t cls = -1;
-        if (e < k) {
-            const uint64_t mine = list[e];
-            to = 0;
-            for (uint32_t f = 0; f < k; ++f)
-                to += list[f] > mine;
-            cls = (int32_t)~(uint32_t)mine;
-        }
+    const auto put = [&](uint32_t to, int32_t cls, Cmp v) {
+        if (TYPE != kI32 && v == 0)
+            v = load_one<TYPE>(src, cls);                 // with its sign
         indices[to] = cls;
         if constexpr (E::kBytes == 4)
-            reinterpret_cast<uint32_t *>(values)[to] =
-                cls >= 0 ? reinterpret_cast<const uint32_t *>(src)[cls]
-                         : TYPE == kI32 ? 0x80000000u : 0xFF800000u;
+            reinterpret_cast<Cmp *>(values)[to] = v;
+        else if constexpr (TYPE == kF16)
+            reinterpret_cast<_Float16 *>(values)[to] = (_Float16)v;
         else
-            reinterpret_cast<uint16_t *>(values)[to] =
-                cls >= 0 ? reinterpret_cast<const uint16_t *>(src)[cls]
-                         : TYPE == kF16 ? 0xFC00u : 0xFF80u;
+            reinterpret_cast<uint16_t *>(values)[to] = __float_as_uint(v) >> 16;
+    };
+    for (uint32_t e = g.t; e < (counted ? found : k); e += G) {
+        const uint64_t mine = list[e];
+        const uint32_t to = counted ? place_of(mine, list, found) : e;
+        if (to < k)
+            put(to, class_of(mine), E::from_key(key_of(mine)));
     }
+    for (uint32_t e = k + g.t; e < (uint32_t)a.k; e += G)
+        put(e, -1, E::lowest());
 }
 
 }  // namespace
@@ -158,8 +210,7 @@ hipError_t launch_top_logits(const void *logits, int32_t type, int64_t n_rows, i
                            n_rows, n, k, inv_t, static_cast<char *>(values), indices, log_norm};
         return with_layout<TYPE>(n, 0, [&](auto layout) {
             typedef decltype(layout) L;
-            const size_t lds = (size_t)L::kGroups * (k < n ? k : n) * sizeof(uint64_t);
-            k_top<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock, lds,
+            k_top<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock, 0,
                              stream>>>(a);
             return hipGetLastError();
         });
