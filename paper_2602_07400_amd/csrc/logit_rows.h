@@ -421,13 +421,154 @@ __device__ __forceinline__ uint32_t wave_mth(uint32_t key, uint32_t m)
             lo = mid;
         else
             hi = mid;
-        if (count >= m && count <= m + m / 8)
+        if (count >= m && count <= m + m / 4)
             break;
     }
     return lo;
 }
 
-// c entries in descending order, in place; room for the next power of two.
+// Appends the row's entries with lo <= logit < hi to a list in LDS (fill: its length,
+// cleared here), as many as it holds, and returns their number.  most: the largest
+// logit of each of the lane's pieces; a piece that has candidates is loaded again, in
+// a loop, since 16 pieces' unrolled searches take longer to fetch than to run.
+template <int TYPE, class L, class R>
+__device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
+                                            const typename Elem<TYPE>::Cmp (&most)[L::NV],
+                                            typename Elem<TYPE>::Cmp lo, bool below,
+                                            typename Elem<TYPE>::Cmp hi, uint64_t *list,
+                                            uint32_t *fill)
+{
+    typedef Elem<TYPE> E;
+    const auto search = [&](int32_t i, const Piece<TYPE, L::VEC> &p) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < L::VEC; ++u) {
+            const typename E::Cmp v = p.get(u);
+            if (v >= lo && !(below && v >= hi)) {
+                const uint32_t to = atomicAdd(fill, 1u);
+                if (to < (uint32_t)L::kList)
+                    list[to] = entry(E::key(v), i + u);
+            }
+        }
+    };
+    g.barrier();
+    if (g.t == 0)
+        *fill = 0;
+    g.barrier();
+    if constexpr (L::RESIDENT) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < L::NV; ++j)
+            hits |= (uint32_t)(most[j] >= lo) << j;
+        while (hits) {
+            const int j = __builtin_ctz(hits);
+            hits &= hits - 1;
+            const int32_t i = (j * L::G + g.t) * L::VEC;
+            Piece<TYPE, L::VEC> p;
+            p.load(row.row, i, row.n);
+            search(i, p);
+        }
+    } else {
+        row.each([&](int, int32_t i, const Piece<TYPE, L::VEC> &p) { search(i, p); });
+    }
+    g.barrier();
+    return *fill;
+}
+
+// A key >= lo that still has k classes at or above it, where lo has (top: the row's
+// largest key), by counting keys in kBins equal intervals up to top in LDS.
+constexpr uint32_t kBins = 2048;
+
+template <int TYPE, class L, class R>
+__device__ __forceinline__ uint32_t raise_bound(Group<L::G> &g, R &row, uint32_t lo,
+                                                uint32_t top, uint32_t k, uint32_t *bins)
+{
+    typedef Elem<TYPE> E;
+    constexpr int kRun = kBins / L::G;
+    uint32_t shift = 0;
+    while ((top - lo) >> shift >= kBins)
+        ++shift;
+    g.barrier();
+    for (uint32_t b = g.t; b < kBins; b += L::G)
+        bins[b] = 0;
+    g.barrier();
+    const typename E::Cmp at = E::from_key(lo);
+    row.each([&](int, int32_t, const Piece<TYPE, L::VEC> &p) {
+#pragma unroll
+        for (int u = 0; u < L::VEC; ++u) {
+            const typename E::Cmp v = p.get(u);
+            if (v >= at)
+                atomicAdd(&bins[(top - E::key(v)) >> shift], 1u);
+        }
+    });
+    g.barrier();
+    uint32_t mine = 0, total, last = 0;
+    for (int b = 0; b < kRun; ++b)
+        mine += bins[g.t * kRun + b];
+    uint32_t before = g.scan(mine, total);
+    for (int b = 0; b < kRun; ++b) {
+        const uint32_t here = bins[g.t * kRun + b];
+        if (before < k && before + here >= k)
+            last = g.t * kRun + b + 1;
+        before += here;
+    }
+    last = g.reduce(last, Max());                         // 1 + the bin with the k-th
+    const uint64_t span = (uint64_t)last << shift;
+    return last && span <= top - lo ? top - (uint32_t)span + 1 : lo;
+}
+
+// Sorting: each lane has EPL neighbouring entries in registers; exchanges within a
+// lane and a wave need no barrier, only those between waves go through LDS.
+template <int EPL, int G>
+__device__ __forceinline__ void sort_runs(Group<G> &g, uint64_t *e, uint32_t p)
+{
+    constexpr uint32_t kInWave = (G < kWave ? G : kWave) * EPL;
+    uint64_t x[EPL];
+    const uint32_t first = g.t * EPL;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+        x[i] = first + i < p ? e[first + i] : 0;
+    for (uint32_t size = 2; size <= p; size *= 2)
+        for (uint32_t stride = size / 2; stride; stride /= 2) {
+            uint64_t y[EPL];
+            if (stride >= kInWave) {
+                g.barrier();
+#pragma unroll
+                for (int i = 0; i < EPL; ++i)
+                    if (first + i < p)
+                        e[first + i] = x[i];
+                g.barrier();
+#pragma unroll
+                for (int i = 0; i < EPL; ++i)
+                    y[i] = first + i < p ? e[(first + i) ^ stride] : 0;
+            } else if (stride >= EPL) {
+#pragma unroll
+                for (int i = 0; i < EPL; ++i)
+                    y[i] = __shfl_xor(x[i], (int)(stride / EPL));
+            } else {
+#pragma unroll
+                for (int d = 1; d < EPL; d *= 2)
+                    if (stride == (uint32_t)d)
+#pragma unroll
+                        for (int i = 0; i < EPL; ++i)
+                            y[i] = x[i ^ d];
+            }
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                const uint32_t at = first + i;
+                const bool larger = !(at & stride) == !(at & size);
+                x[i] = (x[i] > y[i]) == larger ? x[i] : y[i];
+            }
+        }
+    g.barrier();
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+        if (first + i < p)
+            e[first + i] = x[i];
+    g.barrier();
+}
+
+// c entries, at most 4 G of a block and 16 G of a wave, in descending order, in place;
+// room for the next power of two.
 template <int G>
 __device__ __forceinline__ void sort_entries(Group<G> &g, uint64_t *e, uint32_t c)
 {
@@ -436,29 +577,47 @@ __device__ __forceinline__ void sort_entries(Group<G> &g, uint64_t *e, uint32_t 
         p *= 2;
     for (uint32_t i = c + g.t; i < p; i += G)
         e[i] = 0;
-    for (uint32_t size = 2; size <= p; size *= 2)
-        for (uint32_t stride = size / 2; stride; stride /= 2) {
-            g.barrier();
-            for (uint32_t i = g.t; i < p / 2; i += G) {
-                const uint32_t a = 2 * i - (i & (stride - 1)), b = a + stride;
-                const uint64_t x = e[a], y = e[b];
-                if ((x < y) == !(a & size)) {
-                    e[a] = y;
-                    e[b] = x;
-                }
-            }
-        }
     g.barrier();
+    if (p <= G)
+        sort_runs<1>(g, e, p);
+    else if (p <= 2 * G)
+        sort_runs<2>(g, e, p);
+    else if (G > kWave || p <= 4 * G)
+        sort_runs<4>(g, e, p);
+    else if constexpr (G <= kWave)
+        sort_runs<16>(g, e, p);
 }
 
-// How many of c entries are larger than mine.
-__device__ __forceinline__ uint32_t place_of(uint64_t mine, const uint64_t *e, uint32_t c)
+// c entries in descending order to `to`: an entry's place is the number of larger
+// ones, counted by G / (next power of two of c) neighbouring lanes.  f(entry) runs
+// for every entry before the counting, and its result goes to with[place].
+template <int G, class F>
+__device__ __forceinline__ void place_entries(Group<G> &g, const uint64_t *e, uint32_t c,
+                                              uint64_t *to, float *with, F f)
 {
-    uint32_t place = 0;
-#pragma unroll 8
-    for (uint32_t f = 0; f < c; ++f)
-        place += e[f] > mine;
-    return place;
+    uint32_t lanes = G;                                   // for an entry
+    while (lanes > 1 && c * lanes > G)
+        lanes /= 2;
+    lanes = min(lanes, 16u);
+    for (uint32_t base = 0; base < c; base += G / lanes) {
+        const uint32_t at = base + g.t / lanes;
+        const uint64_t mine = at < c ? e[at] : 0;
+        float number = 0.0f;
+        if (at < c && g.t % lanes == 0)
+            number = f(mine);
+        uint32_t place = 0;
+        if (at < c)
+            for (uint32_t i = g.t % lanes; i < c; i += lanes)
+                place += e[i] > mine;
+        for (uint32_t d = 1; d < lanes; d *= 2)
+            place += __shfl_xor(place, (int)d);
+        if (at < c && g.t % lanes == 0) {
+            to[place] = mine;
+            if (with)
+                with[place] = number;
+        }
+    }
+    g.barrier();
 }
 
 // ---- which group holds rows of n classes ----
@@ -468,8 +627,14 @@ struct Layout {
     static constexpr bool RESIDENT = RESIDENT_;
     static constexpr int kBlock = G < 256 ? 256 : G;
     static constexpr int kGroups = kBlock / G;            // rows of a block
-    // candidates of a row that LDS holds (a power of two; all n classes of a wave's row)
-    static constexpr int kList = G == 1024 ? 4096 : G == 256 ? 2048 : NV * VEC * G;
+    // Candidates of a row that LDS holds (a power of two; all the classes of a row
+    // within a wave), and how many are put in order by counting rather than sorting:
+    // c entries compare c^2 / G times a lane, 128 of them as long as a sort takes.
+    static constexpr int kList = G == 1024 ? 4096 : G == 256 ? 1024 : NV * VEC * G;
+    static constexpr int kCounted = G == 1024 ? 352 : G == 256 ? 176 : G == 64 ? 88 : NV * VEC * G;
+    // waves a SIMD to compile for: two blocks of short rows a CU
+    static constexpr int kWavesPerSimd =
+        !RESIDENT || G == kWave || NV * (VEC > 4 ? 4 : VEC) > 16 ? 4 : 8;
 };
 
 // f(Layout) for rows of n classes of a type whose lists have up to k entries a row.

@@ -4,10 +4,11 @@
 // One pass over the row, as it arrives, takes the running maximum and sum of the
 // softmax and every lane's largest logit.  If m lanes in each of a row's W waves have
 // a logit >= lo, W m >= k classes have: the classes >= lo, a few more than k, go to a
-// list in LDS that is put in order.  Where the bound does not hold so few (many equal
-// logits, or k far above the lanes), tau, the k-th largest key, is found by bisection
-// on counts (key >= tau), and the list gets the classes above tau and the first ones
-// equal to it.  Entries (key, class) are unique, so the order in which the list fills
+// list in LDS that is put in order.  Where the bound does not hold so few (k near the
+// number of lanes), counts of keys in 2048 intervals raise it; where that does not
+// either (many equal logits), tau, the k-th largest key, is found by bisection on
+// counts (key >= tau), and the list gets the classes above tau and the first ones equal
+// to it.  Entries (key, class) are unique, so the order in which the list fills
 // does not matter.
 #include "logit_rows.h"
 
@@ -27,12 +28,8 @@ struct TopArgs {
     float *log_norm;           // [rows] or NULL
 };
 
-// Places up to here come from counting the larger entries, more from a sort: at 128
-// entries both take about a microsecond of a block.
-constexpr uint32_t kCounted = 128;
-
 template <int TYPE, class L>
-__global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
+__global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
@@ -40,6 +37,7 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
     constexpr int G = L::G;
     __shared__ Scratch scratch;
     __shared__ uint64_t lists[L::kGroups][L::kList];
+    __shared__ uint64_t placed[L::kGroups][L::kCounted];
     __shared__ uint32_t fills[L::kGroups];
     const int gi = threadIdx.x / G;
     const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
@@ -48,8 +46,6 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
     Group<G> g(threadIdx.x % G, &scratch);
     uint64_t *list = lists[gi];
     uint32_t *fill = &fills[gi];
-    if (g.t == 0)
-        *fill = 0;
     const char *src = a.logits + r * a.stride;
     Row<TYPE, G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
 
@@ -85,26 +81,6 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
     }
     const uint32_t k = min((uint32_t)a.k, g.reduce(valid, Add()));
 
-    // entries of logits >= at into the list, as many as it holds; their number
-    const auto collect = [&](Cmp at) __attribute__((always_inline)) {
-        row.each([&](int j, int32_t i, const P &p) {
-            if constexpr (L::RESIDENT)
-                if (!(most[j] >= at))
-                    return;
-#pragma unroll
-            for (int u = 0; u < L::VEC; ++u) {
-                const Cmp v = p.get(u);
-                if (v >= at) {
-                    const uint32_t to = atomicAdd(fill, 1u);
-                    if (to < (uint32_t)L::kList)
-                        list[to] = entry(E::key(v), i + u);
-                }
-            }
-        });
-        g.barrier();
-        return *fill;
-    };
-
     uint32_t lo = E::kFirstKey, found = 0;
     if (k) {
         if constexpr (G >= kWave) {
@@ -115,7 +91,14 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
                 const uint32_t mine = top > E::lowest() ? E::key(top) : 0;
                 lo = max(lo, ~g.reduce(~wave_mth(mine, m), Max()));
             }
-            found = collect(E::from_key(lo));
+            found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top, list, fill);
+            if constexpr (G > kWave)
+                if (found > (uint32_t)L::kList) {
+                    const uint32_t end = E::key(g.reduce(top, Max()));
+                    lo = raise_bound<TYPE, L>(g, row, lo, end, k, (uint32_t *)list);
+                    found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top, list,
+                                             fill);
+                }
         }
         if (G < kWave || found > (uint32_t)L::kList) {
             // exactly: count(>= lo) >= k > count(>= hi)
@@ -136,6 +119,7 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
             }
             // those above, then the first classes of the equal ones
             const Cmp tau = E::from_key(lo);
+            g.barrier();
             if (g.t == 0)
                 *fill = 0;
             g.barrier();
@@ -172,9 +156,12 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
     }
 
     // the list in order
-    const bool counted = found <= kCounted;
-    if (!counted)
+    if (found <= (uint32_t)L::kCounted) {
+        place_entries(g, list, found, placed[gi], nullptr, [](uint64_t) { return 0.0f; });
+        list = placed[gi];
+    } else if constexpr (G >= kWave) {
         sort_entries(g, list, found);
+    }
     char *values = a.values + r * a.k * E::kBytes;
     int32_t *indices = a.indices + r * a.k;
     const auto put = [&](uint32_t to, int32_t cls, Cmp v) {
@@ -188,12 +175,8 @@ __global__ __launch_bounds__(L::kBlock) void k_top(TopArgs a)
         else
             reinterpret_cast<uint16_t *>(values)[to] = __float_as_uint(v) >> 16;
     };
-    for (uint32_t e = g.t; e < (counted ? found : k); e += G) {
-        const uint64_t mine = list[e];
-        const uint32_t to = counted ? place_of(mine, list, found) : e;
-        if (to < k)
-            put(to, class_of(mine), E::from_key(key_of(mine)));
-    }
+    for (uint32_t e = g.t; e < k; e += G)
+        put(e, class_of(list[e]), E::from_key(key_of(list[e])));
     for (uint32_t e = k + g.t; e < (uint32_t)a.k; e += G)
         put(e, -1, E::lowest());
 }
