@@ -40,17 +40,23 @@ struct DistillArgs {
 };
 
 template <int TYPE, int VEC>
-__device__ __forceinline__ void store_piece(char *row, int32_t i, int32_t n, const float (&v)[VEC])
+__device__ __forceinline__ void store_piece(char *row, int32_t first, int32_t i, int32_t n,
+                                            const float (&v)[VEC])
 {
     if constexpr (TYPE == kF32) {
-        float *o = reinterpret_cast<float *>(row) + i;
+        float *o = reinterpret_cast<float *>(row) + first + (uint32_t)i;
+        i += first;
         if (i + VEC <= n) {
             __builtin_memcpy(o, v, sizeof v);
-        } else {
+        } else if constexpr (VEC > 1) {                   // the end of the row
+            float left[VEC];
+            __builtin_memcpy(left, v, sizeof v);
+            for (int u = 0; u < n - i; ++u) {
+                o[u] = left[0];
 #pragma unroll
-            for (int u = 0; u < VEC; ++u)
-                if (i + u < n)
-                    o[u] = v[u];
+                for (int k = 0; k < VEC - 1; ++k)
+                    left[k] = left[k + 1];
+            }
         }
     } else {
         typedef typename std::conditional<TYPE == kF16, _Float16, __bf16>::type H;
@@ -66,14 +72,20 @@ __device__ __forceinline__ void store_piece(char *row, int32_t i, int32_t n, con
                 h[u + 1] = two[1];
             }
         }
-        H *o = reinterpret_cast<H *>(row) + i;
+        H *o = reinterpret_cast<H *>(row) + first + (uint32_t)i;
+        i += first;
         if (i + VEC <= n) {
             __builtin_memcpy(o, h, sizeof h);
-        } else {
+        } else if constexpr (VEC > 1) {
+            uint32_t left[VEC / 2];
+            __builtin_memcpy(left, h, sizeof h);
+            for (int u = 0; u < n - i; ++u) {
+                reinterpret_cast<uint16_t *>(o)[u] = (uint16_t)left[0];
 #pragma unroll
-            for (int u = 0; u < VEC; ++u)
-                if (i + u < n)
-                    o[u] = h[u];
+                for (int k = 0; k < VEC / 2 - 1; ++k)
+                    left[k] = __builtin_amdgcn_alignbit(left[k + 1], left[k], 16);
+                left[VEC / 2 - 1] >>= 16;
+            }
         }
     }
 }
@@ -93,11 +105,11 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
     __shared__ Scratch scratch;
     __shared__ int32_t heads[L::kBlock];                  // first entry of the lane's list
     __shared__ uint32_t marks[L::kBlock];                 // bit j % 32: an entry in piece j
-    const int gi = threadIdx.x / L::G;
+    const int gi = group_of<L::G>();
     const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
     if (r >= a.n_rows)
         return;
-    Group<L::G> g(threadIdx.x % L::G, &scratch);
+    Group<L::G> g(threadIdx.x - gi * L::G, &scratch);
     Entry *list = entries + (int64_t)gi * a.k;
     int32_t *head = heads + gi * L::G;
     uint32_t *mark = marks + gi * L::G;
@@ -153,7 +165,7 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
         g.barrier();
         const uint32_t marked = rest ? mark[g.t] : 0;
         Softmax sm = {-__builtin_inff(), 0.0f};
-        row.each([&](int j, int32_t, const P &given) {
+        row.each([&](auto j, int32_t, const P &given) {
             P p = given;
             if (marked >> (j % 32) & 1)
                 for (int e = head[g.t]; e >= 0; e = list[e].next)
@@ -220,12 +232,12 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
             return;
         if (scale == 0.0f) {
             const float zero[L::VEC] = {};
-            for (int32_t i = g.t * L::VEC; i < a.n; i += L::G * L::VEC)
-                store_piece<TYPE, L::VEC>(dst, i, a.n, zero);
+            for (int32_t i = 0; i < a.n; i += L::kSpan)
+                store_piece<TYPE, L::VEC>(dst, i, g.t * L::VEC, a.n, zero);
             return;
         }
         const uint32_t marked = mark[g.t];
-        row.each([&](int j, int32_t i, const P &p) {
+        row.each([&](auto j, int32_t i, const P &p) {
             float v[L::VEC];
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
@@ -238,7 +250,7 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
                             if (u == list[e].cls % L::VEC)
                                 v[u] = list[e].t;
                     }
-            store_piece<TYPE, L::VEC>(dst, i, a.n, v);
+            store_piece<TYPE, L::VEC>(dst, i - g.t * L::VEC, g.t * L::VEC, a.n, v);
         });
     }
 }

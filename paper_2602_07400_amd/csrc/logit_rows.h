@@ -27,6 +27,17 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// f(integral_constant 0), ..., f(integral_constant N - 1): indexes of registers that are
+// constants before any loop is unrolled.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void static_for(F &&f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        static_for<N, I + 1>(f);
+    }
+}
+
 // ---- element types ----
 // Cmp: what elements are compared as; kShift: key bits below the type's own.
 template <int TYPE>
@@ -120,10 +131,12 @@ struct Piece {
         for (int i = 0; i < kWords; ++i)
             w[i] = m;
     }
-    // elements [i, i + VEC) of a row of n; those past it are masked
-    __device__ __forceinline__ void load(const char *row, int32_t i, int32_t n)
+    // elements [first + i, first + i + VEC) of a row of n, `first` the same in the whole
+    // wave (an address in scalar registers and a 32-bit offset); those past it are masked
+    __device__ __forceinline__ void load(const char *row, int32_t first, int32_t i, int32_t n)
     {
-        const char *p = row + (int64_t)i * Elem<TYPE>::kBytes;
+        const char *p = row + (int64_t)first * Elem<TYPE>::kBytes + (uint32_t)(i * Elem<TYPE>::kBytes);
+        i += first;
         if (i + VEC <= n) {
             if constexpr (VEC * Elem<TYPE>::kBytes >= 4) {
                 __builtin_memcpy(w, p, sizeof w);
@@ -133,16 +146,21 @@ struct Piece {
             return;
         }
         fill_masked();
-        if constexpr (VEC > 1) {
+        // the end of the row: from its last element on, each pushes the ones behind it up
+        if constexpr (VEC > 1)
+            for (int u = n - i - 1; u >= 0; --u) {
+                if constexpr (Elem<TYPE>::kBytes == 4) {
 #pragma unroll
-            for (int u = 0; u < VEC - 1; ++u)
-                if (i + u < n) {
-                    if constexpr (Elem<TYPE>::kBytes == 4)
-                        w[u] = reinterpret_cast<const uint32_t *>(p)[u];
-                    else
-                        put16(u, reinterpret_cast<const uint16_t *>(p)[u]);
+                    for (int k = kWords - 1; k > 0; --k)
+                        w[k] = w[k - 1];
+                    w[0] = reinterpret_cast<const uint32_t *>(p)[u];
+                } else {
+#pragma unroll
+                    for (int k = kWords - 1; k > 0; --k)
+                        w[k] = __builtin_amdgcn_alignbit(w[k], w[k - 1], 16);
+                    w[0] = w[0] << 16 | reinterpret_cast<const uint16_t *>(p)[u];
                 }
-        }
+            }
     }
     __device__ __forceinline__ void put16(int u, uint32_t v)
     {
@@ -309,7 +327,7 @@ struct Row {
     typedef typename Elem<TYPE>::Cmp Cmp;
     typedef Piece<TYPE, VEC> P;
     static constexpr int kSpan = G * VEC;                 // elements of one piece per lane
-    static constexpr int kFlight = RESIDENT ? 1 : 4;      // pieces loaded together
+    static constexpr int kFlight = 4;                     // pieces that stream() loads together
     const char *row;
     int32_t n, t;
     P piece[RESIDENT ? NV : 1];
@@ -321,39 +339,57 @@ struct Row {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if (j * kSpan < n)
-                    piece[j].load(row, j * kSpan + t * VEC, n);
+                    piece[j].load(row, j * kSpan, t * VEC, n);
                 else
                     piece[j].fill_masked();
             }
         }
     }
 
-    // f(j, its first element, piece j) in index order of the pieces
+    // f(j, its first element, piece j) in index order of the pieces; j is an
+    // integral_constant where the row is in registers
     template <class F>
     __device__ __forceinline__ void each(F f)
     {
-        if constexpr (RESIDENT) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
+        if constexpr (RESIDENT)
+            static_for<NV>([&](auto J) __attribute__((always_inline)) {
+                constexpr int j = decltype(J)::value;
                 if (j * kSpan < n) {
-                    // every pass unpacks the elements again: kept unpacked from an
-                    // earlier one, they would take more registers than there are
-                    if constexpr (VEC > 1)
-#pragma unroll
-                        for (int i = 0; i < P::kWords; ++i)
-                            asm("" : "+v"(piece[j].w[i]));
-                    f(j, j * kSpan + t * VEC, piece[j]);
+                    again<j>();
+                    f(J, j * kSpan + t * VEC, piece[j]);
                 }
-        } else {
-            for (int32_t i = 0; i < n; i += kFlight * kSpan) {
-                P p[kFlight];
+            });
+        else
+            stream<kFlight>([&](int32_t i, const P &p) __attribute__((always_inline)) {
+                f(i / kSpan, i, p);
+            });
+    }
+
+    // Piece j to be unpacked again: kept unpacked from an earlier pass, the elements
+    // would take more registers than there are.
+    template <int j>
+    __device__ __forceinline__ void again()
+    {
+        if constexpr (VEC > 1)
 #pragma unroll
-                for (int j = 0; j < kFlight; ++j)
-                    p[j].load(row, i + j * kSpan + t * VEC, n);
-#pragma unroll
-                for (int j = 0; j < kFlight; ++j)
-                    f(i / kSpan + j, i + j * kSpan + t * VEC, p[j]);
-            }
+            for (int i = 0; i < P::kWords; ++i)
+                asm("" : "+v"(piece[j].w[i]));
+    }
+
+    // f(first element, piece) for all pieces, read again from memory in a loop: what is
+    // seldom done, since unrolled over the registers it makes long code that holds
+    // registers from what is done always
+    template <int FLIGHT = kFlight, class F>
+    __device__ __forceinline__ void stream(F f) const
+    {
+        for (int32_t i = 0; i < n; i += FLIGHT * kSpan) {
+            P p[FLIGHT];
+            static_for<FLIGHT>([&](auto j) __attribute__((always_inline)) {
+                p[j].load(row, i + j * kSpan, t * VEC, n);
+            });
+            static_for<FLIGHT>([&](auto j) __attribute__((always_inline)) {
+                f(i + j * kSpan + t * VEC, p[j]);
+            });
         }
     }
 };
@@ -406,23 +442,49 @@ __device__ __forceinline__ uint64_t entry(uint32_t key, int32_t cls)
 __device__ __forceinline__ int32_t class_of(uint64_t e) { return (int32_t)~(uint32_t)e; }
 __device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
 
-// The largest key of which at least m lanes of a whole wave have as much (1 <= m <=
-// 64), or a little less where that ends the search early: never too much.
-__device__ __forceinline__ uint32_t wave_mth(uint32_t key, uint32_t m)
+// A key that at least m of the group's G keys (one a lane, 1 <= m <= G) reach: the
+// m-th largest, or a little less where that ends the search early.  room: G words of
+// LDS.  A group of several waves leaves the search to its first one.
+template <int G>
+__device__ __forceinline__ uint32_t group_mth(Group<G> &g, uint32_t key, uint32_t m,
+                                              uint32_t *room)
 {
-    uint32_t hi = wave_reduce<kWave>(key, Max()), lo = wave_reduce<kWave>(~key, Max());
-    lo = ~lo;                                             // every lane has it
-    if (m <= 1)
-        return hi;
-    while (hi - lo > 1) {                                 // count(>= lo) >= m > count(> hi)
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const uint32_t count = __popcll(__ballot(key >= mid));
-        if (count >= m)
-            lo = mid;
-        else
-            hi = mid;
-        if (count >= m && count <= m + m / 4)
-            break;
+    constexpr int N = G / kWave;
+    uint32_t lo = 0;
+    if constexpr (N > 1) {
+        room[g.t] = key;
+        g.barrier();
+    }
+    if (g.t < kWave) {
+        uint32_t keys[N], hi = 0, no = 0;                 // no: ~ the least
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            keys[i] = N > 1 ? room[i * kWave + g.t] : key;
+            hi = max(hi, keys[i]);
+            no = max(no, ~keys[i]);
+        }
+        hi = wave_reduce<kWave>(hi, Max());
+        lo = ~wave_reduce<kWave>(no, Max());
+        while (hi - lo > 1) {                             // count(>= lo) >= m
+            const uint32_t mid = lo + (hi - lo) / 2;
+            uint32_t count = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                count += __popcll(__ballot(keys[i] >= mid));
+            if (count >= m)
+                lo = mid;
+            else
+                hi = mid;
+            if (count >= m && count <= m + m / 8)
+                break;
+        }
+    }
+    if constexpr (N > 1) {
+        g.barrier();
+        if (g.t == 0)
+            room[0] = lo;
+        g.barrier();
+        lo = room[0];
     }
     return lo;
 }
@@ -440,15 +502,20 @@ __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
 {
     typedef Elem<TYPE> E;
     const auto search = [&](int32_t i, const Piece<TYPE, L::VEC> &p) __attribute__((always_inline)) {
+        uint32_t in = 0;
 #pragma unroll
-        for (int u = 0; u < L::VEC; ++u) {
-            const typename E::Cmp v = p.get(u);
-            if (v >= lo && !(below && v >= hi)) {
-                const uint32_t to = atomicAdd(fill, 1u);
+        for (int u = 0; u < L::VEC; ++u)
+            in |= (uint32_t)(p.get(u) >= lo && !(below && p.get(u) >= hi)) << u;
+        if (!in)
+            return;
+        uint32_t to = atomicAdd(fill, __builtin_popcount(in));
+#pragma unroll
+        for (int u = 0; u < L::VEC; ++u)
+            if (in >> u & 1) {
                 if (to < (uint32_t)L::kList)
-                    list[to] = entry(E::key(v), i + u);
+                    list[to] = entry(E::key(p.get(u)), i + u);
+                ++to;
             }
-        }
     };
     g.barrier();
     if (g.t == 0)
@@ -456,64 +523,130 @@ __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
     g.barrier();
     if constexpr (L::RESIDENT) {
         uint32_t hits = 0;
-#pragma unroll
-        for (int j = 0; j < L::NV; ++j)
+        static_for<L::NV>([&](auto j) __attribute__((always_inline)) {
             hits |= (uint32_t)(most[j] >= lo) << j;
+        });
         while (hits) {
             const int j = __builtin_ctz(hits);
             hits &= hits - 1;
             const int32_t i = (j * L::G + g.t) * L::VEC;
             Piece<TYPE, L::VEC> p;
-            p.load(row.row, i, row.n);
+            p.load(row.row, 0, i, row.n);
             search(i, p);
         }
     } else {
-        row.each([&](int, int32_t i, const Piece<TYPE, L::VEC> &p) { search(i, p); });
+        row.stream([&](int32_t i, const Piece<TYPE, L::VEC> &p) { search(i, p); });
     }
     g.barrier();
     return *fill;
 }
 
-// A key >= lo that still has k classes at or above it, where lo has (top: the row's
-// largest key), by counting keys in kBins equal intervals up to top in LDS.
-constexpr uint32_t kBins = 2048;
+// Keys [lo, hi) of a block's row in which the sum of `weight` over the order reaches
+// `goal` (1 <= goal <= the row's sum), the sum before them and their own.
+struct Range {
+    uint32_t lo, hi, before, here;
+};
 
-template <int TYPE, class L, class R>
-__device__ __forceinline__ uint32_t raise_bound(Group<L::G> &g, R &row, uint32_t lo,
-                                                uint32_t top, uint32_t k, uint32_t *bins)
+// kCopies interleaved counters an interval, one for every eighth lane: many elements
+// fall in few intervals (16-bit logits near -10 have 16 values a unit), and equal
+// addresses take turns.
+constexpr uint32_t kCopies = 8;
+
+// Narrows a range that holds the goal to one key, or until everything down to its end
+// sums to `enough`: the row's elements are summed in kBins intervals of equal width
+// (in fixed point: their order does not matter), again in the interval that reaches the
+// goal, and so on.  A level takes a factor of kBins off the range.  bins: kBins *
+// kCopies words of LDS.
+template <int TYPE, class L, class R, class W>
+__device__ __forceinline__ Range narrow(Group<L::G> &g, R &row, Range in, uint32_t goal,
+                                        uint32_t enough, uint32_t *bins, W weight)
 {
     typedef Elem<TYPE> E;
-    constexpr int kRun = kBins / L::G;
-    uint32_t shift = 0;
-    while ((top - lo) >> shift >= kBins)
-        ++shift;
-    g.barrier();
-    for (uint32_t b = g.t; b < kBins; b += L::G)
-        bins[b] = 0;
-    g.barrier();
-    const typename E::Cmp at = E::from_key(lo);
-    row.each([&](int, int32_t, const Piece<TYPE, L::VEC> &p) {
-#pragma unroll
-        for (int u = 0; u < L::VEC; ++u) {
-            const typename E::Cmp v = p.get(u);
-            if (v >= at)
-                atomicAdd(&bins[(top - E::key(v)) >> shift], 1u);
+    typedef typename E::Cmp Cmp;
+    constexpr uint32_t kBins = L::kBins, kRun = kBins > (uint32_t)L::G ? kBins / L::G : 1;
+    const uint32_t copy = g.t % kCopies;
+    bool by_key = TYPE == kI32;
+    // No element has the key of -0 (+0's is the next one): as an end of the range it
+    // would stand for +0, which may be outside.
+    constexpr uint32_t kMinusZero = TYPE == kI32 ? 0xFFFFFFFFu : 0x7FFFFFFFu >> E::kShift;
+    const auto off_minus_zero = [&]() __attribute__((always_inline)) {
+        if constexpr (TYPE != kI32) {
+            in.lo += in.lo == kMinusZero;
+            in.hi -= in.hi == kMinusZero + 1;
         }
-    });
-    g.barrier();
-    uint32_t mine = 0, total, last = 0;
-    for (int b = 0; b < kRun; ++b)
-        mine += bins[g.t * kRun + b];
-    uint32_t before = g.scan(mine, total);
-    for (int b = 0; b < kRun; ++b) {
-        const uint32_t here = bins[g.t * kRun + b];
-        if (before < k && before + here >= k)
-            last = g.t * kRun + b + 1;
-        before += here;
+    };
+    off_minus_zero();
+    while (in.hi - in.lo > 1 && in.before + in.here > enough) {
+        // Floats by value, which crosses zero evenly, until that takes less than 15 of 16
+        // keys off the range (an infinity or denormals at its end); integers, exactly, by
+        // key, which takes kBins / 2 - 1 of kBins / 2 off at every level.
+        const Cmp first = E::from_key(in.lo), last = E::from_key(in.hi - 1);
+        uint32_t shift = 0;
+        while ((in.hi - 1 - in.lo) >> shift >= kBins)
+            ++shift;
+        // half of each end, so that their difference does not overflow
+        const float scale = (0.5f * (float)kBins) /
+                            (0.5f * E::to_float(last) - 0.5f * E::to_float(first));
+        const auto bin_of = [&](Cmp v) __attribute__((always_inline)) {
+            const uint32_t b = by_key ? (in.hi - 1 - E::key(v)) >> shift
+                                      : (uint32_t)((E::to_float(last) - E::to_float(v)) * scale);
+            return min(b, kBins - 1);
+        };
+        g.barrier();
+        for (uint32_t b = g.t; b < kBins * kCopies; b += L::G)
+            bins[b] = 0;
+        g.barrier();
+        row.template stream<2>([&](int32_t, const Piece<TYPE, L::VEC> &p) {
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u) {
+                const Cmp v = p.get(u);
+                if (v >= first && v <= last)
+                    atomicAdd(&bins[bin_of(v) * kCopies + copy], weight(v));
+            }
+        });
+        g.barrier();
+        uint32_t part = 0, total;
+        for (uint32_t b = 0; b < kRun; ++b)
+            for (uint32_t c = 0; c < kCopies; ++c)
+                part += g.t * kRun + b < kBins ? bins[(g.t * kRun + b) * kCopies + c] : 0;
+        uint32_t before = in.before + g.scan(part, total), found = 0, here = 0, base = 0;
+        for (uint32_t b = 0; b < kRun; ++b) {
+            uint32_t own = 0;
+            for (uint32_t c = 0; c < kCopies; ++c)
+                own += g.t * kRun + b < kBins ? bins[(g.t * kRun + b) * kCopies + c] : 0;
+            if (before < goal && before + own >= goal) {
+                found = g.t * kRun + b + 1;
+                base = before;
+                here = own;
+            }
+            before += own;
+        }
+        const uint64_t won = g.reduce((uint64_t)found << 32 | base, Max());
+        here = g.reduce(here, Max());
+        found = (uint32_t)(won >> 32);
+        if (!found) {                                     // rounding left the goal outside
+            in = {in.lo, in.lo + 1, goal, 0};
+            break;
+        }
+        // the first key of the intervals up to `bound`, 64 keys at a time in every wave
+        const auto first_key = [&](uint32_t bound) __attribute__((always_inline)) {
+            uint32_t no = in.lo - 1, yes = in.hi - 1;
+            while (yes - no > 1) {
+                const uint64_t left = yes - no, step = (left - 1) / kWave + 1;
+                const uint32_t ahead = (uint32_t)min(step * (g.t % kWave + 1), left);
+                const uint64_t is = __ballot(bin_of(E::from_key(no + ahead)) < bound);
+                const uint32_t at = __builtin_ctzll(is);  // (the last lane's is)
+                yes = no + (uint32_t)min(step * (at + 1), left);
+                no += (uint32_t)step * at;
+            }
+            return yes;
+        };
+        const uint32_t lo = first_key(found), hi = found == 1 ? in.hi : first_key(found - 1);
+        by_key |= hi - lo > (in.hi - in.lo) / 16;
+        in = {lo, hi, (uint32_t)won, here};
+        off_minus_zero();
     }
-    last = g.reduce(last, Max());                         // 1 + the bin with the k-th
-    const uint64_t span = (uint64_t)last << shift;
-    return last && span <= top - lo ? top - (uint32_t)span + 1 : lo;
+    return in;
 }
 
 // Sorting: each lane has EPL neighbouring entries in registers; exchanges within a
@@ -620,18 +753,33 @@ __device__ __forceinline__ void place_entries(Group<G> &g, const uint64_t *e, ui
     g.barrier();
 }
 
+// The lane's group in its block, in a scalar register where a group is whole waves.
+template <int G>
+__device__ __forceinline__ int group_of()
+{
+    if constexpr (G >= 256)
+        return 0;
+    else if constexpr (G == kWave)
+        return __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    else
+        return threadIdx.x / G;
+}
+
 // ---- which group holds rows of n classes ----
 template <int G_, int NV_, int VEC_, bool RESIDENT_>
 struct Layout {
     static constexpr int G = G_, NV = NV_, VEC = VEC_;
     static constexpr bool RESIDENT = RESIDENT_;
+    static constexpr int kSpan = G * VEC;                 // elements of one piece per lane
     static constexpr int kBlock = G < 256 ? 256 : G;
     static constexpr int kGroups = kBlock / G;            // rows of a block
     // Candidates of a row that LDS holds (a power of two; all the classes of a row
     // within a wave), and how many are put in order by counting rather than sorting:
     // c entries compare c^2 / G times a lane, 128 of them as long as a sort takes.
-    static constexpr int kList = G == 1024 ? 4096 : G == 256 ? 1024 : NV * VEC * G;
-    static constexpr int kCounted = G == 1024 ? 352 : G == 256 ? 176 : G == 64 ? 88 : NV * VEC * G;
+    static constexpr int kList = G >= 256 ? 4 * G : NV * VEC * G;
+    static constexpr int kBins = kList * 2 / (int)kCopies;    // in the list's memory
+    static constexpr int kCounted =
+        G == 1024 ? 352 : G == 512 ? 256 : G == 256 ? 176 : G == 64 ? 88 : NV * VEC * G;
     // waves a SIMD to compile for: two blocks of short rows a CU
     static constexpr int kWavesPerSimd =
         !RESIDENT || G == kWave || NV * (VEC > 4 ? 4 : VEC) > 16 ? 4 : 8;
@@ -655,13 +803,12 @@ hipError_t with_layout(int32_t n, int32_t k, F f)
     if (n <= 8192)
         return f(Layout<256, 32 / V, V, true>());
     if (n <= 32768)
-        return f(Layout<1024, 32 / V, V, true>());
-    if (n <= 65536)
-        return f(Layout<1024, 64 / V, V, true>());
-    if constexpr (V == 8) {
-        if (n <= 131072)
-            return f(Layout<1024, 16, V, true>());
-    }
+        return f(Layout<512, 64 / V, V, true>());
+    if constexpr (V == 8)
+        if (n <= 65536)
+            return f(Layout<512, 16, V, true>());
+    if (n <= 1024 * 16 * V)
+        return f(Layout<1024, 16, V, true>());
     return f(Layout<1024, 1, V, false>());
 }
 

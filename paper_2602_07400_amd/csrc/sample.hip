@@ -15,10 +15,9 @@
 // those of a list in LDS, found from the lanes' largest logits as in top_logits.hip
 // and put in order: top-k is a place, top-p a prefix sum, and the kept classes' numbers
 // are all that is read of the noise.  Otherwise the kept set is (key > tau) and the
-// first classes of (key == tau).  For a top-p, sums of w in 2048 intervals of x, in
-// fixed point so that their order does not matter, say which interval the prefix ends
-// in, and that one's classes are put in order; where neither list holds them, tau comes
-// from bisection on the key: on counts for top-k, on sums of w for top-p.
+// first classes of (key == tau); tau is narrowed down by counts, for a top-k, or sums
+// of w, for a top-p, in ever narrower intervals.  Rows of a part of a wave find it by
+// bisection.
 #include "logit_rows.h"
 
 namespace bl {
@@ -41,51 +40,78 @@ struct SampleArgs {
     float *log_prob;                    // [rows] or NULL
 };
 
-// Lanes of each wave whose largest logits bound the list of a top-p without a top-k.
-constexpr uint32_t kNucleusLanes = 4;
-// Intervals of x for the sums of w: kBins of them down to -kRange, where w is 4e-11.
-constexpr float kRange = 24.0f;
-constexpr float kFixed = 1099511627776.0f;                // 2^40 a unit of w
+// Lanes whose largest logits bound the list of a top-p without a top-k.
+constexpr uint32_t kNucleusLanes = 64;
 
-template <int TYPE, class L>
-__global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleArgs a)
+// PLAIN: no filter in any row, so that every class and number counts: the row stays in
+// registers for the draw, and the first numbers are loaded behind it.  Otherwise rows
+// without a filter are read twice.
+template <int TYPE, class L, bool PLAIN>
+__global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sample(SampleArgs a)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
     typedef Piece<TYPE, L::VEC> P;
     constexpr int G = L::G;
-    constexpr bool kLists = G >= kWave;
+    constexpr bool kLists = G >= kWave && !PLAIN;
     constexpr int kCounted = kLists ? L::kCounted : 1;
-    constexpr int kSlots = !kLists ? 1 : G > kWave && L::kList < (int)kBins ? (int)kBins : L::kList;
     __shared__ Scratch scratch;
-    __shared__ uint64_t lists[kLists ? L::kGroups : 1][kSlots];
+    __shared__ uint64_t lists[kLists ? L::kGroups : 1][kLists ? L::kList : 1];
     __shared__ uint64_t placed[kLists ? L::kGroups : 1][kCounted];
     __shared__ float numbers[kLists ? L::kGroups : 1][kCounted];
     __shared__ uint32_t fills[L::kGroups];
-    const int gi = threadIdx.x / G;
+    const int gi = group_of<G>();
     const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
     if (r >= a.n_rows)
         return;
-    Group<G> g(threadIdx.x % G, &scratch);
+    Group<G> g(threadIdx.x - gi * G, &scratch);
     const char *src = a.logits + r * a.stride;
     const float *noise = a.noise + r * a.noise_stride;
     Row<TYPE, G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
     const float temperature = a.temperatures ? a.temperatures[r] : a.temperature;
-    const float top_p = a.top_ps ? a.top_ps[r] : a.top_p;
-    const float min_p = a.min_ps ? a.min_ps[r] : a.min_p;
-    int32_t top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+    const float top_p = PLAIN ? 1.0f : a.top_ps ? a.top_ps[r] : a.top_p;
+    const float min_p = PLAIN ? 0.0f : a.min_ps ? a.min_ps[r] : a.min_p;
+    int32_t top_k = PLAIN ? a.n : a.top_ks ? a.top_ks[r] : a.top_k;
     if (top_k <= 0 || top_k > a.n)
         top_k = a.n;
     const bool by_k = top_k < a.n, by_p = top_p < 1.0f;
     const float inv_t = 1.0f / temperature;
 
+    constexpr int kAhead = !L::RESIDENT ? 1 : L::NV < 32 / L::VEC ? L::NV : 32 / L::VEC;
+    static_assert(!L::RESIDENT || L::NV % kAhead == 0, "whole batches");
+    typedef float Numbers[kAhead][L::VEC];
+    const auto numbers_of = [&](int32_t i, float (&to)[L::VEC]) __attribute__((always_inline)) {
+        const float *from = noise + i + (uint32_t)(g.t * L::VEC);   // i: of the group's first
+        if (i + L::kSpan <= a.n) {
+            __builtin_memcpy(to, from, sizeof to);
+        } else {
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u)
+                to[u] = 0.0f;
+            for (int u = min(a.n - i - g.t * L::VEC, L::VEC) - 1; u >= 0; --u) {
+#pragma unroll
+                for (int k = L::VEC - 1; k > 0; --k)
+                    to[k] = to[k - 1];
+                to[0] = from[u];
+            }
+        }
+    };
+    const bool unfiltered = !by_k && !by_p && !(min_p > 0.0f) && temperature > 0.0f;
+    Numbers early;
+    if constexpr (L::RESIDENT && PLAIN)
+        if (unfiltered)
+            static_for<kAhead>([&](auto j) __attribute__((always_inline)) {
+                numbers_of(j * L::kSpan, early[j]);
+            });
+
     // the lane's and its pieces' largest logits and, for a top-p of all classes, the
     // softmax's sum, as the row arrives
     Cmp mine = E::lowest(), most[L::NV];
+    static_for<L::NV>([&](auto j) __attribute__((always_inline)) { most[j] = E::lowest(); });
     Softmax sm = {-__builtin_inff(), 0.0f};
-    const bool of_all = by_p && !by_k && temperature > 0.0f;
+    const bool of_all = by_p && !by_k && temperature > 0.0f && kLists;
     const float c = inv_t * kLog2e;
-    row.each([&](int j, int32_t, const P &p) {
+    row.each([&](auto j, int32_t, const P &p) {
         Cmp vm = E::lowest();
 #pragma unroll
         for (int u = 0; u < L::VEC; ++u) {
@@ -109,13 +135,26 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
     const Cmp top = g.reduce(mine, Max());
     const auto first_class = [&]() __attribute__((always_inline)) {
         uint32_t first = 0;                               // of the largest, ~class
-        if (mine == top)
-            row.each([&](int, int32_t i, const P &p) {
+        const auto search = [&](int32_t i, const P &p) __attribute__((always_inline)) {
 #pragma unroll
-                for (int u = 0; u < L::VEC; ++u)
-                    if (p.get(u) == top)
-                        first = max(first, ~(uint32_t)(i + u));
+            for (int u = 0; u < L::VEC; ++u)
+                if (p.get(u) == top)
+                    first = max(first, ~(uint32_t)(i + u));
+        };
+        if constexpr (L::RESIDENT) {
+            uint32_t hits = 0;                            // the lane's first piece with it
+            static_for<L::NV>([&](auto j) __attribute__((always_inline)) {
+                hits |= (uint32_t)(most[j] == top) << j;
             });
+            if (hits) {
+                const int32_t i = (__builtin_ctz(hits) * G + g.t) * L::VEC;
+                P p;
+                p.load(src, 0, i, a.n);
+                search(i, p);
+            }
+        } else {
+            row.stream(search);
+        }
         return (int32_t)~g.reduce(first, Max());
     };
     if (!(top > E::lowest()) || !(temperature > 0.0f)) {
@@ -141,7 +180,7 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
         else
             sm.s = 0.0f;                                  // w = 1 at +inf, else 0
         if (ftop == __builtin_inff())
-            row.each([&](int, int32_t, const P &p) {
+            row.stream([&](int32_t, const P &p) {
 #pragma unroll
                 for (int u = 0; u < L::VEC; ++u)
                     sm.s += p.get(u) == top ? 1.0f : 0.0f;
@@ -151,11 +190,11 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
     float sum = 0.0f;                                     // of the kept w
     float best = -__builtin_inff(), best_x = 0.0f;        // x + g of the lane's best class
     int32_t best_class = 0;
-    const auto finish = [&](auto first) __attribute__((always_inline)) {
+    const auto finish = [&](auto &h, auto first) __attribute__((always_inline)) {
         const uint64_t own = best > -__builtin_inff()
                                  ? entry(Elem<kF32>::key(best), best_class) : 0;
-        const uint64_t won = g.reduce(own, Max());
-        sum = g.reduce(sum, Add());
+        const uint64_t won = h.reduce(own, Max());
+        sum = h.reduce(sum, Add());
         int32_t token = best_class;
         if (!won) {
             token = first();
@@ -168,25 +207,100 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
         }
     };
 
+    // a draw among a piece's logits above `at` and those equal to it up to class `last`
+    const auto draw = [&](Cmp at, int32_t last, int32_t i, const P &p,
+                          const float (&number)[L::VEC]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < L::VEC; ++u) {
+            const Cmp v = p.get(u);
+            const float x = x_of(v);
+            const bool kept = (v > at || (v == at && i + u <= last)) && (x >= floor_x || v == top);
+            sum += kept ? exp_fast(x) : 0.0f;
+            const float score = x + number[u];
+            if (kept && score > best) {                   // (the lane's classes ascend)
+                best = score;
+                best_x = x;
+                best_class = i + u;
+            }
+        }
+    };
+    const auto draw_streamed = [&](Cmp at, int32_t last) __attribute__((always_inline)) {
+        constexpr int kFlight = 16 / L::VEC < 4 ? 16 / L::VEC : 4;
+        for (int32_t i = 0; i < a.n; i += kFlight * L::kSpan) {
+            P p[kFlight];
+            float number[kFlight][L::VEC];
+            static_for<kFlight>([&](auto j) __attribute__((always_inline)) {
+                p[j].load(src, i + j * L::kSpan, g.t * L::VEC, a.n);
+                numbers_of(i + j * L::kSpan, number[j]);
+            });
+            static_for<kFlight>([&](auto j) __attribute__((always_inline)) {
+                draw(at, last, i + j * L::kSpan + g.t * L::VEC, p[j], number[j]);
+            });
+        }
+    };
+    // the kept prefix: keys above tau, and `ties` of those equal to it
+    constexpr uint32_t kAll = 0xFFFFFFFFu;
+    const uint32_t end = E::key(top) + 1;
+    uint32_t tau = E::kFirstKey, ties = kAll;
+    const auto cut_at = [&](uint32_t key, float need) __attribute__((always_inline)) {
+        // equal classes until a mass of `need`: at least one
+        const float many = ceilf(need / exp_fast(x_of(E::from_key(key))));
+        const uint32_t take = many >= 4.0e9f ? kAll : many > 1.0f ? (uint32_t)many : 1u;
+        ties = key == tau ? min(take, ties) : take;
+        tau = key;
+    };
     const Cmp all = E::from_key(E::kFirstKey);
+    if (unfiltered) {
+        if constexpr (L::RESIDENT && PLAIN)
+            static_for<L::NV / kAhead>([&](auto B) __attribute__((always_inline)) {
+                constexpr int j0 = decltype(B)::value * kAhead;
+                Numbers number;
+                if (j0 * L::kSpan >= a.n)
+                    return;
+                if constexpr (j0 > 0)
+                    static_for<kAhead>([&](auto j) __attribute__((always_inline)) {
+                        numbers_of((j0 + j) * L::kSpan, number[j]);
+                    });
+                static_for<kAhead>([&](auto j) __attribute__((always_inline)) {
+                    row.template again<j0 + decltype(j)::value>();
+                    const int32_t i = (j0 + j) * L::kSpan + g.t * L::VEC;
+                    if constexpr (j0 > 0)
+                        draw(all, INT32_MAX, i, row.piece[j0 + j], number[j]);
+                    else
+                        draw(all, INT32_MAX, i, row.piece[j], early[j]);
+                });
+            });
+        else
+            draw_streamed(all, INT32_MAX);
+        finish(g, first_class);
+        return;
+    }
     uint32_t *fill = &fills[gi];
     if constexpr (kLists) {
-        constexpr uint32_t W = G / kWave;
         uint64_t *list = lists[gi];
+        uint32_t *fill = &fills[gi];
         uint32_t lo = E::kFirstKey;
-        const uint32_t lanes = by_k ? (top_k + W - 1) / W : kNucleusLanes;
-        if ((by_k || by_p) && lanes <= kWave)
-            lo = max(lo, ~g.reduce(~wave_mth(mine > E::lowest() ? E::key(mine) : 0, lanes),
-                                   Max()));
-        for (int attempt = 0; (by_k || by_p) && attempt < 2; ++attempt) {
+        const uint32_t lanes = by_k ? top_k : min(kNucleusLanes, (uint32_t)G / 2);
+        if ((by_k || by_p) && lanes <= (uint32_t)G)
+            lo = max(lo, group_mth(g, mine > E::lowest() ? E::key(mine) : 0, lanes,
+                                   (uint32_t *)list));
+        while (by_k || by_p) {
             const uint32_t found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top,
                                                     list, fill);
             if (found > (uint32_t)L::kList) {
-                if (!by_k || top_k > L::kList || attempt)
-                    break;
                 if constexpr (G > kWave)
-                    lo = raise_bound<TYPE, L>(g, row, lo, E::key(top), top_k, (uint32_t *)list);
-                continue;
+                    if (by_k) {                           // the k-th key, or nearly
+                        const uint32_t enough = top_k <= L::kList ? L::kList : 0;
+                        const Range at = narrow<TYPE, L>(g, row, {lo, end, 0, found}, top_k,
+                                                         enough, (uint32_t *)list,
+                                                         [](Cmp) { return 1u; });
+                        lo = at.lo;
+                        if (at.before + at.here <= enough)
+                            continue;
+                        tau = lo;
+                        ties = top_k - at.before;
+                    }
+                break;
             }
             const bool counted = found <= (uint32_t)kCounted;
             uint64_t *sorted = counted ? placed[gi] : list;
@@ -196,15 +310,18 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
             else
                 sort_entries(g, list, found);
             const uint32_t n = by_k ? min(found, (uint32_t)top_k) : found;
-            // sums of w before each entry: a run of entries a lane
-            const uint32_t run = (n + G - 1) / G, e0 = min(n, g.t * run), e1 = min(n, e0 + run);
-            float w = 0.0f, total;
-            for (uint32_t e = e0; e < e1; ++e)
-                w += exp_fast(x_of(E::from_key(key_of(sorted[e]))));
-            float before = g.scan(w, total);
-            const float target = top_p * (by_k ? total : row_mass);
-            // the list reaches the target, or holds every class
-            if (!by_p || by_k || total >= target || lo == E::kFirstKey) {
+            // by the block, or by its first wave; whether the list reaches the target
+            const auto draw_listed = [&](auto &h, uint32_t width) __attribute__((always_inline)) {
+                // sums of w before each entry: a run of entries a lane
+                const uint32_t run = (n + width - 1) / width, e0 = min(n, g.t * run),
+                               e1 = min(n, e0 + run);
+                float w = 0.0f, total;
+                for (uint32_t e = e0; e < e1; ++e)
+                    w += exp_fast(x_of(E::from_key(key_of(sorted[e]))));
+                float before = h.scan(w, total);
+                const float target = top_p * (by_k ? total : row_mass);
+                if (by_p && !by_k && total < target && lo != E::kFirstKey)
+                    return false;
                 for (uint32_t e = e0; e < e1; ++e) {
                     const float x = x_of(E::from_key(key_of(sorted[e])));
                     const float we = exp_fast(x);
@@ -220,155 +337,80 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
                     }
                     before += we;
                 }
-                finish([&] { return class_of(sorted[0]); });
-                return;
+                finish(h, [&] { return class_of(sorted[0]); });
+                return true;
+            };
+            bool drawn = false;
+            if (G > kWave && n <= kWave) {
+                if (g.t < kWave) {
+                    Group<kWave> h(g.t, nullptr);
+                    drawn = draw_listed(h, kWave);
+                }
+                if (by_p && !by_k) {                      // (a top-k's list suffices)
+                    if (g.t == 0)
+                        *fill = drawn;
+                    g.barrier();
+                    drawn = *fill;
+                } else {
+                    drawn = true;
+                }
+            } else {
+                drawn = draw_listed(g, G);
             }
-            if (G > kWave)
+            if (drawn)
+                return;
+            if (G > kWave || lo == E::kFirstKey)
                 break;
             lo = E::kFirstKey;                            // a wave's list holds the row
         }
     }
 
-    const auto mass_from = [&](Cmp at) __attribute__((always_inline)) {
-        float part = 0.0f;                                // sum of w over logits >= at
-        row.each([&](int j, int32_t, const P &p) {
-            if constexpr (L::RESIDENT)
-                if (!(most[j] >= at))
-                    return;
+    if constexpr (G < kWave && !PLAIN) {
+        // by bisection: classes and mass from a key on
+        const auto measure = [&](Cmp at, uint32_t &count, float &mass)
+            __attribute__((always_inline)) {
+            count = 0;
+            mass = 0.0f;
+            row.each([&](auto, int32_t, const P &p) {
 #pragma unroll
-            for (int u = 0; u < L::VEC; ++u) {
-                const Cmp v = p.get(u);
-                part += v >= at ? exp_fast(x_of(v)) : 0.0f;
-            }
-        });
-        return g.reduce(part, Add());
-    };
-    const auto count_from = [&](Cmp at) __attribute__((always_inline)) {
-        uint32_t count = 0;
-        row.each([&](int j, int32_t, const P &p) {
-            if constexpr (L::RESIDENT)
-                if (!(most[j] >= at))
-                    return;
-#pragma unroll
-            for (int u = 0; u < L::VEC; ++u)
-                count += p.get(u) >= at;
-        });
-        return g.reduce(count, Add());
-    };
-    // the kept prefix: keys above tau, and of those equal to it `ties`, or the classes
-    // up to `last`
-    const uint32_t end = E::key(top) + 1;
-    uint32_t tau = E::kFirstKey, ties = 0xFFFFFFFFu;
-    int32_t last = INT32_MAX;
-    if (by_k && count_from(all) > (uint32_t)top_k) {
-        uint32_t hi = end;                                // count(>= tau) >= k > count(>= hi)
-        while (hi - tau > 1) {
-            const uint32_t mid = tau + (hi - tau) / 2;
-            if (count_from(E::from_key(mid)) >= (uint32_t)top_k)
-                tau = mid;
-            else
-                hi = mid;
-        }
-        ties = top_k - (hi == end ? 0 : count_from(E::from_key(hi)));
-    }
-    if (by_p) {
-        float target = row_mass;
-        if (by_k) {
-            if (ties != 0xFFFFFFFFu) {
-                const float more = tau + 1 == end ? 0.0f : mass_from(E::from_key(tau + 1));
-                target = more + (float)ties * exp_fast(x_of(E::from_key(tau)));
+                for (int u = 0; u < L::VEC; ++u)
+                    if (p.get(u) >= at) {
+                        ++count;
+                        mass += exp_fast(x_of(p.get(u)));
+                    }
+            });
+            count = g.reduce(count, Add());
+            mass = g.reduce(mass, Add());
+        };
+        uint32_t count, classes = 0;
+        float mass, above = 0.0f, target = 0.0f;
+        measure(all, count, mass);
+        const bool cut = by_k && count > (uint32_t)top_k;
+        uint32_t lo = E::kFirstKey, hi = end;
+        while (cut && hi - lo > 1) {                      // count(>= lo) >= k > count(>= hi)
+            const uint32_t mid = lo + (hi - lo) / 2;
+            float m;
+            measure(E::from_key(mid), count, m);
+            if (count >= (uint32_t)top_k) {
+                lo = mid;
             } else {
-                target = mass_from(all);
+                hi = mid;
+                classes = count;
+                above = m;
             }
         }
-        target *= top_p;
-        uint32_t lo = tau, hi = end;                      // mass(>= lo) >= target > mass(>= hi)
-        float above = 0.0f;                               // mass(>= hi)
-        bool found_last = false;
-        if constexpr (G > kWave)
-            if (!by_k) {
-                constexpr uint32_t kRun = kBins / G;
-                unsigned long long *bins = reinterpret_cast<unsigned long long *>(lists[gi]);
-                const float scale = (float)kBins / kRange;
-                const auto bin_of = [&](Cmp v) __attribute__((always_inline)) {
-                    return -x_of(v) * scale;              // grows as v falls; may be inf
-                };
-                g.barrier();
-                for (uint32_t b = g.t; b < kBins; b += G)
-                    bins[b] = 0;
-                g.barrier();
-                row.each([&](int, int32_t, const P &p) {
-#pragma unroll
-                    for (int u = 0; u < L::VEC; ++u) {
-                        const Cmp v = p.get(u);
-                        const float b = bin_of(v);
-                        if (v >= all && b < (float)kBins)
-                            atomicAdd(&bins[(uint32_t)b],
-                                      (unsigned long long)(exp_fast(x_of(v)) * kFixed));
-                    }
-                });
-                g.barrier();
-                const unsigned long long goal = (unsigned long long)(target * kFixed);
-                unsigned long long part = 0, total;
-                for (uint32_t b = 0; b < kRun; ++b)
-                    part += bins[g.t * kRun + b];
-                unsigned long long before = g.scan(part, total), base = 0;
-                uint32_t in = 0;                          // 1 + the bin that reaches it
-                for (uint32_t b = 0; b < kRun; ++b) {
-                    const unsigned long long here = bins[g.t * kRun + b];
-                    if (before < goal && before + here >= goal) {
-                        in = g.t * kRun + b + 1;
-                        base = before;
-                    }
-                    before += here;
-                }
-                in = g.reduce(in, Max());
-                base = g.reduce((uint64_t)base, Max());
-                if (in) {
-                    // its keys: [lo, hi)
-                    const auto first_key = [&](float bound) __attribute__((always_inline)) {
-                        uint32_t no = E::kFirstKey - 1, yes = end - 1;
-                        while (yes - no > 1) {
-                            const uint32_t mid = no + (yes - no) / 2;
-                            if (bin_of(E::from_key(mid)) < bound)
-                                yes = mid;
-                            else
-                                no = mid;
-                        }
-                        return yes;
-                    };
-                    lo = first_key((float)in);
-                    hi = in == 1 ? end : first_key((float)(in - 1));
-                    above = (float)base / kFixed;
-                    const Cmp to = E::from_key(in == 1 ? lo : hi);
-                    uint64_t *list = lists[gi];
-                    const uint32_t found = collect<TYPE, L>(g, row, most, E::from_key(lo),
-                                                            in != 1, to, list, fill);
-                    if (found && found <= (uint32_t)L::kList) {
-                        sort_entries(g, list, found);
-                        const uint32_t run = (found + G - 1) / G, e0 = min(found, g.t * run),
-                                       e1 = min(found, e0 + run);
-                        float w = 0.0f, listed;
-                        for (uint32_t e = e0; e < e1; ++e)
-                            w += exp_fast(x_of(E::from_key(key_of(list[e]))));
-                        float sums = above + g.scan(w, listed);
-                        uint32_t kept = 1;
-                        for (uint32_t e = e0; e < e1; ++e) {
-                            if (sums < target)
-                                kept = e + 1;
-                            sums += exp_fast(x_of(E::from_key(key_of(list[e]))));
-                        }
-                        const uint64_t x = list[g.reduce(kept, Max()) - 1];
-                        tau = key_of(x);
-                        last = class_of(x);
-                        found_last = true;
-                    }
-                }
-            }
-        if (!found_last) {
-            while (hi - lo > 1) {
+        if (cut) {
+            tau = lo;
+            ties = top_k - classes;
+            mass = above + (float)ties * exp_fast(x_of(E::from_key(tau)));
+        }
+        if (by_p) {
+            target = top_p * mass;
+            hi = end;
+            above = 0.0f;
+            while (hi - lo > 1) {                         // mass(>= lo) >= target > mass(>= hi)
                 const uint32_t mid = lo + (hi - lo) / 2;
-                const float mass = mass_from(E::from_key(mid));
+                measure(E::from_key(mid), count, mass);
                 if (mass >= target) {
                     lo = mid;
                 } else {
@@ -376,20 +418,43 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
                     above = mass;
                 }
             }
-            // equal classes until the target: at least one
-            const float w = exp_fast(x_of(E::from_key(lo)));
-            const float need = ceilf((target - above) / w);
-            const uint32_t take = need >= 4.0e9f ? 0xFFFFFFFFu
-                                                 : need > 1.0f ? (uint32_t)need : 1u;
-            ties = lo == tau ? min(take, ties) : take;
-            tau = lo;
+            cut_at(lo, target - above);
+        }
+    } else if constexpr (G > kWave && !PLAIN) {
+        if (by_p) {
+            if (by_k) {                                   // the mass of the first k
+                float part = 0.0f;
+                const Cmp at = E::from_key(tau);
+                row.template stream<2>([&](int32_t, const P &p) {
+#pragma unroll
+                    for (int u = 0; u < L::VEC; ++u)
+                        part += p.get(u) > at || (p.get(u) == at && ties == kAll)
+                                    ? exp_fast(x_of(p.get(u))) : 0.0f;
+                });
+                row_mass = g.reduce(part, Add());
+                if (ties != kAll)
+                    row_mass += (float)ties * exp_fast(x_of(at));
+            }
+            // Classes with w < (1 - p) sum / n together have less than (1 - p) sum: the
+            // prefix ends before them.  A sum of all classes is 2^31 in fixed point.
+            const float unit = 2147483648.0f / row_mass;
+            const uint32_t goal = max((uint32_t)(top_p * 2147483648.0f), 1u);
+            uint32_t lo = tau;
+            if constexpr (TYPE != kI32)
+                lo = max(lo, E::key(ftop + logf((1.0f - top_p) * row_mass / (float)a.n) *
+                                               temperature) - 1);
+            const Range at = narrow<TYPE, L>(
+                g, row, {lo, end, 0, 0xFFFFFFFFu}, goal, 0, (uint32_t *)lists[gi],
+                [&](Cmp v) { return __float2uint_rn(exp_fast(x_of(v)) * unit); });
+            cut_at(at.lo, (float)(goal - min(at.before, goal)) / unit);
         }
     }
     const Cmp at = E::from_key(tau);
-    if (ties != 0xFFFFFFFFu) {                            // the last kept class equal to tau
+    int32_t last = INT32_MAX;                             // the last kept class equal to tau
+    if (ties != kAll) {
         uint32_t seen = 0;
         int32_t equal = -1;
-        row.each([&](int, int32_t i, const P &p) {
+        row.stream([&](int32_t i, const P &p) {
             if (seen >= ties)
                 return;
             uint32_t here = 0, total;
@@ -405,33 +470,8 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_sample(SampleAr
         });
         last = g.reduce(equal, Max());
     }
-    row.each([&](int j, int32_t i, const P &p) {
-        if constexpr (L::RESIDENT)
-            if (!(most[j] >= at))
-                return;
-        float number[L::VEC];
-        if (i + L::VEC <= a.n) {
-            __builtin_memcpy(number, noise + i, sizeof number);
-        } else {
-#pragma unroll
-            for (int u = 0; u < L::VEC; ++u)
-                number[u] = i + u < a.n ? noise[i + u] : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < L::VEC; ++u) {
-            const Cmp v = p.get(u);
-            const float x = x_of(v);
-            const bool kept = (v > at || (v == at && i + u <= last)) && (x >= floor_x || v == top);
-            sum += kept ? exp_fast(x) : 0.0f;
-            const float score = x + number[u];
-            if (kept && score > best) {                   // (the lane's classes ascend)
-                best = score;
-                best_x = x;
-                best_class = i + u;
-            }
-        }
-    });
-    finish(first_class);
+    draw_streamed(at, last);
+    finish(g, first_class);
 }
 
 }  // namespace
@@ -449,8 +489,13 @@ hipError_t launch_sample(const void *logits, int32_t type, int64_t n_rows, int32
                               sp.top_ps, sp.min_ps, sp.top_ks, token, log_prob};
         return with_layout<TYPE>(n, 0, [&](auto layout) {
             typedef decltype(layout) L;
-            k_sample<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock, 0,
-                                stream>>>(a);
+            const uint32_t blocks = (uint32_t)((n_rows + L::kGroups - 1) / L::kGroups);
+            const bool plain = !a.top_ks && !a.top_ps && !a.min_ps && a.top_p >= 1.0f &&
+                               !(a.min_p > 0.0f) && (a.top_k == 0 || a.top_k >= n);
+            if (plain)
+                k_sample<TYPE, L, true><<<blocks, L::kBlock, 0, stream>>>(a);
+            else
+                k_sample<TYPE, L, false><<<blocks, L::kBlock, 0, stream>>>(a);
             return hipGetLastError();
         });
     });

@@ -2,13 +2,12 @@
 // log-normalizer log sum_i e^(l_i / T): what a teacher hands on to a student.
 //
 // One pass over the row, as it arrives, takes the running maximum and sum of the
-// softmax and every lane's largest logit.  If m lanes in each of a row's W waves have
-// a logit >= lo, W m >= k classes have: the classes >= lo, a few more than k, go to a
-// list in LDS that is put in order.  Where the bound does not hold so few (k near the
-// number of lanes), counts of keys in 2048 intervals raise it; where that does not
-// either (many equal logits), tau, the k-th largest key, is found by bisection on
-// counts (key >= tau), and the list gets the classes above tau and the first ones equal
-// to it.  Entries (key, class) are unique, so the order in which the list fills
+// softmax and every lane's largest logit.  The classes >= lo, the k-th largest of the
+// lanes', are k or a few more: they go to a list in LDS that is put in order.  Where
+// the bound does not hold so few (k near the number of lanes or above), counts of keys
+// in ever narrower intervals raise it; where no bound does (many equal logits), tau, the
+// k-th largest key, is what they end at, and the list gets the classes above tau and the
+// first ones equal to it.  (Groups of less than a wave find tau by bisection.)  Entries (key, class) are unique, so the order in which the list fills
 // does not matter.
 #include "logit_rows.h"
 
@@ -39,11 +38,11 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
     __shared__ uint64_t lists[L::kGroups][L::kList];
     __shared__ uint64_t placed[L::kGroups][L::kCounted];
     __shared__ uint32_t fills[L::kGroups];
-    const int gi = threadIdx.x / G;
+    const int gi = group_of<G>();
     const int64_t r = (int64_t)blockIdx.x * L::kGroups + gi;
     if (r >= a.n_rows)
         return;
-    Group<G> g(threadIdx.x % G, &scratch);
+    Group<G> g(threadIdx.x - gi * G, &scratch);
     uint64_t *list = lists[gi];
     uint32_t *fill = &fills[gi];
     const char *src = a.logits + r * a.stride;
@@ -52,88 +51,96 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
     const float c = a.inv_t * kLog2e;
     Softmax sm = {-__builtin_inff(), 0.0f};
     Cmp top = E::lowest(), most[L::NV];                   // the lane's and its pieces' largest
-    uint32_t valid = 0;
-    row.each([&](int j, int32_t, const P &p) {
+    static_for<L::NV>([&](auto j) __attribute__((always_inline)) { most[j] = E::lowest(); });
+    row.each([&](auto j, int32_t, const P &p) {
         Cmp vm = E::lowest();
 #pragma unroll
-        for (int u = 0; u < L::VEC; ++u) {
-            const Cmp v = p.get(u);
-            const bool in = v > E::lowest();
-            valid += in;
-            vm = in && v > vm ? v : vm;
-        }
-        sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
-        const float from = sm.from();
-#pragma unroll
-        for (int u = 0; u < L::VEC; ++u) {
-            const Cmp v = p.get(u);
-            const float z = v > E::lowest() ? E::to_float(v) : -__builtin_inff();
-            sm.s += __builtin_amdgcn_exp2f((z - from) * c);
-        }
-        top = vm > top ? vm : top;
+        for (int u = 0; u < L::VEC; ++u)
+            vm = Max()(vm, p.get(u));                     // (a NaN never is)
+        top = Max()(top, vm);
         if constexpr (L::RESIDENT)
             most[j] = vm;
+        if (a.log_norm) {
+            sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
+            const float from = sm.from();
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u) {
+                const Cmp v = p.get(u);
+                const float e = __builtin_amdgcn_exp2f((E::to_float(v) - from) * c);
+                sm.s += TYPE == kI32 && v == E::lowest() ? 0.0f : e;
+            }
+        }
     });
     if (a.log_norm) {
+        if (!(sm.s >= 0.0f)) {                            // a NaN, or +inf - inf: without them
+            sm.s = 0.0f;
+            row.stream([&](int32_t, const P &p) {
+#pragma unroll
+                for (int u = 0; u < L::VEC; ++u) {
+                    const float e = E::to_float(p.get(u)) - sm.m;
+                    sm.s += e <= 0.0f ? __builtin_amdgcn_exp2f(e * c) : 0.0f;
+                }
+            });
+        }
         sm = combine(g, sm, c);
         if (g.t == 0)
             a.log_norm[r] = sm.log_norm(a.inv_t);
     }
-    const uint32_t k = min((uint32_t)a.k, g.reduce(valid, Add()));
 
-    uint32_t lo = E::kFirstKey, found = 0;
-    if (k) {
-        if constexpr (G >= kWave) {
-            // W waves of which m lanes each have a logit >= lo: W m >= k of them
-            constexpr uint32_t W = G / kWave;
-            const uint32_t m = (k + W - 1) / W;
-            if (m <= kWave) {
-                const uint32_t mine = top > E::lowest() ? E::key(top) : 0;
-                lo = max(lo, ~g.reduce(~wave_mth(mine, m), Max()));
-            }
-            found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top, list, fill);
-            if constexpr (G > kWave)
-                if (found > (uint32_t)L::kList) {
-                    const uint32_t end = E::key(g.reduce(top, Max()));
-                    lo = raise_bound<TYPE, L>(g, row, lo, end, k, (uint32_t *)list);
-                    found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top, list,
-                                             fill);
-                }
+    uint32_t lo = E::kFirstKey, found = 0xFFFFFFFFu, k = a.k;
+    if constexpr (G >= kWave) {
+        // k lanes each have a logit >= lo; all of the row's classes are where fewer
+        // lanes have any
+        if (k <= (uint32_t)G)
+            lo = max(lo, group_mth(g, top > E::lowest() ? E::key(top) : 0, k, (uint32_t *)list));
+        found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top, list, fill);
+    }
+    if (found > (uint32_t)L::kList) {
+        // the k-th key, or a range of keys around it that fits the list
+        Range at = {lo, E::key(g.reduce(top, Max())) + 1, 0, found};
+        if constexpr (G > kWave) {
+            at = narrow<TYPE, L>(g, row, at, k, L::kList, (uint32_t *)list,
+                                 [](Cmp) { return 1u; });
+            if (at.before + at.here <= (uint32_t)L::kList)
+                found = collect<TYPE, L>(g, row, most, E::from_key(at.lo), false, top, list, fill);
         }
-        if (G < kWave || found > (uint32_t)L::kList) {
-            // exactly: count(>= lo) >= k > count(>= hi)
-            uint32_t hi = E::key(g.reduce(top, Max())) + 1;
-            while (hi - lo > 1) {
-                const uint32_t mid = lo + (hi - lo) / 2;
-                const Cmp at = E::from_key(mid);
+        if constexpr (G < kWave) {
+            const auto count_from = [&](Cmp v) __attribute__((always_inline)) {
                 uint32_t count = 0;
-                row.each([&](int, int32_t, const P &p) {
+                row.each([&](auto, int32_t, const P &p) {
 #pragma unroll
                     for (int u = 0; u < L::VEC; ++u)
-                        count += p.get(u) >= at;
+                        count += p.get(u) >= v;
                 });
-                if (g.reduce(count, Add()) >= k)
-                    lo = mid;
+                return g.reduce(count, Add());
+            };
+            k = min(k, count_from(E::from_key(at.lo)));
+            while (k && at.hi - at.lo > 1) {              // count(>= lo) >= k > count(>= hi)
+                const uint32_t mid = at.lo + (at.hi - at.lo) / 2;
+                if (count_from(E::from_key(mid)) >= k)
+                    at.lo = mid;
                 else
-                    hi = mid;
+                    at.hi = mid;
             }
-            // those above, then the first classes of the equal ones
-            const Cmp tau = E::from_key(lo);
+        }
+        if (found > (uint32_t)L::kList) {
+            // those above it, then the first classes of the equal ones
+            const Cmp tau = E::from_key(at.lo);
             g.barrier();
             if (g.t == 0)
                 *fill = 0;
             g.barrier();
-            row.each([&](int, int32_t i, const P &p) {
+            row.stream([&](int32_t i, const P &p) {
 #pragma unroll
                 for (int u = 0; u < L::VEC; ++u) {
                     const Cmp v = p.get(u);
-                    if (v > tau)
+                    if (k && v > tau)
                         list[atomicAdd(fill, 1u)] = entry(E::key(v), i + u);
                 }
             });
             g.barrier();
             found = *fill;
-            row.each([&](int, int32_t i, const P &p) {
+            row.stream([&](int32_t i, const P &p) {
                 if (found >= k)
                     return;
                 uint32_t mine = 0, total;
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
                 for (int u = 0; u < L::VEC; ++u)
                     if (p.get(u) == tau) {
                         if (place < k)
-                            list[place] = entry(lo, i + u);
+                            list[place] = entry(at.lo, i + u);
                         ++place;
                     }
             });
@@ -154,6 +161,7 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
             g.barrier();
         }
     }
+    k = min(k, found);
 
     // the list in order
     if (found <= (uint32_t)L::kCounted) {
