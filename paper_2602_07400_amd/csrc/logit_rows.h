@@ -379,10 +379,18 @@ struct Row {
     // f(first element, piece) for all pieces, read again from memory in a loop: what is
     // seldom done, since unrolled over the registers it makes long code that holds
     // registers from what is done always
+    // (hits: one bit a piece of the lane, from the first on; pieces without one in any
+    // lane of a wave may be left out)
     template <int FLIGHT = kFlight, class F>
-    __device__ __forceinline__ void stream(F f) const
+    __device__ __forceinline__ void stream(F f, uint32_t hits = 0xFFFFFFFFu) const
     {
         for (int32_t i = 0; i < n; i += FLIGHT * kSpan) {
+            if constexpr (RESIDENT) {
+                const bool any = __any(hits & ((1u << FLIGHT) - 1));
+                hits >>= FLIGHT;
+                if (!any)
+                    continue;
+            }
             P p[FLIGHT];
             static_for<FLIGHT>([&](auto j) __attribute__((always_inline)) {
                 p[j].load(row, i + j * kSpan, t * VEC, n);
@@ -489,15 +497,28 @@ __device__ __forceinline__ uint32_t group_mth(Group<G> &g, uint32_t key, uint32_
     return lo;
 }
 
-// Appends the row's entries with lo <= logit < hi to a list in LDS (fill: its length,
+// The lane's pieces whose largest logits reach `at`, as a bit each.
+template <class L, class Cmp>
+__device__ __forceinline__ uint32_t pieces_from(const Cmp (&most)[L::NV], Cmp at)
+{
+    uint32_t hits = 0xFFFFFFFFu;
+    if constexpr (L::RESIDENT) {
+        hits = 0;
+        static_for<L::NV>([&](auto j) __attribute__((always_inline)) {
+            hits |= (uint32_t)(most[j] >= at) << j;
+        });
+    }
+    return hits;
+}
+
+// Appends the row's entries with lo <= logit to a list in LDS (fill: its length,
 // cleared here), as many as it holds, and returns their number.  most: the largest
 // logit of each of the lane's pieces; a piece that has candidates is loaded again, in
 // a loop, since 16 pieces' unrolled searches take longer to fetch than to run.
 template <int TYPE, class L, class R>
 __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
                                             const typename Elem<TYPE>::Cmp (&most)[L::NV],
-                                            typename Elem<TYPE>::Cmp lo, bool below,
-                                            typename Elem<TYPE>::Cmp hi, uint64_t *list,
+                                            typename Elem<TYPE>::Cmp lo, uint64_t *list,
                                             uint32_t *fill)
 {
     typedef Elem<TYPE> E;
@@ -505,7 +526,7 @@ __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
         uint32_t in = 0;
 #pragma unroll
         for (int u = 0; u < L::VEC; ++u)
-            in |= (uint32_t)(p.get(u) >= lo && !(below && p.get(u) >= hi)) << u;
+            in |= (uint32_t)(p.get(u) >= lo) << u;
         if (!in)
             return;
         uint32_t to = atomicAdd(fill, __builtin_popcount(in));
@@ -522,10 +543,7 @@ __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
         *fill = 0;
     g.barrier();
     if constexpr (L::RESIDENT) {
-        uint32_t hits = 0;
-        static_for<L::NV>([&](auto j) __attribute__((always_inline)) {
-            hits |= (uint32_t)(most[j] >= lo) << j;
-        });
+        uint32_t hits = pieces_from<L>(most, lo);
         while (hits) {
             const int j = __builtin_ctz(hits);
             hits &= hits - 1;
@@ -558,7 +576,9 @@ constexpr uint32_t kCopies = 8;
 // goal, and so on.  A level takes a factor of kBins off the range.  bins: kBins *
 // kCopies words of LDS.
 template <int TYPE, class L, class R, class W>
-__device__ __forceinline__ Range narrow(Group<L::G> &g, R &row, Range in, uint32_t goal,
+__device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
+                                        const typename Elem<TYPE>::Cmp (&most)[L::NV], Range in,
+                                        uint32_t goal,
                                         uint32_t enough, uint32_t *bins, W weight)
 {
     typedef Elem<TYPE> E;
@@ -596,14 +616,14 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row, Range in, uint32
         for (uint32_t b = g.t; b < kBins * kCopies; b += L::G)
             bins[b] = 0;
         g.barrier();
-        row.template stream<2>([&](int32_t, const Piece<TYPE, L::VEC> &p) {
+        row.stream([&](int32_t, const Piece<TYPE, L::VEC> &p) {
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
                 const Cmp v = p.get(u);
                 if (v >= first && v <= last)
                     atomicAdd(&bins[bin_of(v) * kCopies + copy], weight(v));
             }
-        });
+        }, pieces_from<L>(most, first));
         g.barrier();
         uint32_t part = 0, total;
         for (uint32_t b = 0; b < kRun; ++b)

@@ -77,7 +77,8 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
     const bool by_k = top_k < a.n, by_p = top_p < 1.0f;
     const float inv_t = 1.0f / temperature;
 
-    constexpr int kAhead = !L::RESIDENT ? 1 : L::NV < 32 / L::VEC ? L::NV : 32 / L::VEC;
+    constexpr int kRoom = TYPE == kF16 && L::NV == 16 ? 16 : 32;   // registers for them
+    constexpr int kAhead = !L::RESIDENT ? 1 : L::NV < kRoom / L::VEC ? L::NV : kRoom / L::VEC;
     static_assert(!L::RESIDENT || L::NV % kAhead == 0, "whole batches");
     typedef float Numbers[kAhead][L::VEC];
     const auto numbers_of = [&](int32_t i, float (&to)[L::VEC]) __attribute__((always_inline)) {
@@ -142,11 +143,8 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     first = max(first, ~(uint32_t)(i + u));
         };
         if constexpr (L::RESIDENT) {
-            uint32_t hits = 0;                            // the lane's first piece with it
-            static_for<L::NV>([&](auto j) __attribute__((always_inline)) {
-                hits |= (uint32_t)(most[j] == top) << j;
-            });
-            if (hits) {
+            const uint32_t hits = pieces_from<L>(most, top);
+            if (hits) {                                   // the lane's first piece with it
                 const int32_t i = (__builtin_ctz(hits) * G + g.t) * L::VEC;
                 P p;
                 p.load(src, 0, i, a.n);
@@ -168,74 +166,87 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         return;
     }
 
-    const float ftop = E::to_float(top);
+    // (a row with +inf draws among those: x = 0 there, hugely negative elsewhere)
+    const bool endless = E::to_float(top) == __builtin_inff();
+    const float ftop = endless ? 3.4028234663852886e38f : E::to_float(top);
     const float floor_x = min_p > 0.0f ? logf(min_p) : -__builtin_inff();
     const auto x_of = [&](Cmp v) __attribute__((always_inline)) {
-        return v == top ? 0.0f : (E::to_float(v) - ftop) * inv_t;
+        return fminf((E::to_float(v) - ftop) * inv_t, 0.0f);
     };
     float row_mass = 0.0f;                                // sum of w
     if (of_all) {
-        if (ftop < __builtin_inff())
-            sm.raise(ftop, c);
-        else
-            sm.s = 0.0f;                                  // w = 1 at +inf, else 0
-        if (ftop == __builtin_inff())
+        if (endless) {
+            sm.s = 0.0f;
             row.stream([&](int32_t, const P &p) {
 #pragma unroll
                 for (int u = 0; u < L::VEC; ++u)
                     sm.s += p.get(u) == top ? 1.0f : 0.0f;
             });
+        } else {
+            sm.raise(ftop, c);
+        }
         row_mass = g.reduce(sm.s, Add());
     }
     float sum = 0.0f;                                     // of the kept w
-    float best = -__builtin_inff(), best_x = 0.0f;        // x + g of the lane's best class
-    int32_t best_class = 0;
-    const auto finish = [&](auto &h, auto first) __attribute__((always_inline)) {
+    float best = -__builtin_inff(), best_x = 0.0f;        // the lane's best x + g (and x),
+    int32_t best_class = 0;                               // and its class
+    const auto finish = [&](auto &h, auto first, auto x_best) __attribute__((always_inline)) {
         const uint64_t own = best > -__builtin_inff()
                                  ? entry(Elem<kF32>::key(best), best_class) : 0;
         const uint64_t won = h.reduce(own, Max());
         sum = h.reduce(sum, Add());
-        int32_t token = best_class;
-        if (!won) {
-            token = first();
-            best_x = 0.0f;
-        }
+        const int32_t token = won ? best_class : first();
         if (won ? own == won : g.t == 0) {
             a.token[r] = token;
             if (a.log_prob)
-                a.log_prob[r] = best_x - logf(sum);
+                a.log_prob[r] = (won ? x_best() : 0.0f) - logf(sum);
         }
     };
+    const auto x_listed = [&] { return best_x; };
+    const auto x_loaded = [&] { return x_of(load_one<TYPE>(src, best_class)); };
 
-    // a draw among a piece's logits above `at` and those equal to it up to class `last`
-    const auto draw = [&](Cmp at, int32_t last, int32_t i, const P &p,
+    // a draw among a piece's logits above `in`, if the piece's classes end at or before
+    // `last`, and above `out` in classes after it
+    const auto draw = [&](Cmp in, Cmp out, int32_t last, int32_t i, const P &p,
                           const float (&number)[L::VEC]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < L::VEC; ++u) {
-            const Cmp v = p.get(u);
-            const float x = x_of(v);
-            const bool kept = (v > at || (v == at && i + u <= last)) && (x >= floor_x || v == top);
+        const bool split = i <= last && i + L::VEC - 1 > last;
+        const Cmp over = i <= last ? in : out;
+        int at = -1;
+        const auto one = [&](int u, bool kept) __attribute__((always_inline)) {
+            const float x = x_of(p.get(u));
             sum += kept ? exp_fast(x) : 0.0f;
-            const float score = x + number[u];
-            if (kept && score > best) {                   // (the lane's classes ascend)
-                best = score;
-                best_x = x;
-                best_class = i + u;
-            }
+            const float score = kept ? x + number[u] : -__builtin_inff();
+            at = score > best ? u : at;                   // (the lane's classes ascend)
+            best = fmaxf(best, score);
+        };
+        if (!__any(split)) {
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u)
+                one(u, p.get(u) > over);
+        } else {
+#pragma unroll
+            for (int u = 0; u < L::VEC; ++u)
+                one(u, p.get(u) > (i + u <= last ? in : out));
         }
+        best_class = at >= 0 ? i + at : best_class;
     };
-    const auto draw_streamed = [&](Cmp at, int32_t last) __attribute__((always_inline)) {
-        constexpr int kFlight = 16 / L::VEC < 4 ? 16 / L::VEC : 4;
+    const auto draw_streamed = [&](Cmp at, Cmp in, int32_t last) __attribute__((always_inline)) {
+        uint32_t hits = pieces_from<L>(most, at);
+        constexpr int kFlight = L::RESIDENT && L::NV < 4 ? L::NV : 4;
         for (int32_t i = 0; i < a.n; i += kFlight * L::kSpan) {
-            P p[kFlight];
-            float number[kFlight][L::VEC];
-            static_for<kFlight>([&](auto j) __attribute__((always_inline)) {
-                p[j].load(src, i + j * L::kSpan, g.t * L::VEC, a.n);
-                numbers_of(i + j * L::kSpan, number[j]);
-            });
-            static_for<kFlight>([&](auto j) __attribute__((always_inline)) {
-                draw(at, last, i + j * L::kSpan + g.t * L::VEC, p[j], number[j]);
-            });
+            if (__any(hits & ((1u << kFlight) - 1))) {
+                P p[kFlight];
+                float number[kFlight][L::VEC];
+                static_for<kFlight>([&](auto j) __attribute__((always_inline)) {
+                    p[j].load(src, i + j * L::kSpan, g.t * L::VEC, a.n);
+                    numbers_of(i + j * L::kSpan, number[j]);
+                });
+                static_for<kFlight>([&](auto j) __attribute__((always_inline)) {
+                    draw(in, at, last, i + j * L::kSpan + g.t * L::VEC, p[j], number[j]);
+                });
+            }
+            if constexpr (L::RESIDENT)
+                hits >>= kFlight;
         }
     };
     // the kept prefix: keys above tau, and `ties` of those equal to it
@@ -265,33 +276,31 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     row.template again<j0 + decltype(j)::value>();
                     const int32_t i = (j0 + j) * L::kSpan + g.t * L::VEC;
                     if constexpr (j0 > 0)
-                        draw(all, INT32_MAX, i, row.piece[j0 + j], number[j]);
+                        draw(E::lowest(), all, INT32_MAX, i, row.piece[j0 + j], number[j]);
                     else
-                        draw(all, INT32_MAX, i, row.piece[j], early[j]);
+                        draw(E::lowest(), all, INT32_MAX, i, row.piece[j], early[j]);
                 });
             });
         else
-            draw_streamed(all, INT32_MAX);
-        finish(g, first_class);
+            draw_streamed(all, E::lowest(), INT32_MAX);
+        finish(g, first_class, x_loaded);
         return;
     }
     uint32_t *fill = &fills[gi];
     if constexpr (kLists) {
         uint64_t *list = lists[gi];
-        uint32_t *fill = &fills[gi];
         uint32_t lo = E::kFirstKey;
         const uint32_t lanes = by_k ? top_k : min(kNucleusLanes, (uint32_t)G / 2);
         if ((by_k || by_p) && lanes <= (uint32_t)G)
             lo = max(lo, group_mth(g, mine > E::lowest() ? E::key(mine) : 0, lanes,
                                    (uint32_t *)list));
         while (by_k || by_p) {
-            const uint32_t found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top,
-                                                    list, fill);
+            const uint32_t found = collect<TYPE, L>(g, row, most, E::from_key(lo), list, fill);
             if (found > (uint32_t)L::kList) {
                 if constexpr (G > kWave)
                     if (by_k) {                           // the k-th key, or nearly
                         const uint32_t enough = top_k <= L::kList ? L::kList : 0;
-                        const Range at = narrow<TYPE, L>(g, row, {lo, end, 0, found}, top_k,
+                        const Range at = narrow<TYPE, L>(g, row, most, {lo, end, 0, found}, top_k,
                                                          enough, (uint32_t *)list,
                                                          [](Cmp) { return 1u; });
                         lo = at.lo;
@@ -337,7 +346,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     }
                     before += we;
                 }
-                finish(h, [&] { return class_of(sorted[0]); });
+                finish(h, [&] { return class_of(sorted[0]); }, x_listed);
                 return true;
             };
             bool drawn = false;
@@ -444,13 +453,61 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                 lo = max(lo, E::key(ftop + logf((1.0f - top_p) * row_mass / (float)a.n) *
                                                temperature) - 1);
             const Range at = narrow<TYPE, L>(
-                g, row, {lo, end, 0, 0xFFFFFFFFu}, goal, 0, (uint32_t *)lists[gi],
-                [&](Cmp v) { return __float2uint_rn(exp_fast(x_of(v)) * unit); });
+                g, row, most, {lo, end, 0, 0xFFFFFFFFu}, goal, 0, (uint32_t *)lists[gi],
+                [&](Cmp v) __attribute__((always_inline)) {
+                    const float w = __builtin_amdgcn_exp2f((E::to_float(v) - ftop) * c);
+                    return (uint32_t)__builtin_fmaf(fminf(w, 1.0f), unit, 0.5f);
+                });
             cut_at(at.lo, (float)(goal - min(at.before, goal)) / unit);
         }
     }
+    if (min_p > 0.0f) {                                   // as a key: x grows with it
+        uint32_t no = tau - 1, yes = end - 1;
+        while (yes - no > 1) {
+            const uint32_t mid = no + (yes - no) / 2;
+            if (x_of(E::from_key(mid)) >= floor_x)
+                yes = mid;
+            else
+                no = mid;
+        }
+        if (yes > tau)
+            ties = kAll;
+        tau = yes;
+    }
     const Cmp at = E::from_key(tau);
     int32_t last = INT32_MAX;                             // the last kept class equal to tau
+    if constexpr (G > kWave && !PLAIN) {
+        // the kept classes in a list, if they are few: a list of many takes longer to
+        // fill, a piece of every lane at a time, than the row to be read again
+        uint64_t *list = lists[gi];
+        const uint32_t pieces = g.reduce((uint32_t)__popc(pieces_from<L>(most, at)), Add());
+        uint32_t found = 0xFFFFFFFFu;
+        if (pieces <= (uint32_t)G)
+            found = collect<TYPE, L>(g, row, most, at, list, fill);
+        if (found <= (uint32_t)L::kList) {
+            if (ties != kAll) {
+                sort_entries(g, list, found);
+                uint32_t above = 0;
+                for (uint32_t e = g.t; e < found; e += G)
+                    above += key_of(list[e]) > tau;
+                above = g.reduce(above, Add());
+                found = above + min(ties, found - above);
+            }
+            for (uint32_t e = g.t; e < found; e += G) {
+                const float x = x_of(E::from_key(key_of(list[e])));
+                const int32_t cls = class_of(list[e]);
+                const float score = x + noise[cls];
+                sum += exp_fast(x);
+                if (score > best || (score == best && cls < best_class)) {
+                    best = score;
+                    best_x = x;
+                    best_class = cls;
+                }
+            }
+            finish(g, first_class, x_listed);
+            return;
+        }
+    }
     if (ties != kAll) {
         uint32_t seen = 0;
         int32_t equal = -1;
@@ -470,8 +527,12 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         });
         last = g.reduce(equal, Max());
     }
-    draw_streamed(at, last);
-    finish(g, first_class);
+    // the largest logit below tau's (no element has the key of -0)
+    uint32_t below = tau - 1;
+    if (TYPE != kI32 && below == 0x7FFFFFFFu >> E::kShift)
+        --below;
+    draw_streamed(at, E::from_key(below), last);
+    finish(g, first_class, x_loaded);
 }
 
 }  // namespace

@@ -93,16 +93,16 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
         // lanes have any
         if (k <= (uint32_t)G)
             lo = max(lo, group_mth(g, top > E::lowest() ? E::key(top) : 0, k, (uint32_t *)list));
-        found = collect<TYPE, L>(g, row, most, E::from_key(lo), false, top, list, fill);
+        found = collect<TYPE, L>(g, row, most, E::from_key(lo), list, fill);
     }
     if (found > (uint32_t)L::kList) {
         // the k-th key, or a range of keys around it that fits the list
         Range at = {lo, E::key(g.reduce(top, Max())) + 1, 0, found};
         if constexpr (G > kWave) {
-            at = narrow<TYPE, L>(g, row, at, k, L::kList, (uint32_t *)list,
+            at = narrow<TYPE, L>(g, row, most, at, k, L::kList, (uint32_t *)list,
                                  [](Cmp) { return 1u; });
             if (at.before + at.here <= (uint32_t)L::kList)
-                found = collect<TYPE, L>(g, row, most, E::from_key(at.lo), false, top, list, fill);
+                found = collect<TYPE, L>(g, row, most, E::from_key(at.lo), list, fill);
         }
         if constexpr (G < kWave) {
             const auto count_from = [&](Cmp v) __attribute__((always_inline)) {
