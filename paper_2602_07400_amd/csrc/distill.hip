@@ -119,7 +119,8 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
 
     Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, w == 0.0f ? 0 : a.n, g.t);
     const bool rest = a.top_log_norm != nullptr;
-    float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f, from = 0.0f;
+    float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f, from = 0.0f,
+          from_out = 0.0f;
     const float c = a.inv_t * kLog2e;
     if (w != 0.0f) {
         head[g.t] = -1;
@@ -132,7 +133,9 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
             if (cls >= 0 && cls < a.n) {
                 x.cls = cls;
                 x.t = load_float(a.top_values, a.top_type, r * a.k + e) * a.inv_top_t;
-                x.z = Elem<TYPE>::to_float(load_one<TYPE>(src, cls));
+                const typename Elem<TYPE>::Cmp v = load_one<TYPE>(src, cls);
+                x.z = TYPE == kI32 && v == Elem<TYPE>::lowest() ? -__builtin_inff()
+                                                                : Elem<TYPE>::to_float(v);
                 const int piece = cls / L::VEC, owner = piece % L::G;
                 atomicOr(&mark[owner], 1u << (piece / L::G % 32));
                 x.next = atomicExch(&head[owner], e);
@@ -185,15 +188,22 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
             for (int u = 0; u < L::VEC; ++u)
                 sm.s += __builtin_amdgcn_exp2f((z[u] - from) * c);
         });
-        // everything relative to the row's maximum
-        const float m = g.reduce(fmaxf(sm.m, rest ? listed.m : sm.m), Max());
-        sm.raise(m, c);
-        listed.raise(m, c);
-        from = sm.from();
-        const float s_out = g.reduce(sm.s, Add());
+        // The rest relative to its own maximum, where its mass cannot vanish; the whole
+        // row relative to the larger of that and the list's.
+        sm = combine(g, sm, c);
+        const float s_out = sm.s;
+        from_out = sm.from();
+        from = from_out;
+        float share = 1.0f;                               // e^(from_out - from)
         S = s_out;
-        if (rest)
-            S += g.reduce(listed.s, Add());
+        if (rest) {
+            listed = combine(g, listed, c);
+            const float m = fmaxf(sm.m, listed.m);
+            share = sm.m == m ? 1.0f : __builtin_amdgcn_exp2f((sm.m - m) * c);
+            listed.raise(m, c);
+            from = listed.from();
+            S = s_out * share + listed.s;
+        }
         const float log_s = __builtin_amdgcn_logf(S) * kLn2;
         if (a.loss) {
             float sum = 0.0f;
@@ -205,7 +215,8 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
                 }
             sum = g.reduce(sum, Add());
             if (q_rest > 0.0f)
-                sum += q_rest * (logf(q_rest) - (__builtin_amdgcn_logf(s_out) * kLn2 - log_s));
+                sum += q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
+                                                 __builtin_amdgcn_logf(s_out) * kLn2 - log_s));
             if (g.t == 0)
                 a.loss[r] = w * sum;
         }
@@ -213,10 +224,10 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
         if (Q + q_rest == 0.0f)
             scale = 0.0f;                                 // a teacher without classes
         in_list = scale * (Q + q_rest) / S;
-        outside = in_list;
+        outside = in_list * share;
         if (q_rest > 0.0f)
             outside = s_out == 0.0f && S > 0.0f
-                          ? 0.0f : scale * ((Q + q_rest) / S - q_rest / s_out);
+                          ? 0.0f : scale * ((Q + q_rest) * share / S - q_rest / s_out);
         if (dst) {
             for (int e = g.t; e < a.k; e += L::G)
                 if (list[e].cls >= 0)
@@ -241,7 +252,7 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
             float v[L::VEC];
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
-                v[u] = outside * __builtin_amdgcn_exp2f((p.get(u) - from) * c);
+                v[u] = outside * __builtin_amdgcn_exp2f((p.get(u) - from_out) * c);
             if (marked >> (j % 32) & 1)
                 for (int e = head[g.t]; e >= 0; e = list[e].next)
                     if (list[e].cls / (L::G * L::VEC) == j) {
@@ -252,6 +263,134 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
                     }
             store_piece<TYPE, L::VEC>(dst, i - g.t * L::VEC, g.t * L::VEC, a.n, v);
         });
+    }
+}
+
+// A lane a row (k <= kLaneEntries): the list's classes leave the tile for their entries
+// before it is summed, the exponentials take the logits' places in it, then the
+// gradients theirs.
+constexpr int32_t kLaneEntries = 32;
+
+template <int TYPE>
+__global__ __launch_bounds__(kWave) void k_distill_lanes(DistillArgs a)
+{
+    extern __shared__ uint32_t tile[];                    // [64][pitch], then [64][step] of
+    const int32_t pitch = lane_pitch(a.n), step = a.k | 1, lane = threadIdx.x;
+    float *const tops = reinterpret_cast<float *>(tile) + kWave * pitch;   // teacher / Tt
+    float *const zs = tops + kWave * step;                                 // student
+    int32_t *const classes = reinterpret_cast<int32_t *>(zs + kWave * step);
+    const int64_t r0 = (int64_t)blockIdx.x * kWave;
+    const int32_t rows = (int32_t)min((int64_t)kWave, a.n_rows - r0);
+    for (int32_t e = lane; e < rows * a.k; e += kWave) {
+        const int32_t to = e / a.k * step + e % a.k, cls = a.top_indices[r0 * a.k + e];
+        classes[to] = cls >= 0 && cls < a.n ? cls : -1;
+        tops[to] = load_float(a.top_values, a.top_type, r0 * a.k + e) * a.inv_top_t;
+    }
+    load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, tile);
+    wave_sync();
+
+    if (lane < rows) {
+        const int64_t r = r0 + lane;
+        const float w = a.row_weight ? a.row_weight[r] : 1.0f;
+        float *z = reinterpret_cast<float *>(tile) + lane * pitch;
+        const float *top = tops + lane * step;
+        float *listed = zs + lane * step;
+        const int32_t *cls = classes + lane * step;
+        const float c = a.inv_t * kLog2e;
+        float scale = 0.0f, loss = 0.0f;
+        if (w != 0.0f) {
+            // the list leaves the tile; both relative to their own maxima
+            float m_list = -__builtin_inff(), m = -__builtin_inff();
+            for (int e = 0; e < a.k; ++e)
+                if (cls[e] >= 0) {
+                    const int32_t v = __float_as_int(z[cls[e]]);
+                    listed[e] = TYPE != kI32 ? z[cls[e]]
+                                : v == INT32_MIN ? -__builtin_inff() : (float)v;
+                    z[cls[e]] = TYPE == kI32 ? __int_as_float(INT32_MIN) : -__builtin_inff();
+                    m_list = fmaxf(m_list, listed[e]);
+                }
+#pragma unroll 8
+            for (int i = 0; i < a.n; ++i) {
+                if constexpr (TYPE == kI32) {
+                    const int32_t v = __float_as_int(z[i]);
+                    z[i] = v == INT32_MIN ? -__builtin_inff() : (float)v;
+                }
+                m = fmaxf(m, z[i]);
+            }
+            const float from_out = m == -__builtin_inff() ? 0.0f : m;
+            const float share = m >= m_list ? 1.0f : __builtin_amdgcn_exp2f((m - m_list) * c);
+            m = fmaxf(m, m_list);
+            const float from = m == -__builtin_inff() ? 0.0f : m;
+            float log_norm;
+            if (a.top_log_norm) {
+                log_norm = a.top_log_norm[r];
+            } else {
+                float tm = -__builtin_inff(), sum = 0.0f;
+                for (int e = 0; e < a.k; ++e)
+                    tm = fmaxf(tm, cls[e] >= 0 ? top[e] : -__builtin_inff());
+                for (int e = 0; e < a.k; ++e)
+                    sum += cls[e] >= 0 ? exp_fast(top[e] - tm) : 0.0f;
+                log_norm = tm + logf(sum);
+            }
+            float Q = 0.0f, s_list = 0.0f, s_out = 0.0f;
+            for (int e = 0; e < a.k; ++e)
+                if (cls[e] >= 0) {
+                    Q += exp_fast(top[e] - log_norm);
+                    s_list += __builtin_amdgcn_exp2f((listed[e] - from) * c);
+                }
+#pragma unroll 8
+            for (int i = 0; i < a.n; ++i) {
+                const float e = __builtin_amdgcn_exp2f((z[i] - from_out) * c);
+                s_out += e;
+                z[i] = e;
+            }
+            const float S = s_out * share + s_list, log_s = __builtin_amdgcn_logf(S) * kLn2;
+            const float q_rest = a.top_log_norm ? fmaxf(0.0f, 1.0f - Q) : 0.0f;
+            if (Q + q_rest != 0.0f)                       // (a teacher without classes)
+                scale = w * a.inv_t;
+            const float in_list = scale * (Q + q_rest) / S;
+            float outside = in_list * share;
+            if (q_rest > 0.0f) {
+                loss = q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
+                                                 __builtin_amdgcn_logf(s_out) * kLn2 - log_s));
+                outside = s_out == 0.0f && S > 0.0f
+                              ? 0.0f : scale * ((Q + q_rest) * share / S - q_rest / s_out);
+            }
+            if (a.grad && scale != 0.0f)
+#pragma unroll 8
+                for (int i = 0; i < a.n; ++i)
+                    z[i] *= outside;
+            for (int e = 0; e < a.k; ++e)
+                if (cls[e] >= 0) {
+                    const float log_q = top[e] - log_norm, q = exp_fast(log_q);
+                    const float x = (listed[e] - from) * a.inv_t;
+                    loss += q == 0.0f ? 0.0f : q * (log_q - (x - log_s));
+                    if (scale != 0.0f)
+                        z[cls[e]] = in_list * __builtin_amdgcn_exp2f((listed[e] - from) * c) -
+                                    scale * q;
+                }
+            loss *= w;
+        }
+        if (a.loss)
+            a.loss[r] = loss;
+        if (a.grad && scale == 0.0f)
+            for (int i = 0; i < a.n; ++i)
+                z[i] = 0.0f;
+    }
+    if constexpr (TYPE != kI32) {
+        if (!a.grad)
+            return;
+        wave_sync();
+        typedef typename std::conditional<TYPE == kF32, float, typename std::conditional<
+            TYPE == kF16, _Float16, __bf16>::type>::type Out;
+        const uint32_t inverse = ((1u << 20) + a.n - 1) / a.n, count = (uint32_t)(rows * a.n);
+        char *dst = a.grad + r0 * a.grad_stride;
+#pragma unroll 4
+        for (uint32_t e = lane; e < count; e += kWave) {
+            const uint32_t row = e * inverse >> 20, col = e - row * a.n;
+            reinterpret_cast<Out *>(dst + row * a.grad_stride)[col] =
+                (Out)__uint_as_float(tile[row * pitch + col]);
+        }
     }
 }
 
@@ -270,6 +409,12 @@ hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int3
                                inv_top_t, static_cast<const char *>(top_values), top_indices,
                                top_log_norm, row_weight, loss, static_cast<char *>(grad),
                                grad_stride * Elem<TYPE>::kBytes};
+        if (n <= kLaneClasses && k <= kLaneEntries && n_rows >= kLaneRows) {
+            const size_t words = (size_t)kWave * (lane_pitch(n) + 3 * (k | 1));
+            k_distill_lanes<TYPE><<<(uint32_t)((n_rows + kWave - 1) / kWave), kWave, words * 4,
+                                    stream>>>(a);
+            return hipGetLastError();
+        }
         return with_layout<TYPE>(n, k, [&](auto layout) {
             typedef decltype(layout) L;
             k_distill<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock,

@@ -189,6 +189,122 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
         put(e, -1, E::lowest());
 }
 
+// The larger and the smaller of two positive doubles (plain v_max and v_min: the
+// compiler's own put a canonicalization before each).
+__device__ __forceinline__ double max_of(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double min_of(double a, double b)
+{
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// A lane a row, k <= K: every class is carried down a sorted list in registers.  Class
+// and key are the mantissa of a double (52 bits: 32 of key, then the class reversed), so
+// that a step of the list is one maximum and one minimum.
+template <int TYPE, int K>
+__global__ __launch_bounds__(kWave) void k_top_lanes(TopArgs a)
+{
+    typedef Elem<TYPE == kI32 ? kI32 : kF32> E;           // (the tile's elements)
+    typedef typename E::Cmp Cmp;
+    extern __shared__ uint32_t tile[];
+    const int64_t r0 = (int64_t)blockIdx.x * kWave;
+    const int32_t rows = (int32_t)min((int64_t)kWave, a.n_rows - r0);
+    load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, tile);
+    wave_sync();
+    const uint32_t *own = tile + min((int32_t)threadIdx.x, rows - 1) * lane_pitch(a.n);
+    const auto at = [&](int i) __attribute__((always_inline)) {
+        Cmp v;
+        __builtin_memcpy(&v, &own[i], 4);
+        return v;
+    };
+    constexpr uint32_t kOne = 0x43300000u;                // 2^52
+    double best[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        best[j] = __hiloint2double(kOne, 0);
+#pragma unroll 4
+    for (int i = 0; i < a.n; ++i) {
+        const Cmp v = at(i);
+        const uint32_t key = v > E::lowest() ? E::key(v) : 0;
+        double x = __hiloint2double(kOne | key >> 12, key << 20 | (kLaneClasses - 1 - i));
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const double down = min_of(best[j], x);
+            best[j] = max_of(best[j], x);
+            x = down;
+        }
+    }
+    const auto key_at = [&](int j) __attribute__((always_inline)) {
+        return (uint32_t)__double2hiint(best[j]) << 12 | (uint32_t)__double2loint(best[j]) >> 20;
+    };
+    if (a.log_norm) {
+        const uint32_t first = key_at(0);
+        const float m = first ? E::to_float(E::from_key(first)) : -__builtin_inff();
+        const float from = first ? m : 0.0f, c = a.inv_t * kLog2e;
+        Softmax sm = {m, 0.0f};
+#pragma unroll 4
+        for (int i = 0; i < a.n; ++i) {
+            const Cmp v = at(i);
+            sm.s += v > E::lowest() ? __builtin_amdgcn_exp2f((E::to_float(v) - from) * c) : 0.0f;
+        }
+        if ((int32_t)threadIdx.x < rows)
+            a.log_norm[r0 + threadIdx.x] = sm.log_norm(a.inv_t);
+    }
+    // the lists by way of the tile, to be stored in whole lines
+    uint32_t value[K];
+    int32_t cls[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        cls[j] = key_at(j) ? kLaneClasses - 1 - (int32_t)(__double2loint(best[j]) & 0xFFFFF) : -1;
+        const Cmp none = E::lowest();
+        __builtin_memcpy(&value[j], &none, 4);
+        if (j < a.k && cls[j] >= 0)
+            value[j] = own[cls[j]];
+    }
+    wave_sync();
+    const int32_t half = kWave * a.k;
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        if (j < a.k) {
+            tile[threadIdx.x * a.k + j] = value[j];
+            tile[half + threadIdx.x * a.k + j] = (uint32_t)cls[j];
+        }
+    wave_sync();
+    for (int32_t e = threadIdx.x; e < rows * a.k; e += kWave) {
+        const int64_t to = r0 * a.k + e;
+        a.indices[to] = (int32_t)tile[half + e];
+        const uint32_t v = tile[e];
+        if constexpr (TYPE == kF16)
+            reinterpret_cast<_Float16 *>(a.values)[to] = (_Float16)__uint_as_float(v);
+        else if constexpr (TYPE == kBf16)
+            reinterpret_cast<uint16_t *>(a.values)[to] = (uint16_t)(v >> 16);
+        else
+            reinterpret_cast<uint32_t *>(a.values)[to] = v;
+    }
+}
+
+// Entries a lane's list has room for.
+template <int TYPE>
+hipError_t launch_lanes(const TopArgs &a, hipStream_t stream)
+{
+    const uint32_t blocks = (uint32_t)((a.n_rows + kWave - 1) / kWave);
+    const size_t words = (size_t)kWave * (lane_pitch(a.n) > 2 * a.k ? lane_pitch(a.n) : 2 * a.k);
+    if (a.k <= 4)
+        k_top_lanes<TYPE, 4><<<blocks, kWave, words * 4, stream>>>(a);
+    else if (a.k <= 8)
+        k_top_lanes<TYPE, 8><<<blocks, kWave, words * 4, stream>>>(a);
+    else
+        k_top_lanes<TYPE, 12><<<blocks, kWave, words * 4, stream>>>(a);
+    return hipGetLastError();
+}
+constexpr int32_t kLaneEntries = 12;
+
 }  // namespace
 
 hipError_t launch_top_logits(const void *logits, int32_t type, int64_t n_rows, int32_t n,
@@ -199,6 +315,8 @@ hipError_t launch_top_logits(const void *logits, int32_t type, int64_t n_rows, i
         constexpr int TYPE = decltype(ty)::value;
         const TopArgs a = {static_cast<const char *>(logits), row_stride * Elem<TYPE>::kBytes,
                            n_rows, n, k, inv_t, static_cast<char *>(values), indices, log_norm};
+        if (n <= kLaneClasses && k <= kLaneEntries && n_rows >= kLaneRows)
+            return launch_lanes<TYPE>(a, stream);
         return with_layout<TYPE>(n, 0, [&](auto layout) {
             typedef decltype(layout) L;
             k_top<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock, 0,

@@ -46,11 +46,13 @@ def distill(z, temperature, t, idx, top_temperature, log_norm=None):
         out = np.ones(n, bool)
         out[at] = False
         q_rest = 0.0 if log_norm is None else max(0.0, 1 - qj.sum())
-        p_rest = p[out].sum()
+        log_rest = log_sum(log_p[out]) if out.any() else -np.inf   # (p itself may vanish)
+        p_rest = np.exp(log_rest)
         grad = (qj.sum() + q_rest) * p - q
         if q_rest > 0:
-            loss += q_rest * (np.log(q_rest) - np.log(p_rest))
-            grad[out] -= np.where(p[out] > 0, q_rest * p[out] / p_rest, 0.0)
+            loss += q_rest * (np.log(q_rest) - log_rest)
+            if log_rest > -np.inf or np.isnan(log_rest) or not np.isfinite(z).any():
+                grad[out] -= q_rest * np.exp(log_p[out] - log_rest)
         if qj.sum() + q_rest == 0:
             grad[:] = 0.0
     return loss, grad / temperature, p, q, q_rest, p_rest

@@ -148,14 +148,15 @@ def _norm(t, idx, top_temperature, share):
 
 def _check_distill(z, t, idx, log_norm, temperature, top_temperature, weight, got):
     loss, grad = (v.cpu() if v is not None else None for v in got)
-    x, _ = _host(z)
+    x, masked = _host(z)
+    x[masked & ~np.isnan(x)] = -np.inf                    # (the lowest int32 is a mask too)
     tv, iv = _host(t)[0], idx.cpu().numpy()
     for r in range(z.shape[0]):
         w = 1.0 if weight is None else float(weight[r])
         ln = None if log_norm is None else float(log_norm[r])
         want, g, p, q, q_rest, p_rest = oracle.distill(x[r], temperature, tv[r], iv[r],
                                                        top_temperature, ln)
-        have = (iv[r] >= 0) & (iv[r] < z.shape[1])
+        have = have_list = (iv[r] >= 0) & (iv[r] < z.shape[1])
         M = max(np.abs(x[r][np.isfinite(x[r])]).max(initial=0) / temperature,
                 np.abs(tv[r][have]).max(initial=0) / top_temperature,
                 abs(ln) if ln is not None and np.isfinite(ln) else 0)
@@ -175,7 +176,11 @@ def _check_distill(z, t, idx, log_norm, temperature, top_temperature, weight, go
             g = w * g
             assert np.array_equal(np.isnan(have), np.isnan(g)), r
             fine = ~np.isnan(g)
-            back = np.where((q == 0) & (p_rest > 0), q_rest * p / (p_rest or 1), 0)
+            listed = np.zeros(len(p), bool)
+            listed[iv[r][have_list]] = True
+            rest = np.where(listed, -np.inf, x[r] / temperature)
+            top = oracle.log_sum(rest)
+            back = q_rest * np.exp(rest - top) if np.isfinite(top) else np.zeros(len(p))
             tol = (abs(w) / temperature * ((q.sum() + q_rest) * p + q + back) * rel
                    + EPS[z.dtype] * np.abs(g) + TINY[z.dtype])
             assert (np.abs(have - g)[fine] <= tol[fine]).all(), r
@@ -433,6 +438,57 @@ def test_sample_frequencies():
     count = np.bincount(token.cpu().numpy(), minlength=c)
     assert (np.abs(count - n * p) <= 6 * np.sqrt(n * p * (1 - p)) + 1e-9).all()
     assert np.allclose(np.exp(log_prob.cpu().numpy()), p[token.cpu().numpy()], rtol=3 * REL)
+
+
+# ------------------------------------------------------------ many short rows
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("c", [1, 2, 10, 37, 63, 64, 65, 100, 127, 128])
+def test_many_short_rows(c, dtype):
+    """From 16384 rows on a lane takes a row: masks, ties, empty lists and strides among
+    17003 rows, of which the oracle checks the first 150 and the last 60."""
+    rng = _rng(16, c, TYPES.index(dtype))
+    n = 17003
+    wide = _logits(rng, n, c + 3, dtype)
+    low = torch.iinfo(dtype).min if dtype == torch.int32 else -np.inf
+    wide[::7, :] = torch.round(wide[::7, :].float()).to(dtype)
+    wide[3, :] = low
+    wide[4, 1:] = low
+    wide[5, rng.integers(0, c, c)] = low
+    wide[6] = 7
+    if dtype != torch.int32:
+        wide[8, ::2] = np.nan
+        wide[9] = torch.finfo(dtype).min
+        wide[10, :] = torch.where(torch.arange(c + 3) % 2 == 0, 0.0, -0.0)
+    wide = wide.to(DEV)
+    some = np.r_[0:150, n - 60:n]
+    for x in (wide[:, 1:c + 1], wide[:, :c].contiguous()):
+        for k in sorted({1, min(c, 4), 7, 12}):
+            v, i, norm = bl.bitlogic_top_logits(x, k, 1.5)
+            few = bl.bitlogic_top_logits(x[some], k, 1.5)
+            assert torch.equal(i[some], few[1]) and torch.equal(v[some], few[0])
+            d = (norm[some] - few[2]).abs()
+            assert ((d <= 2 * REL + 2.0 ** -21 * few[2].abs()) | (norm[some] == few[2])).all()
+            _check_top(x[some], k, 1.5)
+        k = min(c, 9)
+        t, idx = _teacher(rng, n, c, k, dtype)
+        idx[20] = -1
+        idx[21, 1:] = c
+        tt = 20.0 if dtype == torch.int32 else 1.0
+        weight = torch.from_numpy(rng.uniform(0.2, 2, n).astype(np.float32))
+        weight[::11] = 0
+        for rest in (False, True):
+            if rest and k == c:
+                continue
+            ln = _norm(t, idx, tt, 0.8) if rest else None
+            if rest:
+                ln[20] = 0.0
+            loss, grad = bl.bitlogic_distill(
+                x, t.to(DEV), idx.to(DEV), None if ln is None else ln.to(DEV), 2.0, tt,
+                weight.to(DEV), want_grad=dtype != torch.int32)
+            torch.cuda.synchronize()
+            _check_distill(x[some], t[some], idx[some], None if ln is None else ln[some], 2.0, tt,
+                           weight[some], (loss[some], None if grad is None else grad[some]))
 
 
 # ------------------------------------------------ addresses, streams, graphs
