@@ -266,57 +266,73 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
     }
 }
 
-// A lane a row (k <= kLaneEntries): the list's classes leave the tile for their entries
-// before it is summed, the exponentials take the logits' places in it, then the
-// gradients theirs.
+// Four lanes a row, 16 rows a wave (k <= kLaneEntries): the list's classes leave the tile
+// for their entries before it is summed, the exponentials take the logits' places in it,
+// then the gradients theirs.  (A lane a row has a quarter of the waves, and their chains
+// of LDS accesses take four times as long: 148 us for 262144 rows of 100 classes.)
 constexpr int32_t kLaneEntries = 32;
+constexpr int kRowLanes = 4;
+constexpr int kWaveRows = kWave / kRowLanes;
+constexpr int kLaneThreads = 256;
+
+// Rows an odd number of 4 words apart: 16 rows' lanes are in 64 different banks.
+__host__ __device__ inline int32_t quad_pitch(int32_t n) { return ((n + 3) / 4 | 1) * 4; }
 
 template <int TYPE>
-__global__ __launch_bounds__(kWave) void k_distill_lanes(DistillArgs a)
+__global__ __launch_bounds__(kLaneThreads) void k_distill_lanes(DistillArgs a)
 {
-    extern __shared__ uint32_t tile[];                    // [64][pitch], then [64][step] of
-    const int32_t pitch = lane_pitch(a.n), step = a.k | 1, lane = threadIdx.x;
-    float *const tops = reinterpret_cast<float *>(tile) + kWave * pitch;   // teacher / Tt
-    float *const zs = tops + kWave * step;                                 // student
-    int32_t *const classes = reinterpret_cast<int32_t *>(zs + kWave * step);
-    const int64_t r0 = (int64_t)blockIdx.x * kWave;
-    const int32_t rows = (int32_t)min((int64_t)kWave, a.n_rows - r0);
+    extern __shared__ uint32_t tiles[];                   // a wave's [16][pitch], and [16][k] of
+    const int32_t pitch = quad_pitch(a.n), lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    uint32_t *const tile = tiles + wave * kWaveRows * (pitch + 3 * a.k);
+    float *const tops = reinterpret_cast<float *>(tile) + kWaveRows * pitch;   // teacher / Tt
+    float *const zs = tops + kWaveRows * a.k;                                  // student
+    int32_t *const classes = reinterpret_cast<int32_t *>(zs + kWaveRows * a.k);
+    const int64_t r0 = ((int64_t)blockIdx.x * (kLaneThreads / kWave) + wave) * kWaveRows;
+    if (r0 >= a.n_rows)
+        return;
+    const int32_t rows = (int32_t)min((int64_t)kWaveRows, a.n_rows - r0);
     for (int32_t e = lane; e < rows * a.k; e += kWave) {
-        const int32_t to = e / a.k * step + e % a.k, cls = a.top_indices[r0 * a.k + e];
-        classes[to] = cls >= 0 && cls < a.n ? cls : -1;
-        tops[to] = load_float(a.top_values, a.top_type, r0 * a.k + e) * a.inv_top_t;
+        const int32_t cls = a.top_indices[r0 * a.k + e];
+        classes[e] = cls >= 0 && cls < a.n ? cls : -1;
+        tops[e] = load_float(a.top_values, a.top_type, r0 * a.k + e) * a.inv_top_t;
     }
-    load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, tile);
+    load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, pitch, tile);
     wave_sync();
 
-    if (lane < rows) {
-        const int64_t r = r0 + lane;
+    Group<kRowLanes> g(lane % kRowLanes, nullptr);
+    const int32_t own = lane / kRowLanes;
+    if (own < rows) {
+        const int64_t r = r0 + own;
         const float w = a.row_weight ? a.row_weight[r] : 1.0f;
-        float *z = reinterpret_cast<float *>(tile) + lane * pitch;
-        const float *top = tops + lane * step;
-        float *listed = zs + lane * step;
-        const int32_t *cls = classes + lane * step;
+        float *z = reinterpret_cast<float *>(tile) + own * pitch;
+        const float *top = tops + own * a.k;
+        float *listed = zs + own * a.k;
+        const int32_t *cls = classes + own * a.k;
         const float c = a.inv_t * kLog2e;
         float scale = 0.0f, loss = 0.0f;
         if (w != 0.0f) {
             // the list leaves the tile; both relative to their own maxima
-            float m_list = -__builtin_inff(), m = -__builtin_inff();
-            for (int e = 0; e < a.k; ++e)
+            float m_list = -__builtin_inff(), m = -__builtin_inff(), tm = -__builtin_inff();
+            for (int e = g.t; e < a.k; e += kRowLanes)
                 if (cls[e] >= 0) {
                     const int32_t v = __float_as_int(z[cls[e]]);
                     listed[e] = TYPE != kI32 ? z[cls[e]]
                                 : v == INT32_MIN ? -__builtin_inff() : (float)v;
                     z[cls[e]] = TYPE == kI32 ? __int_as_float(INT32_MIN) : -__builtin_inff();
                     m_list = fmaxf(m_list, listed[e]);
+                    tm = fmaxf(tm, top[e]);
                 }
+            m_list = g.reduce(m_list, Max());
+            wave_sync();
 #pragma unroll 8
-            for (int i = 0; i < a.n; ++i) {
+            for (int i = g.t; i < a.n; i += kRowLanes) {
                 if constexpr (TYPE == kI32) {
                     const int32_t v = __float_as_int(z[i]);
                     z[i] = v == INT32_MIN ? -__builtin_inff() : (float)v;
                 }
                 m = fmaxf(m, z[i]);
             }
+            m = g.reduce(m, Max());
             const float from_out = m == -__builtin_inff() ? 0.0f : m;
             const float share = m >= m_list ? 1.0f : __builtin_amdgcn_exp2f((m - m_list) * c);
             m = fmaxf(m, m_list);
@@ -325,42 +341,42 @@ __global__ __launch_bounds__(kWave) void k_distill_lanes(DistillArgs a)
             if (a.top_log_norm) {
                 log_norm = a.top_log_norm[r];
             } else {
-                float tm = -__builtin_inff(), sum = 0.0f;
-                for (int e = 0; e < a.k; ++e)
-                    tm = fmaxf(tm, cls[e] >= 0 ? top[e] : -__builtin_inff());
-                for (int e = 0; e < a.k; ++e)
+                tm = g.reduce(tm, Max());
+                float sum = 0.0f;
+                for (int e = g.t; e < a.k; e += kRowLanes)
                     sum += cls[e] >= 0 ? exp_fast(top[e] - tm) : 0.0f;
-                log_norm = tm + logf(sum);
+                log_norm = tm + logf(g.reduce(sum, Add()));
             }
             float Q = 0.0f, s_list = 0.0f, s_out = 0.0f;
-            for (int e = 0; e < a.k; ++e)
+            for (int e = g.t; e < a.k; e += kRowLanes)
                 if (cls[e] >= 0) {
                     Q += exp_fast(top[e] - log_norm);
                     s_list += __builtin_amdgcn_exp2f((listed[e] - from) * c);
                 }
 #pragma unroll 8
-            for (int i = 0; i < a.n; ++i) {
+            for (int i = g.t; i < a.n; i += kRowLanes) {
                 const float e = __builtin_amdgcn_exp2f((z[i] - from_out) * c);
                 s_out += e;
                 z[i] = e;
             }
+            Q = g.reduce(Q, Add());
+            s_list = g.reduce(s_list, Add());
+            s_out = g.reduce(s_out, Add());
             const float S = s_out * share + s_list, log_s = __builtin_amdgcn_logf(S) * kLn2;
             const float q_rest = a.top_log_norm ? fmaxf(0.0f, 1.0f - Q) : 0.0f;
             if (Q + q_rest != 0.0f)                       // (a teacher without classes)
                 scale = w * a.inv_t;
             const float in_list = scale * (Q + q_rest) / S;
             float outside = in_list * share;
-            if (q_rest > 0.0f) {
-                loss = q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
-                                                 __builtin_amdgcn_logf(s_out) * kLn2 - log_s));
+            if (q_rest > 0.0f)
                 outside = s_out == 0.0f && S > 0.0f
                               ? 0.0f : scale * ((Q + q_rest) * share / S - q_rest / s_out);
-            }
             if (a.grad && scale != 0.0f)
 #pragma unroll 8
-                for (int i = 0; i < a.n; ++i)
+                for (int i = g.t; i < a.n; i += kRowLanes)
                     z[i] *= outside;
-            for (int e = 0; e < a.k; ++e)
+            wave_sync();
+            for (int e = g.t; e < a.k; e += kRowLanes)
                 if (cls[e] >= 0) {
                     const float log_q = top[e] - log_norm, q = exp_fast(log_q);
                     const float x = (listed[e] - from) * a.inv_t;
@@ -369,12 +385,16 @@ __global__ __launch_bounds__(kWave) void k_distill_lanes(DistillArgs a)
                         z[cls[e]] = in_list * __builtin_amdgcn_exp2f((listed[e] - from) * c) -
                                     scale * q;
                 }
+            loss = g.reduce(loss, Add());
+            if (q_rest > 0.0f)
+                loss += q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
+                                                  __builtin_amdgcn_logf(s_out) * kLn2 - log_s));
             loss *= w;
         }
-        if (a.loss)
+        if (a.loss && g.t == 0)
             a.loss[r] = loss;
         if (a.grad && scale == 0.0f)
-            for (int i = 0; i < a.n; ++i)
+            for (int i = g.t; i < a.n; i += kRowLanes)
                 z[i] = 0.0f;
     }
     if constexpr (TYPE != kI32) {
@@ -410,9 +430,10 @@ hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int3
                                top_log_norm, row_weight, loss, static_cast<char *>(grad),
                                grad_stride * Elem<TYPE>::kBytes};
         if (n <= kLaneClasses && k <= kLaneEntries && n_rows >= kLaneRows) {
-            const size_t words = (size_t)kWave * (lane_pitch(n) + 3 * (k | 1));
-            k_distill_lanes<TYPE><<<(uint32_t)((n_rows + kWave - 1) / kWave), kWave, words * 4,
-                                    stream>>>(a);
+            constexpr int kRows = kLaneThreads / kRowLanes;
+            const size_t words = (size_t)kRows * (quad_pitch(n) + 3 * k);
+            k_distill_lanes<TYPE><<<(uint32_t)((n_rows + kRows - 1) / kRows), kLaneThreads,
+                                    words * 4, stream>>>(a);
             return hipGetLastError();
         }
         return with_layout<TYPE>(n, k, [&](auto layout) {

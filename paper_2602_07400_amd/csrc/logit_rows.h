@@ -844,14 +844,13 @@ hipError_t with_type(int32_t type, F f)
 }
 
 // ---- a lane a row: many short rows ----
-// A wave takes 64 rows of up to kLaneClasses classes through a tile in LDS, rows an odd
-// number of words apart, and each lane goes through its row by itself: no reductions,
-// and everything that is done once a row is done for 64 of them.  It pays once there
-// are rows for all the GPU's waves: from kLaneRows rows on.
+// A wave takes 64 or 16 rows of up to kLaneClasses classes through a tile in LDS, and a
+// lane or four go through a row: few reductions or none, and what is done once a row is
+// done for many of them.  It pays once there are rows for all the GPU's waves: from
+// kLaneRows rows on.
 constexpr int32_t kLaneClasses = 128;
 constexpr int64_t kLaneRows = 16384;
 
-__host__ __device__ inline int32_t lane_pitch(int32_t n) { return n | 1; }
 
 // Orders a wave's LDS accesses: they run in order; the compiler keeps them so.
 __device__ __forceinline__ void wave_sync()
@@ -864,13 +863,12 @@ __device__ __forceinline__ void wave_sync()
 // rows' n * rows is in row e / n = e * ceil(2^20 / n) >> 20: exact below 2^13, n <= 128.
 template <int TYPE>
 __device__ __forceinline__ void load_tile(const char *src, int64_t stride, int32_t rows,
-                                          int32_t n, uint32_t *tile)
+                                          int32_t n, int32_t pitch, uint32_t *tile)
 {
     typedef typename Elem<TYPE>::Cmp Cmp;
     constexpr int kFlight = 16;
-    const int32_t pitch = lane_pitch(n);
     const uint32_t inverse = ((1u << 20) + n - 1) / n, count = (uint32_t)(rows * n);
-    for (uint32_t e = threadIdx.x; e < count; e += kFlight * kWave) {
+    for (uint32_t e = threadIdx.x % kWave; e < count; e += kFlight * kWave) {
         Cmp v[kFlight];
         uint32_t to[kFlight];
 #pragma unroll

@@ -215,9 +215,9 @@ __global__ __launch_bounds__(kWave) void k_top_lanes(TopArgs a)
     extern __shared__ uint32_t tile[];
     const int64_t r0 = (int64_t)blockIdx.x * kWave;
     const int32_t rows = (int32_t)min((int64_t)kWave, a.n_rows - r0);
-    load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, tile);
+    load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, a.n | 1, tile);
     wave_sync();
-    const uint32_t *own = tile + min((int32_t)threadIdx.x, rows - 1) * lane_pitch(a.n);
+    const uint32_t *own = tile + min((int32_t)threadIdx.x, rows - 1) * (a.n | 1);
     const auto at = [&](int i) __attribute__((always_inline)) {
         Cmp v;
         __builtin_memcpy(&v, &own[i], 4);
@@ -294,7 +294,7 @@ template <int TYPE>
 hipError_t launch_lanes(const TopArgs &a, hipStream_t stream)
 {
     const uint32_t blocks = (uint32_t)((a.n_rows + kWave - 1) / kWave);
-    const size_t words = (size_t)kWave * (lane_pitch(a.n) > 2 * a.k ? lane_pitch(a.n) : 2 * a.k);
+    const size_t words = (size_t)kWave * ((a.n | 1) > 2 * a.k ? a.n | 1 : 2 * a.k);
     if (a.k <= 4)
         k_top_lanes<TYPE, 4><<<blocks, kWave, words * 4, stream>>>(a);
     else if (a.k <= 8)
