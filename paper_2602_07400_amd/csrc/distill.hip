@@ -93,12 +93,13 @@ __device__ __forceinline__ void store_piece(char *row, int32_t first, int32_t i,
 // A teacher's entry in LDS.
 struct Entry {
     int32_t cls, next;                  // class (-1: none); next entry of the owning lane
-    float t;                            // teacher logit / Tt; later the gradient
-    float z;                            // the student's logit
+    float t, z;                         // teacher logit / Tt, student's logit
+    float grad;
 };
 
-template <int TYPE, class L>
-__global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
+// GRAD: with the gradient; the loss alone reads the row once and keeps none of it.
+template <int TYPE, class L, bool GRAD>
+__global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_distill(DistillArgs a)
 {
     typedef Piece<TYPE, L::VEC> P;
     extern __shared__ Entry entries[];                    // [rows of the block][k]
@@ -110,14 +111,19 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
     if (r >= a.n_rows)
         return;
     Group<L::G> g(threadIdx.x - gi * L::G, &scratch);
+    // What the list sums to is worked out by every wave for itself: lists are short, and
+    // a reduction over the block costs two of its barriers (4099 x 32003, loss: 67 us with
+    // them).
+    constexpr int H = L::G < kWave ? L::G : kWave;
+    Group<H> h(g.t % H, nullptr);
     Entry *list = entries + (int64_t)gi * a.k;
     int32_t *head = heads + gi * L::G;
     uint32_t *mark = marks + gi * L::G;
     const char *src = a.logits + r * a.stride;
-    char *dst = a.grad ? a.grad + r * a.grad_stride : nullptr;
+    char *dst = GRAD ? a.grad + r * a.grad_stride : nullptr;
     const float w = a.row_weight ? a.row_weight[r] : 1.0f;
 
-    Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT> row(src, w == 0.0f ? 0 : a.n, g.t);
+    Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT, GRAD> row(src, w == 0.0f ? 0 : a.n, g.t);
     const bool rest = a.top_log_norm != nullptr;
     float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f, from = 0.0f,
           from_out = 0.0f;
@@ -126,10 +132,9 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
         head[g.t] = -1;
         mark[g.t] = 0;
         g.barrier();
-        float tm = -__builtin_inff();
         for (int e = g.t; e < a.k; e += L::G) {
             const int32_t cls = a.top_indices[r * a.k + e];
-            Entry x = {-1, -1, -__builtin_inff(), 0.0f};
+            Entry x = {-1, -1, -__builtin_inff(), 0.0f, 0.0f};
             if (cls >= 0 && cls < a.n) {
                 x.cls = cls;
                 x.t = load_float(a.top_values, a.top_type, r * a.k + e) * a.inv_top_t;
@@ -139,33 +144,34 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
                 const int piece = cls / L::VEC, owner = piece % L::G;
                 atomicOr(&mark[owner], 1u << (piece / L::G % 32));
                 x.next = atomicExch(&head[owner], e);
-                tm = fmaxf(tm, x.t);
             }
             list[e] = x;
         }
+        g.barrier();
         // the teacher's normalizer: of the list, or given
         float log_norm;
         if (rest) {
             log_norm = a.top_log_norm[r];
         } else {
-            tm = g.reduce(tm, Max());
-            float sum = 0.0f;
-            for (int e = g.t; e < a.k; e += L::G)
+            float tm = -__builtin_inff(), sum = 0.0f;
+            for (int e = h.t; e < a.k; e += H)
+                tm = fmaxf(tm, list[e].t);                // (-inf where there is none)
+            tm = h.reduce(tm, Max());
+            for (int e = h.t; e < a.k; e += H)
                 if (list[e].cls >= 0)
                     sum += exp_fast(list[e].t - tm);
-            log_norm = tm + logf(g.reduce(sum, Add()));
+            log_norm = tm + logf(h.reduce(sum, Add()));
         }
         Softmax listed = {-__builtin_inff(), 0.0f};
-        for (int e = g.t; e < a.k; e += L::G)
+        for (int e = h.t; e < a.k; e += H)
             if (list[e].cls >= 0) {
                 Q += exp_fast(list[e].t - log_norm);
                 listed.raise(list[e].z, c);
                 listed.s += __builtin_amdgcn_exp2f((list[e].z - listed.from()) * c);
             }
-        Q = g.reduce(Q, Add());
+        Q = h.reduce(Q, Add());
         const float q_rest = rest ? fmaxf(0.0f, 1.0f - Q) : 0.0f;
 
-        g.barrier();
         const uint32_t marked = rest ? mark[g.t] : 0;
         Softmax sm = {-__builtin_inff(), 0.0f};
         row.each([&](auto j, int32_t, const P &given) {
@@ -197,7 +203,7 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
         float share = 1.0f;                               // e^(from_out - from)
         S = s_out;
         if (rest) {
-            listed = combine(g, listed, c);
+            listed = combine(h, listed, c);
             const float m = fmaxf(sm.m, listed.m);
             share = sm.m == m ? 1.0f : __builtin_amdgcn_exp2f((sm.m - m) * c);
             listed.raise(m, c);
@@ -207,13 +213,13 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
         const float log_s = __builtin_amdgcn_logf(S) * kLn2;
         if (a.loss) {
             float sum = 0.0f;
-            for (int e = g.t; e < a.k; e += L::G)
+            for (int e = h.t; e < a.k; e += H)
                 if (list[e].cls >= 0) {
                     const float log_q = list[e].t - log_norm, q = exp_fast(log_q);
                     const float log_p = (list[e].z - from) * a.inv_t - log_s;
                     sum += q == 0.0f ? 0.0f : q * (log_q - log_p);
                 }
-            sum = g.reduce(sum, Add());
+            sum = h.reduce(sum, Add());
             if (q_rest > 0.0f)
                 sum += q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
                                                  __builtin_amdgcn_logf(s_out) * kLn2 - log_s));
@@ -228,19 +234,17 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
         if (q_rest > 0.0f)
             outside = s_out == 0.0f && S > 0.0f
                           ? 0.0f : scale * ((Q + q_rest) * share / S - q_rest / s_out);
-        if (dst) {
+        if (GRAD) {
             for (int e = g.t; e < a.k; e += L::G)
                 if (list[e].cls >= 0)
-                    list[e].t = in_list * __builtin_amdgcn_exp2f((list[e].z - from) * c) -
+                    list[e].grad = in_list * __builtin_amdgcn_exp2f((list[e].z - from) * c) -
                                 scale * exp_fast(list[e].t - log_norm);
             g.barrier();
         }
     } else if (a.loss && g.t == 0) {
         a.loss[r] = 0.0f;
     }
-    if constexpr (TYPE != kI32) {
-        if (!dst)
-            return;
+    if constexpr (GRAD) {
         if (scale == 0.0f) {
             const float zero[L::VEC] = {};
             for (int32_t i = 0; i < a.n; i += L::kSpan)
@@ -259,7 +263,7 @@ __global__ __launch_bounds__(L::kBlock) void k_distill(DistillArgs a)
 #pragma unroll
                         for (int u = 0; u < L::VEC; ++u)
                             if (u == list[e].cls % L::VEC)
-                                v[u] = list[e].t;
+                                v[u] = list[e].grad;
                     }
             store_piece<TYPE, L::VEC>(dst, i - g.t * L::VEC, g.t * L::VEC, a.n, v);
         });
@@ -438,8 +442,14 @@ hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int3
         }
         return with_layout<TYPE>(n, k, [&](auto layout) {
             typedef decltype(layout) L;
-            k_distill<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock,
-                                 (size_t)L::kGroups * k * sizeof(Entry), stream>>>(a);
+            const uint32_t blocks = (uint32_t)((n_rows + L::kGroups - 1) / L::kGroups);
+            const size_t lds = (size_t)L::kGroups * k * sizeof(Entry);
+            if constexpr (TYPE != kI32)
+                if (grad) {
+                    k_distill<TYPE, L, true><<<blocks, L::kBlock, lds, stream>>>(a);
+                    return hipGetLastError();
+                }
+            k_distill<TYPE, L, false><<<blocks, L::kBlock, lds, stream>>>(a);
             return hipGetLastError();
         });
     });

@@ -322,7 +322,9 @@ struct Group {
 };
 
 // ---- a row in a group's registers, or in memory ----
-template <int TYPE, int G, int NV, int VEC, bool RESIDENT>
+// KEEP: the pieces stay in registers from pass to pass.  Without, a row is read once by
+// each(), kBatch pieces at a time: half the registers, twice the blocks on a CU.
+template <int TYPE, int G, int NV, int VEC, bool RESIDENT, bool KEEP = true>
 struct Row {
     typedef typename Elem<TYPE>::Cmp Cmp;
     typedef Piece<TYPE, VEC> P;
@@ -330,12 +332,13 @@ struct Row {
     static constexpr int kFlight = 4;                     // pieces that stream() loads together
     const char *row;
     int32_t n, t;
-    P piece[RESIDENT ? NV : 1];
+    static constexpr int kBatch = NV < 8 ? NV : 8;
+    P piece[RESIDENT && KEEP ? NV : 1];
 
     __device__ __forceinline__ Row(const char *r, int32_t classes, int lane)
         : row(r), n(classes), t(lane)
     {
-        if constexpr (RESIDENT) {
+        if constexpr (RESIDENT && KEEP) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if (j * kSpan < n)
@@ -351,7 +354,21 @@ struct Row {
     template <class F>
     __device__ __forceinline__ void each(F f)
     {
-        if constexpr (RESIDENT)
+        if constexpr (RESIDENT && !KEEP)
+            static_for<NV / kBatch>([&](auto B) __attribute__((always_inline)) {
+                constexpr int j0 = decltype(B)::value * kBatch;
+                if (j0 * kSpan >= n)
+                    return;
+                P p[kBatch];
+                static_for<kBatch>([&](auto j) __attribute__((always_inline)) {
+                    p[j].load(row, (j0 + j) * kSpan, t * VEC, n);
+                });
+                static_for<kBatch>([&](auto j) __attribute__((always_inline)) {
+                    f(std::integral_constant<int, j0 + decltype(j)::value>(),
+                      (j0 + j) * kSpan + t * VEC, p[j]);
+                });
+            });
+        else if constexpr (RESIDENT)
             static_for<NV>([&](auto J) __attribute__((always_inline)) {
                 constexpr int j = decltype(J)::value;
                 if (j * kSpan < n) {
@@ -822,11 +839,10 @@ hipError_t with_layout(int32_t n, int32_t k, F f)
         return f(Layout<64, 16 / V, V, true>());
     if (n <= 8192)
         return f(Layout<256, 32 / V, V, true>());
-    if (n <= 32768)
-        return f(Layout<512, 64 / V, V, true>());
-    if constexpr (V == 8)
-        if (n <= 65536)
-            return f(Layout<512, 16, V, true>());
+    if (n <= 512 * 8 * V)
+        return f(Layout<512, 8, V, true>());
+    if (n <= 1024 * 8 * V)
+        return f(Layout<1024, 8, V, true>());
     if (n <= 1024 * 16 * V)
         return f(Layout<1024, 16, V, true>());
     return f(Layout<1024, 1, V, false>());

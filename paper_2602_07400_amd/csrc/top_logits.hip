@@ -28,7 +28,7 @@ struct TopArgs {
 };
 
 template <int TYPE, class L>
-__global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
+__global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArgs a)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(L::kBlock, L::kWavesPerSimd) void k_top(TopArgs a)
     uint64_t *list = lists[gi];
     uint32_t *fill = &fills[gi];
     const char *src = a.logits + r * a.stride;
-    Row<TYPE, G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
+    Row<TYPE, G, L::NV, L::VEC, L::RESIDENT, (G < kWave)> row(src, a.n, g.t);
 
     const float c = a.inv_t * kLog2e;
     Softmax sm = {-__builtin_inff(), 0.0f};
