@@ -18,6 +18,12 @@
 // first classes of (key == tau); tau is narrowed down by counts, for a top-k, or sums
 // of w, for a top-p, in ever narrower intervals.  Rows of a part of a wave find it by
 // bisection.
+//
+// What bounds it: short prefixes, the block's chain after the load (1 x 131072 bf16, top-k
+// 50 and top-p 0.95: 15 us, of which 4 to 5 are the load); wide ones, the passes over
+// the row, of 16 instructions an element each: 256 x 131072 with parameters per row 90
+// us, when a few rows keep thousands of classes and the others are done in 20; without
+// filters, HBM: 1024 x 50021 float32 88 us, 4.6 TB/s.
 #include "logit_rows.h"
 
 namespace bl {
