@@ -24,7 +24,6 @@ constexpr int32_t kMaxClasses = 1 << 30;
 enum : int { kI32 = 0, kF32 = 1, kF16 = 2, kBf16 = 3 };
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // f(integral_constant 0), ..., f(integral_constant N - 1): indexes of registers that are
@@ -817,7 +816,7 @@ struct Layout {
     static constexpr int kBins = kList * 2 / (int)kCopies;    // in the list's memory
     static constexpr int kCounted =
         G == 1024 ? 352 : G == 512 ? 256 : G == 256 ? 176 : G == 64 ? 88 : NV * VEC * G;
-    // waves a SIMD to compile for: two blocks of short rows a CU
+    // waves a SIMD to compile for, where a row stays in registers
     static constexpr int kWavesPerSimd =
         !RESIDENT || G == kWave || NV * (VEC > 4 ? 4 : VEC) > 16 ? 4 : 8;
 };
@@ -862,8 +861,9 @@ hipError_t with_type(int32_t type, F f)
 // ---- a lane a row: many short rows ----
 // A wave takes 64 or 16 rows of up to kLaneClasses classes through a tile in LDS, and a
 // lane or four go through a row: few reductions or none, and what is done once a row is
-// done for many of them.  It pays once there are rows for all the GPU's waves: from
-// kLaneRows rows on.
+// done for many of them.  It pays once there are rows for all the GPU's waves: top 10 of
+// 100 float32 classes 23 us at 8192 and 16384 rows and 25 at 32768, against 13, 21 and 35
+// with a group of 32 lanes a row; distillation 10, 10.6 and 13 against 8.7, 11.3 and 18.5.
 constexpr int32_t kLaneClasses = 128;
 constexpr int64_t kLaneRows = 16384;
 
