@@ -576,18 +576,20 @@ __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
 }
 
 // Keys [lo, hi) of a block's row in which the sum of `weight` over the order reaches
-// `goal` (1 <= goal <= the row's sum), the sum before them and their own.
+// `goal` (>= 1), the sum before them and their own (kUnknown: not yet summed; 0: the
+// goal is above the whole sum, which is `before`).
 struct Range {
     uint32_t lo, hi, before, here;
 };
+constexpr uint32_t kUnknown = 0xFFFFFFFFu;
 
 // kCopies interleaved counters an interval, one for every eighth lane: many elements
 // fall in few intervals (16-bit logits near -10 have 16 values a unit), and equal
 // addresses take turns.
 constexpr uint32_t kCopies = 8;
 
-// Narrows a range that holds the goal to one key, or until everything down to its end
-// sums to `enough`: the row's elements are summed in kBins intervals of equal width
+// Narrows a range to the one key that reaches the goal, or until everything down to its
+// end sums to `enough`; the sum from in.lo on may not pass 32 bits.  The row's elements are summed in kBins intervals of equal width
 // (in fixed point: their order does not matter), again in the interval that reaches the
 // goal, and so on.  A level takes a factor of kBins off the range.  bins: kBins *
 // kCopies words of LDS.
@@ -612,7 +614,7 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
         }
     };
     off_minus_zero();
-    while (in.hi - in.lo > 1 && in.before + in.here > enough) {
+    while ((in.hi - in.lo > 1 || in.here == kUnknown) && in.before + in.here > enough) {
         // Floats by value, which crosses zero evenly, until that takes less than 15 of 16
         // keys off the range (an infinity or denormals at its end); integers, exactly, by
         // key, which takes kBins / 2 - 1 of kBins / 2 off at every level.
@@ -660,8 +662,8 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
         const uint64_t won = g.reduce((uint64_t)found << 32 | base, Max());
         here = g.reduce(here, Max());
         found = (uint32_t)(won >> 32);
-        if (!found) {                                     // rounding left the goal outside
-            in = {in.lo, in.lo + 1, goal, 0};
+        if (!found) {
+            in = {in.lo, in.lo + 1, in.before + total, 0};
             break;
         }
         // the first key of the intervals up to `bound`, 64 keys at a time in every wave

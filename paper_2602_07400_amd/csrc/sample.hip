@@ -312,8 +312,8 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                         lo = at.lo;
                         if (at.before + at.here <= enough)
                             continue;
-                        tau = lo;
-                        ties = top_k - at.before;
+                        tau = lo;                         // (or all, where they are fewer)
+                        ties = top_k - at.before < at.here ? top_k - at.before : kAll;
                     }
                 break;
             }
@@ -451,20 +451,34 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     row_mass += (float)ties * exp_fast(x_of(at));
             }
             // Classes with w < (1 - p) sum / n together have less than (1 - p) sum: the
-            // prefix ends before them.  A sum of all classes is 2^31 in fixed point.
+            // prefix ends before them.  A sum of all classes is 2^31 in fixed point; those
+            // of a tau that a top-k cuts stay out of it: equal classes beyond the k-th, of
+            // any number, are not of the sum.
             const float unit = 2147483648.0f / row_mass;
             const uint32_t goal = max((uint32_t)(top_p * 2147483648.0f), 1u);
-            uint32_t lo = tau;
+            const bool cut = ties != kAll;
+            const uint32_t least = tau + cut;
+            uint32_t lo = least;
             if constexpr (TYPE != kI32)
                 lo = max(lo, E::key(ftop + logf((1.0f - top_p) * row_mass / (float)a.n) *
                                                temperature) - 1);
-            const Range at = narrow<TYPE, L>(
-                g, row, most, {lo, end, 0, 0xFFFFFFFFu}, goal, 0, (uint32_t *)lists[gi],
-                [&](Cmp v) __attribute__((always_inline)) {
-                    const float w = __builtin_amdgcn_exp2f((E::to_float(v) - ftop) * c);
-                    return (uint32_t)__builtin_fmaf(fminf(w, 1.0f), unit, 0.5f);
-                });
-            cut_at(at.lo, (float)(goal - min(at.before, goal)) / unit);
+            Range at = {lo, lo + 1, 0, 0};
+            if (lo != end)                                // (0 past the largest integer)
+                at = narrow<TYPE, L>(
+                    g, row, most, {lo, end, 0, kUnknown}, goal, 0, (uint32_t *)lists[gi],
+                    [&](Cmp v) __attribute__((always_inline)) {
+                        const float w = __builtin_amdgcn_exp2f((E::to_float(v) - ftop) * c);
+                        return (uint32_t)__builtin_fmaf(fminf(w, 1.0f), unit, 0.5f);
+                    });
+            const float need = (float)(goal - min(at.before, goal)) / unit;
+            if (at.here) {
+                cut_at(at.lo, need);
+            } else if (cut && lo == least) {
+                cut_at(tau, need);                        // the goal is among tau's classes
+            } else {                                      // rounding left the goal outside
+                tau = at.lo;
+                ties = kAll;
+            }
         }
     }
     if (min_p > 0.0f) {                                   // as a key: x grows with it
