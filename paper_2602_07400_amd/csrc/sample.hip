@@ -304,16 +304,16 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
             const uint32_t found = collect<TYPE, L>(g, row, most, E::from_key(lo), list, fill);
             if (found > (uint32_t)L::kList) {
                 if constexpr (G > kWave)
-                    if (by_k) {                           // the k-th key, or nearly
+                    if (by_k && (uint32_t)top_k < found) {    // the k-th key, or nearly
                         const uint32_t enough = top_k <= L::kList ? L::kList : 0;
-                        const Range at = narrow<TYPE, L>(g, row, most, {lo, end, 0, found}, top_k,
-                                                         enough, (uint32_t *)list,
-                                                         [](Cmp) { return 1u; });
+                        const Range at = narrow<TYPE, L, false>(
+                            g, row, most, {lo, end, 0, found}, top_k, enough, (uint32_t *)list,
+                            [](Cmp) { return 1u; });
                         lo = at.lo;
                         if (at.before + at.here <= enough)
                             continue;
-                        tau = lo;                         // (or all, where they are fewer)
-                        ties = top_k - at.before < at.here ? top_k - at.before : kAll;
+                        tau = lo;
+                        ties = top_k - at.before;
                     }
                 break;
             }
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                                                temperature) - 1);
             Range at = {lo, lo + 1, 0, 0};
             if (lo != end)                                // (0 past the largest integer)
-                at = narrow<TYPE, L>(
+                at = narrow<TYPE, L, true>(
                     g, row, most, {lo, end, 0, kUnknown}, goal, 0, (uint32_t *)lists[gi],
                     [&](Cmp v) __attribute__((always_inline)) {
                         const float w = __builtin_amdgcn_exp2f((E::to_float(v) - ftop) * c);
