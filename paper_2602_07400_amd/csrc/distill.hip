@@ -189,7 +189,7 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
                     sum += expf(list[e].t - tm);
             log_norm = tm + logf(h.reduce(sum, Add()));
         }
-        Softmax listed = {-__builtin_inff(), 0.0f};
+        Softmax<> listed;
         for (int e = h.t; e < a.k; e += H)
             if (list[e].cls >= 0) {
                 Q += expf(list[e].t - log_norm);
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
         const float q_rest = rest ? fmaxf(0.0f, 1.0f - Q) : 0.0f;
 
         const uint32_t marked = rest ? mark[g.t] : 0;
-        Softmax sm = {-__builtin_inff(), 0.0f};
+        Softmax<!L::RESIDENT> sm;
         row.each([&](auto j, int32_t, const P &given) {
             P p = given;
             if (marked >> (j % 32) & 1)
@@ -217,9 +217,11 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
             }
             sm.raise(zm, c.hi);
             const float from = sm.from();
+            float part = sm.start();
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
-                sm.s += c.pow(z[u] - from);
+                part += c.pow(z[u] - from);
+            sm.add(part);
         });
         // The rest relative to its own maximum, where its mass cannot vanish; the whole
         // row relative to the larger of that and the list's.

@@ -428,17 +428,43 @@ __device__ __forceinline__ float exp_fast(float x)
     return __builtin_amdgcn_exp2f(x * kLog2e);
 }
 
+// A lane's sum s of a row's terms, a piece at a time: part = start(), the piece's terms
+// added to it, add(part).  LONG (a row in memory, any number of pieces): a piece's own sum
+// goes to the total together with what the total's last rounding lost.  Added one by one,
+// equal terms round the same way: over 2^24 classes, 2^14 a lane, 1.2e-4 of the sum.
+template <bool LONG>
+struct Total {
+    float s = 0.0f, lost = 0.0f;
+    __device__ __forceinline__ float start() const { return LONG ? 0.0f : s; }
+    __device__ __forceinline__ void add(float part)
+    {
+        if constexpr (LONG) {
+            const float more = part + lost, to = s + more;
+            lost = more - (to - s);
+            s = to;
+        } else {
+            s = part;
+        }
+    }
+};
+
 // A running maximum m of z and the sum s of 2^(c (z - m)): with c = log2(e) / T the
 // exponentials of a softmax at temperature T.  The difference comes first: c z alone
 // overflows where z is its type's lowest value, which masks are made of.
-struct Softmax {
-    float m, s;
+template <bool LONG = false>
+struct Softmax : Total<LONG> {
+    using Total<LONG>::s;
+    using Total<LONG>::lost;
+    float m = -__builtin_inff();
     __device__ __forceinline__ float from() const { return m == -__builtin_inff() ? 0.0f : m; }
     __device__ __forceinline__ void raise(float to, float c)
     {
         const float old = from();
         m = fmaxf(m, to);
-        s *= __builtin_amdgcn_exp2f(s == 0.0f ? 0.0f : (old - from()) * c);
+        const float f = __builtin_amdgcn_exp2f(s == 0.0f ? 0.0f : (old - from()) * c);
+        s *= f;
+        if constexpr (LONG)
+            lost *= f;
     }
     // log sum e^(z / T)
     __device__ __forceinline__ float log_norm(float inv_t) const
@@ -449,8 +475,8 @@ struct Softmax {
 };
 
 // Over a group: the maximum first, then the sums relative to it.
-template <class Grp>
-__device__ __forceinline__ Softmax combine(Grp &g, Softmax a, float c)
+template <class Grp, bool LONG>
+__device__ __forceinline__ Softmax<LONG> combine(Grp &g, Softmax<LONG> a, float c)
 {
     a.raise(g.reduce(a.m, Max()), c);
     a.s = g.reduce(a.s, Add());

@@ -115,7 +115,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
     // softmax's sum, as the row arrives
     Cmp mine = E::lowest(), most[L::NV];
     static_for<L::NV>([&](auto j) __attribute__((always_inline)) { most[j] = E::lowest(); });
-    Softmax sm = {-__builtin_inff(), 0.0f};
+    Softmax<!L::RESIDENT> sm;
     const bool of_all = by_p && !by_k && temperature > 0.0f && kLists;
     const float c = inv_t * kLog2e;
     row.each([&](auto j, int32_t, const P &p) {
@@ -131,12 +131,14 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         if (of_all) {
             sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
             const float from = sm.from();
+            float part = sm.start();
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
                 const Cmp v = p.get(u);
-                sm.s += v > E::lowest() ? __builtin_amdgcn_exp2f((E::to_float(v) - from) * c)
+                part += v > E::lowest() ? __builtin_amdgcn_exp2f((E::to_float(v) - from) * c)
                                         : 0.0f;
             }
+            sm.add(part);
         }
     });
     const Cmp top = g.reduce(mine, Max());
@@ -193,19 +195,19 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         }
         row_mass = g.reduce(sm.s, Add());
     }
-    float sum = 0.0f;                                     // of the kept w
+    Total<!L::RESIDENT> sum;                              // of the kept w
     float best = -__builtin_inff(), best_x = 0.0f;        // the lane's best x + g (and x),
     int32_t best_class = 0;                               // and its class
     const auto finish = [&](auto &h, auto first, auto x_best) __attribute__((always_inline)) {
         const uint64_t own = best > -__builtin_inff()
                                  ? entry(Elem<kF32>::key(best), best_class) : 0;
         const uint64_t won = h.reduce(own, Max());
-        sum = h.reduce(sum, Add());
+        const float total = h.reduce(sum.s, Add());
         const int32_t token = won ? best_class : first();
         if (won ? own == won : g.t == 0) {
             a.token[r] = token;
             if (a.log_prob)
-                a.log_prob[r] = (won ? x_best() : 0.0f) - logf(sum);
+                a.log_prob[r] = (won ? x_best() : 0.0f) - logf(total);
         }
     };
     const auto x_listed = [&] { return best_x; };
@@ -218,9 +220,10 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         const bool split = i <= last && i + L::VEC - 1 > last;
         const Cmp over = i <= last ? in : out;
         int at = -1;
+        float part = sum.start();
         const auto one = [&](int u, bool kept) __attribute__((always_inline)) {
             const float x = x_of(p.get(u));
-            sum += kept ? exp_fast(x) : 0.0f;
+            part += kept ? exp_fast(x) : 0.0f;
             const float score = kept ? x + number[u] : -__builtin_inff();
             at = score > best ? u : at;                   // (the lane's classes ascend)
             best = fmaxf(best, score);
@@ -234,6 +237,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
             for (int u = 0; u < L::VEC; ++u)
                 one(u, p.get(u) > (i + u <= last ? in : out));
         }
+        sum.add(part);
         best_class = at >= 0 ? i + at : best_class;
     };
     const auto draw_streamed = [&](Cmp at, Cmp in, int32_t last) __attribute__((always_inline)) {
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     const float we = exp_fast(x);
                     if (e == 0 || ((!by_p || before < target) && x >= floor_x)) {
                         const int32_t cls = class_of(sorted[e]);
-                        sum += we;
+                        sum.s += we;
                         const float score = x + (counted ? numbers[gi][e] : noise[cls]);
                         if (score > best || (score == best && cls < best_class)) {
                             best = score;
@@ -438,15 +442,17 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
     } else if constexpr (G > kWave && !PLAIN) {
         if (by_p) {
             if (by_k) {                                   // the mass of the first k
-                float part = 0.0f;
+                Total<!L::RESIDENT> mass;
                 const Cmp at = E::from_key(tau);
                 row.template stream<2>([&](int32_t, const P &p) {
+                    float part = mass.start();
 #pragma unroll
                     for (int u = 0; u < L::VEC; ++u)
                         part += p.get(u) > at || (p.get(u) == at && ties == kAll)
                                     ? exp_fast(x_of(p.get(u))) : 0.0f;
+                    mass.add(part);
                 });
-                row_mass = g.reduce(part, Add());
+                row_mass = g.reduce(mass.s, Add());
                 if (ties != kAll)
                     row_mass += (float)ties * exp_fast(x_of(at));
             }
@@ -517,7 +523,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                 const float x = x_of(E::from_key(key_of(list[e])));
                 const int32_t cls = class_of(list[e]);
                 const float score = x + noise[cls];
-                sum += exp_fast(x);
+                sum.s += exp_fast(x);
                 if (score > best || (score == best && cls < best_class)) {
                     best = score;
                     best_x = x;

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArg
     Row<TYPE, G, L::NV, L::VEC, L::RESIDENT, (G < kWave)> row(src, a.n, g.t);
 
     const float c = a.inv_t * kLog2e;
-    Softmax sm = {-__builtin_inff(), 0.0f};
+    Softmax<!L::RESIDENT> sm;
     Cmp top = E::lowest(), most[L::NV];                   // the lane's and its pieces' largest
     static_for<L::NV>([&](auto j) __attribute__((always_inline)) { most[j] = E::lowest(); });
     row.each([&](auto j, int32_t, const P &p) {
@@ -69,23 +69,27 @@ __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArg
         if (a.log_norm) {
             sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
             const float from = sm.from();
+            float part = sm.start();
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
                 const Cmp v = p.get(u);
                 const float e = __builtin_amdgcn_exp2f((E::to_float(v) - from) * c);
-                sm.s += TYPE == kI32 && v == E::lowest() ? 0.0f : e;
+                part += TYPE == kI32 && v == E::lowest() ? 0.0f : e;
             }
+            sm.add(part);
         }
     });
     if (a.log_norm) {
         if (!(sm.s >= 0.0f)) {                            // a NaN, or +inf - inf: without them
-            sm.s = 0.0f;
+            sm.s = sm.lost = 0.0f;
             row.stream([&](int32_t, const P &p) {
+                float part = sm.start();
 #pragma unroll
                 for (int u = 0; u < L::VEC; ++u) {
                     const float e = E::to_float(p.get(u)) - sm.m;
-                    sm.s += e <= 0.0f ? __builtin_amdgcn_exp2f(e * c) : 0.0f;
+                    part += e <= 0.0f ? __builtin_amdgcn_exp2f(e * c) : 0.0f;
                 }
+                sm.add(part);
             });
         }
         sm = combine(g, sm, c);
@@ -255,7 +259,8 @@ __global__ __launch_bounds__(kWave) void k_top_lanes(TopArgs a)
         const uint32_t first = key_at(0);
         const float m = first ? E::to_float(E::from_key(first)) : -__builtin_inff();
         const float from = first ? m : 0.0f, c = a.inv_t * kLog2e;
-        Softmax sm = {m, 0.0f};
+        Softmax<> sm;
+        sm.m = m;
 #pragma unroll 4
         for (int i = 0; i < a.n; ++i) {
             const Cmp v = at(i);

@@ -62,3 +62,49 @@ def test_sample_top_k_above_the_rows_classes(p):
     got = bl.bitlogic_sample(x.to(DEV), noise.to(DEV), 2.0 ** 30, 100000, p)
     torch.cuda.synchronize()
     _check_sample(x, noise, 2.0 ** 30, 100000, p, 0.0, got)
+
+
+# ---------------------------------------------- rows of millions of classes
+
+def _levels(rng, c, low, dtype):
+    """One row of c classes, the second half (shuffled) `low` below the others."""
+    x = torch.zeros(c, dtype=dtype)
+    x[torch.from_numpy(rng.permutation(c)[c // 2:])] = low
+    return x[None]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("c", [1 << 20, (1 << 22) + 5, (1 << 24) + 3])
+def test_sums_over_millions_of_classes(c, dtype):
+    rng = _rng(22, c)
+    x = torch.full((1, c), -1.2, dtype=dtype)
+    x[0, c // 3] = 0
+    w = np.exp(float(x[0, 0]))
+    total = 1 + (c - 1) * w
+    v, i, norm = bl.bitlogic_top_logits(x.to(DEV), 3)
+    assert i.tolist() == [[c // 3, 0, 1]]
+    assert abs(float(norm) - np.log(total)) <= REL + 2.0 ** -22 * np.log(total)
+    noise = _gumbel(rng, 1, c)
+    for min_p in (0.0, 0.2):                              # (every class is kept)
+        token, log_prob = bl.bitlogic_sample(x.to(DEV), noise.to(DEV), 1.0, min_p=min_p)
+        at = int(token)
+        score = (x.float() + noise)[0]
+        assert float(score[at]) == float(score.max())
+        want = float(x[0, at]) - np.log(total)
+        assert abs(float(log_prob) - want) <= 2 * REL + 2.0 ** -22 * abs(want)
+    # two classes of a teacher's, the rest of 30%
+    t, idx = torch.tensor([[1.0, 0.5]]), torch.tensor([[c // 3, 7]], dtype=torch.int32)
+    ln = _norm(t, idx, 1.0, 0.7)
+    loss, grad = bl.bitlogic_distill(x.to(DEV), t.to(DEV), idx.to(DEV), ln.to(DEV))
+    q = np.exp(t.double().numpy()[0] - float(ln))
+    p, p_rest, q_rest = np.array([1, w]) / total, (c - 2) * w / total, 1 - q.sum()
+    want = (q * np.log(q / p)).sum() + q_rest * np.log(q_rest / p_rest)
+    rel = 3 * REL + 2.0 ** -20 * 2
+    assert abs(float(loss) - want) <= rel * (1 + abs(want))
+    g = grad.cpu().double()[0]
+    out = (1 - q_rest / p_rest) * w / total               # of each class outside the list
+    tol = (1 + q_rest / p_rest) * w / total * rel + EPS[dtype] * abs(out) + TINY[dtype]
+    rest = torch.ones(c, dtype=torch.bool)
+    rest[[c // 3, 7]] = False
+    assert float((g[rest] - out).abs().max()) <= tol
+    assert (np.abs(g[~rest].flip(0).numpy() - (p - q)) <= (p + q) * rel + EPS[dtype]).all()
