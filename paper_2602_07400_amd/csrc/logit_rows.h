@@ -483,6 +483,19 @@ __device__ __forceinline__ Softmax<LONG> combine(Grp &g, Softmax<LONG> a, float 
     return a;
 }
 
+// A value that all lanes of a wave have, in scalar registers.
+template <class T>
+__device__ __forceinline__ T uniform(T v)
+{
+    int w[sizeof(T) / 4];
+    __builtin_memcpy(w, &v, sizeof v);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 4; ++i)
+        w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    __builtin_memcpy(&v, w, sizeof v);
+    return v;
+}
+
 // ---- lists of candidates ----
 // An element with its place in the order: larger entries come first.
 __device__ __forceinline__ uint64_t entry(uint32_t key, int32_t cls)
@@ -601,35 +614,50 @@ __device__ __forceinline__ uint32_t collect(Group<L::G> &g, R &row,
     return *fill;
 }
 
+// A mass in fixed point: the low 52 bits.  to_mass leaves a double's exponent above them,
+// which sums carry along until kMassBits takes it off: two instructions instead of the
+// seven of a conversion to 64-bit integers.  In 32 bits a class's share of the mass of n
+// would be rounded by up to n / 2^32 of itself, the same way wherever logits are equal:
+// 1e-5 of the sum at 2^17 classes, 1e-3 at 2^24.
+typedef unsigned long long Mass;
+constexpr Mass kMassBits = (1ull << 52) - 1;
+__device__ __forceinline__ Mass to_mass(float w, double unit)
+{
+    return (Mass)__double_as_longlong(__builtin_fma((double)w, unit, 0x1p52));
+}
+
 // Keys [lo, hi) of a block's row in which the sum of `weight` over the order reaches
 // `goal` (>= 1), the sum before them and their own (for masses kUnknown: not yet summed,
 // and 0: the goal is above the whole sum, which is `before`).
+template <class Sum>
 struct Range {
-    uint32_t lo, hi, before, here;
+    uint32_t lo, hi;
+    Sum before, here;
 };
-constexpr uint32_t kUnknown = 0xFFFFFFFFu;
-
-// kCopies interleaved counters an interval, one for every eighth lane: many elements
-// fall in few intervals (16-bit logits near -10 have 16 values a unit), and equal
-// addresses take turns.
-constexpr uint32_t kCopies = 8;
+constexpr Mass kUnknown = ~0ull;
 
 // Narrows a range to the one key that reaches the goal, or until everything down to its
-// end sums to `enough`; the sum from in.lo on may not pass 32 bits.  MASS: the sums are of
-// masses, not of classes, which are known beforehand to reach the goal (what else it takes
-// costs registers: top 64 of 2048 x 131072 in bfloat16 125 us instead of 105).  The row's elements are summed in kBins intervals of equal width
+// end sums to `enough`: the row's elements are summed in kBins intervals of equal width
 // (in fixed point: their order does not matter), again in the interval that reaches the
-// goal, and so on.  A level takes a factor of kBins off the range.  bins: kBins *
-// kCopies words of LDS.
-template <int TYPE, class L, bool MASS, class R, class W>
-__device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
-                                        const typename Elem<TYPE>::Cmp (&most)[L::NV], Range in,
-                                        uint32_t goal,
-                                        uint32_t enough, uint32_t *bins, W weight)
+// goal, and so on.  A level takes a factor of kBins off the range.  Sum: Mass, or uint32_t
+// for numbers of classes, which are known beforehand to reach the goal (what else it takes
+// costs registers: top 64 of 2048 x 131072 in bfloat16 125 us instead of 105).
+// kCopies interleaved counters an interval, one for every eighth or fourth lane: many
+// elements fall in few intervals (16-bit logits near -10 have 16 values a unit), and equal
+// addresses take turns.  bins: kBins * kCopies sums, in the memory of the list (masses by 2,
+// 4, 8 and 16 copies, draws from 256 x 131072: 97, 98, 105 and 112 us).
+template <int TYPE, class L, class Sum, class R, class W>
+__device__ __forceinline__ Range<Sum> narrow(Group<L::G> &g, R &row,
+                                             const typename Elem<TYPE>::Cmp (&most)[L::NV],
+                                             Range<Sum> in, Sum goal, Sum enough, Sum *bins,
+                                             W weight)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
-    constexpr uint32_t kBins = L::kBins, kRun = kBins > (uint32_t)L::G ? kBins / L::G : 1;
+    constexpr bool kMass = sizeof(Sum) == 8;
+    constexpr uint32_t kCopies = kMass ? 4 : 8;
+    constexpr uint32_t kBins = L::kList * sizeof(uint64_t) / sizeof(Sum) / kCopies;
+    constexpr uint32_t kRun = kBins > (uint32_t)L::G ? kBins / L::G : 1;
     const uint32_t copy = g.t % kCopies;
     bool by_key = TYPE == kI32;
     // No element has the key of -0 (+0's is the next one): as an end of the range it
@@ -642,7 +670,8 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
         }
     };
     off_minus_zero();
-    while ((in.hi - in.lo > 1 || (MASS && in.here == kUnknown)) && in.before + in.here > enough) {
+    while ((in.hi - in.lo > 1 || (kMass && in.here == kUnknown)) &&
+           in.before + in.here > enough) {
         // Floats by value, which crosses zero evenly, until that takes less than 15 of 16
         // keys off the range (an infinity or denormals at its end); integers, exactly, by
         // key, which takes kBins / 2 - 1 of kBins / 2 off at every level.
@@ -671,15 +700,21 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
             }
         }, pieces_from<L>(most, first));
         g.barrier();
-        uint32_t part = 0, total;
+        const auto sum_of = [&](uint32_t b) __attribute__((always_inline)) {
+            Sum sum = 0;
+            for (uint32_t c = 0; c < kCopies; ++c) {
+                const Sum own = b < kBins ? bins[b * kCopies + c] : 0;
+                sum += kMass ? own & (Sum)kMassBits : own;
+            }
+            return sum;
+        };
+        Sum part = 0, total;
         for (uint32_t b = 0; b < kRun; ++b)
-            for (uint32_t c = 0; c < kCopies; ++c)
-                part += g.t * kRun + b < kBins ? bins[(g.t * kRun + b) * kCopies + c] : 0;
-        uint32_t before = in.before + g.scan(part, total), found = 0, here = 0, base = 0;
+            part += sum_of(g.t * kRun + b);
+        Sum before = in.before + g.scan(part, total), here = 0, base = 0;
+        uint32_t found = 0;
         for (uint32_t b = 0; b < kRun; ++b) {
-            uint32_t own = 0;
-            for (uint32_t c = 0; c < kCopies; ++c)
-                own += g.t * kRun + b < kBins ? bins[(g.t * kRun + b) * kCopies + c] : 0;
+            const Sum own = sum_of(g.t * kRun + b);
             if (before < goal && before + own >= goal) {
                 found = g.t * kRun + b + 1;
                 base = before;
@@ -687,11 +722,17 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
             }
             before += own;
         }
-        const uint64_t won = g.reduce((uint64_t)found << 32 | base, Max());
+        if constexpr (kMass) {
+            found = g.reduce(found, Max());
+            base = g.reduce(base, Max());
+        } else {
+            const uint64_t won = g.reduce((uint64_t)found << 32 | base, Max());
+            found = (uint32_t)(won >> 32);
+            base = (uint32_t)won;
+        }
         here = g.reduce(here, Max());
-        found = (uint32_t)(won >> 32);
         if (!found) {
-            in = {in.lo, in.lo + 1, MASS ? in.before + total : goal, 0};
+            in = {in.lo, in.lo + 1, kMass ? in.before + total : goal, 0};
             break;
         }
         // the first key of the intervals up to `bound`, 64 keys at a time in every wave
@@ -709,8 +750,10 @@ __device__ __forceinline__ Range narrow(Group<L::G> &g, R &row,
         };
         const uint32_t lo = first_key(found), hi = found == 1 ? in.hi : first_key(found - 1);
         by_key |= hi - lo > (in.hi - in.lo) / 16;
-        in = {lo, hi, (uint32_t)won, here};
+        in = {lo, hi, base, here};
         off_minus_zero();
+        if constexpr (kMass)
+            in = {uniform(in.lo), uniform(in.hi), uniform(in.before), uniform(in.here)};
     }
     return in;
 }
@@ -843,7 +886,6 @@ struct Layout {
     // within a wave), and how many are put in order by counting rather than sorting:
     // c entries compare c^2 / G times a lane, 128 of them as long as a sort takes.
     static constexpr int kList = G >= 256 ? 4 * G : NV * VEC * G;
-    static constexpr int kBins = kList * 2 / (int)kCopies;    // in the list's memory
     static constexpr int kCounted =
         G == 1024 ? 352 : G == 512 ? 256 : G == 256 ? 176 : G == 64 ? 88 : NV * VEC * G;
     // waves a SIMD to compile for, where a row stays in registers

@@ -73,7 +73,8 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
     Group<G> g(threadIdx.x - gi * G, &scratch);
     const char *src = a.logits + r * a.stride;
     const float *noise = a.noise + r * a.noise_stride;
-    Row<TYPE, G, L::NV, L::VEC, L::RESIDENT> row(src, a.n, g.t);
+    // (only what plain draws and bisection read again stays in registers)
+    Row<TYPE, G, L::NV, L::VEC, L::RESIDENT, (PLAIN || G < kWave)> row(src, a.n, g.t);
     const float temperature = a.temperatures ? a.temperatures[r] : a.temperature;
     const float top_p = PLAIN ? 1.0f : a.top_ps ? a.top_ps[r] : a.top_p;
     const float min_p = PLAIN ? 0.0f : a.min_ps ? a.min_ps[r] : a.min_p;
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                 if constexpr (G > kWave)
                     if (by_k && (uint32_t)top_k < found) {    // the k-th key, or nearly
                         const uint32_t enough = top_k <= L::kList ? L::kList : 0;
-                        const Range at = narrow<TYPE, L, false>(
+                        const auto at = narrow<TYPE, L, uint32_t>(
                             g, row, most, {lo, end, 0, found}, top_k, enough, (uint32_t *)list,
                             [](Cmp) { return 1u; });
                         lo = at.lo;
@@ -457,26 +458,26 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     row_mass += (float)ties * exp_fast(x_of(at));
             }
             // Classes with w < (1 - p) sum / n together have less than (1 - p) sum: the
-            // prefix ends before them.  A sum of all classes is 2^31 in fixed point; those
+            // prefix ends before them.  A sum of all classes is 2^51 in fixed point; those
             // of a tau that a top-k cuts stay out of it: equal classes beyond the k-th, of
             // any number, are not of the sum.
-            const float unit = 2147483648.0f / row_mass;
-            const uint32_t goal = max((uint32_t)(top_p * 2147483648.0f), 1u);
+            const double unit = uniform(0x1p51 / (double)row_mass);
+            const Mass goal = uniform(max((Mass)(top_p * 0x1p51f), (Mass)1));
             const bool cut = ties != kAll;
             const uint32_t least = tau + cut;
             uint32_t lo = least;
             if constexpr (TYPE != kI32)
                 lo = max(lo, E::key(ftop + logf((1.0f - top_p) * row_mass / (float)a.n) *
                                                temperature) - 1);
-            Range at = {lo, lo + 1, 0, 0};
+            Range<Mass> at = {lo, lo + 1, 0, 0};
             if (lo != end)                                // (0 past the largest integer)
-                at = narrow<TYPE, L, true>(
-                    g, row, most, {lo, end, 0, kUnknown}, goal, 0, (uint32_t *)lists[gi],
+                at = narrow<TYPE, L, Mass>(
+                    g, row, most, {lo, end, 0, kUnknown}, goal, 0, (Mass *)lists[gi],
                     [&](Cmp v) __attribute__((always_inline)) {
                         const float w = __builtin_amdgcn_exp2f((E::to_float(v) - ftop) * c);
-                        return (uint32_t)__builtin_fmaf(fminf(w, 1.0f), unit, 0.5f);
+                        return to_mass(fminf(w, 1.0f), unit);
                     });
-            const float need = (float)(goal - min(at.before, goal)) / unit;
+            const float need = (float)((double)(goal - min(at.before, goal)) / unit);
             if (at.here) {
                 cut_at(at.lo, need);
             } else if (cut && lo == least) {

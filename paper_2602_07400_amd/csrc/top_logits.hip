@@ -107,10 +107,10 @@ __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArg
     }
     if (found > (uint32_t)L::kList) {
         // the k-th key, or a range of keys around it that fits the list
-        Range at = {lo, E::key(g.reduce(top, Max())) + 1, 0, found};
+        Range<uint32_t> at = {lo, E::key(g.reduce(top, Max())) + 1, 0, found};
         if constexpr (G > kWave) {
-            at = narrow<TYPE, L, false>(g, row, most, at, k, L::kList, (uint32_t *)list,
-                                 [](Cmp) { return 1u; });
+            at = narrow<TYPE, L, uint32_t>(g, row, most, at, k, L::kList, (uint32_t *)list,
+                                           [](Cmp) { return 1u; });
             if (at.before + at.here <= (uint32_t)L::kList)
                 found = collect<TYPE, L>(g, row, most, E::from_key(at.lo), list, fill);
         }

@@ -108,3 +108,30 @@ def test_sums_over_millions_of_classes(c, dtype):
     rest[[c // 3, 7]] = False
     assert float((g[rest] - out).abs().max()) <= tol
     assert (np.abs(g[~rest].flip(0).numpy() - (p - q)) <= (p + q) * rel + EPS[dtype]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("c", [1 << 17, 1 << 20, (1 << 22) + 5, (1 << 24) + 3])
+def test_top_p_boundary_over_millions_of_classes(c, dtype):
+    """Two levels, and a nucleus that ends among the lower ones: the kept mass is the
+    target's to REL, whatever a class's share of it."""
+    rng = _rng(23, c)
+    x = _levels(rng, c, -0.2, dtype)
+    noise = _gumbel(rng, 1, c)
+    low = np.nonzero(x[0].float().numpy() < 0)[0]
+    w, n = np.exp(float(x.min())), c - len(low)
+    score = (x.float() + noise)[0].numpy()
+    for top_p in (0.6, 0.9, 0.999):
+        token, log_prob = bl.bitlogic_sample(x.to(DEV), noise.to(DEV), 1.0, top_p=top_p)
+        total = n + len(low) * w
+        need = float(np.float32(top_p)) * total - n
+        assert need > 0
+        slack = REL * total / w + 1
+        kept = np.ones(c, bool)
+        few, many = (int(np.clip(np.ceil(need / w) + s, 0, len(low))) for s in (-slack, slack))
+        kept[low[few:]] = False
+        best = score[kept].max()
+        kept[low[few:many]] = True
+        assert best <= score[int(token)] <= score[kept].max()
+        want = float(x[0, int(token)]) - np.log(n + np.ceil(need / w) * w)
+        assert abs(float(log_prob) - want) <= 3 * REL + 2.0 ** -22 * abs(want)
