@@ -520,17 +520,23 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                 above = g.reduce(above, Add());
                 found = above + min(ties, found - above);
             }
+            // The list's order is that of its atomics: its sum in integers, whose order
+            // does not matter.  Units of 2^-40: 4096 weights from 1 down, within 2^-29 of
+            // their sum.
+            uint64_t units = 0;
             for (uint32_t e = g.t; e < found; e += G) {
                 const float x = x_of(E::from_key(key_of(list[e])));
                 const int32_t cls = class_of(list[e]);
                 const float score = x + noise[cls];
-                sum.s += exp_fast(x);
+                units += (uint64_t)(exp_fast(x) * 0x1p40f + 0.5f);
                 if (score > best || (score == best && cls < best_class)) {
                     best = score;
                     best_x = x;
                     best_class = cls;
                 }
             }
+            units = g.reduce(units, Add());
+            sum.s = g.t == 0 ? (float)units * 0x1p-40f : 0.0f;
             finish(g, first_class, x_listed);
             return;
         }

@@ -135,3 +135,26 @@ def test_top_p_boundary_over_millions_of_classes(c, dtype):
         assert best <= score[int(token)] <= score[kept].max()
         want = float(x[0, int(token)]) - np.log(n + np.ceil(need / w) * w)
         assert abs(float(log_prob) - want) <= 3 * REL + 2.0 ** -22 * abs(want)
+
+
+# ------------------------------------------------------------------- repeats
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("c", [3000, 20000, 131072])
+def test_sample_repeats_bit_for_bit(c, dtype):
+    """Kept sets whose classes reach LDS in whatever order the waves get there: the
+    log-probability's bits do not depend on it."""
+    rng = _rng(24, c, TYPES.index(dtype))
+    n = 64
+    scale = 30.0 if dtype == torch.int32 else 1.0
+    x = _logits(rng, n, c, torch.float32, 2.0 * scale).round() if dtype == torch.int32 \
+        else _logits(rng, n, c, torch.float32, 2.0)
+    x = x.to(dtype).to(DEV)
+    noise = _gumbel(rng, n, c).to(DEV)
+    for k, p, m in ((0, 1.0, 0.02), (0, 1.0, 0.002), (0, 0.95, 0.01), (2500, 1.0, 0.01),
+                    (2500, 0.9, 0.0), (0, 0.9, 0.0)):
+        first = bl.bitlogic_sample(x, noise, scale, k, p, m)
+        for _ in range(12):
+            again = bl.bitlogic_sample(x, noise, scale, k, p, m)
+            torch.cuda.synchronize()
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1]), (k, p, m)
