@@ -436,7 +436,9 @@ enum {
     BITLOGIC_LOGITS_BF16 = 3
 };
 /* A row's order is descending logit, then ascending class.  Softmax statistics,
- * sums and losses are held in 32 bits whatever the type; results do not depend on
+ * sums and losses are held in 32 bits or more whatever the type, and differences of
+ * int32 logits are taken in integers (a log_norm is a float: it resolves 2^-24 of
+ * itself); results do not depend on
  * how a launch is scheduled.  Buffers need their elements' natural alignment only.
  * Limits: 1 <= n_classes <= 2^30, 0 <= n_rows < 2^31 (0 enqueues nothing, with any
  * pointers), 1 <= k <= BITLOGIC_TOP_MAX, temperatures positive and finite
@@ -495,7 +497,8 @@ typedef struct bitlogic_sampling {
 } bitlogic_sampling;
 
 /* A class per row, drawn with given random numbers.  With m the row's largest logit,
- * x_i = (l_i - m) * (1 / T) (0 where l_i = m) and w_i = e^x_i, in 32-bit arithmetic:
+ * x_i = (l_i - m) * (1 / T) (0 where l_i = m; int32 differences are exact before they
+ * become float) and w_i = e^x_i, in 32-bit arithmetic:
  *   top-k  keeps the first k classes of the row's order;
  *   top-p  of those, the ones before which the sum of w is below top_p times the
  *          sum over them all (top_p >= 1: every one; the first one always);

@@ -118,18 +118,41 @@ __device__ __forceinline__ void store_piece(char *row, int32_t first, int32_t i,
 }
 
 // A teacher's entry in LDS.
+template <class Cmp>
 struct Entry {
     int32_t cls, next;                  // class (-1: none); next entry of the owning lane
-    float t, z;                         // teacher logit / Tt, student's logit
+    float t;                            // teacher's logit as load_teacher gives it
+    Cmp z;                              // student's logit
     float grad;
 };
+
+// A teacher's logit: t / Tt, or the bits of an int32, whose list's maximum is taken off in
+// integers before anything is rounded.
+__device__ __forceinline__ float load_teacher(const DistillArgs &a, int64_t i)
+{
+    return a.top_type == kI32 ? __int_as_float(load_one<kI32>(a.top_values, i))
+                              : load_float(a.top_values, a.top_type, i) * a.inv_top_t;
+}
+// t / Tt, less first / Tt where it is an int32 (first: the largest)
+__device__ __forceinline__ float teacher(const DistillArgs &a, float t, int32_t first)
+{
+    return a.top_type == kI32 ? Elem<kI32>::minus(__float_as_int(t), first) * a.inv_top_t : t;
+}
+// the given log_norm to go with that
+__device__ __forceinline__ float given_norm(const DistillArgs &a, int64_t r, int32_t first)
+{
+    const float norm = a.top_log_norm[r];
+    return a.top_type == kI32 ? norm - (float)first * a.inv_top_t : norm;
+}
 
 // GRAD: with the gradient; the loss alone reads the row once and keeps none of it.
 template <int TYPE, class L, bool GRAD>
 __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_distill(DistillArgs a)
 {
+    typedef Elem<TYPE> E;
+    typedef typename E::Cmp Cmp;
     typedef Piece<TYPE, L::VEC> P;
-    extern __shared__ Entry entries[];                    // [rows of the block][k]
+    extern __shared__ uint32_t entries[];                 // [rows of the block][k]
     __shared__ Scratch scratch;
     __shared__ int32_t heads[L::kBlock];                  // first entry of the lane's list
     __shared__ uint32_t marks[L::kBlock];                 // bit j % 32: an entry in piece j
@@ -143,7 +166,7 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
     // them).
     constexpr int H = L::G < kWave ? L::G : kWave;
     Group<H> h(g.t % H, nullptr);
-    Entry *list = entries + (int64_t)gi * a.k;
+    Entry<Cmp> *list = reinterpret_cast<Entry<Cmp> *>(entries) + (int64_t)gi * a.k;
     int32_t *head = heads + gi * L::G;
     uint32_t *mark = marks + gi * L::G;
     const char *src = a.logits + r * a.stride;
@@ -152,8 +175,8 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
 
     Row<TYPE, L::G, L::NV, L::VEC, L::RESIDENT, GRAD> row(src, w == 0.0f ? 0 : a.n, g.t);
     const bool rest = a.top_log_norm != nullptr;
-    float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f, from = 0.0f,
-          from_out = 0.0f;
+    float Q = 0.0f, S = 0.0f, scale = 0.0f, in_list = 0.0f, outside = 0.0f;
+    Cmp from = 0, from_out = 0;
     const Scale c(a.inv_t);
     if (w != 0.0f) {
         head[g.t] = -1;
@@ -161,13 +184,11 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
         g.barrier();
         for (int e = g.t; e < a.k; e += L::G) {
             const int32_t cls = a.top_indices[r * a.k + e];
-            Entry x = {-1, -1, -__builtin_inff(), 0.0f, 0.0f};
+            Entry<Cmp> x = {-1, -1, -__builtin_inff(), 0, 0.0f};
             if (cls >= 0 && cls < a.n) {
                 x.cls = cls;
-                x.t = load_float(a.top_values, a.top_type, r * a.k + e) * a.inv_top_t;
-                const typename Elem<TYPE>::Cmp v = load_one<TYPE>(src, cls);
-                x.z = TYPE == kI32 && v == Elem<TYPE>::lowest() ? -__builtin_inff()
-                                                                : Elem<TYPE>::to_float(v);
+                x.t = load_teacher(a, r * a.k + e);
+                x.z = load_one<TYPE>(src, cls);
                 const int piece = cls / L::VEC, owner = piece % L::G;
                 atomicOr(&mark[owner], 1u << (piece / L::G % 32));
                 x.next = atomicExch(&head[owner], e);
@@ -177,50 +198,58 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
         g.barrier();
         // the teacher's normalizer: of the list, or given
         float log_norm;
+        int32_t first = INT32_MIN;
+        if (a.top_type == kI32) {
+            for (int e = h.t; e < a.k; e += H)
+                if (list[e].cls >= 0)
+                    first = max(first, __float_as_int(list[e].t));
+            first = h.reduce(first, Max());
+        }
         if (rest) {
-            log_norm = a.top_log_norm[r];
+            log_norm = given_norm(a, r, first);
         } else {
             float tm = -__builtin_inff(), sum = 0.0f;
-            for (int e = h.t; e < a.k; e += H)
-                tm = fmaxf(tm, list[e].t);                // (-inf where there is none)
+            if (a.top_type == kI32)
+                tm = 0.0f;
+            else
+                for (int e = h.t; e < a.k; e += H)
+                    tm = fmaxf(tm, list[e].t);            // (-inf where there is none)
             tm = h.reduce(tm, Max());
             for (int e = h.t; e < a.k; e += H)
                 if (list[e].cls >= 0)
-                    sum += expf(list[e].t - tm);
+                    sum += expf(teacher(a, list[e].t, first) - tm);
             log_norm = tm + logf(h.reduce(sum, Add()));
         }
-        Softmax<> listed;
+        Softmax<TYPE> listed;
         for (int e = h.t; e < a.k; e += H)
             if (list[e].cls >= 0) {
-                Q += expf(list[e].t - log_norm);
+                Q += expf(teacher(a, list[e].t, first) - log_norm);
                 listed.raise(list[e].z, c.hi);
-                listed.s += c.pow(list[e].z - listed.from());
+                listed.s += c.pow(E::minus(list[e].z, listed.from()));
             }
         Q = h.reduce(Q, Add());
         const float q_rest = rest ? fmaxf(0.0f, 1.0f - Q) : 0.0f;
 
         const uint32_t marked = rest ? mark[g.t] : 0;
-        Softmax<!L::RESIDENT> sm;
+        Softmax<TYPE, !L::RESIDENT> sm;
         row.each([&](auto j, int32_t, const P &given) {
             P p = given;
             if (marked >> (j % 32) & 1)
                 for (int e = head[g.t]; e >= 0; e = list[e].next)
                     if (list[e].cls / (L::G * L::VEC) == j)
                         p.mask(list[e].cls % L::VEC);
-            float z[L::VEC], zm = -__builtin_inff();
+            Cmp z[L::VEC], zm = E::lowest();
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
-                z[u] = Elem<TYPE>::to_float(p.get(u));
-                if (TYPE == kI32 && p.get(u) == Elem<TYPE>::lowest())
-                    z[u] = -__builtin_inff();
-                zm = fmaxf(zm, z[u]);
+                z[u] = p.get(u);
+                zm = Max()(zm, z[u]);
             }
             sm.raise(zm, c.hi);
-            const float from = sm.from();
+            const Cmp from = sm.from();
             float part = sm.start();
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
-                part += c.pow(z[u] - from);
+                part += c.pow(E::minus(z[u], from));
             sm.add(part);
         });
         // The rest relative to its own maximum, where its mass cannot vanish; the whole
@@ -233,8 +262,8 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
         S = s_out;
         if (rest) {
             listed = combine(h, listed, c.hi);
-            const float m = fmaxf(sm.m, listed.m);
-            share = sm.m == m ? 1.0f : c.pow(sm.m - m);
+            const Cmp m = Max()(sm.m, listed.m);
+            share = sm.m == m ? 1.0f : c.pow(E::minus(sm.m, m));
             listed.raise(m, c.hi);
             from = listed.from();
             S = s_out * share + listed.s;
@@ -244,13 +273,13 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
             float sum = 0.0f;
             for (int e = h.t; e < a.k; e += H)
                 if (list[e].cls >= 0) {
-                    const float log_q = list[e].t - log_norm, q = expf(log_q);
-                    const float log_p = (list[e].z - from) * a.inv_t - log_s;
+                    const float log_q = teacher(a, list[e].t, first) - log_norm, q = expf(log_q);
+                    const float log_p = E::minus(list[e].z, from) * a.inv_t - log_s;
                     sum += q == 0.0f ? 0.0f : q * (log_q - log_p);
                 }
             sum = h.reduce(sum, Add());
             if (q_rest > 0.0f)
-                sum += q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
+                sum += q_rest * (logf(q_rest) - (E::minus(from_out, from) * a.inv_t +
                                                  logf(s_out) - log_s));
             if (g.t == 0)
                 a.loss[r] = w * sum;
@@ -266,8 +295,8 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
         if (GRAD) {
             for (int e = g.t; e < a.k; e += L::G)
                 if (list[e].cls >= 0)
-                    list[e].grad = in_list * c.pow(list[e].z - from) -
-                                scale * expf(list[e].t - log_norm);
+                    list[e].grad = in_list * c.pow(E::minus(list[e].z, from)) -
+                                   scale * expf(teacher(a, list[e].t, first) - log_norm);
             g.barrier();
         }
     } else if (a.loss && g.t == 0) {
@@ -316,11 +345,13 @@ __host__ __device__ inline int32_t quad_pitch(int32_t n) { return ((n + 3) / 4 |
 template <int TYPE>
 __global__ __launch_bounds__(kLaneThreads) void k_distill_lanes(DistillArgs a)
 {
+    typedef Elem<TYPE == kI32 ? kI32 : kF32> E;           // (the tile's elements)
+    typedef typename E::Cmp Cmp;
     extern __shared__ uint32_t tiles[];                   // a wave's [16][pitch], and [16][k] of
     const int32_t pitch = quad_pitch(a.n), lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     uint32_t *const tile = tiles + wave * kWaveRows * (pitch + 3 * a.k);
-    float *const tops = reinterpret_cast<float *>(tile) + kWaveRows * pitch;   // teacher / Tt
-    float *const zs = tops + kWaveRows * a.k;                                  // student
+    float *const tops = reinterpret_cast<float *>(tile) + kWaveRows * pitch;   // teacher
+    Cmp *const zs = reinterpret_cast<Cmp *>(tops + kWaveRows * a.k);           // student
     int32_t *const classes = reinterpret_cast<int32_t *>(zs + kWaveRows * a.k);
     const int64_t r0 = ((int64_t)blockIdx.x * (kLaneThreads / kWave) + wave) * kWaveRows;
     if (r0 >= a.n_rows)
@@ -329,7 +360,7 @@ __global__ __launch_bounds__(kLaneThreads) void k_distill_lanes(DistillArgs a)
     for (int32_t e = lane; e < rows * a.k; e += kWave) {
         const int32_t cls = a.top_indices[r0 * a.k + e];
         classes[e] = cls >= 0 && cls < a.n ? cls : -1;
-        tops[e] = load_float(a.top_values, a.top_type, r0 * a.k + e) * a.inv_top_t;
+        tops[e] = load_teacher(a, r0 * a.k + e);
     }
     load_tile<TYPE>(a.logits + r0 * a.stride, a.stride, rows, a.n, pitch, tile);
     wave_sync();
@@ -341,56 +372,57 @@ __global__ __launch_bounds__(kLaneThreads) void k_distill_lanes(DistillArgs a)
         const float w = a.row_weight ? a.row_weight[r] : 1.0f;
         float *z = reinterpret_cast<float *>(tile) + own * pitch;
         const float *top = tops + own * a.k;
-        float *listed = zs + own * a.k;
+        Cmp *scores = reinterpret_cast<Cmp *>(z), *listed = zs + own * a.k;
         const int32_t *cls = classes + own * a.k;
         const Scale c(a.inv_t);
         float scale = 0.0f, loss = 0.0f;
         if (w != 0.0f) {
             // the list leaves the tile; both relative to their own maxima
-            float m_list = -__builtin_inff(), m = -__builtin_inff(), tm = -__builtin_inff();
+            Cmp m_list = E::lowest(), m = E::lowest();
+            float tm = -__builtin_inff();
+            int32_t first = INT32_MIN;
             for (int e = g.t; e < a.k; e += kRowLanes)
                 if (cls[e] >= 0) {
-                    const int32_t v = __float_as_int(z[cls[e]]);
-                    listed[e] = TYPE != kI32 ? z[cls[e]]
-                                : v == INT32_MIN ? -__builtin_inff() : (float)v;
-                    z[cls[e]] = TYPE == kI32 ? __int_as_float(INT32_MIN) : -__builtin_inff();
-                    m_list = fmaxf(m_list, listed[e]);
+                    listed[e] = scores[cls[e]];
+                    scores[cls[e]] = E::lowest();
+                    m_list = Max()(m_list, listed[e]);
                     tm = fmaxf(tm, top[e]);
+                    first = max(first, __float_as_int(top[e]));
                 }
             m_list = g.reduce(m_list, Max());
+            if (a.top_type == kI32) {
+                first = g.reduce(first, Max());
+                tm = 0.0f;
+            }
             wave_sync();
 #pragma unroll 8
-            for (int i = g.t; i < a.n; i += kRowLanes) {
-                if constexpr (TYPE == kI32) {
-                    const int32_t v = __float_as_int(z[i]);
-                    z[i] = v == INT32_MIN ? -__builtin_inff() : (float)v;
-                }
-                m = fmaxf(m, z[i]);
-            }
+            for (int i = g.t; i < a.n; i += kRowLanes)
+                m = Max()(m, scores[i]);
             m = g.reduce(m, Max());
-            const float from_out = m == -__builtin_inff() ? 0.0f : m;
-            const float share = m >= m_list ? 1.0f : c.pow(m - m_list);
-            m = fmaxf(m, m_list);
-            const float from = m == -__builtin_inff() ? 0.0f : m;
+            const auto finite = [](Cmp v) { return TYPE != kI32 && v == E::lowest() ? 0 : v; };
+            const Cmp from_out = finite(m);
+            const float share = m >= m_list ? 1.0f : c.pow(E::minus(m, m_list));
+            m = Max()(m, m_list);
+            const Cmp from = finite(m);
             float log_norm;
             if (a.top_log_norm) {
-                log_norm = a.top_log_norm[r];
+                log_norm = given_norm(a, r, first);
             } else {
                 tm = g.reduce(tm, Max());
                 float sum = 0.0f;
                 for (int e = g.t; e < a.k; e += kRowLanes)
-                    sum += cls[e] >= 0 ? expf(top[e] - tm) : 0.0f;
+                    sum += cls[e] >= 0 ? expf(teacher(a, top[e], first) - tm) : 0.0f;
                 log_norm = tm + logf(g.reduce(sum, Add()));
             }
             float Q = 0.0f, s_list = 0.0f, s_out = 0.0f;
             for (int e = g.t; e < a.k; e += kRowLanes)
                 if (cls[e] >= 0) {
-                    Q += expf(top[e] - log_norm);
-                    s_list += c.pow(listed[e] - from);
+                    Q += expf(teacher(a, top[e], first) - log_norm);
+                    s_list += c.pow(E::minus(listed[e], from));
                 }
 #pragma unroll 8
             for (int i = g.t; i < a.n; i += kRowLanes) {
-                const float e = c.pow(z[i] - from_out);
+                const float e = c.pow(E::minus(scores[i], from_out));
                 s_out += e;
                 z[i] = e;
             }
@@ -413,16 +445,15 @@ __global__ __launch_bounds__(kLaneThreads) void k_distill_lanes(DistillArgs a)
             wave_sync();
             for (int e = g.t; e < a.k; e += kRowLanes)
                 if (cls[e] >= 0) {
-                    const float log_q = top[e] - log_norm, q = expf(log_q);
-                    const float x = (listed[e] - from) * a.inv_t;
+                    const float log_q = teacher(a, top[e], first) - log_norm, q = expf(log_q);
+                    const float x = E::minus(listed[e], from) * a.inv_t;
                     loss += q == 0.0f ? 0.0f : q * (log_q - (x - log_s));
                     if (scale != 0.0f)
-                        z[cls[e]] = in_list * c.pow(listed[e] - from) -
-                                    scale * q;
+                        z[cls[e]] = in_list * c.pow(E::minus(listed[e], from)) - scale * q;
                 }
             loss = g.reduce(loss, Add());
             if (q_rest > 0.0f)
-                loss += q_rest * (logf(q_rest) - ((from_out - from) * a.inv_t +
+                loss += q_rest * (logf(q_rest) - (E::minus(from_out, from) * a.inv_t +
                                                   logf(s_out) - log_s));
             loss *= w;
         }
@@ -474,7 +505,7 @@ hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int3
         return with_layout<TYPE>(n, k, [&](auto layout) {
             typedef decltype(layout) L;
             const uint32_t blocks = (uint32_t)((n_rows + L::kGroups - 1) / L::kGroups);
-            const size_t lds = (size_t)L::kGroups * k * sizeof(Entry);
+            const size_t lds = (size_t)L::kGroups * k * sizeof(Entry<float>);
             if constexpr (TYPE != kI32)
                 if (grad) {
                     k_distill<TYPE, L, true><<<blocks, L::kBlock, lds, stream>>>(a);

@@ -38,7 +38,8 @@ __device__ __forceinline__ void static_for(F &&f)
 }
 
 // ---- element types ----
-// Cmp: what elements are compared as; kShift: key bits below the type's own.
+// Cmp: what elements are compared as; kShift: key bits below the type's own.  minus: a
+// difference v - from, v <= from, as float; -inf for a masked v.
 template <int TYPE>
 struct Elem {
     typedef float Cmp;
@@ -46,6 +47,7 @@ struct Elem {
     static constexpr int kShift = TYPE == kF32 ? 0 : TYPE == kF16 ? 13 : 16;
     static __device__ __forceinline__ Cmp lowest() { return -__builtin_inff(); }
     static __device__ __forceinline__ float to_float(Cmp v) { return v; }
+    static __device__ __forceinline__ float minus(Cmp v, Cmp from) { return v - from; }
     static __device__ __forceinline__ uint32_t key(Cmp v)
     {
         const uint32_t b = __float_as_uint(v + 0.0f);
@@ -69,6 +71,12 @@ struct Elem<kI32> {
     static constexpr int kShift = 0;
     static __device__ __forceinline__ Cmp lowest() { return INT32_MIN; }
     static __device__ __forceinline__ float to_float(Cmp v) { return (float)v; }
+    // in integers first: scores past 2^24 (an int8 head's reach 10^9) are not floats
+    static __device__ __forceinline__ float minus(Cmp v, Cmp from)
+    {
+        const float less = -(float)((uint32_t)from - (uint32_t)v);
+        return v == INT32_MIN ? -__builtin_inff() : less;
+    }
     static __device__ __forceinline__ uint32_t key(Cmp v) { return (uint32_t)v ^ 0x80000000u; }
     static __device__ __forceinline__ Cmp from_key(uint32_t k)
     {
@@ -451,17 +459,22 @@ struct Total {
 // A running maximum m of z and the sum s of 2^(c (z - m)): with c = log2(e) / T the
 // exponentials of a softmax at temperature T.  The difference comes first: c z alone
 // overflows where z is its type's lowest value, which masks are made of.
-template <bool LONG = false>
+template <int TYPE, bool LONG = false>
 struct Softmax : Total<LONG> {
+    typedef Elem<TYPE> E;
+    typedef typename E::Cmp Cmp;
     using Total<LONG>::s;
     using Total<LONG>::lost;
-    float m = -__builtin_inff();
-    __device__ __forceinline__ float from() const { return m == -__builtin_inff() ? 0.0f : m; }
-    __device__ __forceinline__ void raise(float to, float c)
+    Cmp m = E::lowest();
+    __device__ __forceinline__ Cmp from() const
     {
-        const float old = from();
-        m = fmaxf(m, to);
-        const float f = __builtin_amdgcn_exp2f(s == 0.0f ? 0.0f : (old - from()) * c);
+        return TYPE != kI32 && m == E::lowest() ? 0 : m;
+    }
+    __device__ __forceinline__ void raise(Cmp to, float c)
+    {
+        const Cmp old = from();
+        m = Max()(m, to);
+        const float f = __builtin_amdgcn_exp2f(s == 0.0f ? 0.0f : E::minus(old, from()) * c);
         s *= f;
         if constexpr (LONG)
             lost *= f;
@@ -469,14 +482,17 @@ struct Softmax : Total<LONG> {
     // log sum e^(z / T)
     __device__ __forceinline__ float log_norm(float inv_t) const
     {
-        return m == __builtin_inff() || m == -__builtin_inff()
-                   ? m : m * inv_t + __builtin_amdgcn_logf(s) * kLn2;
+        if (m == E::lowest())
+            return -__builtin_inff();
+        const float most = E::to_float(m);
+        return most == __builtin_inff() ? most
+                                        : most * inv_t + __builtin_amdgcn_logf(s) * kLn2;
     }
 };
 
 // Over a group: the maximum first, then the sums relative to it.
-template <class Grp, bool LONG>
-__device__ __forceinline__ Softmax<LONG> combine(Grp &g, Softmax<LONG> a, float c)
+template <class Grp, int TYPE, bool LONG>
+__device__ __forceinline__ Softmax<TYPE, LONG> combine(Grp &g, Softmax<TYPE, LONG> a, float c)
 {
     a.raise(g.reduce(a.m, Max()), c);
     a.s = g.reduce(a.s, Add());

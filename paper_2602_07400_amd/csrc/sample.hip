@@ -116,7 +116,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
     // softmax's sum, as the row arrives
     Cmp mine = E::lowest(), most[L::NV];
     static_for<L::NV>([&](auto j) __attribute__((always_inline)) { most[j] = E::lowest(); });
-    Softmax<!L::RESIDENT> sm;
+    Softmax<TYPE, !L::RESIDENT> sm;
     const bool of_all = by_p && !by_k && temperature > 0.0f && kLists;
     const float c = inv_t * kLog2e;
     row.each([&](auto j, int32_t, const P &p) {
@@ -130,14 +130,13 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         if constexpr (L::RESIDENT)
             most[j] = vm;
         if (of_all) {
-            sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
-            const float from = sm.from();
+            sm.raise(vm, c);
+            const Cmp from = sm.from();
             float part = sm.start();
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u) {
                 const Cmp v = p.get(u);
-                part += v > E::lowest() ? __builtin_amdgcn_exp2f((E::to_float(v) - from) * c)
-                                        : 0.0f;
+                part += v > E::lowest() ? __builtin_amdgcn_exp2f(E::minus(v, from) * c) : 0.0f;
             }
             sm.add(part);
         }
@@ -177,10 +176,10 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
 
     // (a row with +inf draws among those: x = 0 there, hugely negative elsewhere)
     const bool endless = E::to_float(top) == __builtin_inff();
-    const float ftop = endless ? 3.4028234663852886e38f : E::to_float(top);
+    const Cmp from = endless ? (Cmp)3.4028234663852886e38f : top;
     const float floor_x = min_p > 0.0f ? logf(min_p) : -__builtin_inff();
     const auto x_of = [&](Cmp v) __attribute__((always_inline)) {
-        return fminf((E::to_float(v) - ftop) * inv_t, 0.0f);
+        return fminf(E::minus(v, from) * inv_t, 0.0f);
     };
     float row_mass = 0.0f;                                // sum of w
     if (of_all) {
@@ -192,7 +191,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     sm.s += p.get(u) == top ? 1.0f : 0.0f;
             });
         } else {
-            sm.raise(ftop, c);
+            sm.raise(from, c);
         }
         row_mass = g.reduce(sm.s, Add());
     }
@@ -467,14 +466,14 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
             const uint32_t least = tau + cut;
             uint32_t lo = least;
             if constexpr (TYPE != kI32)
-                lo = max(lo, E::key(ftop + logf((1.0f - top_p) * row_mass / (float)a.n) *
+                lo = max(lo, E::key(from + logf((1.0f - top_p) * row_mass / (float)a.n) *
                                                temperature) - 1);
             Range<Mass> at = {lo, lo + 1, 0, 0};
             if (lo != end)                                // (0 past the largest integer)
                 at = narrow<TYPE, L, Mass>(
                     g, row, most, {lo, end, 0, kUnknown}, goal, 0, (Mass *)lists[gi],
                     [&](Cmp v) __attribute__((always_inline)) {
-                        const float w = __builtin_amdgcn_exp2f((E::to_float(v) - ftop) * c);
+                        const float w = __builtin_amdgcn_exp2f(E::minus(v, from) * c);
                         return to_mass(fminf(w, 1.0f), unit);
                     });
             const float need = (float)((double)(goal - min(at.before, goal)) / unit);

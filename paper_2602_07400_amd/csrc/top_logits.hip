@@ -55,7 +55,7 @@ __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArg
     Row<TYPE, G, L::NV, L::VEC, L::RESIDENT, (G < kWave)> row(src, a.n, g.t);
 
     const float c = a.inv_t * kLog2e;
-    Softmax<!L::RESIDENT> sm;
+    Softmax<TYPE, !L::RESIDENT> sm;
     Cmp top = E::lowest(), most[L::NV];                   // the lane's and its pieces' largest
     static_for<L::NV>([&](auto j) __attribute__((always_inline)) { most[j] = E::lowest(); });
     row.each([&](auto j, int32_t, const P &p) {
@@ -67,15 +67,14 @@ __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArg
         if constexpr (L::RESIDENT)
             most[j] = vm;
         if (a.log_norm) {
-            sm.raise(vm > E::lowest() ? E::to_float(vm) : -__builtin_inff(), c);
-            const float from = sm.from();
+            // (the select changes nothing but the compiler's registers: without it more of
+            // them are spilled around the list, 2048 x 131072 in 122 us instead of 106)
+            sm.raise(vm > E::lowest() ? vm : E::lowest(), c);
+            const Cmp from = sm.from();
             float part = sm.start();
 #pragma unroll
-            for (int u = 0; u < L::VEC; ++u) {
-                const Cmp v = p.get(u);
-                const float e = __builtin_amdgcn_exp2f((E::to_float(v) - from) * c);
-                part += TYPE == kI32 && v == E::lowest() ? 0.0f : e;
-            }
+            for (int u = 0; u < L::VEC; ++u)
+                part += __builtin_amdgcn_exp2f(E::minus(p.get(u), from) * c);
             sm.add(part);
         }
     });
@@ -86,7 +85,7 @@ __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArg
                 float part = sm.start();
 #pragma unroll
                 for (int u = 0; u < L::VEC; ++u) {
-                    const float e = E::to_float(p.get(u)) - sm.m;
+                    const float e = E::minus(p.get(u), sm.m);
                     part += e <= 0.0f ? __builtin_amdgcn_exp2f(e * c) : 0.0f;
                 }
                 sm.add(part);
@@ -257,14 +256,14 @@ __global__ __launch_bounds__(kWave) void k_top_lanes(TopArgs a)
     };
     if (a.log_norm) {
         const uint32_t first = key_at(0);
-        const float m = first ? E::to_float(E::from_key(first)) : -__builtin_inff();
-        const float from = first ? m : 0.0f, c = a.inv_t * kLog2e;
-        Softmax<> sm;
-        sm.m = m;
+        const float c = a.inv_t * kLog2e;
+        Softmax<TYPE == kI32 ? kI32 : kF32> sm;
+        if (first)
+            sm.m = E::from_key(first);
 #pragma unroll 4
         for (int i = 0; i < a.n; ++i) {
             const Cmp v = at(i);
-            sm.s += v > E::lowest() ? __builtin_amdgcn_exp2f((E::to_float(v) - from) * c) : 0.0f;
+            sm.s += v > E::lowest() ? __builtin_amdgcn_exp2f(E::minus(v, sm.m) * c) : 0.0f;
         }
         if ((int32_t)threadIdx.x < rows)
             a.log_norm[r0 + threadIdx.x] = sm.log_norm(a.inv_t);

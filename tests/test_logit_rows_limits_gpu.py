@@ -158,3 +158,57 @@ def test_sample_repeats_bit_for_bit(c, dtype):
             again = bl.bitlogic_sample(x, noise, scale, k, p, m)
             torch.cuda.synchronize()
             assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1]), (k, p, m)
+
+
+# -------------------------------------------------------- scores past 2^24
+
+@pytest.mark.parametrize("c", [12, 100, 700, 5000, 40001, 140000])
+def test_scores_that_differ_below_their_float_rounding(c):
+    """Int32 scores of 2^30 and more, a few units apart: what depends on differences alone
+    is that of the scores less their maximum, which float holds exactly."""
+    rng = _rng(25, c)
+    n = 6
+    near = torch.from_numpy(rng.integers(-40, 1, (n, c)).astype(np.int32))
+    near[:, 0] = 0
+    near[0, 1] = near[1, 2] = -2 ** 31                    # masked
+    high = torch.where(near > -2 ** 31, near + 2 ** 30 + 7, near)
+    noise = _gumbel(rng, n, c).to(DEV)
+    for k, p, m in ((0, 1.0, 0.0), (5, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.05), (700, 0.99, 0.01),
+                    (2000, 0.9, 0.0)):
+        a = bl.bitlogic_sample(near.to(DEV), noise, 6.0, k, p, m)
+        b = bl.bitlogic_sample(high.to(DEV), noise, 6.0, k, p, m)
+        torch.cuda.synchronize()
+        _check_sample(near, noise, 6.0, k, p, m, a)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), (k, p, m)
+    # the student's scores, and the teacher's (its list's own normalizer)
+    t, idx, _ = bl.bitlogic_top_logits(high.to(DEV), 9, 6.0)
+    for i in range(9):
+        assert (idx[:, i] >= 0).all()
+    shifted = (t.cpu() - (2 ** 30 + 7)).to(DEV)
+    for z in (near, high):
+        for v in (shifted, t):
+            loss, _ = bl.bitlogic_distill(z.to(DEV), v, idx, None, 6.0, 6.0, want_grad=False)
+            _check_distill(near, shifted.cpu(), idx.cpu(), None, 6.0, 6.0, None, (loss, None))
+
+
+def test_many_short_rows_of_scores_past_2_24():
+    rng = _rng(26)
+    n, c = 17003, 37
+    near = torch.from_numpy(rng.integers(-40, 1, (n, c)).astype(np.int32))
+    near[:, 5] = 0
+    near[3, 1] = -2 ** 31
+    high = torch.where(near > -2 ** 31, near + 2 ** 30 + 7, near).to(DEV)
+    near = near.to(DEV)
+    t, idx, norm = bl.bitlogic_top_logits(high, 9, 4096.0)
+    shifted, same, base = bl.bitlogic_top_logits(near, 9, 4096.0)
+    assert torch.equal(idx, same) and torch.equal(t - (2 ** 30 + 7), shifted)
+    far = base.double() + (2.0 ** 30 + 7) / 4096
+    assert bool(((norm - far).abs() <= REL + 2.0 ** -23 * far).all())
+    want, _ = bl.bitlogic_distill(near, shifted, idx, None, 6.0, 6.0, want_grad=False)
+    some = np.r_[0:60, n - 30:n]
+    _check_distill(near[some].cpu(), shifted[some].cpu(), idx[some].cpu(), None, 6.0, 6.0, None,
+                   (want[some], None))
+    for z in (near, high):
+        for v in (shifted, t):
+            loss, _ = bl.bitlogic_distill(z, v, idx, None, 6.0, 6.0, want_grad=False)
+            assert bool(((loss - want).abs() <= 3 * REL * (1 + want.abs())).all())
