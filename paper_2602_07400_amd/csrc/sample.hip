@@ -499,6 +499,8 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         if (yes > tau)
             ties = kAll;
         tau = yes;
+        if (floor_x > 0.0f)                               // none: the first class alone
+            ties = 1;
     }
     const Cmp at = E::from_key(tau);
     int32_t last = INT32_MAX;                             // the last kept class equal to tau

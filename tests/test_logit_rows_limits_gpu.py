@@ -212,3 +212,20 @@ def test_many_short_rows_of_scores_past_2_24():
         for v in (shifted, t):
             loss, _ = bl.bitlogic_distill(z, v, idx, None, 6.0, 6.0, want_grad=False)
             assert bool(((loss - want).abs() <= 3 * REL * (1 + want.abs())).all())
+
+
+# ---------------------------------------------- ends of the parameters' ranges
+
+@pytest.mark.parametrize("c", [12, 100, 700, 5000, 140000])
+def test_sample_min_p_above_one_keeps_the_first_class(c):
+    rng = _rng(27, c)
+    x = torch.zeros((3, c))
+    x[1, c // 2:] = -1.0
+    x[2, ::2] = 3.0
+    noise = _gumbel(rng, 3, c)
+    m = torch.tensor([1.5, 2.0, 100.0])
+    for k, p in ((0, 1.0), (5, 1.0), (0, 0.9), (2000, 0.9)):
+        got = bl.bitlogic_sample(x.to(DEV), noise.to(DEV), 1.0, k, p, m.to(DEV))
+        torch.cuda.synchronize()
+        _check_sample(x, noise, 1.0, k, p, m, got)
+        assert got[0].tolist() == [0, 0, 0] and (got[1] == 0).all()
