@@ -174,12 +174,12 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
         return;
     }
 
-    // (a row with +inf draws among those: x = 0 there, hugely negative elsewhere)
+    // (a row with +inf draws among those: x = 0 there, the minimum's answer to the NaN of
+    // inf - inf, and -inf elsewhere)
     const bool endless = E::to_float(top) == __builtin_inff();
-    const Cmp from = endless ? (Cmp)3.4028234663852886e38f : top;
     const float floor_x = min_p > 0.0f ? logf(min_p) : -__builtin_inff();
     const auto x_of = [&](Cmp v) __attribute__((always_inline)) {
-        return fminf(E::minus(v, from) * inv_t, 0.0f);
+        return fminf(E::minus(v, top) * inv_t, 0.0f);
     };
     float row_mass = 0.0f;                                // sum of w
     if (of_all) {
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
                     sm.s += p.get(u) == top ? 1.0f : 0.0f;
             });
         } else {
-            sm.raise(from, c);
+            sm.raise(top, c);
         }
         row_mass = g.reduce(sm.s, Add());
     }
@@ -466,14 +466,14 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
             const uint32_t least = tau + cut;
             uint32_t lo = least;
             if constexpr (TYPE != kI32)
-                lo = max(lo, E::key(from + logf((1.0f - top_p) * row_mass / (float)a.n) *
+                lo = max(lo, E::key(top + logf((1.0f - top_p) * row_mass / (float)a.n) *
                                                temperature) - 1);
             Range<Mass> at = {lo, lo + 1, 0, 0};
             if (lo != end)                                // (0 past the largest integer)
                 at = narrow<TYPE, L, Mass>(
                     g, row, most, {lo, end, 0, kUnknown}, goal, 0, (Mass *)lists[gi],
                     [&](Cmp v) __attribute__((always_inline)) {
-                        const float w = __builtin_amdgcn_exp2f(E::minus(v, from) * c);
+                        const float w = __builtin_amdgcn_exp2f(E::minus(v, top) * c);
                         return to_mass(fminf(w, 1.0f), unit);
                     });
             const float need = (float)((double)(goal - min(at.before, goal)) / unit);

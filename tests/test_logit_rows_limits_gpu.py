@@ -229,3 +229,24 @@ def test_sample_min_p_above_one_keeps_the_first_class(c):
         torch.cuda.synchronize()
         _check_sample(x, noise, 1.0, k, p, m, got)
         assert got[0].tolist() == [0, 0, 0] and (got[1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("c", [12, 100, 700, 5000, 140000])
+def test_sample_infinite_logits_at_any_temperature(c, dtype):
+    """Beside a logit of +inf no finite one has mass: not the type's largest either, nor
+    at a temperature of 1e38."""
+    rng = _rng(28, c, FLOATS.index(dtype))
+    x = _logits(rng, 4, c, dtype)
+    x[0, c // 3] = np.inf
+    x[1, c // 3] = np.inf
+    x[1, c // 2] = torch.finfo(dtype).max
+    x[2] = torch.finfo(dtype).max
+    x[2, [1, c - 2]] = np.inf
+    noise = _gumbel(rng, 4, c)
+    for t in (1.0, 1e38):
+        for k, p, m in ((0, 1.0, 0.0), (5, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.05),
+                        (700, 0.99, 0.01), (5, 0.9, 0.0)):
+            got = bl.bitlogic_sample(x.to(DEV), noise.to(DEV), t, k, p, m)
+            torch.cuda.synchronize()
+            _check_sample(x, noise, t, k, p, m, got)
