@@ -442,7 +442,8 @@ enum {
  * how a launch is scheduled.  Buffers need their elements' natural alignment only.
  * Limits: 1 <= n_classes <= 2^30, 0 <= n_rows < 2^31 (0 enqueues nothing, with any
  * pointers), 1 <= k <= BITLOGIC_TOP_MAX, temperatures positive and finite
- * (BITLOGIC_ERR_SHAPE; an unknown type or a larger k: BITLOGIC_ERR_UNSUPPORTED). */
+ * (BITLOGIC_ERR_SHAPE; an unknown type or a larger k: BITLOGIC_ERR_UNSUPPORTED).
+ * Temperatures below 2^-126 count as 2^-126. */
 #define BITLOGIC_TOP_MAX 1024
 
 /* The k largest logits of every row and the row's log-normalizer: what a teacher

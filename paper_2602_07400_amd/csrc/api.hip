@@ -955,8 +955,8 @@ int bitlogic_top_logits(const void *logits, int32_t type, int64_t n_rows, int32_
         !aligned(indices, 4) || !aligned(log_norm, 4))
         return fail(BITLOGIC_ERR_ALIGN, "top_logits: misaligned buffer");
     return hip_status(bl::launch_top_logits(logits, type, n_rows, n_classes, row_stride, k,
-                                            1.0f / temperature, values, indices, log_norm,
-                                            (hipStream_t)stream),
+                                            bl::rows::inverse(temperature), values, indices,
+                                            log_norm, (hipStream_t)stream),
                       "top_logits launch");
 }
 
@@ -988,9 +988,10 @@ int bitlogic_distill(const void *logits, int32_t type, int64_t n_rows, int32_t n
         !aligned(top_log_norm, 4) || !aligned(row_weight, 4) || !aligned(loss, 4))
         return fail(BITLOGIC_ERR_ALIGN, "distill: misaligned buffer");
     return hip_status(bl::launch_distill(logits, type, n_rows, n_classes, row_stride,
-                                         1.0f / temperature, top_values, top_type, top_indices,
-                                         k, top_log_norm, 1.0f / top_temperature, row_weight,
-                                         loss, grad, grad_stride, (hipStream_t)stream),
+                                         bl::rows::inverse(temperature), top_values, top_type,
+                                         top_indices, k, top_log_norm,
+                                         bl::rows::inverse(top_temperature), row_weight, loss,
+                                         grad, grad_stride, (hipStream_t)stream),
                       "distill launch");
 }
 

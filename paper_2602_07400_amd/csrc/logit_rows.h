@@ -426,6 +426,12 @@ struct Row {
     }
 };
 
+// 1 / T, and for a T below the normal numbers, where that may be no float, 2^126.
+__host__ __device__ __forceinline__ float inverse(float temperature)
+{
+    return fminf(1.0f / temperature, 0x1p126f);
+}
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 

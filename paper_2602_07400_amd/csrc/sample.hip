@@ -82,7 +82,7 @@ __global__ __launch_bounds__(L::kBlock, PLAIN ? L::kWavesPerSimd : 4) void k_sam
     if (top_k <= 0 || top_k > a.n)
         top_k = a.n;
     const bool by_k = top_k < a.n, by_p = top_p < 1.0f;
-    const float inv_t = 1.0f / temperature;
+    const float inv_t = inverse(temperature);
 
     constexpr int kRoom = TYPE == kF16 && L::NV == 16 ? 16 : 32;   // registers for them
     constexpr int kAhead = !L::RESIDENT ? 1 : L::NV < kRoom / L::VEC ? L::NV : kRoom / L::VEC;

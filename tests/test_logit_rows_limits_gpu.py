@@ -250,3 +250,41 @@ def test_sample_infinite_logits_at_any_temperature(c, dtype):
             got = bl.bitlogic_sample(x.to(DEV), noise.to(DEV), t, k, p, m)
             torch.cuda.synchronize()
             _check_sample(x, noise, t, k, p, m, got)
+
+
+@pytest.mark.parametrize("n", [3, 17003])
+@pytest.mark.parametrize("c", [12, 100, 700, 5000, 140000])
+def test_temperatures_below_the_normal_numbers(c, n):
+    """A temperature below 2^-126, whose reciprocal may be no float, counts as 2^-126:
+    the largest logits share all the mass."""
+    if n > 3 and c > 128:
+        pytest.skip("many short rows only")
+    rng = _rng(29, c, n)
+    x = _logits(rng, n, c, torch.float32)
+    x = x - x.max(1, keepdim=True).values
+    x[:, [1, c // 2]] = 0                                 # the largest, equal
+    noise = _gumbel(rng, n, c).to(DEV)
+    x = x.to(DEV)
+    top = (x == 0)
+    first, count = top.int().argmax(1).int(), top.sum(1)
+    t, idx = torch.zeros((n, 2), device=DEV), torch.zeros((n, 2), dtype=torch.int32, device=DEV)
+    idx[:, 0], idx[:, 1] = 1, c // 2
+    for temperature in (1e-39, 2.0 ** -126):
+        v, i, norm = bl.bitlogic_top_logits(x, 3, temperature)
+        assert torch.equal(i[:, 0], first)
+        assert bool(((norm - count.log()).abs() <= REL).all())
+        loss, grad = bl.bitlogic_distill(x, t, idx, None, temperature, 1.0)
+        assert bool(((loss - (count.log() - np.log(2))).abs() <= 3 * REL).all())
+        assert bool((grad[~top] == 0).all())
+        loss, _ = bl.bitlogic_distill(x, t, idx, None, 1.0, temperature, want_grad=False)
+        assert bool(torch.isfinite(loss).all())
+        same, _ = bl.bitlogic_distill(x, t, idx, None, 1.0, 1.0, want_grad=False)
+        assert torch.equal(loss, same)                    # (equal entries at any temperature)
+        if n > 3:
+            continue
+        for p in (1.0, 0.9):
+            for given in (temperature, torch.full((n,), temperature, device=DEV)):
+                token, log_prob = bl.bitlogic_sample(x, noise, given, 0, p)
+                kept = torch.ceil(count * float(np.float32(p)))
+                assert bool(top.gather(1, token.long()[:, None]).all())
+                assert bool(((log_prob + kept.log()).abs() <= 2 * REL).all())
