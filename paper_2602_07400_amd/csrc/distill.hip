@@ -47,7 +47,8 @@ struct DistillArgs {
 // 2^(x log2(e) / T) = e^(x / T).  The factor in two parts: rounded to one, it would put
 // the same relative error on every exponent, 7e-7 on the many classes at e^-10 of the
 // largest, which a sum over them does not average out (one gradient can bear it).
-// The second part is positive, so that -inf stays -inf.
+// The second part is positive, so that -inf stays -inf: the smallest float at least, since
+// hi itself comes down to 4e-39.
 struct Scale {
     float hi, lo;
     __device__ __forceinline__ float left(float inv_t) const
@@ -58,7 +59,7 @@ struct Scale {
     {
         if (!(left(inv_t) > 0.0f))
             hi = __uint_as_float(__float_as_uint(hi) - 1);
-        lo = fmaxf(left(inv_t), 1.1754944e-38f);
+        lo = fmaxf(left(inv_t), 1.4e-45f);
     }
     __device__ __forceinline__ float pow(float x) const
     {

@@ -288,3 +288,15 @@ def test_temperatures_below_the_normal_numbers(c, n):
                 kept = torch.ceil(count * float(np.float32(p)))
                 assert bool(top.gather(1, token.long()[:, None]).all())
                 assert bool(((log_prob + kept.log()).abs() <= 2 * REL).all())
+
+
+def test_distill_at_the_largest_temperatures():
+    """Logits of the size of a temperature of 1e38: differences of the order of one."""
+    rng = _rng(30)
+    for c in (12, 700, 5000):
+        x = torch.from_numpy(rng.uniform(-1.4e38, 1.4e38, (4, c)).astype(np.float32))
+        t, idx = _teacher(rng, 4, c, 5)
+        ln = _norm(t, idx, 1.0, 0.7)
+        got = bl.bitlogic_distill(x.to(DEV), t.to(DEV), idx.to(DEV), ln.to(DEV), 1e38)
+        torch.cuda.synchronize()
+        _check_distill(x, t, idx, ln, 1e38, 1.0, None, (got[0], None))
