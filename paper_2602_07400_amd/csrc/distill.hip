@@ -42,6 +42,18 @@ struct DistillArgs {
     float *loss;                        // [rows] or NULL
     char *grad;                         // or NULL, the logits' type
     int64_t grad_stride;                // bytes
+
+    void skip(int64_t rows)
+    {
+        const auto on = [](auto *&p, int64_t by) { p = p ? p + by : p; };
+        logits += rows * stride;
+        top_values += rows * k * (top_type == kI32 || top_type == kF32 ? 4 : 2);
+        top_indices += rows * k;
+        on(top_log_norm, rows);
+        on(row_weight, rows);
+        on(loss, rows);
+        on(grad, rows * grad_stride);
+    }
 };
 
 // 2^(x log2(e) / T) = e^(x / T).  The factor in two parts: rounded to one, it would put
@@ -499,21 +511,23 @@ hipError_t launch_distill(const void *logits, int32_t type, int64_t n_rows, int3
         if (n <= kLaneClasses && k <= kLaneEntries && n_rows >= kLaneRows) {
             constexpr int kRows = kLaneThreads / kRowLanes;
             const size_t words = (size_t)kRows * (quad_pitch(n) + 3 * k);
-            k_distill_lanes<TYPE><<<(uint32_t)((n_rows + kRows - 1) / kRows), kLaneThreads,
-                                    words * 4, stream>>>(a);
-            return hipGetLastError();
+            return in_launches(a, kLaneThreads, kRows,
+                               [&](const DistillArgs &part, uint32_t blocks) {
+                k_distill_lanes<TYPE><<<blocks, kLaneThreads, words * 4, stream>>>(part);
+            });
         }
         return with_layout<TYPE>(n, k, [&](auto layout) {
             typedef decltype(layout) L;
-            const uint32_t blocks = (uint32_t)((n_rows + L::kGroups - 1) / L::kGroups);
             const size_t lds = (size_t)L::kGroups * k * sizeof(Entry<float>);
-            if constexpr (TYPE != kI32)
-                if (grad) {
-                    k_distill<TYPE, L, true><<<blocks, L::kBlock, lds, stream>>>(a);
-                    return hipGetLastError();
-                }
-            k_distill<TYPE, L, false><<<blocks, L::kBlock, lds, stream>>>(a);
-            return hipGetLastError();
+            return in_launches(a, L::kBlock, L::kGroups,
+                               [&](const DistillArgs &part, uint32_t blocks) {
+                if constexpr (TYPE != kI32)
+                    if (grad) {
+                        k_distill<TYPE, L, true><<<blocks, L::kBlock, lds, stream>>>(part);
+                        return;
+                    }
+                k_distill<TYPE, L, false><<<blocks, L::kBlock, lds, stream>>>(part);
+            });
         });
     });
 }

@@ -952,6 +952,22 @@ hipError_t with_type(int32_t type, F f)
     }
 }
 
+// launch(args, blocks) for all rows: a launch has fewer than 2^32 lanes, so that from 2^24
+// rows of a block of 256 on it takes several.  args.skip(n) moves its pointers n rows on.
+template <class Args, class F>
+hipError_t in_launches(Args a, int block, int rows_a_block, F launch)
+{
+    const int64_t most = (((int64_t)1 << 32) / block - 1) * rows_a_block;
+    hipError_t err = hipSuccess;
+    for (int64_t left = a.n_rows; left > 0 && err == hipSuccess; left -= most) {
+        a.n_rows = left < most ? left : most;
+        launch(a, (uint32_t)((a.n_rows + rows_a_block - 1) / rows_a_block));
+        err = hipGetLastError();
+        a.skip(a.n_rows);
+    }
+    return err;
+}
+
 // ---- a lane a row: many short rows ----
 // A wave takes 64 or 16 rows of up to kLaneClasses classes through a tile in LDS, and a
 // lane or four go through a row: few reductions or none, and what is done once a row is

@@ -44,6 +44,19 @@ struct SampleArgs {
     const int32_t *top_ks;
     int32_t *token;                     // [rows]
     float *log_prob;                    // [rows] or NULL
+
+    void skip(int64_t rows)
+    {
+        const auto on = [](auto *&p, int64_t by) { p = p ? p + by : p; };
+        logits += rows * stride;
+        on(noise, rows * noise_stride);
+        on(temperatures, rows);
+        on(top_ps, rows);
+        on(min_ps, rows);
+        on(top_ks, rows);
+        token += rows;
+        on(log_prob, rows);
+    }
 };
 
 // Lanes whose largest logits bound the list of a top-p without a top-k.
@@ -584,14 +597,15 @@ hipError_t launch_sample(const void *logits, int32_t type, int64_t n_rows, int32
                               sp.top_ps, sp.min_ps, sp.top_ks, token, log_prob};
         return with_layout<TYPE>(n, 0, [&](auto layout) {
             typedef decltype(layout) L;
-            const uint32_t blocks = (uint32_t)((n_rows + L::kGroups - 1) / L::kGroups);
             const bool plain = !a.top_ks && !a.top_ps && !a.min_ps && a.top_p >= 1.0f &&
                                !(a.min_p > 0.0f) && (a.top_k == 0 || a.top_k >= n);
-            if (plain)
-                k_sample<TYPE, L, true><<<blocks, L::kBlock, 0, stream>>>(a);
-            else
-                k_sample<TYPE, L, false><<<blocks, L::kBlock, 0, stream>>>(a);
-            return hipGetLastError();
+            return in_launches(a, L::kBlock, L::kGroups,
+                               [&](const SampleArgs &part, uint32_t blocks) {
+                if (plain)
+                    k_sample<TYPE, L, true><<<blocks, L::kBlock, 0, stream>>>(part);
+                else
+                    k_sample<TYPE, L, false><<<blocks, L::kBlock, 0, stream>>>(part);
+            });
         });
     });
 }

@@ -33,6 +33,18 @@ struct TopArgs {
     float *log_norm;           // [rows] or NULL
 };
 
+template <int TYPE>
+struct TopRows : TopArgs {
+    void skip(int64_t rows)
+    {
+        logits += rows * stride;
+        values += rows * k * Elem<TYPE>::kBytes;
+        indices += rows * k;
+        if (log_norm)
+            log_norm += rows;
+    }
+};
+
 template <int TYPE, class L>
 __global__ __launch_bounds__(L::kBlock, L::G == kWave ? 4 : 8) void k_top(TopArgs a)
 {
@@ -331,9 +343,10 @@ hipError_t launch_top_logits(const void *logits, int32_t type, int64_t n_rows, i
             return launch_lanes<TYPE>(a, stream);
         return with_layout<TYPE>(n, 0, [&](auto layout) {
             typedef decltype(layout) L;
-            k_top<TYPE, L><<<(uint32_t)((n_rows + L::kGroups - 1) / L::kGroups), L::kBlock, 0,
-                             stream>>>(a);
-            return hipGetLastError();
+            return in_launches(TopRows<TYPE>{a}, L::kBlock, L::kGroups,
+                               [&](const TopArgs &part, uint32_t blocks) {
+                k_top<TYPE, L><<<blocks, L::kBlock, 0, stream>>>(part);
+            });
         });
     });
 }

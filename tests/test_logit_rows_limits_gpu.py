@@ -300,3 +300,53 @@ def test_distill_at_the_largest_temperatures():
         got = bl.bitlogic_distill(x.to(DEV), t.to(DEV), idx.to(DEV), ln.to(DEV), 1e38)
         torch.cuda.synchronize()
         _check_distill(x, t, idx, ln, 1e38, 1.0, None, (got[0], None))
+
+
+# ----------------------------------------------------- more rows than one launch
+
+def _windows(n, c, rng):
+    """n rows of c classes that start one element apart."""
+    block = torch.from_numpy(rng.normal(0, 3, 1 << 20).astype(np.float32)).to(DEV)
+    flat = block.repeat((n + c) // (1 << 20) + 1)
+    flat.add_(torch.arange(flat.numel(), device=DEV) % 8191, alpha=2.0 ** -10)
+    return flat[:n + c].as_strided((n, c), (1, 1))
+
+
+def test_rows_past_one_launch():
+    """2^24 rows of a block of 256 lanes are 2^32 lanes, which no launch has."""
+    rng = _rng(33)
+    n, c = (1 << 24) + 3, 1025
+    x, noise = _windows(n, c, rng), _windows(n, c, rng)
+    some = torch.tensor([0, 1, 77, n // 2, *range(n - 262, n)], device=DEV)
+    for a, b in zip(bl.bitlogic_top_logits(x, 2), bl.bitlogic_top_logits(x[some], 2)):
+        assert torch.equal(a[some], b)
+    t = torch.rand((n, 1), device=DEV)
+    idx = (torch.arange(n, device=DEV, dtype=torch.int32) % c)[:, None]
+    norm, weight = t[:, 0] + 0.25, 1 + t[:, 0]
+    loss, _ = bl.bitlogic_distill(x, t, idx, norm, 1.1, row_weight=weight, want_grad=False)
+    few, _ = bl.bitlogic_distill(x[some], t[some], idx[some], norm[some], 1.1,
+                                 row_weight=weight[some], want_grad=False)
+    assert torch.equal(loss[some], few)
+    k = torch.arange(n, device=DEV, dtype=torch.int32) % 60
+    for each in ((0.5 + t[:, 0], k, 0.3 + 0.7 * t[:, 0], 0.1 * t[:, 0]), (0.9, 0, 1.0, 0.0)):
+        of = [v[some] if torch.is_tensor(v) else v for v in each]
+        token, log_prob = bl.bitlogic_sample(x, noise, *each)
+        few = bl.bitlogic_sample(x[some], noise[some], *of)
+        assert torch.equal(token[some], few[0]) and torch.equal(log_prob[some], few[1])
+
+
+def test_short_rows_past_one_launch():
+    """2^30 rows of four lanes each."""
+    n = (1 << 30) + 70
+    x = _windows(n, 2, _rng(34))
+    t = torch.ones((n, 1), device=DEV)
+    idx = torch.zeros((n, 1), dtype=torch.int32, device=DEV)
+    t[n - 64:] = 2
+    idx[n - 70:n - 10] = 1
+    norm = t[:, 0] + 0.25
+    loss, _ = bl.bitlogic_distill(x, t, idx, norm, 1.1, want_grad=False)
+    some = torch.arange(n - 20000, n, device=DEV)
+    few, _ = bl.bitlogic_distill(x[some], t[some], idx[some], norm[some], 1.1, want_grad=False)
+    assert torch.equal(loss[some], few) and torch.equal(
+        loss[:20000], bl.bitlogic_distill(x[:20000], t[:20000], idx[:20000], norm[:20000], 1.1,
+                                          want_grad=False)[0])
