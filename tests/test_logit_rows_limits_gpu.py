@@ -350,3 +350,44 @@ def test_short_rows_past_one_launch():
     assert torch.equal(loss[some], few) and torch.equal(
         loss[:20000], bl.bitlogic_distill(x[:20000], t[:20000], idx[:20000], norm[:20000], 1.1,
                                           want_grad=False)[0])
+
+
+# ------------------------------------------------------------------ long lists
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("c", [10, 16, 17, 64, 65, 128, 129, 512, 513, 1024, 1025, 8193, 70001,
+                               140000])
+def test_distill_long_lists(c, dtype, rest):
+    """Lists of up to 1024 entries, some longer than the row (places left empty)."""
+    rng = _rng(31, c, FLOATS.index(dtype), rest)
+    n = 9 if c <= 1024 else 3
+    z = _logits(rng, n, c, dtype).to(DEV)
+    for k in (257, 820, 1024):
+        t, idx = _teacher(rng, n, c, k, dtype)
+        ln = _norm(t, idx, 1.5, 0.8) if rest and k < c else None
+        weight = torch.from_numpy(rng.uniform(0.2, 2, n).astype(np.float32))
+        args = (z, t.to(DEV), idx.to(DEV), None if ln is None else ln.to(DEV), 2.0, 1.5,
+                weight.to(DEV))
+        got = bl.bitlogic_distill(*args)
+        alone, _ = bl.bitlogic_distill(*args, want_grad=False)
+        torch.cuda.synchronize()
+        _check_distill(z, t, idx, ln, 2.0, 1.5, weight, got)
+        assert torch.equal(alone, got[0])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_distill_autograd_in_every_type(dtype):
+    rng = _rng(32, FLOATS.index(dtype))
+    for c in (10, 100, 3001, 70001):
+        t, idx = _teacher(rng, 5, c, 7, dtype)
+        ln = _norm(t, idx, 1.3, 0.9).to(DEV)
+        z = _logits(rng, 5, c, dtype).to(DEV).requires_grad_()
+        loss = bl.bitlogic_distill_loss(z, t.to(DEV), idx.to(DEV), ln, 1.1, 1.3)
+        weight = torch.from_numpy(rng.uniform(-1, 2, 5).astype(np.float32)).to(DEV)
+        (loss * weight).sum().backward()
+        want, grad = bl.bitlogic_distill(z.detach(), t.to(DEV), idx.to(DEV), ln, 1.1, 1.3, weight)
+        assert z.grad.dtype == dtype and torch.equal(z.grad, grad)
+        assert torch.equal(loss.detach() * weight, want) or bool(
+            ((loss.detach() * weight - want).abs() <= 2.0 ** -22 * want.abs()).all())
+        _check_distill(z.detach(), t, idx, ln.cpu(), 1.1, 1.3, weight, (None, grad))
