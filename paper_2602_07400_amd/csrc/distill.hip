@@ -348,6 +348,13 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
 // classes with k 10, against 74 here and 112 with a group of 32 lanes and the row in
 // registers.)
 constexpr int32_t kLaneEntries = 32;
+// Rows from which on: lanes against groups, float32 with the gradient, k 10, in us:
+//   rows        8192      16384      32768      65536     262144
+//   10 cl.   7.3, 7.2   7.2, 7.0   7.8, 7.5   9.4, 9.7    27, 30
+//   37       7.8, 7.1   7.9, 7.7  8.9, 10.3  12.5, 17.2   34, 56
+//   100     10.1, 8.5  10.7, 11.6 13.2, 19.0 18.7, 33.6   58, 113
+//   128     10.8, 8.8  11.5, 12.2 14.7, 19.6 25.0, 34.8   88, 130
+constexpr int64_t kLaneRows = 16384;
 constexpr int kRowLanes = 4;
 constexpr int kWaveRows = kWave / kRowLanes;
 constexpr int kLaneThreads = 256;

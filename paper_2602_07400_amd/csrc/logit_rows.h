@@ -971,12 +971,9 @@ hipError_t in_launches(Args a, int block, int rows_a_block, F launch)
 // ---- a lane a row: many short rows ----
 // A wave takes 64 or 16 rows of up to kLaneClasses classes through a tile in LDS, and a
 // lane or four go through a row: few reductions or none, and what is done once a row is
-// done for many of them.  It pays once there are rows for all the GPU's waves: top 10 of
-// 100 float32 classes 23 us at 8192 and 16384 rows and 25 at 32768, against 13, 21 and 35
-// with a group of 32 lanes a row; distillation 10, 10.6 and 13 against 8.7, 11.3 and 18.5.
+// done for many of them.  It pays once there are rows for all the GPU's waves: how many is
+// at the kernels' launches.
 constexpr int32_t kLaneClasses = 128;
-constexpr int64_t kLaneRows = 16384;
-
 
 // Orders a wave's LDS accesses: they run in order; the compiler keeps them so.
 __device__ __forceinline__ void wave_sync()

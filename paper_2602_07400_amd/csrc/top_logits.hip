@@ -313,7 +313,6 @@ __global__ __launch_bounds__(kWave) void k_top_lanes(TopArgs a)
     }
 }
 
-// Entries a lane's list has room for.
 template <int TYPE>
 hipError_t launch_lanes(const TopArgs &a, hipStream_t stream)
 {
@@ -327,6 +326,18 @@ hipError_t launch_lanes(const TopArgs &a, hipStream_t stream)
         k_top_lanes<TYPE, 12><<<blocks, kWave, words * 4, stream>>>(a);
     return hipGetLastError();
 }
+
+// Rows that go to lanes: a lane's time grows with a row's classes, a group's with the
+// number of rows.  float32, k 10, lanes against groups in us:
+//   rows       4096       8192      16384      32768      65536     262144
+//   10 cl.   5.6, 8.3   5.6, 8.2   5.4, 8.5  5.9, 10.5  6.2, 16.5  10.6, 49
+//   37      10.7, 9.4  10.7, 9.6  10.8, 11.8 11.7, 18.8 12.0, 31.5  23, 107
+//   100     22.8, 10.4 23.0, 12.8 23.0, 20.3 24.9, 34.4 26.0, 62.4  87, 231
+//   128     27.5, 10.4 27.7, 13.0 27.8, 20.6 30.4, 35.0 31.1, 64.0 133, 236
+// (at 128 x 32768 bfloat16 31, 28).
+constexpr int64_t kLaneRowsAClass = 256;
+// Entries a lane's list has room for.  Lists of 16 and 24 entries, which are not built,
+// take 99 and 121 us at 262144 x 100 float32, groups 234 and 250.
 constexpr int32_t kLaneEntries = 12;
 
 }  // namespace
@@ -339,7 +350,7 @@ hipError_t launch_top_logits(const void *logits, int32_t type, int64_t n_rows, i
         constexpr int TYPE = decltype(ty)::value;
         const TopArgs a = {static_cast<const char *>(logits), row_stride * Elem<TYPE>::kBytes,
                            n_rows, n, k, inv_t, static_cast<char *>(values), indices, log_norm};
-        if (n <= kLaneClasses && k <= kLaneEntries && n_rows >= kLaneRows)
+        if (n <= kLaneClasses && k <= kLaneEntries && n_rows >= kLaneRowsAClass * n)
             return launch_lanes<TYPE>(a, stream);
         return with_layout<TYPE>(n, 0, [&](auto layout) {
             typedef decltype(layout) L;

@@ -391,3 +391,26 @@ def test_distill_autograd_in_every_type(dtype):
         assert torch.equal(loss.detach() * weight, want) or bool(
             ((loss.detach() * weight - want).abs() <= 2.0 ** -22 * want.abs()).all())
         _check_distill(z.detach(), t, idx, ln.cpu(), 1.1, 1.3, weight, (None, grad))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("c", [10, 100, 127, 128])
+def test_top_lists_by_lanes(c, dtype):
+    """Enough rows that a lane takes one, 256 a class, and one row less: the same lists."""
+    rng = _rng(35, c, TYPES.index(dtype))
+    n = 256 * c
+    x = _logits(rng, n, c, dtype)
+    low = torch.iinfo(dtype).min if dtype == torch.int32 else -np.inf
+    x[3] = low
+    x[4, 1:] = low
+    x[5] = 7
+    x[n - 1, ::2] = low
+    x = x.to(DEV)
+    some = np.r_[0:60, n - 30:n]
+    for k in (1, 5, 8, 12):
+        v, i, norm = bl.bitlogic_top_logits(x, k, 1.5)
+        few = bl.bitlogic_top_logits(x[1:], k, 1.5)
+        assert torch.equal(v[1:], few[0]) and torch.equal(i[1:], few[1])
+        d = (norm[1:] - few[2]).abs()
+        assert bool(((d <= 2 * REL + 2.0 ** -21 * few[2].abs()) | (norm[1:] == few[2])).all())
+        _check_top(x[some], k, 1.5)
