@@ -14,9 +14,9 @@
 // that of the list and q_r = 0.
 //
 // What bounds it: HBM with the gradient, 4096 x 65536 bf16, k 64: 215 us, 5.0 TB/s of
-// the 5.8 of a plain copy (an eighth of the rows has weight 0 and is written only); the
-// loss alone, its exponentials and the list in front of each row, 4099 x 32003 bf16: 65
-// us (92 with 1024 lanes that keep the row).
+// the 5.8 of a plain copy, the VALU active in 75 of 100 cycles (an eighth of the rows has
+// weight 0 and is written only); the loss alone, its exponentials (66 of 100) and the list
+// in front of each row, 4099 x 32003 bf16: 65 us (92 with 1024 lanes that keep the row).
 //
 // The row is loaded once and stays in registers; the running maximum and sum of the
 // softmax are taken as it arrives.  The list lies in LDS, linked per owning lane: a
@@ -325,6 +325,8 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
         const uint32_t marked = mark[g.t];
         row.each([&](auto j, int32_t i, const P &p) {
             float v[L::VEC];
+            // (the factor's first part: at most 2.5 |z - from| / T 2^-24 of the gradient, of
+            // which the rounding of 1 / T is one)
 #pragma unroll
             for (int u = 0; u < L::VEC; ++u)
                 v[u] = outside * __builtin_amdgcn_exp2f((p.get(u) - from_out) * c.hi);
@@ -345,8 +347,9 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
 // for their entries before it is summed, the exponentials take the logits' places in it,
 // then the gradients theirs.  (A lane a row has a quarter of the waves, and their chains
 // of LDS accesses take four times as long: 148 us for 262144 rows of 100 float32
-// classes with k 10, against 74 here and 112 with a group of 32 lanes and the row in
-// registers.)
+// classes with k 10, against 75 here and 112 with a group of 32 lanes and the row in
+// registers.  Here the VALU is active in 65 of 100 cycles, the LDS in 19, at 12 waves a
+// CU, which the tiles' LDS allows.)
 constexpr int32_t kLaneEntries = 32;
 // Rows from which on: lanes against groups, float32 with the gradient, k 10, in us:
 //   rows        8192      16384      32768      65536     262144

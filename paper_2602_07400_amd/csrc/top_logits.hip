@@ -11,8 +11,8 @@
 // (key, class) are unique, so the order in which the list fills does not matter.
 //
 // What bounds it: long rows, the exponentials and unpacking (about 9 instructions an
-// element) beside the read: 2048 x 131072 bf16, k 64, 105 us, 5.1 TB/s of the 7.0 that
-// a plain read reaches (161 with the row kept in registers and one block a CU, 646 with
+// element; the VALU is active in 76 of 100 cycles) beside the read: 2048 x 131072 bf16,
+// k 64, 105 us, 5.1 TB/s of the 7.0 that a plain read reaches (161 with the row kept in registers and one block a CU, 646 with
 // bisection over the row); single rows, the block's chain of barriers: 1 x 50021
 // float32, k 256, 21 us; many short rows, see k_top_lanes.
 #include "logit_rows.h"
@@ -228,8 +228,9 @@ __device__ __forceinline__ double min_of(double a, double b)
 // A lane a row, k <= K: every class is carried down a sorted list in registers.  Class
 // and key are the mantissa of a double (52 bits: 32 of key, then the class reversed), so
 // that a step of the list is one maximum and one minimum.  262144 x 100 int32, k 10: 92
-// us (216 with a group of 32 lanes a row and bisection), 24 of some 40 instructions a
-// class in the list.
+// us (216 with a group of 32 lanes a row and bisection).  What bounds it is how few waves
+// there are to take turns: 26 KB of LDS each leave a CU 4.3 of them on average, and the
+// VALU is active in 40 of 100 cycles (24 of some 40 instructions a class in the list).
 template <int TYPE, int K>
 __global__ __launch_bounds__(kWave) void k_top_lanes(TopArgs a)
 {
