@@ -739,7 +739,7 @@ __device__ __forceinline__ Range<Sum> narrow(Group<L::G> &g, R &row,
         Sum before = in.before + g.scan(part, total), here = 0, base = 0;
         uint32_t found = 0;
         for (uint32_t b = 0; b < kRun; ++b) {
-            const Sum own = sum_of(g.t * kRun + b);
+            const Sum own = kMass ? part : sum_of(g.t * kRun + b);
             if (before < goal && before + own >= goal) {
                 found = g.t * kRun + b + 1;
                 base = before;
@@ -748,14 +748,23 @@ __device__ __forceinline__ Range<Sum> narrow(Group<L::G> &g, R &row,
             before += own;
         }
         if constexpr (kMass) {
-            found = g.reduce(found, Max());
-            base = g.reduce(base, Max());
+            // the lane that has it tells the others through the bins, which all have read
+            static_assert(kRun == 1 && kBins >= 3, "an interval a lane");
+            if (found) {
+                bins[0] = found;
+                bins[1] = base;
+                bins[2] = here;
+            }
+            g.barrier();
+            found = in.before + total >= goal ? (uint32_t)bins[0] : 0;
+            base = bins[1];
+            here = bins[2];
         } else {
             const uint64_t won = g.reduce((uint64_t)found << 32 | base, Max());
             found = (uint32_t)(won >> 32);
             base = (uint32_t)won;
+            here = g.reduce(here, Max());
         }
-        here = g.reduce(here, Max());
         if (!found) {
             in = {in.lo, in.lo + 1, kMass ? in.before + total : goal, 0};
             break;
