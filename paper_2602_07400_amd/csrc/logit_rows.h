@@ -669,8 +669,9 @@ constexpr Mass kUnknown = ~0ull;
 // costs registers: top 64 of 2048 x 131072 in bfloat16 125 us instead of 105).
 // kCopies interleaved counters an interval, one for every eighth or fourth lane: many
 // elements fall in few intervals (16-bit logits near -10 have 16 values a unit), and equal
-// addresses take turns.  bins: kBins * kCopies sums, in the memory of the list (masses by 2,
-// 4, 8 and 16 copies, draws from 256 x 131072: 97, 98, 105 and 112 us).
+// addresses take turns.  bins: kBins * kCopies sums, in the memory of the list.  Masses by 8
+// copies, and by 4 with twice the intervals: draws from 256 x 131072 (1024 lanes a row) 89.7
+// and 91.5 us, from 108418 x 1051 (256 lanes) 1904 and 1846.
 template <int TYPE, class L, class Sum, class R, class W>
 __device__ __forceinline__ Range<Sum> narrow(Group<L::G> &g, R &row,
                                              const typename Elem<TYPE>::Cmp (&most)[L::NV],
@@ -680,7 +681,7 @@ __device__ __forceinline__ Range<Sum> narrow(Group<L::G> &g, R &row,
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
     constexpr bool kMass = sizeof(Sum) == 8;
-    constexpr uint32_t kCopies = kMass ? 4 : 8;
+    constexpr uint32_t kCopies = kMass && L::G == 256 ? 4 : 8;
     constexpr uint32_t kBins = L::kList * sizeof(uint64_t) / sizeof(Sum) / kCopies;
     constexpr uint32_t kRun = kBins > (uint32_t)L::G ? kBins / L::G : 1;
     const uint32_t copy = g.t % kCopies;
