@@ -475,8 +475,9 @@ int bitlogic_top_logits(const void *logits, int32_t type, int64_t n_rows, int32_
  * grad may not overlap logits.  The loss alone is the forward pass; the gradient
  * alone, with row_weight the gradient of a sum over the losses, the backward pass;
  * both together read the logits once.  A row of weight 0 is not read and gets zeros,
- * a row whose list is empty loss and gradient 0; a row whose logits are all -inf,
- * or that holds a NaN, NaNs.  Masked classes outside J get gradient 0. */
+ * a row whose list is empty (or holds masked values alone) loss and gradient 0; a row
+ * whose logits are all -inf, or that holds a NaN, NaNs.  Masked classes outside J get
+ * gradient 0. */
 int bitlogic_distill(const void *logits, int32_t type, int64_t n_rows, int32_t n_classes,
                      int64_t row_stride, float temperature, const void *top_values,
                      int32_t top_type, const int32_t *top_indices, int32_t k,

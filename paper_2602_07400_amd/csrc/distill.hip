@@ -146,6 +146,8 @@ __device__ __forceinline__ float load_teacher(const DistillArgs &a, int64_t i)
     return a.top_type == kI32 ? __int_as_float(load_one<kI32>(a.top_values, i))
                               : load_float(a.top_values, a.top_type, i) * a.inv_top_t;
 }
+// a maximum to take differences from: 0 where there is none
+__device__ __forceinline__ float finite(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 // t / Tt, less first / Tt where it is an int32 (first: the largest)
 __device__ __forceinline__ float teacher(const DistillArgs &a, float t, int32_t first)
 {
@@ -227,11 +229,12 @@ __global__ __launch_bounds__(L::kBlock, GRAD ? L::kWavesPerSimd : 8) void k_dist
             else
                 for (int e = h.t; e < a.k; e += H)
                     tm = fmaxf(tm, list[e].t);            // (-inf where there is none)
-            tm = h.reduce(tm, Max());
+            tm = finite(h.reduce(tm, Max()));
             for (int e = h.t; e < a.k; e += H)
                 if (list[e].cls >= 0)
                     sum += expf(teacher(a, list[e].t, first) - tm);
-            log_norm = tm + logf(h.reduce(sum, Add()));
+            sum = h.reduce(sum, Add());
+            log_norm = sum == 0.0f ? 0.0f : tm + logf(sum);    // (0: no class, or masked ones)
         }
         Softmax<TYPE> listed;
         for (int e = h.t; e < a.k; e += H)
@@ -422,20 +425,21 @@ __global__ __launch_bounds__(kLaneThreads) void k_distill_lanes(DistillArgs a)
             for (int i = g.t; i < a.n; i += kRowLanes)
                 m = Max()(m, scores[i]);
             m = g.reduce(m, Max());
-            const auto finite = [](Cmp v) { return TYPE != kI32 && v == E::lowest() ? 0 : v; };
-            const Cmp from_out = finite(m);
+            const auto start = [](Cmp v) { return TYPE != kI32 && v == E::lowest() ? 0 : v; };
+            const Cmp from_out = start(m);
             const float share = m >= m_list ? 1.0f : c.pow(E::minus(m, m_list));
             m = Max()(m, m_list);
-            const Cmp from = finite(m);
+            const Cmp from = start(m);
             float log_norm;
             if (a.top_log_norm) {
                 log_norm = given_norm(a, r, first);
             } else {
-                tm = g.reduce(tm, Max());
+                tm = finite(g.reduce(tm, Max()));
                 float sum = 0.0f;
                 for (int e = g.t; e < a.k; e += kRowLanes)
                     sum += cls[e] >= 0 ? expf(teacher(a, top[e], first) - tm) : 0.0f;
-                log_norm = tm + logf(g.reduce(sum, Add()));
+                sum = g.reduce(sum, Add());
+                log_norm = sum == 0.0f ? 0.0f : tm + logf(sum);    // (0: no class, or masked ones)
             }
             float Q = 0.0f, s_list = 0.0f, s_out = 0.0f;
             for (int e = g.t; e < a.k; e += kRowLanes)

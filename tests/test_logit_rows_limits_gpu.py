@@ -414,3 +414,26 @@ def test_top_lists_by_lanes(c, dtype):
         d = (norm[1:] - few[2]).abs()
         assert bool(((d <= 2 * REL + 2.0 ** -21 * few[2].abs()) | (norm[1:] == few[2])).all())
         _check_top(x[some], k, 1.5)
+
+
+@pytest.mark.parametrize("top_type", TYPES)
+@pytest.mark.parametrize("c,n", [(12, 5), (100, 17003), (700, 5), (9000, 5)])
+def test_distill_lists_of_masked_values(c, n, top_type):
+    """A list whose values are all masked is an empty one; masked values beside others have
+    no mass."""
+    rng = _rng(36, c, TYPES.index(top_type))
+    z = _logits(rng, n, c, torch.float32).to(DEV)
+    t, idx = _teacher(rng, n, c, 6, top_type)
+    low = torch.iinfo(torch.int32).min if top_type == torch.int32 else -np.inf
+    t[0] = low
+    t[1, 2:] = low
+    tt = 20.0 if top_type == torch.int32 else 1.0
+    loss, grad = bl.bitlogic_distill(z, t.to(DEV), idx.to(DEV), None, 1.5, tt)
+    assert float(loss[0]) == 0 and bool((grad[0] == 0).all())
+    empty = idx.clone()
+    empty[1, 2:] = -1
+    want = bl.bitlogic_distill(z, t.to(DEV), empty.to(DEV), None, 1.5, tt)
+    assert abs(float(loss[1] - want[0][1])) <= 3 * REL * (1 + abs(float(want[0][1])))
+    # (the gradient of a class that is listed with no mass is p, as of one that is not)
+    assert bool(((grad[1] - want[1][1]).abs() <= 3 * REL * want[1][1].abs() + 1e-37).all())
+    _check_distill(z[2:5].cpu(), t[2:5], idx[2:5], None, 1.5, tt, None, (loss[2:5], grad[2:5]))
