@@ -828,7 +828,7 @@ def bitlogic_sample(logits: torch.Tensor, noise: Optional[torch.Tensor] = None,
     if isinstance(top_k, torch.Tensor):
         sp.top_ks = _like(top_k, "top_k", _I32, (n,), dev)
     else:
-        sp.top_k = top_k
+        sp.top_k = min(top_k, c)          # (the same set, and 32 bits)
     if isinstance(top_p, torch.Tensor):
         sp.top_ps = _like(top_p, "top_p", _F32, (n,), dev)
     else:

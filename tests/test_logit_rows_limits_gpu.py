@@ -437,3 +437,14 @@ def test_distill_lists_of_masked_values(c, n, top_type):
     # (the gradient of a class that is listed with no mass is p, as of one that is not)
     assert bool(((grad[1] - want[1][1]).abs() <= 3 * REL * want[1][1].abs() + 1e-37).all())
     _check_distill(z[2:5].cpu(), t[2:5], idx[2:5], None, 1.5, tt, None, (loss[2:5], grad[2:5]))
+
+
+def test_sample_top_k_past_32_bits():
+    rng = _rng(37)
+    x, noise = _logits(rng, 4, 50, torch.float32).to(DEV), _gumbel(rng, 4, 50).to(DEV)
+    want = bl.bitlogic_sample(x, noise, 2.0)
+    for k in (51, 2 ** 31, 2 ** 32 + 1):
+        got = bl.bitlogic_sample(x, noise, 2.0, k)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with pytest.raises(Exception, match="top_k"):
+        bl.bitlogic_sample(x, noise, 2.0, -1)
