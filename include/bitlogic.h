@@ -521,6 +521,77 @@ int bitlogic_sample(const void *logits, int32_t type, int64_t n_rows, int32_t n_
                     const bitlogic_sampling *sampling, int32_t *token, float *log_prob,
                     void *stream);
 
+/* Verification of drafted classes: a small network draws up to n_drafted classes a
+ * request one after another (bitlogic_sample), a target scores them all at once, and the
+ * classes that stand are distributed as if the target had drawn them.  Request s has the
+ * target's rows l_0 .. l_D (D = n_drafted) and the drafter's rows d_0 .. d_{D-1}; row i
+ * belongs to the draft t_i = drafted[s][i].  With p_i = softmax(l_i / T) and
+ * q_i = softmax(d_i / T_draft), for i = 0, 1, ... below lengths[s]:
+ *   t_i is accepted if uniform[s][i] < p_i(t_i) / q_i(t_i), else the walk ends.
+ * Where it ended at j by a rejection, the next class is drawn from max(0, p_j - q_j),
+ * after lengths[s] accepted drafts from p_j, j = lengths[s]: the class with the largest
+ * log(its mass) + noise[s][i], the lowest one of equals.  uniform: independent numbers in
+ * [0, 1); noise: standard Gumbel numbers, as for bitlogic_sample.  Both decisions are those
+ * of 64-bit arithmetic: where 32 bits leave one open it is taken again.
+ *   logits        target rows of `type`, row_stride elements from row to row of a request
+ *                 and request_stride from request to request (both >= 0)
+ *   draft_logits  drafter's rows of draft_type with their own strides, or NULL: drafts
+ *                 without probabilities (a table's), q_i is one at t_i
+ *   drafted       int32 [n_requests][n_drafted]; a class outside [0, n_classes) is rejected
+ *   lengths       int32 [n_requests], clamped to [0, n_drafted], or NULL: n_drafted each.
+ *                 Rows behind a request's last one are not read
+ *   temperature, draft_temperature  of all requests or, where the array [n_requests]
+ *                 (device memory) is not NULL, of each.  T <= 0: greedy, p_i is one at the
+ *                 first class of the row's order, and uniform and noise are not read;
+ *                 T_draft <= 0: q_i is one at t_i, and the draft's row is not read
+ *   accepted      int32 [n_requests]: drafts that stand
+ *   token         int32 [n_requests]: the class after them; -1 where the target's row is
+ *                 masked altogether
+ *   log_prob      float [n_requests] or NULL: log p_j(token) (0 where greedy, -inf for -1)
+ * Masked classes and NaNs have no mass on either side; +inf takes all of it.  Where no class
+ * has p_j > q_j the draw is from p_j, and where no number in question is above -inf the
+ * token is the first class of the row's order.  Limits as above; n_drafted >= 0,
+ * n_requests * (n_drafted + 1) < 2^31; at n_drafted = 0 drafted, uniform and draft_logits
+ * may be NULL.  The workspace (8-byte aligned) may hold anything, before and after. */
+typedef struct bitlogic_drafts {
+    const int32_t *drafted;
+    const int32_t *lengths;
+    const void *draft_logits;
+    int32_t draft_type;
+    int32_t n_drafted;
+    int64_t draft_row_stride, draft_request_stride;
+    const float *uniform;                     /* [n_requests][n_drafted]                  */
+    float temperature, draft_temperature;
+    const float *temperatures;                /* [n_requests] or NULL                     */
+    const float *draft_temperatures;          /* [n_requests] or NULL                     */
+} bitlogic_drafts;
+
+size_t bitlogic_verify_workspace_bytes(int64_t n_requests, int32_t n_drafted,
+                                       int32_t n_classes);
+int bitlogic_verify(const void *logits, int32_t type, int64_t n_requests, int32_t n_classes,
+                    int64_t row_stride, int64_t request_stride, const bitlogic_drafts *drafts,
+                    const float *noise, int64_t noise_stride, int32_t *accepted,
+                    int32_t *token, float *log_prob, void *workspace, size_t workspace_bytes,
+                    void *stream);
+
+/* Dropout of rows of any of the types, with a mask that is never stored: element (s, i) is
+ * kept if its number is at least round(p 2^16) and then multiplied by
+ * 2^16 / (2^16 - round(p 2^16)) in 32 bits and rounded once; the others become 0, whatever
+ * they are.  The numbers are the 16-bit halves, low ones first, of the four words of Philox
+ * 4x32 with ten rounds (Salmon et al. 2011) at the key (low, high word of seed) and the
+ * counter (i / 8, s, low, high word of the offset): the same call on the gradient is the
+ * backward pass, and rows are numbered from 0 in every call.  Calls whose masks have to
+ * differ take different offsets (a step's number and a layer's, say).
+ *   offset_at  NULL, or device memory (8-byte aligned) whose value is added to `offset`
+ *              when the kernel runs: a captured graph draws a new mask at every replay
+ *              after whose end the caller raises it
+ *   out        of `type` (int32 counts: float), out_stride >= n_cols elements from row to
+ *              row; x itself with its own stride, or a range of memory apart from x's
+ * Limits as above with n_cols for n_classes; 0 <= p <= 1 (1 drops everything). */
+int bitlogic_dropout(const void *x, int32_t type, int64_t n_rows, int32_t n_cols,
+                     int64_t row_stride, float p, uint64_t seed, uint64_t offset,
+                     const uint64_t *offset_at, void *out, int64_t out_stride, void *stream);
+
 /* ---- Peak probes (measurement, not part of the inference path) ---------- */
 
 /* Integer VALU probe: `blocks` blocks of 256 lanes.  Lane l (global index)
@@ -620,8 +691,9 @@ const char *bitlogic_last_error(void);
  * instruction-rate and gather probes; 0.7.0 bitlogic_forward_info.jump_layers
  * and the node-per-wave layer kernel, whose per-node records enlarge the
  * forward workspace of networks that use it; 0.8.0 bitlogic_network_path; 0.9.0
- * bitlogic_top_logits, bitlogic_distill and bitlogic_sample). */
-#define BITLOGIC_VERSION 900
+ * bitlogic_top_logits, bitlogic_distill and bitlogic_sample; 0.10.0 bitlogic_verify
+and bitlogic_dropout). */
+#define BITLOGIC_VERSION 1000
 int bitlogic_version(void);
 
 #ifdef __cplusplus

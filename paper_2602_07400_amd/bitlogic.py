@@ -27,6 +27,7 @@ __all__ = [
     "bitlogic_network_forward_noalloc", "NOALLOC_SCRATCH_BYTES",
     "bitlogic_groupsum_head_workspace_bytes", "bitlogic_status_string", "bitlogic_version",
     "bitlogic_top_logits", "bitlogic_distill", "bitlogic_distill_loss", "bitlogic_sample",
+    "bitlogic_verify", "bitlogic_dropout",
     "BitlogicModel", "bitlogic_specialize_layer", "bitlogic_specialize_network", "library_path",
     "load_library", "words",
 ]
@@ -74,6 +75,15 @@ class _Sampling(ctypes.Structure):
                 ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p)]
 
 
+class _Drafts(ctypes.Structure):
+    _fields_ = [("drafted", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("draft_logits", ctypes.c_void_p), ("draft_type", ctypes.c_int32),
+                ("n_drafted", ctypes.c_int32), ("draft_row_stride", ctypes.c_int64),
+                ("draft_request_stride", ctypes.c_int64), ("uniform", ctypes.c_void_p),
+                ("temperature", ctypes.c_float), ("draft_temperature", ctypes.c_float),
+                ("temperatures", ctypes.c_void_p), ("draft_temperatures", ctypes.c_void_p)]
+
+
 _PATHS = ("slab", "columns", "block")      # BITLOGIC_PATH_*
 MAX_FANIN = 6
 SPECIALIZE_PASS = 32          # nodes per entry of a specialized layer's fan-in array
@@ -94,7 +104,7 @@ def load_library():
             "(hipcc --offload-arch=gfx950); there is no fallback path")
     lib = ctypes.CDLL(_LIB_PATH)
     P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-    f32 = ctypes.c_float
+    f32, u64 = ctypes.c_float, ctypes.c_uint64
     sig = {
         "bitlogic_encode": ([P, i64, i32, P, i32, P, P], ctypes.c_int),
         "bitlogic_lut_layer": ([P, i32, i64, P, P, i32, i32, P, P], ctypes.c_int),
@@ -123,6 +133,10 @@ def load_library():
         "bitlogic_distill": ([P, i32, i64, i32, i64, f32, P, i32, P, i32, P, f32, P, P, P, i64,
                               P], ctypes.c_int),
         "bitlogic_sample": ([P, i32, i64, i32, i64, P, i64, P, P, P, P], ctypes.c_int),
+        "bitlogic_verify_workspace_bytes": ([i64, i32, i32], sz),
+        "bitlogic_verify": ([P, i32, i64, i32, i64, i64, P, P, i64, P, P, P, P, sz, P],
+                            ctypes.c_int),
+        "bitlogic_dropout": ([P, i32, i64, i32, i64, f32, u64, u64, P, P, i64, P], ctypes.c_int),
         "bitlogic_probe_valu": ([P, i32, i32, ctypes.c_uint32, P], ctypes.c_int),
         "bitlogic_probe_hbm": ([i32, P, P, i64, i32, i32, P], ctypes.c_int),
         "bitlogic_probe_valu_op": ([i32, P, i32, i32, ctypes.c_uint32, P], ctypes.c_int),
@@ -852,6 +866,147 @@ def bitlogic_sample(logits: torch.Tensor, noise: Optional[torch.Tensor] = None,
         _like(log_prob, "log_prob", _F32, (n,), dev) if log_prob is not None else None,
         _stream(stream, dev)))
     return token, log_prob
+
+
+def _call(device, f, *args) -> None:
+    """A call whose launches belong to `device`, which need not be the current one."""
+    if device.index == torch.cuda.current_device():
+        _check(f(*args))
+    else:
+        with torch.cuda.device(device):
+            _check(f(*args))
+
+
+def _rows3(t: torch.Tensor, name: str, shape, device) -> Tuple[int, int, int]:
+    """Address, row and request stride of a tensor [requests][rows][classes] on the GPU
+    whose rows are contiguous; shape: what it must have, None where any size will do."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    if t.dtype not in _LOGITS:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {tuple(_LOGITS)}")
+    if t.dim() != 3 or any(want not in (None, got) for want, got in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return (t.data_ptr(), t.stride(1) if t.shape[1] > 1 else t.shape[2],
+            t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
+
+
+def bitlogic_verify(logits: torch.Tensor, drafted: torch.Tensor,
+                    draft_logits: Optional[torch.Tensor], uniform: torch.Tensor,
+                    noise: Optional[torch.Tensor], lengths: Optional[torch.Tensor] = None,
+                    temperature=1.0, draft_temperature=None,
+                    accepted: Optional[torch.Tensor] = None,
+                    token: Optional[torch.Tensor] = None,
+                    log_prob: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None,
+                    want_log_prob: bool = True):
+    """Drafted classes int32 [R][D] against a target's logits [R][D+1][c], with the drafter's
+    logits [R][D][c] (None: drafts without probabilities), uniform numbers float32 [R][D] and
+    Gumbel numbers float32 [R][c] (None only if every request is greedy): (accepted int32 [R],
+    the class after the accepted ones int32 [R], its log-probability float32 [R] or None).
+    lengths int32 [R]: drafts of each request (None: D).  temperature (0: greedy) and
+    draft_temperature (None: temperature) are numbers or float32 tensors [R].  Logits are of
+    any row type each, with strides of their own from row to row and request to request."""
+    ptr, row_stride, request_stride = _rows3(logits, "logits", (None, None, None), None)
+    n, c, dev = logits.shape[0], logits.shape[2], logits.device
+    d = logits.shape[1] - 1
+    if d < 0:
+        raise ValueError("logits must hold a row more than there are drafts")
+    dr = _Drafts(n_drafted=d, temperature=1.0, draft_temperature=1.0)
+    if d > 0:
+        dr.drafted = _like(drafted, "drafted", _I32, (n, d), dev)
+        dr.uniform = _like(uniform, "uniform", _F32, (n, d), dev)
+        if draft_logits is not None:
+            dr.draft_logits, dr.draft_row_stride, dr.draft_request_stride = _rows3(
+                draft_logits, "draft_logits", (n, d, c), dev)
+            dr.draft_type = _LOGITS[draft_logits.dtype]
+    if lengths is not None:
+        dr.lengths = _like(lengths, "lengths", _I32, (n,), dev)
+    if draft_temperature is None:
+        draft_temperature = temperature
+    if isinstance(temperature, torch.Tensor):
+        dr.temperatures = _like(temperature, "temperature", _F32, (n,), dev)
+    else:
+        dr.temperature = temperature
+    if isinstance(draft_temperature, torch.Tensor):
+        dr.draft_temperatures = _like(draft_temperature, "draft_temperature", _F32, (n,), dev)
+    else:
+        dr.draft_temperature = draft_temperature
+    noise_ptr, noise_stride = None, 0
+    if noise is not None:
+        noise_ptr, noise_stride = _rows(noise, "noise", _F32)
+        if tuple(noise.shape) != (n, c) or noise.device != dev:
+            raise ValueError(f"noise must be [{n}][{c}] on {dev}")
+    if accepted is None:
+        accepted = _empty((n,), torch.int32, dev, stream)
+    if token is None:
+        token = _empty((n,), torch.int32, dev, stream)
+    if log_prob is None and want_log_prob:
+        log_prob = _empty((n,), torch.float32, dev, stream)
+    lib = load_library()
+    ws_ptr, ws_bytes = _workspace(int(lib.bitlogic_verify_workspace_bytes(n, d, c)), dev,
+                                  workspace, stream)
+    _call(dev, lib.bitlogic_verify,
+          ptr, _LOGITS[logits.dtype], n, c, row_stride, request_stride, ctypes.addressof(dr),
+          noise_ptr, noise_stride, _like(accepted, "accepted", _I32, (n,), dev),
+          _like(token, "token", _I32, (n,), dev),
+          _like(log_prob, "log_prob", _F32, (n,), dev) if log_prob is not None else None,
+          ws_ptr, ws_bytes, _stream(stream, dev))
+    return accepted, token, log_prob
+
+
+def _dropout(x, p, seed, offset, out, stream):
+    ptr, stride = _rows(x, "x")
+    n, c = x.shape
+    dev = x.device
+    dtype = torch.float32 if x.dtype == torch.int32 else x.dtype
+    if out is None:
+        out = _empty((n, c), dtype, dev, stream)
+    out_ptr, out_stride = _rows(out, "out", (dtype,))
+    if out.shape != x.shape or out.device != dev:
+        raise ValueError("out must have x's shape and device")
+    number, at = offset, None
+    if isinstance(offset, torch.Tensor):
+        number, at = 0, _like(offset, "offset", (torch.int64,), (1,), dev)
+    if not 0 <= seed < 1 << 64 or not 0 <= number < 1 << 64:
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    _call(dev, load_library().bitlogic_dropout, ptr, _LOGITS[x.dtype], n, c, stride, p, seed,
+          number, at, out_ptr, out_stride, _stream(stream, dev))
+    return out
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, offset):
+        ctx.mask = p, seed
+        ctx.offset = offset
+        if isinstance(offset, torch.Tensor):      # saved: raised before the backward pass,
+            ctx.save_for_backward(offset)         # it would give another mask
+        return _dropout(x, p, seed, offset, None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        offset = ctx.saved_tensors[0] if ctx.saved_tensors else ctx.offset
+        return _dropout(grad.contiguous(), *ctx.mask, offset, None, None), None, None, None
+
+
+def bitlogic_dropout(x: torch.Tensor, p: float, seed: int, offset=0,
+                     out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Dropout of rows x [N][c] (float32, float16, bfloat16, or int32 counts, which become
+    float32; rows may be strided) with probability p, by a mask that (seed, offset) alone
+    decide and that is never stored.  offset is a number or an int64 tensor [1] on the GPU,
+    which a captured graph reads at every replay.  Differentiable in a float x where neither
+    out (which may be x) nor stream is given; both passes run on the current stream."""
+    if out is None and stream is None and isinstance(x, torch.Tensor) and x.requires_grad \
+            and torch.is_grad_enabled():
+        return _Dropout.apply(x, p, seed, offset)
+    return _dropout(x, p, seed, offset, out, stream)
 
 
 # ---------------------------------------------------------------- peak probes

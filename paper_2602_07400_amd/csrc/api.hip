@@ -2,6 +2,7 @@
 // carving, launches.  Every check runs before any HIP runtime call, so a
 // rejected call enqueues nothing (and needs no GPU to be rejected).
 #include <float.h>
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -109,6 +110,7 @@ int check_head(const uint64_t *bits, int32_t w, int64_t n, int32_t c, const int3
 
 // Rows of class scores or logits: type, sizes and stride.
 constexpr int64_t kMaxStride = 1 << 30;
+constexpr int64_t kMaxRequestStride = (int64_t)1 << 40;
 
 size_t logit_bytes(int32_t type)
 {
@@ -126,6 +128,17 @@ int check_rows(const char *who, int32_t type, int64_t n_rows, int32_t n_classes,
     if (row_stride < 0 || row_stride > kMaxStride)
         return fail(BITLOGIC_ERR_SHAPE, "%s: need 0 <= row_stride <= 2^30", who);
     return BITLOGIC_OK;
+}
+
+// Bytes from a buffer's first element to behind its last one.
+size_t span_bytes(int64_t n_rows, int64_t n_cols, int64_t stride, int32_t type)
+{
+    return (size_t)((n_rows - 1) * stride + n_cols) * logit_bytes(type);
+}
+
+bool overlaps(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
 
 int check_list(const char *who, int32_t k, float temperature)
@@ -1030,6 +1043,104 @@ int bitlogic_sample(const void *logits, int32_t type, int64_t n_rows, int32_t n_
     return hip_status(bl::launch_sample(logits, type, n_rows, n_classes, row_stride, noise,
                                         noise_stride, sp, token, log_prob, (hipStream_t)stream),
                       "sample launch");
+}
+
+size_t bitlogic_verify_workspace_bytes(int64_t n_requests, int32_t n_drafted,
+                                       int32_t n_classes)
+{
+    if (n_requests < 0 || n_drafted < 0 || n_requests > kMaxRows / ((int64_t)n_drafted + 1) ||
+        n_classes < 1 || n_classes > bl::rows::kMaxClasses)
+        return 0;
+    return bl::verify_workspace_bytes(n_requests, n_drafted, n_classes);
+}
+
+int bitlogic_verify(const void *logits, int32_t type, int64_t n_requests, int32_t n_classes,
+                    int64_t row_stride, int64_t request_stride, const bitlogic_drafts *drafts,
+                    const float *noise, int64_t noise_stride, int32_t *accepted,
+                    int32_t *token, float *log_prob, void *workspace, size_t workspace_bytes,
+                    void *stream)
+{
+    if (int rc = check_rows("verify", type, n_requests, n_classes, row_stride))
+        return rc;
+    if (!drafts)
+        return fail(BITLOGIC_ERR_NULL, "verify: NULL drafts");
+    const bitlogic_drafts &d = *drafts;
+    if (d.n_drafted < 0 || n_requests > kMaxRows / ((int64_t)d.n_drafted + 1))
+        return fail(BITLOGIC_ERR_SHAPE, "verify: need n_drafted >= 0, n_requests * "
+                    "(n_drafted + 1) < 2^31");
+    if (request_stride < 0 || request_stride > kMaxRequestStride)
+        return fail(BITLOGIC_ERR_SHAPE, "verify: need 0 <= request_stride <= 2^40");
+    if (d.draft_logits) {
+        if (int rc = check_rows("verify", d.draft_type, n_requests, n_classes,
+                                d.draft_row_stride))
+            return rc;
+        if (d.draft_request_stride < 0 || d.draft_request_stride > kMaxRequestStride)
+            return fail(BITLOGIC_ERR_SHAPE, "verify: need 0 <= draft_request_stride <= 2^40");
+    }
+    if (noise_stride < 0 || noise_stride > kMaxStride)
+        return fail(BITLOGIC_ERR_SHAPE, "verify: need 0 <= noise_stride <= 2^30");
+    if (!d.temperatures && !(d.temperature >= 0.0f && d.temperature <= FLT_MAX))
+        return fail(BITLOGIC_ERR_SHAPE, "verify: temperature %g is not in [0, inf)",
+                    (double)d.temperature);
+    if (!d.draft_temperatures && !(d.draft_temperature >= 0.0f && d.draft_temperature <= FLT_MAX))
+        return fail(BITLOGIC_ERR_SHAPE, "verify: draft_temperature %g is not in [0, inf)",
+                    (double)d.draft_temperature);
+    if (n_requests == 0)
+        return ok();
+    const bool greedy = !d.temperatures && d.temperature == 0.0f;
+    if (!logits || !accepted || !token || (!noise && !greedy) ||
+        (d.n_drafted > 0 && (!d.drafted || (!d.uniform && !greedy))))
+        return fail(BITLOGIC_ERR_NULL, "verify: NULL pointer");
+    if (!aligned(logits, logit_bytes(type)) ||
+        (d.draft_logits && !aligned(d.draft_logits, logit_bytes(d.draft_type))) ||
+        !aligned(d.drafted, 4) || !aligned(d.lengths, 4) || !aligned(d.uniform, 4) ||
+        !aligned(d.temperatures, 4) || !aligned(d.draft_temperatures, 4) || !aligned(noise, 4) ||
+        !aligned(accepted, 4) || !aligned(token, 4) || !aligned(log_prob, 4))
+        return fail(BITLOGIC_ERR_ALIGN, "verify: misaligned buffer");
+    const size_t need = bl::verify_workspace_bytes(n_requests, d.n_drafted, n_classes);
+    if (workspace_bytes < need || (need > 0 && !workspace))
+        return fail(BITLOGIC_ERR_WORKSPACE, "verify: workspace of %zu bytes, %zu needed",
+                    workspace_bytes, need);
+    if (need > 0 && !aligned(workspace, 8))
+        return fail(BITLOGIC_ERR_ALIGN, "verify: workspace not 8-byte aligned");
+    const bl::VerifySide target = {logits, type, row_stride, request_stride, d.temperature,
+                                   d.temperatures};
+    const bl::VerifySide draft = {d.draft_logits, d.draft_logits ? d.draft_type : type,
+                                  d.draft_row_stride, d.draft_request_stride,
+                                  d.draft_temperature, d.draft_temperatures};
+    return hip_status(bl::launch_verify(target, draft, n_requests, n_classes, d.n_drafted,
+                                        d.drafted, d.lengths, d.uniform, noise, noise_stride,
+                                        accepted, token, log_prob, workspace,
+                                        (hipStream_t)stream),
+                      "verify launch");
+}
+
+int bitlogic_dropout(const void *x, int32_t type, int64_t n_rows, int32_t n_cols,
+                     int64_t row_stride, float p, uint64_t seed, uint64_t offset,
+                     const uint64_t *offset_at, void *out, int64_t out_stride, void *stream)
+{
+    if (int rc = check_rows("dropout", type, n_rows, n_cols, row_stride))
+        return rc;
+    if (!(p >= 0.0f && p <= 1.0f))
+        return fail(BITLOGIC_ERR_SHAPE, "dropout: p %g is not in [0, 1]", (double)p);
+    if (out_stride < n_cols || out_stride > kMaxStride)
+        return fail(BITLOGIC_ERR_SHAPE, "dropout: need n_cols <= out_stride <= 2^30");
+    if (n_rows == 0)
+        return ok();
+    if (!x || !out)
+        return fail(BITLOGIC_ERR_NULL, "dropout: NULL pointer");
+    if (!aligned(x, logit_bytes(type)) || !aligned(out, logit_bytes(type)) ||
+        !aligned(offset_at, 8))
+        return fail(BITLOGIC_ERR_ALIGN, "dropout: misaligned buffer");
+    if (overlaps(x, span_bytes(n_rows, n_cols, row_stride, type), out,
+                 span_bytes(n_rows, n_cols, out_stride, type)) &&
+        !(x == out && (row_stride == out_stride || n_rows == 1)))
+        return fail(BITLOGIC_ERR_SHAPE, "dropout: out overlaps x without being x");
+    const uint32_t border = (uint32_t)floor((double)p * 65536.0 + 0.5);
+    return hip_status(bl::launch_dropout(x, type, n_rows, n_cols, row_stride, border, seed,
+                                         offset, offset_at, out, out_stride,
+                                         (hipStream_t)stream),
+                      "dropout launch");
 }
 
 int bitlogic_probe_valu(uint32_t *out, int32_t blocks, int32_t iters, uint32_t seed,

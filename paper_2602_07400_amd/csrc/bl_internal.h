@@ -263,6 +263,27 @@ hipError_t launch_sample(const void *logits, int32_t type, int64_t n_rows, int32
                          const SampleParams &sp, int32_t *token, float *log_prob,
                          hipStream_t stream);
 
+// Draft verification (verify.hip): strides in elements; logits of the drafter NULL where
+// drafts come without probabilities.
+struct VerifySide {
+    const void *logits;
+    int32_t type;
+    int64_t row_stride, request_stride;
+    float temperature;
+    const float *temperatures;
+};
+size_t verify_workspace_bytes(int64_t n_requests, int32_t drafts, int32_t n);
+hipError_t launch_verify(const VerifySide &target, const VerifySide &draft, int64_t n_requests,
+                         int32_t n, int32_t drafts, const int32_t *drafted,
+                         const int32_t *lengths, const float *uniform, const float *noise,
+                         int64_t noise_stride, int32_t *accepted, int32_t *token,
+                         float *log_prob, void *workspace, hipStream_t stream);
+// border: numbers below are dropped, 65536 all.
+hipError_t launch_dropout(const void *x, int32_t type, int64_t n_rows, int32_t n,
+                          int64_t row_stride, uint32_t border, uint64_t seed, uint64_t offset,
+                          const uint64_t *offset_at, void *out, int64_t out_stride,
+                          hipStream_t stream);
+
 // Peak probes (probes.hip): kProbeThreads = 256 lanes a block.
 hipError_t launch_probe_valu(uint32_t *out, int32_t blocks, int32_t iters, uint32_t seed,
                              hipStream_t stream);
