@@ -592,6 +592,73 @@ int bitlogic_dropout(const void *x, int32_t type, int64_t n_rows, int32_t n_cols
                      int64_t row_stride, float p, uint64_t seed, uint64_t offset,
                      const uint64_t *offset_at, void *out, int64_t out_stride, void *stream);
 
+/* ---- Adapters beside a shared projection --------------------------------
+ * Many requests' or clients' low-rank corrections of one projection -- the quantized head, or
+ * any float one -- computed together: row s of adapter a = ids[s] gets
+ *     out[s] = base_scale * base[s] + scale_a * up_a (down_a x[s])
+ * next to the shared projection's base[s].  An id outside [0, n_adapters) is none: that row
+ * is base_scale * base[s].  Adapters of a lower rank than the set's are filled up with zeros. */
+typedef struct bitlogic_adapter_set {
+    const void *down;               /* [n_adapters][rank][n_in]                      */
+    const void *up;                 /* [n_adapters][n_out][rank]                     */
+    int32_t weight_type;            /* BITLOGIC_LOGITS_F32, _F16 or _BF16            */
+    int32_t n_adapters;             /* 1..BITLOGIC_MAX_ADAPTERS                      */
+    int32_t rank;                   /* 1..BITLOGIC_MAX_RANK                          */
+    int32_t n_in, n_out;            /* 1..2^24                                       */
+    float scale;                    /* scale_a of all adapters or, where scales      */
+    const float *scales;            /* [n_adapters] (device memory) is not NULL, each */
+} bitlogic_adapter_set;
+#define BITLOGIC_MAX_ADAPTERS 4096
+#define BITLOGIC_MAX_RANK 128
+
+/* Rows in the order of their groups (a group's in ascending order), with the tables that the
+ * calls below divide their work by.  plan (device memory, 16-byte aligned,
+ * bitlogic_group_rows_bytes: 0 for sizes outside the limits) serves every call on rows with
+ * these ids -- other layers' adapters, the backward pass -- until it is written again.
+ *   ids  int32 [n_rows], 0 <= n_rows <= 2^27; any value may occur
+ *   n_groups  1..BITLOGIC_MAX_ADAPTERS: the n_adapters of the calls that take the plan */
+size_t bitlogic_group_rows_bytes(int64_t n_rows, int32_t n_groups);
+int bitlogic_group_rows(const int32_t *ids, int64_t n_rows, int32_t n_groups, void *plan,
+                        size_t plan_bytes, void *stream);
+
+/* Forward.
+ *   x       [n_rows][n_in] of the weights' type or, with float32 weights, int32 counts;
+ *           x_stride >= 0 elements from row to row
+ *   ids     int32 [n_rows], read where plan is NULL: each row by itself then, which suits
+ *           few rows (at most 2^20)
+ *   plan    of n_rows ids and n_adapters groups, or NULL.  A plan of other sizes, or one that
+ *           bitlogic_group_rows did not write, is the caller's error, which is not detected
+ *   base    [n_rows][n_out] of the weights' type or, with float32 weights, int32 logits
+ *           (base_type); base_stride >= 0; NULL: zero
+ *   out     [n_rows][n_out] of the weights' type, out_stride >= n_out: base itself with its
+ *           own stride (not int32), or memory apart from x and base
+ *   hidden  float [n_rows][rank] or NULL: down_a x[s], 0 where there is no adapter; what the
+ *           backward pass takes.  out may be NULL if hidden is not
+ * Sums are held in 32 bits; down_a x goes into the second product to 2^-17 of itself or
+ * better.  Results do not depend on how a launch is scheduled, nor a row's on other rows. */
+int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_stride,
+                      const bitlogic_adapter_set *set, const int32_t *ids, const void *plan,
+                      const void *base, int32_t base_type, int64_t base_stride,
+                      float base_scale, void *out, int64_t out_stride, float *hidden,
+                      void *stream);
+
+/* Backward: with g[s] the gradient of out[s] (weights' type, grad_stride >= 0),
+ *   grad_x[s]   = scale_a down_a^T (up_a^T g[s]), 0 where there is no adapter; weights' type,
+ *                 grad_x_stride >= n_in
+ *   grad_down_a = scale_a sum_s (up_a^T g[s]) x[s]^T      [n_adapters][rank][n_in]
+ *   grad_up_a   = scale_a sum_s g[s] hidden[s]^T          [n_adapters][n_out][rank]
+ * over the rows s of adapter a (none: zeros), in the weights' type; each may be NULL, not all.
+ * (The gradient of base is base_scale * g.)  x and hidden are read for the weights' gradients
+ * alone, which also need a plan.  The outputs may not overlap each other or any input. */
+size_t bitlogic_adapters_backward_workspace_bytes(const bitlogic_adapter_set *set,
+                                                  int64_t n_rows);
+int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_stride,
+                               const void *x, int32_t x_type, int64_t x_stride,
+                               const float *hidden, const bitlogic_adapter_set *set,
+                               const int32_t *ids, const void *plan, void *grad_x,
+                               int64_t grad_x_stride, void *grad_down, void *grad_up,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- Peak probes (measurement, not part of the inference path) ---------- */
 
 /* Integer VALU probe: `blocks` blocks of 256 lanes.  Lane l (global index)
@@ -691,8 +758,8 @@ const char *bitlogic_last_error(void);
  * instruction-rate and gather probes; 0.7.0 bitlogic_forward_info.jump_layers
  * and the node-per-wave layer kernel, whose per-node records enlarge the
  * forward workspace of networks that use it; 0.8.0 bitlogic_network_path; 0.9.0
- * bitlogic_top_logits, bitlogic_distill and bitlogic_sample; 0.10.0 bitlogic_verify
-and bitlogic_dropout). */
+ * bitlogic_top_logits, bitlogic_distill and bitlogic_sample; 0.10.0 bitlogic_verify,
+bitlogic_dropout, bitlogic_group_rows and bitlogic_adapters with its backward pass). */
 #define BITLOGIC_VERSION 1000
 int bitlogic_version(void);
 

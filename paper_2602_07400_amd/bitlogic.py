@@ -27,7 +27,8 @@ __all__ = [
     "bitlogic_network_forward_noalloc", "NOALLOC_SCRATCH_BYTES",
     "bitlogic_groupsum_head_workspace_bytes", "bitlogic_status_string", "bitlogic_version",
     "bitlogic_top_logits", "bitlogic_distill", "bitlogic_distill_loss", "bitlogic_sample",
-    "bitlogic_verify", "bitlogic_dropout",
+    "bitlogic_verify", "bitlogic_dropout", "bitlogic_group_rows", "RowGroups",
+    "bitlogic_adapters", "bitlogic_adapters_backward", "bitlogic_adapt",
     "BitlogicModel", "bitlogic_specialize_layer", "bitlogic_specialize_network", "library_path",
     "load_library", "words",
 ]
@@ -84,6 +85,13 @@ class _Drafts(ctypes.Structure):
                 ("temperatures", ctypes.c_void_p), ("draft_temperatures", ctypes.c_void_p)]
 
 
+class _AdapterSet(ctypes.Structure):
+    _fields_ = [("down", ctypes.c_void_p), ("up", ctypes.c_void_p),
+                ("weight_type", ctypes.c_int32), ("n_adapters", ctypes.c_int32),
+                ("rank", ctypes.c_int32), ("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("scales", ctypes.c_void_p)]
+
+
 _PATHS = ("slab", "columns", "block")      # BITLOGIC_PATH_*
 MAX_FANIN = 6
 SPECIALIZE_PASS = 32          # nodes per entry of a specialized layer's fan-in array
@@ -137,6 +145,13 @@ def load_library():
         "bitlogic_verify": ([P, i32, i64, i32, i64, i64, P, P, i64, P, P, P, P, sz, P],
                             ctypes.c_int),
         "bitlogic_dropout": ([P, i32, i64, i32, i64, f32, u64, u64, P, P, i64, P], ctypes.c_int),
+        "bitlogic_group_rows_bytes": ([i64, i32], sz),
+        "bitlogic_group_rows": ([P, i64, i32, P, sz, P], ctypes.c_int),
+        "bitlogic_adapters": ([P, i32, i64, i64, P, P, P, P, i32, i64, f32, P, i64, P, P],
+                              ctypes.c_int),
+        "bitlogic_adapters_backward_workspace_bytes": ([P, i64], sz),
+        "bitlogic_adapters_backward": ([P, i64, i64, P, i32, i64, P, P, P, P, P, i64, P, P, P,
+                                        sz, P], ctypes.c_int),
         "bitlogic_probe_valu": ([P, i32, i32, ctypes.c_uint32, P], ctypes.c_int),
         "bitlogic_probe_hbm": ([i32, P, P, i64, i32, i32, P], ctypes.c_int),
         "bitlogic_probe_valu_op": ([i32, P, i32, i32, ctypes.c_uint32, P], ctypes.c_int),
@@ -713,7 +728,7 @@ def _rows(t: torch.Tensor, name: str, dtypes=_LOGITS) -> Tuple[int, int]:
     if t.dim() != 2:
         raise ValueError(f"{name} must be 2-D")
     stride, step = t.stride()
-    if step != 1 and t.shape[1] > 1:
+    if step != 1 and t.numel() > 0 and t.shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
     return t.data_ptr(), stride if t.shape[0] > 1 else t.shape[1]
 
@@ -890,7 +905,7 @@ def _rows3(t: torch.Tensor, name: str, shape, device) -> Tuple[int, int, int]:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    if t.stride(2) != 1 and t.numel() > 0 and t.shape[2] > 1:
         raise ValueError(f"{name} must have contiguous rows")
     return (t.data_ptr(), t.stride(1) if t.shape[1] > 1 else t.shape[2],
             t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
@@ -1007,6 +1022,205 @@ def bitlogic_dropout(x: torch.Tensor, p: float, seed: int, offset=0,
             and torch.is_grad_enabled():
         return _Dropout.apply(x, p, seed, offset)
     return _dropout(x, p, seed, offset, out, stream)
+
+
+# ------------------------------------------- adapters beside a projection
+
+MAX_ADAPTERS, MAX_RANK = 4096, 128    # BITLOGIC_MAX_ADAPTERS, BITLOGIC_MAX_RANK
+# Up to as many rows go through adapters without a plan: a row reads its adapter by itself
+_LONE_ROWS = 16
+
+
+@dataclass
+class RowGroups:
+    """Rows by group, as bitlogic_group_rows leaves them in device memory."""
+    plan: Optional[torch.Tensor]
+    n_rows: int
+    n_groups: int
+
+
+def bitlogic_group_rows(ids: torch.Tensor, n_groups: int,
+                        plan: Optional[torch.Tensor] = None, stream=None) -> RowGroups:
+    """Rows in the order of their groups: ids int32 [N] (a value outside [0, n_groups) is no
+    group).  Serves all calls of bitlogic_adapters, bitlogic_adapters_backward and
+    bitlogic_adapt on rows with these ids.  plan: uint8, at least
+    bitlogic_group_rows_bytes(N, n_groups)."""
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids must be a tensor [N]")
+    n, dev = ids.shape[0], ids.device
+    ptr = _dev(ids, "ids", _I32)
+    lib = load_library()
+    need = int(lib.bitlogic_group_rows_bytes(n, n_groups))
+    if plan is None:
+        plan = _empty((max(need, 1),), torch.uint8, dev, stream)
+    if plan.device != dev:
+        raise ValueError(f"plan is on {plan.device}, expected {dev}")
+    _call(dev, lib.bitlogic_group_rows, ptr, n, n_groups, _dev(plan, "plan", (torch.uint8,)),
+          plan.numel(), _stream(stream, dev))
+    return RowGroups(plan, n, n_groups)
+
+
+def _adapter_set(x, down, up, scales):
+    """The C struct of a set of adapters for rows x."""
+    for t, name in ((down, "down"), (up, "up")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError(f"{name} must be a tensor of three dimensions")
+    g, r, f = down.shape
+    c = up.shape[1]
+    dev, dtype = x.device, down.dtype
+    if dtype not in _LOGITS or dtype == torch.int32:
+        raise TypeError(f"down has dtype {dtype}, expected a float type")
+    if x.shape[1] != f:
+        raise ValueError(f"x has {x.shape[1]} columns, the adapters {f}")
+    if x.dtype != dtype and not (x.dtype == torch.int32 and dtype == torch.float32):
+        raise TypeError(f"x has dtype {x.dtype} beside adapters of {dtype}")
+    s = _AdapterSet(_like(down, "down", (dtype,), (g, r, f), dev),
+                    _like(up, "up", (dtype,), (g, c, r), dev), _LOGITS[dtype], g, r, f, c, 1.0,
+                    None)
+    if isinstance(scales, torch.Tensor):
+        s.scales = _like(scales, "scales", _F32, (g,), dev)
+    else:
+        s.scale = scales
+    return s
+
+
+def _grouped(ids, plan, n, groups, dev, stream, lone=True):
+    """(ids' address, plan's address, the plan) for n rows: the plan given, one made here, or
+    none for few rows."""
+    if plan is not None:
+        if (plan.n_rows, plan.n_groups) != (n, groups):
+            raise ValueError(f"the plan is of {plan.n_rows} rows and {plan.n_groups} groups, not "
+                             f"{n} and {groups}")
+        if plan.plan.device != dev:
+            raise ValueError(f"the plan is on {plan.plan.device}, expected {dev}")
+        return None, plan.plan.data_ptr(), plan
+    ptr = _like(ids, "ids", _I32, (n,), dev)
+    if n == 0 or (lone and n <= _LONE_ROWS):
+        return ptr, None, None
+    plan = bitlogic_group_rows(ids, groups, stream=stream)
+    return ptr, plan.plan.data_ptr(), plan
+
+
+def bitlogic_adapters(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
+                      ids: Optional[torch.Tensor], scales=1.0,
+                      base: Optional[torch.Tensor] = None, base_scale: float = 1.0,
+                      plan: Optional[RowGroups] = None, out: Optional[torch.Tensor] = None,
+                      hidden: Optional[torch.Tensor] = None, stream=None,
+                      want_hidden: bool = False):
+    """Low-rank adapters of many requests beside a shared projection: row s of x [N][f] with
+    a = ids[s] (int32 [N]; outside the adapters: none) gets
+    base_scale * base[s] + scales[a] * up[a] (down[a] x[s]): (out [N][c], hidden = down x
+    float32 [N][r] or None).  down [G][r][f] and up [G][c][r] of one float type; x and base
+    [N][c] (None: zero) of that type or, beside float32, int32 counts and logits; rows may be
+    strided.  scales: a number or float32 [G].  out may be base.  plan: bitlogic_group_rows of
+    these ids, made here otherwise (ids may be None where it is given)."""
+    ptr, stride = _rows(x, "x")
+    s = _adapter_set(x, down, up, scales)
+    n, c, dev, dtype = x.shape[0], s.n_out, x.device, down.dtype
+    base_ptr, base_type, base_stride = None, s.weight_type, 0
+    if base is not None:
+        base_ptr, base_stride = _rows(base, "base", (dtype, torch.int32)
+                                      if dtype == torch.float32 else (dtype,))
+        base_type = _LOGITS[base.dtype]
+        if tuple(base.shape) != (n, c) or base.device != dev:
+            raise ValueError(f"base must be [{n}][{c}] on {dev}")
+    if out is None:
+        out = _empty((n, c), dtype, dev, stream)
+    out_ptr, out_stride = _rows(out, "out", (dtype,))
+    if tuple(out.shape) != (n, c) or out.device != dev:
+        raise ValueError(f"out must be [{n}][{c}] on {dev}")
+    if hidden is None and want_hidden:
+        hidden = _empty((n, s.rank), torch.float32, dev, stream)
+    ids_ptr, plan_ptr, plan = _grouped(ids, plan, n, s.n_adapters, dev, stream)
+    _call(dev, load_library().bitlogic_adapters, ptr, _LOGITS[x.dtype], n, stride,
+          ctypes.addressof(s), ids_ptr, plan_ptr, base_ptr, base_type, base_stride, base_scale,
+          out_ptr, out_stride,
+          _like(hidden, "hidden", _F32, (n, s.rank), dev) if hidden is not None else None,
+          _stream(stream, dev))
+    return out, hidden
+
+
+def bitlogic_adapters_backward(grad: torch.Tensor, x: torch.Tensor,
+                               hidden: Optional[torch.Tensor], down: torch.Tensor,
+                               up: torch.Tensor, ids: Optional[torch.Tensor], scales=1.0,
+                               plan: Optional[RowGroups] = None,
+                               grad_x: Optional[torch.Tensor] = None,
+                               grad_down: Optional[torch.Tensor] = None,
+                               grad_up: Optional[torch.Tensor] = None,
+                               workspace: Optional[torch.Tensor] = None, stream=None,
+                               want_x: bool = True, want_down: bool = True,
+                               want_up: bool = True):
+    """Gradients of bitlogic_adapters for grad [N][c], that of out: (of x [N][f], of down, of
+    up), each None where it is not wanted.  hidden: bitlogic_adapters' (for that of up)."""
+    ptr, stride = _rows(grad, "grad")
+    x_ptr, x_stride = _rows(x, "x")
+    s = _adapter_set(x, down, up, scales)
+    n, dev, dtype = x.shape[0], x.device, down.dtype
+    if tuple(grad.shape) != (n, s.n_out) or grad.device != dev or grad.dtype != dtype:
+        raise ValueError(f"grad must be [{n}][{s.n_out}] of {dtype} on {dev}")
+    if grad_x is None and want_x:
+        grad_x = _empty((n, s.n_in), dtype, dev, stream)
+    if grad_down is None and want_down:
+        grad_down = _empty(tuple(down.shape), dtype, dev, stream)
+    if grad_up is None and want_up:
+        grad_up = _empty(tuple(up.shape), dtype, dev, stream)
+    gx_ptr, gx_stride = None, 0
+    if grad_x is not None:
+        gx_ptr, gx_stride = _rows(grad_x, "grad_x", (dtype,))
+        if tuple(grad_x.shape) != (n, s.n_in) or grad_x.device != dev:
+            raise ValueError("grad_x must have x's shape and device")
+    weights = grad_down is not None or grad_up is not None
+    ids_ptr, plan_ptr, plan = _grouped(ids, plan, n, s.n_adapters, dev, stream, not weights)
+    lib = load_library()
+    need = int(lib.bitlogic_adapters_backward_workspace_bytes(ctypes.addressof(s), n))
+    ws_ptr, ws_bytes = _workspace(need, dev, workspace, stream)
+    like = lambda t, name, ty, of: (_like(t, name, ty, tuple(of), dev)           # noqa: E731
+                                    if t is not None else None)
+    _call(dev, lib.bitlogic_adapters_backward, ptr, n, stride, x_ptr, _LOGITS[x.dtype], x_stride,
+          like(hidden, "hidden", _F32, (n, s.rank)), ctypes.addressof(s), ids_ptr, plan_ptr,
+          gx_ptr, gx_stride, like(grad_down, "grad_down", (dtype,), down.shape),
+          like(grad_up, "grad_up", (dtype,), up.shape), ws_ptr, ws_bytes, _stream(stream, dev))
+    return grad_x, grad_down, grad_up
+
+
+class _Adapt(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, down, up, base, ids, scales, base_scale, plan):
+        need = ctx.needs_input_grad
+        if plan is None and (need[1] or need[2]) and x.shape[0] > 0:
+            plan = bitlogic_group_rows(ids, down.shape[0])        # the backward pass's, too
+        out, hidden = bitlogic_adapters(x, down, up, ids, scales, base, base_scale, plan,
+                                        want_hidden=need[2])
+        ctx.save_for_backward(x, down, up, ids, hidden,
+                              scales if isinstance(scales, torch.Tensor) else None)
+        ctx.rest = (None if isinstance(scales, torch.Tensor) else scales), base_scale, plan
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, down, up, ids, hidden, scales = ctx.saved_tensors
+        number, base_scale, plan = ctx.rest
+        need = ctx.needs_input_grad
+        grad = grad.contiguous()
+        grads = (None, None, None)
+        if any(need[:3]):
+            grads = bitlogic_adapters_backward(
+                grad, x, hidden, down, up, ids, number if scales is None else scales, plan,
+                want_x=need[0], want_down=need[1], want_up=need[2])
+        grad_base = None
+        if need[3]:
+            grad_base = grad if base_scale == 1.0 else grad * base_scale
+        return (*grads, grad_base, None, None, None, None)
+
+
+def bitlogic_adapt(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
+                   ids: Optional[torch.Tensor], scales=1.0,
+                   base: Optional[torch.Tensor] = None, base_scale: float = 1.0,
+                   plan: Optional[RowGroups] = None) -> torch.Tensor:
+    """bitlogic_adapters' out as a differentiable function of x, down, up and base (scales
+    have no gradient).  Both passes run on the current stream."""
+    return _Adapt.apply(x, down, up, base, ids, scales, base_scale, plan)
 
 
 # ---------------------------------------------------------------- peak probes

@@ -15,7 +15,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["encode.hip", "lut_layer.hip", "lut_jump.hip", "columns.hip", "head.hip", "fit.hip",
            "specialize.hip", "probes.hip", "top_logits.hip", "distill.hip", "sample.hip",
-           "verify.hip", "dropout.hip", "api.hip"]
+           "verify.hip", "dropout.hip", "group_rows.hip",
+           "adapters_f32.hip", "adapters_f16.hip", "adapters_bf16.hip", "api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,131 @@
+// Low-rank adapters (internal): what the plan of grouped rows holds, and the arguments of the
+// kernels.
+#pragma once
+
+#include <algorithm>
+
+#include "logit_rows.h"
+
+namespace bl {
+namespace adapt {
+
+using rows::kBf16;
+using rows::kF16;
+using rows::kF32;
+using rows::kI32;
+
+constexpr int kTile = 32;               // rows of a tile, all of one group
+constexpr int32_t kMaxGroups = 4096;    // (a wave's counters in LDS)
+constexpr int32_t kMaxRank = 128;
+constexpr int32_t kMaxRuns = 1024;
+
+// Rows [first, first + count) of the order, of one group (-1: no piece).  slot: of a group of
+// several chunks, the chunk's partial sums in the workspace.
+struct Piece4 {
+    int32_t group, first, count, slot;
+};
+
+// ---- the plan: rows by group ----
+struct GroupLayout {
+    size_t order, starts, tile_starts, chunk_starts, slot_starts, tiles, chunks, totals, counts,
+        bytes;
+    int64_t n_tiles, n_chunks, n_slots, run;
+    int32_t chunk, runs;
+};
+
+// chunk: rows that a gradient's partial sum goes over, whole tiles; a sixty-fourth of the rows
+// within limits, so that partial sums stay small beside the rows they are made of.
+inline GroupLayout group_layout(int64_t n_rows, int32_t groups)
+{
+    GroupLayout l;
+    l.chunk = (int32_t)std::min<int64_t>(4096, std::max<int64_t>(256, n_rows / 64 / 32 * 32));
+    l.n_tiles = n_rows / kTile + groups + 1;              // at most a partial one a group
+    l.n_chunks = n_rows / l.chunk + groups + 1;
+    l.n_slots = 2 * (n_rows / l.chunk);                   // k > 1 chunks: over (k - 1) chunk rows
+    l.run = std::max<int64_t>(1024, (n_rows + kMaxRuns - 1) / kMaxRuns);
+    l.run = (l.run + 63) / 64 * 64;
+    l.runs = (int32_t)((n_rows + l.run - 1) / l.run);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    const size_t all = (size_t)groups + 2;
+    l.order = take((size_t)n_rows * 4);
+    l.starts = take(all * 4);
+    l.tile_starts = take(all * 4);
+    l.chunk_starts = take(all * 4);
+    l.slot_starts = take(all * 4);
+    l.tiles = take((size_t)l.n_tiles * sizeof(Piece4));
+    l.chunks = take((size_t)l.n_chunks * sizeof(Piece4));
+    l.totals = take(all * 4);
+    l.counts = take((size_t)l.runs * (groups + 1) * 4);
+    l.bytes = at;
+    return l;
+}
+
+struct GroupArgs {
+    const int32_t *ids;
+    int64_t rows, n_tiles, n_chunks, run;
+    int32_t groups, chunk, runs;
+    int32_t *order, *starts, *tile_starts, *chunk_starts, *slot_starts;
+    Piece4 *tiles, *chunks;
+    uint32_t *totals, *counts;
+};
+
+// ---- a pass through adapters ----
+// Forward: out = base_scale base + scale up (down x), hidden = down x.  Back: the same with
+// x the gradient of out, down^T and up^T in each other's places, and no base.
+struct PassArgs {
+    const char *x;
+    int64_t x_stride;                   // strides in bytes from row to row
+    const char *w1, *w2;                // forward: down [rank][k], up [m][rank];
+                                        // back: up [k][rank], down [rank][m]
+    int64_t w1_step, w2_step;           // bytes from adapter to adapter
+    int32_t k, m, rank, groups;
+    const float *scales;                // [groups] or NULL
+    float scale;
+    const char *base;                   // or NULL
+    int64_t base_stride;
+    int32_t base_i32;
+    float base_scale;
+    char *out;                          // or NULL: hidden alone
+    int64_t out_stride;
+    float *hidden;                      // [rows][rank] or NULL
+    // rows by a plan, or (tiles NULL) a tile each by their ids
+    const Piece4 *tiles;
+    const int32_t *order, *ids;
+    int64_t n_tiles;
+    int32_t splits;                     // blocks a tile, each with its columns of out
+};
+
+// Gradients: d down [groups][rank][n_in] = sum scale back x^T, d up [groups][n_out][rank] =
+// sum scale grad hidden^T, over a group's rows.
+struct GradJob {
+    const char *y;                      // rows of x, or of the gradient of out
+    int64_t y_stride;
+    int32_t y_i32, cols, blocks;        // columns, and blocks of them
+    const float *h;                     // [rows][rank]: back, or hidden
+    char *out;                          // or NULL: no such job
+    int32_t transposed;                 // out [cols][rank] instead of [rank][cols]
+    float *partial;                     // [slots][rank][cols]
+};
+struct GradArgs {
+    GradJob job[2];
+    const Piece4 *chunks;
+    const int32_t *order, *chunk_starts, *slot_starts;   // (chunk_starts NULL: no rows)
+    int64_t n_chunks;
+    int32_t rank, groups;
+    const float *scales;
+    float scale;
+};
+
+template <int W> hipError_t launch_pass(const PassArgs &a, bool x_i32, bool back,
+                                        hipStream_t stream);
+template <int W> hipError_t launch_grads(const GradArgs &a, hipStream_t stream);
+// columns that a block of launch_grads takes
+template <int W> int32_t grad_block();
+
+}  // namespace adapt
+}  // namespace bl

@@ -1,0 +1,12 @@
+// Low-rank adapters with float32 weights.
+#include "adapters_pass.h"
+
+namespace bl {
+namespace adapt {
+
+template hipError_t launch_pass<kF32>(const PassArgs &, bool, bool, hipStream_t);
+template hipError_t launch_grads<kF32>(const GradArgs &, hipStream_t);
+template int32_t grad_block<kF32>();
+
+}  // namespace adapt
+}  // namespace bl

@@ -13,6 +13,7 @@
 
 #include "bitlogic.h"
 #include "bl_internal.h"
+#include "adapters.h"
 #include "logit_rows.h"
 
 // Scratch of bitlogic_network_forward_noalloc: one copy of this array per GPU
@@ -312,6 +313,104 @@ int plan_forward(int64_t n, int32_t d, int32_t b, const bitlogic_layer *layers, 
     fp->off_rec = fp->off_head + round_up(fp->head.ws_bytes);
     fp->total = fp->off_rec + (fp->jump_mask ? round_up(bl::jump_records_bytes(rec_w)) : 0);
     return BITLOGIC_OK;
+}
+
+}  // namespace
+
+// ---- adapters: checks and layouts ----
+
+static_assert(bl::adapt::kMaxGroups == BITLOGIC_MAX_ADAPTERS &&
+              bl::adapt::kMaxRank == BITLOGIC_MAX_RANK, "the interface's limits");
+
+namespace {
+
+constexpr int64_t kMaxGroupedRows = (int64_t)1 << 27;   // a launch's lanes stay below 2^32
+constexpr int64_t kMaxLoneRows = (int64_t)1 << 20;
+constexpr int32_t kMaxWidth = 1 << 24;
+
+int check_set(const char *who, const bitlogic_adapter_set *set, int64_t n_rows)
+{
+    if (!set)
+        return fail(BITLOGIC_ERR_NULL, "%s: NULL adapter set", who);
+    if (set->weight_type < BITLOGIC_LOGITS_F32 || set->weight_type > BITLOGIC_LOGITS_BF16)
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "%s: weights of type %d", who, set->weight_type);
+    if (n_rows < 0 || n_rows > kMaxGroupedRows)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: need 0 <= n_rows <= 2^27", who);
+    if (set->n_adapters < 1 || set->rank < 1 || set->n_in < 1 || set->n_out < 1 ||
+        set->n_in > kMaxWidth || set->n_out > kMaxWidth)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: need n_adapters >= 1, rank >= 1, 1 <= n_in, n_out "
+                    "<= 2^24", who);
+    if (set->n_adapters > BITLOGIC_MAX_ADAPTERS || set->rank > BITLOGIC_MAX_RANK)
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "%s: %d adapters of rank %d, at most %d of rank %d",
+                    who, set->n_adapters, set->rank, BITLOGIC_MAX_ADAPTERS, BITLOGIC_MAX_RANK);
+    return BITLOGIC_OK;
+}
+
+// x's type, and whether x, base: the weights' type, or int32 beside float32 weights.
+int check_beside(const char *who, const char *what, int32_t type, int32_t weight_type)
+{
+    if (type != weight_type &&
+        !(type == BITLOGIC_LOGITS_I32 && weight_type == BITLOGIC_LOGITS_F32))
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "%s: %s of type %d beside weights of type %d", who,
+                    what, type, weight_type);
+    return BITLOGIC_OK;
+}
+
+int check_stride(const char *who, const char *what, int64_t stride, int64_t least)
+{
+    if (stride < least || stride > kMaxStride)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: need %lld <= %s <= 2^30", who, (long long)least,
+                    what);
+    return BITLOGIC_OK;
+}
+
+// Rows by plan or by ids into a pass's arguments.
+int take_rows(const char *who, bl::adapt::PassArgs &a, int64_t n_rows, int32_t groups,
+              const int32_t *ids, const void *plan)
+{
+    if (!plan && !ids)
+        return fail(BITLOGIC_ERR_NULL, "%s: neither a plan nor ids", who);
+    if (!aligned(plan, 16) || !aligned(ids, 4))
+        return fail(BITLOGIC_ERR_ALIGN, "%s: plan or ids misaligned", who);
+    if (!plan && n_rows > kMaxLoneRows)
+        return fail(BITLOGIC_ERR_SHAPE, "%s: more than 2^20 rows need a plan", who);
+    a.groups = groups;
+    if (plan) {
+        const auto l = bl::adapt::group_layout(n_rows, groups);
+        const char *p = static_cast<const char *>(plan);
+        a.tiles = reinterpret_cast<const bl::adapt::Piece4 *>(p + l.tiles);
+        a.order = reinterpret_cast<const int32_t *>(p + l.order);
+        a.n_tiles = l.n_tiles;
+    } else {
+        a.ids = ids;
+        a.n_tiles = n_rows;
+    }
+    return BITLOGIC_OK;
+}
+
+template <class F>
+hipError_t by_weight(int32_t type, F f)
+{
+    switch (type) {
+    case BITLOGIC_LOGITS_F32: return f(std::integral_constant<int, bl::rows::kF32>());
+    case BITLOGIC_LOGITS_F16: return f(std::integral_constant<int, bl::rows::kF16>());
+    default: return f(std::integral_constant<int, bl::rows::kBf16>());
+    }
+}
+
+struct BackwardLayout {
+    size_t back, partial_down, partial_up, bytes;
+};
+
+BackwardLayout backward_layout(const bitlogic_adapter_set &s, int64_t n_rows)
+{
+    const auto l = bl::adapt::group_layout(n_rows, s.n_adapters);
+    BackwardLayout b;
+    b.back = 0;
+    b.partial_down = round_up((size_t)n_rows * s.rank * 4);
+    b.partial_up = b.partial_down + round_up((size_t)l.n_slots * s.rank * s.n_in * 4);
+    b.bytes = b.partial_up + round_up((size_t)l.n_slots * s.rank * s.n_out * 4);
+    return b;
 }
 
 }  // namespace
@@ -1141,6 +1240,229 @@ int bitlogic_dropout(const void *x, int32_t type, int64_t n_rows, int32_t n_cols
                                          offset, offset_at, out, out_stride,
                                          (hipStream_t)stream),
                       "dropout launch");
+}
+
+// ---- adapters ----
+
+size_t bitlogic_group_rows_bytes(int64_t n_rows, int32_t n_groups)
+{
+    if (n_rows < 0 || n_rows > kMaxGroupedRows || n_groups < 1 ||
+        n_groups > BITLOGIC_MAX_ADAPTERS)
+        return 0;
+    return bl::adapt::group_layout(n_rows, n_groups).bytes;
+}
+
+int bitlogic_group_rows(const int32_t *ids, int64_t n_rows, int32_t n_groups, void *plan,
+                        size_t plan_bytes, void *stream)
+{
+    if (n_rows < 0 || n_rows > kMaxGroupedRows || n_groups < 1)
+        return fail(BITLOGIC_ERR_SHAPE, "group_rows: need 0 <= n_rows <= 2^27, n_groups >= 1");
+    if (n_groups > BITLOGIC_MAX_ADAPTERS)
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "group_rows: %d groups > %d", n_groups,
+                    BITLOGIC_MAX_ADAPTERS);
+    if (n_rows == 0)
+        return ok();
+    if (!ids || !plan)
+        return fail(BITLOGIC_ERR_NULL, "group_rows: NULL pointer");
+    if (!aligned(ids, 4) || !aligned(plan, 16))
+        return fail(BITLOGIC_ERR_ALIGN, "group_rows: ids or plan misaligned");
+    if (plan_bytes < bitlogic_group_rows_bytes(n_rows, n_groups))
+        return fail(BITLOGIC_ERR_WORKSPACE, "group_rows: plan of %zu bytes, %zu needed",
+                    plan_bytes, bitlogic_group_rows_bytes(n_rows, n_groups));
+    return hip_status(bl::launch_group_rows(ids, n_rows, n_groups, plan, (hipStream_t)stream),
+                      "group_rows launch");
+}
+
+int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_stride,
+                      const bitlogic_adapter_set *set, const int32_t *ids, const void *plan,
+                      const void *base, int32_t base_type, int64_t base_stride,
+                      float base_scale, void *out, int64_t out_stride, float *hidden,
+                      void *stream)
+{
+    const char *who = "adapters";
+    if (int rc = check_set(who, set, n_rows))
+        return rc;
+    const bitlogic_adapter_set &s = *set;
+    if (int rc = check_beside(who, "x", x_type, s.weight_type))
+        return rc;
+    if (int rc = check_stride(who, "x_stride", x_stride, 0))
+        return rc;
+    if (base) {
+        if (int rc = check_beside(who, "base", base_type, s.weight_type))
+            return rc;
+        if (int rc = check_stride(who, "base_stride", base_stride, 0))
+            return rc;
+    }
+    if (out)
+        if (int rc = check_stride(who, "out_stride", out_stride, s.n_out))
+            return rc;
+    if (n_rows == 0)
+        return ok();
+    if (!x || !s.down || !s.up || (!out && !hidden))
+        return fail(BITLOGIC_ERR_NULL, "adapters: NULL input, or both outputs NULL");
+    const size_t el = logit_bytes(s.weight_type);
+    if (!aligned(x, el) || !aligned(s.down, el) || !aligned(s.up, el) || !aligned(base, el) ||
+        !aligned(out, el) || !aligned(hidden, 4) || !aligned(s.scales, 4))
+        return fail(BITLOGIC_ERR_ALIGN, "adapters: misaligned buffer");
+    if (out) {
+        const size_t out_span = span_bytes(n_rows, s.n_out, out_stride, s.weight_type);
+        if (overlaps(x, span_bytes(n_rows, s.n_in, x_stride, s.weight_type), out, out_span))
+            return fail(BITLOGIC_ERR_SHAPE, "adapters: out overlaps x");
+        if (base &&
+            overlaps(base, span_bytes(n_rows, s.n_out, base_stride, s.weight_type), out,
+                     out_span) &&
+            !(base == out && (base_stride == out_stride || n_rows == 1) &&
+              base_type == s.weight_type))
+            return fail(BITLOGIC_ERR_SHAPE, "adapters: out overlaps base without being base");
+    }
+    bl::adapt::PassArgs a = {};
+    if (int rc = take_rows(who, a, n_rows, s.n_adapters, ids, plan))
+        return rc;
+    a.x = static_cast<const char *>(x);
+    a.x_stride = x_stride * (int64_t)el;
+    a.w1 = static_cast<const char *>(s.down);
+    a.w2 = static_cast<const char *>(s.up);
+    a.w1_step = (int64_t)s.rank * s.n_in * (int64_t)el;
+    a.w2_step = (int64_t)s.rank * s.n_out * (int64_t)el;
+    a.k = s.n_in;
+    a.m = s.n_out;
+    a.rank = s.rank;
+    a.scales = s.scales;
+    a.scale = s.scale;
+    a.base = static_cast<const char *>(base);
+    a.base_stride = base_stride * (int64_t)el;
+    a.base_i32 = base_type == BITLOGIC_LOGITS_I32;
+    a.base_scale = base_scale;
+    a.out = static_cast<char *>(out);
+    a.out_stride = out_stride * (int64_t)el;
+    a.hidden = hidden;
+    return hip_status(by_weight(s.weight_type, [&](auto W) {
+        return bl::adapt::launch_pass<decltype(W)::value>(a, x_type == BITLOGIC_LOGITS_I32, false,
+                                                          (hipStream_t)stream);
+    }), "adapters launch");
+}
+
+size_t bitlogic_adapters_backward_workspace_bytes(const bitlogic_adapter_set *set,
+                                                  int64_t n_rows)
+{
+    if (check_set("adapters_backward", set, n_rows) != BITLOGIC_OK)
+        return 0;
+    return backward_layout(*set, n_rows).bytes;
+}
+
+int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_stride,
+                               const void *x, int32_t x_type, int64_t x_stride,
+                               const float *hidden, const bitlogic_adapter_set *set,
+                               const int32_t *ids, const void *plan, void *grad_x,
+                               int64_t grad_x_stride, void *grad_down, void *grad_up,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "adapters_backward";
+    if (int rc = check_set(who, set, n_rows))
+        return rc;
+    const bitlogic_adapter_set &s = *set;
+    if (int rc = check_beside(who, "x", x_type, s.weight_type))
+        return rc;
+    if (int rc = check_stride(who, "grad_stride", grad_stride, 0))
+        return rc;
+    if (int rc = check_stride(who, "x_stride", x_stride, 0))
+        return rc;
+    if (grad_x)
+        if (int rc = check_stride(who, "grad_x_stride", grad_x_stride, s.n_in))
+            return rc;
+    const size_t el = logit_bytes(s.weight_type);
+    const bool weights = grad_down || grad_up;
+    if (!aligned(grad, el) || !aligned(x, el) || !aligned(hidden, 4) || !aligned(s.down, el) ||
+        !aligned(s.up, el) || !aligned(s.scales, 4) || !aligned(grad_x, el) ||
+        !aligned(grad_down, el) || !aligned(grad_up, el))
+        return fail(BITLOGIC_ERR_ALIGN, "adapters_backward: misaligned buffer");
+    if (!grad_x && !weights)
+        return fail(BITLOGIC_ERR_NULL, "adapters_backward: all outputs NULL");
+    bl::adapt::PassArgs a = {};
+    if (n_rows > 0) {
+        if (!grad || !s.up || (grad_x && !s.down) || (grad_down && !x) || (grad_up && !hidden))
+            return fail(BITLOGIC_ERR_NULL, "adapters_backward: NULL input");
+        if (weights && !plan)
+            return fail(BITLOGIC_ERR_NULL, "adapters_backward: weights' gradients need a plan");
+        if (int rc = take_rows(who, a, n_rows, s.n_adapters, ids, plan))
+            return rc;
+        const size_t need = bitlogic_adapters_backward_workspace_bytes(set, n_rows);
+        if (!workspace || workspace_bytes < need)
+            return fail(BITLOGIC_ERR_WORKSPACE, "adapters_backward: workspace of %zu bytes, %zu "
+                        "needed", workspace_bytes, need);
+        if (!aligned(workspace, 16))
+            return fail(BITLOGIC_ERR_ALIGN, "adapters_backward: workspace not 16-byte aligned");
+    }
+    const auto l = bl::adapt::group_layout(n_rows, s.n_adapters);
+    const BackwardLayout b = backward_layout(s, n_rows);
+    char *ws = static_cast<char *>(workspace);
+    float *back = reinterpret_cast<float *>(ws + b.back);
+    bl::adapt::GradArgs g = {};
+    int32_t block = 0;
+    by_weight(s.weight_type, [&](auto W) {
+        block = bl::adapt::grad_block<decltype(W)::value>();
+        return hipSuccess;
+    });
+    if (weights) {
+        const char *p = static_cast<const char *>(plan);
+        g.rank = s.rank;
+        g.groups = s.n_adapters;
+        g.scales = s.scales;
+        g.scale = s.scale;
+        g.job[0].cols = s.n_in;
+        g.job[1].cols = s.n_out;
+        g.job[0].out = static_cast<char *>(grad_down);
+        g.job[1].out = static_cast<char *>(grad_up);
+        g.job[1].transposed = 1;
+        if (n_rows > 0) {
+            g.chunks = reinterpret_cast<const bl::adapt::Piece4 *>(p + l.chunks);
+            g.order = reinterpret_cast<const int32_t *>(p + l.order);
+            g.chunk_starts = reinterpret_cast<const int32_t *>(p + l.chunk_starts);
+            g.slot_starts = reinterpret_cast<const int32_t *>(p + l.slot_starts);
+            g.n_chunks = l.n_chunks;
+            g.job[0].y = static_cast<const char *>(x);
+            g.job[0].y_stride = x_stride * (int64_t)el;
+            g.job[0].y_i32 = x_type == BITLOGIC_LOGITS_I32;
+            g.job[0].blocks = grad_down ? (s.n_in + block - 1) / block : 0;
+            g.job[0].h = back;
+            g.job[0].partial = reinterpret_cast<float *>(ws + b.partial_down);
+            g.job[1].y = static_cast<const char *>(grad);
+            g.job[1].y_stride = grad_stride * (int64_t)el;
+            g.job[1].blocks = grad_up ? (s.n_out + block - 1) / block : 0;
+            g.job[1].h = hidden;
+            g.job[1].partial = reinterpret_cast<float *>(ws + b.partial_up);
+        }
+        if (g.n_chunks * ((int64_t)g.job[0].blocks + g.job[1].blocks) >= 1 << 24)
+            return fail(BITLOGIC_ERR_UNSUPPORTED, "adapters_backward: n_rows * (n_in + n_out) too "
+                        "large for one launch");
+    }
+    if (n_rows > 0 && (grad_x || grad_down)) {
+        a.x = static_cast<const char *>(grad);
+        a.x_stride = grad_stride * (int64_t)el;
+        a.w1 = static_cast<const char *>(s.up);
+        a.w2 = static_cast<const char *>(s.down);
+        a.w1_step = (int64_t)s.rank * s.n_out * (int64_t)el;
+        a.w2_step = (int64_t)s.rank * s.n_in * (int64_t)el;
+        a.k = s.n_out;
+        a.m = s.n_in;
+        a.rank = s.rank;
+        a.scales = s.scales;
+        a.scale = s.scale;
+        a.out = static_cast<char *>(grad_x);
+        a.out_stride = grad_x_stride * (int64_t)el;
+        a.hidden = grad_down ? back : nullptr;
+        const hipError_t err = by_weight(s.weight_type, [&](auto W) {
+            return bl::adapt::launch_pass<decltype(W)::value>(a, false, true,
+                                                              (hipStream_t)stream);
+        });
+        if (err != hipSuccess)
+            return hip_status(err, "adapters_backward launch");
+    }
+    if (!weights)
+        return ok();
+    return hip_status(by_weight(s.weight_type, [&](auto W) {
+        return bl::adapt::launch_grads<decltype(W)::value>(g, (hipStream_t)stream);
+    }), "adapters_backward launch");
 }
 
 int bitlogic_probe_valu(uint32_t *out, int32_t blocks, int32_t iters, uint32_t seed,

@@ -284,6 +284,10 @@ hipError_t launch_dropout(const void *x, int32_t type, int64_t n_rows, int32_t n
                           const uint64_t *offset_at, void *out, int64_t out_stride,
                           hipStream_t stream);
 
+// Rows by group (group_rows.hip); the plan's layout is in adapters.h.
+hipError_t launch_group_rows(const int32_t *ids, int64_t rows, int32_t groups, void *plan,
+                             hipStream_t stream);
+
 // Peak probes (probes.hip): kProbeThreads = 256 lanes a block.
 hipError_t launch_probe_valu(uint32_t *out, int32_t blocks, int32_t iters, uint32_t seed,
                              hipStream_t stream);

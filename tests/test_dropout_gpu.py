@@ -93,6 +93,9 @@ def test_offsets_and_refusals():
     _check(bl.bitlogic_dropout(on, 0.4, 2 ** 64 - 1, 2 ** 64 - 1), x, 0.4, 2 ** 64 - 1,
            2 ** 64 - 1)
     assert bl.bitlogic_dropout(on[:0], 0.4, 3).shape == (0, 70)
+    leaf = on[:0].clone().requires_grad_()
+    bl.bitlogic_dropout(leaf, 0.4, 3).sum().backward()
+    assert leaf.grad.shape == (0, 70)
     for seed, offset in ((-1, 0), (2 ** 64, 0), (0, -1), (0, 2 ** 64)):
         with pytest.raises(ValueError, match="seed and offset"):
             bl.bitlogic_dropout(on, 0.4, seed, offset)
