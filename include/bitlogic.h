@@ -634,13 +634,17 @@ int bitlogic_group_rows(const int32_t *ids, int64_t n_rows, int32_t n_groups, vo
  *           own stride (not int32), or memory apart from x and base
  *   hidden  float [n_rows][rank] or NULL: down_a x[s], 0 where there is no adapter; what the
  *           backward pass takes.  out may be NULL if hidden is not
- * Sums are held in 32 bits; down_a x goes into the second product to 2^-17 of itself or
- * better.  Results do not depend on how a launch is scheduled, nor a row's on other rows. */
+ * Sums are held in 32 bits; down_a x goes into the second product to 2^-17 of itself or, with
+ * float16 weights, 2^-22 of the row's largest.  Results do not depend on how a launch is
+ * scheduled, nor a row's on other rows' values.  The workspace (16-byte aligned) may hold
+ * anything, before and after; its bytes: for calls with a plan, or without. */
+size_t bitlogic_adapters_workspace_bytes(const bitlogic_adapter_set *set, int64_t n_rows,
+                                         int32_t planned);
 int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_stride,
                       const bitlogic_adapter_set *set, const int32_t *ids, const void *plan,
                       const void *base, int32_t base_type, int64_t base_stride,
                       float base_scale, void *out, int64_t out_stride, float *hidden,
-                      void *stream);
+                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* Backward: with g[s] the gradient of out[s] (weights' type, grad_stride >= 0),
  *   grad_x[s]   = scale_a down_a^T (up_a^T g[s]), 0 where there is no adapter; weights' type,

@@ -147,7 +147,8 @@ def load_library():
         "bitlogic_dropout": ([P, i32, i64, i32, i64, f32, u64, u64, P, P, i64, P], ctypes.c_int),
         "bitlogic_group_rows_bytes": ([i64, i32], sz),
         "bitlogic_group_rows": ([P, i64, i32, P, sz, P], ctypes.c_int),
-        "bitlogic_adapters": ([P, i32, i64, i64, P, P, P, P, i32, i64, f32, P, i64, P, P],
+        "bitlogic_adapters_workspace_bytes": ([P, i64, i32], sz),
+        "bitlogic_adapters": ([P, i32, i64, i64, P, P, P, P, i32, i64, f32, P, i64, P, P, sz, P],
                               ctypes.c_int),
         "bitlogic_adapters_backward_workspace_bytes": ([P, i64], sz),
         "bitlogic_adapters_backward": ([P, i64, i64, P, i32, i64, P, P, P, P, P, i64, P, P, P,
@@ -1105,7 +1106,8 @@ def bitlogic_adapters(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
                       ids: Optional[torch.Tensor], scales=1.0,
                       base: Optional[torch.Tensor] = None, base_scale: float = 1.0,
                       plan: Optional[RowGroups] = None, out: Optional[torch.Tensor] = None,
-                      hidden: Optional[torch.Tensor] = None, stream=None,
+                      hidden: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None,
                       want_hidden: bool = False):
     """Low-rank adapters of many requests beside a shared projection: row s of x [N][f] with
     a = ids[s] (int32 [N]; outside the adapters: none) gets
@@ -1132,11 +1134,14 @@ def bitlogic_adapters(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
     if hidden is None and want_hidden:
         hidden = _empty((n, s.rank), torch.float32, dev, stream)
     ids_ptr, plan_ptr, plan = _grouped(ids, plan, n, s.n_adapters, dev, stream)
-    _call(dev, load_library().bitlogic_adapters, ptr, _LOGITS[x.dtype], n, stride,
+    lib = load_library()
+    need = int(lib.bitlogic_adapters_workspace_bytes(ctypes.addressof(s), n, plan is not None))
+    ws_ptr, ws_bytes = _workspace(need, dev, workspace, stream)
+    _call(dev, lib.bitlogic_adapters, ptr, _LOGITS[x.dtype], n, stride,
           ctypes.addressof(s), ids_ptr, plan_ptr, base_ptr, base_type, base_stride, base_scale,
           out_ptr, out_stride,
           _like(hidden, "hidden", _F32, (n, s.rank), dev) if hidden is not None else None,
-          _stream(stream, dev))
+          ws_ptr, ws_bytes, _stream(stream, dev))
     return out, hidden
 
 

@@ -26,23 +26,27 @@ struct Piece4 {
 };
 
 // ---- the plan: rows by group ----
+// Gradients of the weights are partial sums over chunks of a group's rows.  The plan has the
+// chunks of two cuts: small ones give narrow adapters blocks enough, large ones keep the
+// partial sums of wide adapters few.
+struct CutLayout {
+    size_t chunks, starts, slots;
+    int64_t n, n_slots;
+    int32_t rows;
+};
 struct GroupLayout {
-    size_t order, starts, tile_starts, chunk_starts, slot_starts, tiles, chunks, totals, counts,
-        bytes;
-    int64_t n_tiles, n_chunks, n_slots, run;
-    int32_t chunk, runs;
+    size_t order, starts, tile_starts, tiles, totals, counts, bytes;
+    CutLayout cut[2];
+    int64_t n_tiles, run;
+    int32_t runs;
 };
 
-// chunk: rows that a gradient's partial sum goes over, whole tiles; a sixty-fourth of the rows
-// within limits, so that partial sums stay small beside the rows they are made of.
 inline GroupLayout group_layout(int64_t n_rows, int32_t groups)
 {
     GroupLayout l;
-    l.chunk = (int32_t)std::min<int64_t>(4096, std::max<int64_t>(256, n_rows / 64 / 32 * 32));
+    const int64_t small = std::max<int64_t>(256, n_rows / 1024 / kTile * kTile);
     l.n_tiles = n_rows / kTile + groups + 1;              // at most a partial one a group
-    l.n_chunks = n_rows / l.chunk + groups + 1;
-    l.n_slots = 2 * (n_rows / l.chunk);                   // k > 1 chunks: over (k - 1) chunk rows
-    l.run = std::max<int64_t>(1024, (n_rows + kMaxRuns - 1) / kMaxRuns);
+    l.run = std::max<int64_t>(256, (n_rows + kMaxRuns - 1) / kMaxRuns);
     l.run = (l.run + 63) / 64 * 64;
     l.runs = (int32_t)((n_rows + l.run - 1) / l.run);
     size_t at = 0;
@@ -55,22 +59,35 @@ inline GroupLayout group_layout(int64_t n_rows, int32_t groups)
     l.order = take((size_t)n_rows * 4);
     l.starts = take(all * 4);
     l.tile_starts = take(all * 4);
-    l.chunk_starts = take(all * 4);
-    l.slot_starts = take(all * 4);
     l.tiles = take((size_t)l.n_tiles * sizeof(Piece4));
-    l.chunks = take((size_t)l.n_chunks * sizeof(Piece4));
+    for (int c = 0; c < 2; ++c) {
+        CutLayout &k = l.cut[c];
+        k.rows = (int32_t)(c ? 4 * small : small);
+        k.n = n_rows / k.rows + groups + 1;
+        k.n_slots = 2 * (n_rows / k.rows);                // k > 1 chunks: over (k - 1) rows rows
+        k.chunks = take((size_t)k.n * sizeof(Piece4));
+        k.starts = take(all * 4);
+        k.slots = take(all * 4);
+    }
     l.totals = take(all * 4);
     l.counts = take((size_t)l.runs * (groups + 1) * 4);
     l.bytes = at;
     return l;
 }
 
+struct Cut {
+    Piece4 *chunks;
+    int32_t *starts, *slots;
+    int64_t n;
+    int32_t rows;
+};
 struct GroupArgs {
     const int32_t *ids;
-    int64_t rows, n_tiles, n_chunks, run;
-    int32_t groups, chunk, runs;
-    int32_t *order, *starts, *tile_starts, *chunk_starts, *slot_starts;
-    Piece4 *tiles, *chunks;
+    int64_t rows, n_tiles, run;
+    int32_t groups, runs;
+    int32_t *order, *starts, *tile_starts;
+    Piece4 *tiles;
+    Cut cut[2];
     uint32_t *totals, *counts;
 };
 
@@ -96,9 +113,44 @@ struct PassArgs {
     // rows by a plan, or (tiles NULL) a tile each by their ids
     const Piece4 *tiles;
     const int32_t *order, *ids;
-    int64_t n_tiles;
-    int32_t splits;                     // blocks a tile, each with its columns of out
+    int64_t n_rows, n_tiles;
+    // wide adapters: h by parts [splits][n_rows][rank] (hidden itself, if that is one part);
+    // splits 0: narrow ones, in one kernel
+    float *partial;
+    int32_t splits;
 };
+
+// One kernel, a wave a tile, where rows come by a plan and a row of x and one of out are a few
+// units of 128 bytes each.
+inline bool is_narrow(bool planned, int32_t k, int32_t m, int32_t el_bytes)
+{
+    return planned && k <= 1024 / el_bytes && m <= 1024 / el_bytes;
+}
+
+// Parts of the k terms of wide adapters: for about 2048 blocks of 4 waves, each wave with a unit
+// of 128 bytes or more.
+inline int32_t split_terms(int64_t n_tiles, int32_t k, int32_t el_bytes)
+{
+    const int64_t most = ((int64_t)k * el_bytes + 511) / 512;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({most, 16, 2048 / n_tiles}));
+}
+
+struct PassLayout {
+    bool narrow;
+    int64_t n_tiles;
+    int32_t splits;
+    size_t bytes;                       // of partial
+};
+inline PassLayout pass_layout(int64_t n_rows, int32_t groups, int32_t rank, int32_t k, int32_t m,
+                              int32_t el_bytes, bool planned)
+{
+    PassLayout l;
+    l.n_tiles = planned ? group_layout(n_rows, groups).n_tiles : n_rows;
+    l.narrow = is_narrow(planned, k, m, el_bytes);
+    l.splits = l.narrow || n_rows == 0 ? 0 : split_terms(l.n_tiles, k, el_bytes);
+    l.bytes = (size_t)l.splits * n_rows * rank * 4;
+    return l;
+}
 
 // Gradients: d down [groups][rank][n_in] = sum scale back x^T, d up [groups][n_out][rank] =
 // sum scale grad hidden^T, over a group's rows.

@@ -2,17 +2,23 @@
 // float16, bfloat16); x of type X, W or int32.
 //
 // A tile has up to 32 rows of one adapter.  out = base + scale up (down x) is two products on
-// the matrix cores, the small one in between never leaving the registers:
+// the matrix cores:
 //
-//   h [rank][rows]    = down [rank][k] x^T [k][rows]      (k long: its waves split it, LDS joins)
-//   out^T [m][rows]   = up [m][rank] h [rank][rows]       (m long: its waves split it)
+//   h [rank][rows]    = down [rank][k] x^T [k][rows]
+//   out^T [m][rows]   = up [m][rank] h [rank][rows]
 //
 // With rows in the columns of both, a lane ends the first product with h at row l % 16 and
 // ranks 4 (l / 16) + i, i < 4 (l its place in the wave), which is what it has to hand to the
-// second, if the order of its terms is chosen so: no exchange between lanes.  16-bit weights
-// take h as the sum of two bfloat16 (h to 2^-17 of itself; one alone would round it to 2^-9),
-// in the two halves of one instruction's terms.  float16 weights are split alike for this
-// product, since h may be past float16's range; their first product is in float16.
+// second, if the order of its terms is chosen so.  Narrow adapters are one kernel, a wave a
+// tile, and h never leaves its registers.  Wide ones are two, k_shrink with the k terms dealt to
+// waves and blocks and k_expand with the m columns, since a tile's waves alone are too few to
+// keep memory busy (8192 rows, 4096 -> 4096, rank 64: 162 us in one kernel of 4 waves a tile);
+// h goes through the workspace, a few bytes beside the row it is made of.
+//
+// 16-bit weights take h as the sum of two terms of their type, in the two halves of one
+// instruction's terms: 2^-17 of h in bfloat16, 2^-22 of the row's largest in float16, whose
+// rows of h are scaled by powers of two, since h may be past its range.  One term alone would
+// round h to 2^-9 or 2^-12.
 //
 // Operands come from memory in the lanes' own layout, 16 bytes a load, without LDS: a row's
 // 128 bytes by 8 loads of 16 lanes each.  Where a matrix lies the other way round (the
@@ -131,47 +137,67 @@ __device__ __forceinline__ Frag to_terms(Frag f)          // int32 terms as floa
     return f;
 }
 
-// The rows' h as terms of the second product: 4 ranks, in 16-bit types their two parts.
-template <int W>
-__device__ __forceinline__ Frag h_terms(f32x4 h)
+// A tile's h as terms of the second product, by 4 ranks: in 16-bit types their two parts.
+// factor: what the rows' sums are to be multiplied by for it.
+template <int W, int RT, int CT>
+__device__ __forceinline__ void make_terms(const f32x4 (&h)[RT][CT], Frag (&terms)[RT][CT],
+                                           float (&factor)[RT])
 {
-    Frag f;
-    if constexpr (W == kF32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f.w[i] = __float_as_uint(h[i]);
-    } else {
-        uint32_t hi[4], lo[4];
+    for (int rt = 0; rt < RT; ++rt) {
+        factor[rt] = 1.0f;
+        float up = 1.0f;
+        if constexpr (W == kF16) {
+            // the row's largest to [2^8, 2^9): parts of it down to 2^-24 remain
+            float most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            split(h[i], hi[i], lo[i]);
-        f.w[0] = hi[0] | hi[1] << 16;
-        f.w[1] = hi[2] | hi[3] << 16;
-        f.w[2] = lo[0] | lo[1] << 16;
-        f.w[3] = lo[2] | lo[3] << 16;
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    most = fmaxf(most, fabsf(h[rt][ct][i]));
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const int power = min(max(262 - (int)(__float_as_uint(most) >> 23), 1), 253);
+            up = __uint_as_float((uint32_t)power << 23);
+            factor[rt] = __uint_as_float((uint32_t)(254 - power) << 23);
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            Frag &f = terms[rt][ct];
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (W == kF32) {
+                    f.w[i] = __float_as_uint(h[rt][ct][i]);
+                } else if constexpr (W == kBf16) {
+                    split(h[rt][ct][i], hi[i], lo[i]);
+                } else {
+                    const float v = h[rt][ct][i] * up;
+                    const _Float16 part = (_Float16)v;
+                    const float rest = v - (float)part;
+                    hi[i] = __builtin_bit_cast(uint16_t, part);
+                    lo[i] = __builtin_bit_cast(uint16_t, (_Float16)((hi[i] & 0x7FFFu) == 0x7C00u
+                                                                        ? 0.0f : rest));
+                }
+            }
+            if constexpr (W != kF32) {
+                f.w[0] = hi[0] | hi[1] << 16;
+                f.w[1] = hi[2] | hi[3] << 16;
+                f.w[2] = lo[0] | lo[1] << 16;
+                f.w[3] = lo[2] | lo[3] << 16;
+            }
+        }
     }
-    return f;
 }
 
 // c += w h for 4 ranks of w (two words of 16-bit weights, four of float32).
 template <int W>
 __device__ __forceinline__ f32x4 mma_h(const uint32_t (&w)[kSize<W>], Frag h, f32x4 c)
 {
-    if constexpr (W == kF32) {
+    if constexpr (W == kF32)
         return mma_f32({w[0], w[1], w[2], w[3]}, h, c);
-    } else if constexpr (W == kBf16) {
-        return mma_bf16({w[0], w[1], w[0], w[1]}, h, c);
-    } else {
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint16_t bits = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-            split((float)__builtin_bit_cast(_Float16, bits), hi[i], lo[i]);
-        }
-        const uint32_t h0 = hi[0] | hi[1] << 16, h1 = hi[2] | hi[3] << 16;
-        const uint32_t l0 = lo[0] | lo[1] << 16, l1 = lo[2] | lo[3] << 16;
-        return mma_bf16({l0, l1, l0, l1}, h, mma_bf16({h0, h1, h0, h1}, h, c));
-    }
+    else
+        return mma<W>({w[0], w[1], w[0], w[1]}, h, c);
 }
 
 // base and out of one row: out columns [m, m + kEls) from their sums, as many as there are.
@@ -227,193 +253,184 @@ struct Output {
     }
 };
 
-// NW waves a tile (1: a block has four tiles, each wave its own), 16 RT rows of it, 16 CT
-// ranks.
-template <int W, int X, int CT, int RT, int NW, bool BACK>
-__global__ __launch_bounds__(NW == 1 ? 256 : NW * kWave) void k_pass(PassArgs a)
-{
-    constexpr int E = kEls<W>, S = kSize<W>, kUnit = 2 * 4 * E;   // terms of 128 bytes of a row
-    constexpr int kAcc = CT * RT * 4;
-    __shared__ float joined[NW > 1 ? NW * kAcc * kWave : 1];
-    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
-    const int wave = NW > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) : 0;
-    int64_t tile = blockIdx.x / a.splits;
-    const int split_at = (int)(blockIdx.x - tile * a.splits);
-    if constexpr (NW == 1) {
-        tile = tile * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-        if (tile >= a.n_tiles)
-            return;
-    }
+// A tile and the lane's rows in it: 16 rt + l % 16.
+template <int RT>
+struct Tile {
     Piece4 p;
-    if (a.tiles) {
-        p = a.tiles[tile];
-        if (p.group < 0)
-            return;
-    } else {
-        const int32_t id = a.ids[tile];
-        p = {id >= 0 && id < a.groups ? id : a.groups, (int32_t)tile, 1, 0};
-    }
     int32_t row[RT];
     bool there[RT];
+
+    // false: no tile
+    __device__ __forceinline__ bool take(const PassArgs &a, int64_t tile, int col)
+    {
+        if (a.tiles) {
+            p = a.tiles[tile];
+            if (p.group < 0)
+                return false;
+        } else {
+            const int32_t id = a.ids[tile];
+            p = {id >= 0 && id < a.groups ? id : a.groups, (int32_t)tile, 1, 0};
+        }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int32_t at = rt * 16 + col;
-        there[rt] = at < p.count;
-        const int32_t place = p.first + (there[rt] ? at : 0);
-        row[rt] = a.order ? a.order[place] : place;
+        for (int rt = 0; rt < RT; ++rt) {
+            const int32_t at = rt * 16 + col;
+            there[rt] = at < p.count;
+            const int32_t place = p.first + (there[rt] ? at : 0);
+            row[rt] = a.order ? a.order[place] : place;
+        }
+        return true;
     }
-    const bool adapted = p.group < a.groups;
-    f32x4 h[RT][CT];
+};
+
+// h += w1 x over terms [from, to): units of 128 bytes of a row, every `deal`-th from the
+// `turn`-th on; `to` is k or a multiple of the unit.
+template <int W, int X, int CT, int RT, bool BACK>
+__device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, int col, int quad,
+                                       int32_t from, int32_t to, int turn, int deal,
+                                       f32x4 (&h)[RT][CT])
+{
+    constexpr int E = kEls<W>, S = kSize<W>, kUnit = 8 * E;
+    const char *x[RT], *w1[CT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+        x[rt] = a.x + tile.row[rt] * a.x_stride;
+    const char *first = a.w1 + tile.p.group * a.w1_step;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        // ranks behind the last one read its weights: what comes of it is cleared afterwards
+        const int32_t r = min(ct * 16 + col, a.rank - 1);
+        w1[ct] = first + (BACK ? (int64_t)r : (int64_t)r * a.k) * S;
+    }
+    const auto load_w1 = [&](int ct, int32_t k, int32_t left) __attribute__((always_inline)) {
+        if constexpr (!BACK) {
+            return load_frag<W>(w1[ct] + (int64_t)k * S, left);
+        } else {
+            Frag f;
+            const char *at = w1[ct] + (int64_t)k * a.rank * S;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                f.w[i] = 0;
+#pragma unroll
+            for (int u = 0; u < E; ++u)
+                if (u < left) {
+                    const char *el = at + (int64_t)u * a.rank * S;
+                    if constexpr (S == 4)
+                        f.w[u] = *reinterpret_cast<const uint32_t *>(el);
+                    else
+                        f.w[u / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(el)
+                                      << (16 * (u & 1));
+                }
+            return f;
+        }
+    };
+    const auto step = [&](int32_t k0, bool whole) __attribute__((always_inline)) {
+        Frag fx[2][RT], fw[2][CT];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int32_t k = k0 + half * 4 * E + quad * E;
+            const int32_t left = whole ? E : a.k - k;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                fx[half][rt] = load_frag<W>(x[rt] + (int64_t)k * S, left);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+                fw[half][ct] = load_w1(ct, k, left);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const Frag t = to_terms<X>(fx[half][rt]);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    h[rt][ct] = mma<W>(fw[half][ct], t, h[rt][ct]);
+            }
+    };
+    const int32_t whole = min(to, a.k / kUnit * kUnit);
+    int32_t k0 = from + turn * kUnit;
+#pragma unroll(CT <= 2 ? 2 : 1)
+    for (; k0 < whole; k0 += deal * kUnit)
+        step(k0, true);
+    if (k0 < to)
+        step(k0, false);
+}
+
+template <int RT, int CT>
+__device__ __forceinline__ void clear(f32x4 (&h)[RT][CT])
+{
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
             h[rt][ct] = f32x4{0, 0, 0, 0};
-    if (adapted) {
-        // ---- h = w1 x ----
-        const char *x[RT], *w1[CT];
+}
+
+template <int RT, int CT>
+__device__ __forceinline__ void clear_past_rank(int32_t rank, int quad, f32x4 (&h)[RT][CT])
+{
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-            x[rt] = a.x + row[rt] * a.x_stride;
-        const char *first = a.w1 + p.group * a.w1_step;
+    for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            // ranks behind the last one read its weights: what comes of it is cleared below
-            const int32_t r = min(ct * 16 + col, a.rank - 1);
-            w1[ct] = first + (BACK ? (int64_t)r : (int64_t)r * a.k) * S;
-        }
-        const auto load_w1 = [&](int ct, int32_t k, int32_t left) __attribute__((always_inline)) {
-            if constexpr (!BACK) {
-                return load_frag<W>(w1[ct] + (int64_t)k * S, left);
-            } else {
-                Frag f;
-                const char *at = w1[ct] + (int64_t)k * a.rank * S;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    f.w[i] = 0;
-#pragma unroll
-                for (int u = 0; u < E; ++u)
-                    if (u < left) {
-                        const char *el = at + (int64_t)u * a.rank * S;
-                        if constexpr (S == 4)
-                            f.w[u] = *reinterpret_cast<const uint32_t *>(el);
-                        else
-                            f.w[u / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(el)
-                                          << (16 * (u & 1));
-                    }
-                return f;
-            }
-        };
-        const auto step = [&](int32_t k0, bool whole) __attribute__((always_inline)) {
-            Frag fx[2][RT], fw[2][CT];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int32_t k = k0 + half * 4 * E + quad * E;
-                const int32_t left = whole ? E : a.k - k;
+        for (int i = 0; i < 4; ++i)
+            if (ct * 16 + quad * 4 + i >= rank)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    fx[half][rt] = load_frag<W>(x[rt] + (int64_t)k * S, left);
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-                    fw[half][ct] = load_w1(ct, k, left);
-            }
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const Frag t = to_terms<X>(fx[half][rt]);
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
-                        h[rt][ct] = mma<W>(fw[half][ct], t, h[rt][ct]);
-                }
-        };
-        const int32_t whole = a.k / kUnit * kUnit;
-        int32_t k0 = wave * kUnit;
-#pragma unroll(CT <= 2 ? 2 : 1)
-        for (; k0 < whole; k0 += NW * kUnit)
-            step(k0, true);
-        if (k0 < a.k)
-            step(k0, false);
-        // ---- the waves' parts, joined in order ----
-        if constexpr (NW > 1) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        joined[(wave * kAcc + (rt * CT + ct) * 4 + i) * kWave + lane] =
-                            h[rt][ct][i];
-            __syncthreads();
-            for (int e = threadIdx.x; e < kAcc * kWave; e += NW * kWave) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w)
-                    sum += joined[w * kAcc * kWave + e];
-                joined[e] = sum;                          // (only this lane reads or writes e)
-            }
-            __syncthreads();
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        h[rt][ct][i] = joined[((rt * CT + ct) * 4 + i) * kWave + lane];
-        }
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (ct * 16 + quad * 4 + i >= a.rank)
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-                        h[rt][ct][i] = 0.0f;
-    }
-    if (a.hidden && split_at == 0 && wave == 0) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-            if (there[rt])
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int32_t r = ct * 16 + quad * 4 + i;
-                        if (r < a.rank)
-                            a.hidden[(int64_t)row[rt] * a.rank + r] = h[rt][ct][i];
-                    }
-    }
-    if (!a.out)
-        return;
-    // ---- out = base + scale w2 h ----
-    Output<W> o[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        o[rt].base = a.base ? a.base + row[rt] * a.base_stride : nullptr;
-        o[rt].out = a.out + row[rt] * a.out_stride;
-        o[rt].base_i32 = a.base_i32;
-        o[rt].there = there[rt];
-        o[rt].base_scale = a.base_scale;
-        o[rt].scale = !adapted ? 0.0f : a.scales ? a.scales[p.group] : a.scale;
-        o[rt].m = a.m;
-    }
-    Frag terms[RT][CT];
+                    h[rt][ct][i] = 0.0f;
+}
+
+template <int RT, int CT>
+__device__ __forceinline__ void store_hidden(float *to, int32_t rank, const Tile<RT> &tile,
+                                             int quad, const f32x4 (&h)[RT][CT])
+{
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
+        if (tile.there[rt])
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-            terms[rt][ct] = h_terms<W>(h[rt][ct]);
-    const char *w2 = a.w2 + (adapted ? p.group * a.w2_step : 0);
+            for (int ct = 0; ct < CT; ++ct) {
+                const int32_t r = ct * 16 + quad * 4;
+                float *at = to + (int64_t)tile.row[rt] * rank + r;
+                if (r + 4 <= rank) {
+                    __builtin_memcpy(at, &h[rt][ct], 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i)
+                        if (r + i < rank)
+                            at[i] = h[rt][ct][i];
+                }
+            }
+}
+
+// out = base + scale w2 h: units of columns, every `deal`-th from the `turn`-th on.
+template <int W, int CT, int RT, bool BACK>
+__device__ __forceinline__ void expand(const PassArgs &a, const Tile<RT> &tile, int col, int quad,
+                                       int turn, int deal, const f32x4 (&h)[RT][CT])
+{
+    constexpr int E = kEls<W>, S = kSize<W>;
+    const bool adapted = tile.p.group < a.groups;
+    Frag terms[RT][CT];
+    float factor[RT];
+    make_terms<W>(h, terms, factor);
+    Output<W> o[RT];
+    const float scale = !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        o[rt].base = a.base ? a.base + tile.row[rt] * a.base_stride : nullptr;
+        o[rt].out = a.out + tile.row[rt] * a.out_stride;
+        o[rt].base_i32 = a.base_i32;
+        o[rt].there = tile.there[rt];
+        o[rt].base_scale = a.base_scale;
+        o[rt].scale = scale * factor[rt];
+        o[rt].m = a.m;
+    }
+    const char *w2 = a.w2 + (adapted ? tile.p.group * a.w2_step : 0);
     if constexpr (!BACK) {
         // a unit: two tiles of 16 columns.  16-bit types give a lane 8 neighbours of them.
-        constexpr int kCols = 32;
+        constexpr int kCols = 32, kPieces = S == 2 ? 1 : 2;
         const bool fours = a.rank % 4 == 0;
         const auto column = [&](int t, int place) __attribute__((always_inline)) {
             return S == 2 ? place / 4 * 8 + t * 4 + place % 4 : t * 16 + place;
         };
-        for (int32_t m0 = (split_at * NW + wave) * kCols; m0 < a.m;
-             m0 += a.splits * NW * kCols) {
-            constexpr int kPieces = S == 2 ? 1 : 2;
+        for (int32_t m0 = turn * kCols; m0 < a.m; m0 += deal * kCols) {
             Frag b[RT][kPieces];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
@@ -421,11 +438,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * kWave) void k_pass(PassArgs a)
                 for (int i = 0; i < kPieces; ++i)
                     b[rt][i] = o[rt].load_base(m0 + i * 16 + quad * E);
             f32x4 sum[2][RT];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    sum[t][rt] = f32x4{0, 0, 0, 0};
+            clear(sum);
             if (adapted)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -468,14 +481,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * kWave) void k_pass(PassArgs a)
     } else {
         // a unit: E tiles of 16 columns; tile t has columns t, E + t, 2 E + t, ...
         constexpr int kCols = 16 * E;
-        for (int32_t m0 = (split_at * NW + wave) * kCols; m0 < a.m;
-             m0 += a.splits * NW * kCols) {
+        for (int32_t m0 = turn * kCols; m0 < a.m; m0 += deal * kCols) {
             f32x4 sum[E][RT];
-#pragma unroll
-            for (int t = 0; t < E; ++t)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    sum[t][rt] = f32x4{0, 0, 0, 0};
+            clear(sum);
             if (adapted)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
@@ -494,8 +502,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * kWave) void k_pass(PassArgs a)
                             for (int i = 0; i < 4; ++i)
                                 w[i] = f[i].w[t];
                         } else {
-                            constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-                            const uint32_t pick = t & 1 ? kHigh : kLow;
+                            const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
                             for (int i = 0; i < 2; ++i)
                                 w[i] = __builtin_amdgcn_perm(f[2 * i + 1].w[t / 2],
@@ -521,27 +528,155 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * kWave) void k_pass(PassArgs a)
     }
 }
 
+// ---- narrow adapters: a wave a tile ----
+template <int W, int X, int CT, bool BACK>
+__global__ __launch_bounds__(256) void k_narrow(PassArgs a)
+{
+    constexpr int RT = kTile / 16;
+    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
+    const int64_t at = (int64_t)blockIdx.x * 4 +
+                       __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    Tile<RT> tile;
+    if (at >= a.n_tiles || !tile.take(a, at, col))
+        return;
+    f32x4 h[RT][CT];
+    clear(h);
+    if (tile.p.group < a.groups) {
+        shrink<W, X, CT, RT, BACK>(a, tile, col, quad, 0, a.k, 0, 1, h);
+        clear_past_rank(a.rank, quad, h);
+    }
+    if (a.hidden)
+        store_hidden(a.hidden, a.rank, tile, quad, h);
+    if (a.out)
+        expand<W, CT, RT, BACK>(a, tile, col, quad, 0, 1, h);
+}
+
+// ---- wide adapters ----
+constexpr int kWideWaves = 4;
+
+// Part `blockIdx % splits` of a tile's h, to [part][row][rank].
+template <int W, int X, int CT, int RT, bool BACK>
+__global__ __launch_bounds__(kWideWaves * kWave) void k_shrink(PassArgs a)
+{
+    constexpr int NW = kWideWaves, kAcc = CT * RT * 4, kUnit = 8 * kEls<W>;
+    __shared__ float joined[NW * kAcc * kWave];
+    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t at = blockIdx.x / a.splits;
+    const int part = (int)(blockIdx.x - at * a.splits);
+    Tile<RT> tile;
+    if (!tile.take(a, at, col))
+        return;
+    f32x4 h[RT][CT];
+    clear(h);
+    if (tile.p.group < a.groups) {
+        const int32_t units = (a.k + kUnit - 1) / kUnit;
+        const int32_t each = (units + a.splits - 1) / a.splits;
+        const int32_t from = min(part * each, units) * kUnit;
+        const int32_t to = min(min((part + 1) * each, units) * kUnit, a.k);
+        shrink<W, X, CT, RT, BACK>(a, tile, col, quad, from, to, wave, NW, h);
+        clear_past_rank(a.rank, quad, h);
+        // the waves' sums, added in order; each wave adds up some of them
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    joined[(wave * kAcc + (rt * CT + ct) * 4 + i) * kWave + lane] = h[rt][ct][i];
+        __syncthreads();
+    }
+    // wave w stores fragments w, w + NW, ... of the tile's RT * CT
+#pragma unroll
+    for (int f = 0; f < RT * CT; ++f) {
+        if (f % NW != wave)
+            continue;
+        f32x4 sum = {0, 0, 0, 0};
+        if (tile.p.group < a.groups)
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sum[i] += joined[(w * kAcc + f * 4 + i) * kWave + lane];
+        const int rt = f / CT, r = f % CT * 16 + quad * 4;
+        if (!tile.there[rt] || r >= a.rank)
+            continue;
+        float *to = a.partial + ((int64_t)part * a.n_rows + tile.row[rt]) * a.rank + r;
+        if (r + 4 <= a.rank) {
+            __builtin_memcpy(to, &sum, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (r + i < a.rank)
+                    to[i] = sum[i];
+        }
+    }
+}
+
+template <int W, int CT, int RT, bool BACK>
+__global__ __launch_bounds__(kWideWaves * kWave) void k_expand(PassArgs a, int32_t blocks)
+{
+    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t at = blockIdx.x / blocks;
+    const int block = (int)(blockIdx.x - at * blocks);
+    Tile<RT> tile;
+    if (!tile.take(a, at, col))
+        return;
+    f32x4 h[RT][CT];
+    clear(h);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const int32_t r = ct * 16 + quad * 4;
+            const float *from = a.partial + (int64_t)tile.row[rt] * a.rank + r;
+            for (int32_t p = 0; p < a.splits; ++p, from += a.n_rows * a.rank) {
+                f32x4 one = {0, 0, 0, 0};
+                if (r + 4 <= a.rank) {
+                    __builtin_memcpy(&one, from, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i)
+                        if (r + i < a.rank)
+                            one[i] = from[i];
+                }
+                h[rt][ct] += one;
+            }
+        }
+    if (a.hidden && a.hidden != a.partial && block == 0 && wave == 0)
+        store_hidden(a.hidden, a.rank, tile, quad, h);
+    if (a.out)
+        expand<W, CT, RT, BACK>(a, tile, col, quad, block * kWideWaves + wave,
+                                blocks * kWideWaves, h);
+}
+
 template <int W, int X, int CT, bool BACK>
 hipError_t pass_of(const PassArgs &a, hipStream_t stream)
 {
-    // one wave a tile where a tile's two products are a few units of 128 bytes each
-    constexpr int kNarrow = 8 * 128 / kSize<W>;
-    constexpr int NW = CT > 2 ? 4 : 8;
-    PassArgs b = a;
-    b.splits = 1;
-    if (a.tiles && a.k <= kNarrow && a.m <= kNarrow) {
-        hipLaunchKernelGGL((k_pass<W, X, CT, 2, 1, BACK>), dim3((uint32_t)((a.n_tiles + 3) / 4)),
-                           dim3(256), 0, stream, b);
+    if (a.splits == 0) {
+        hipLaunchKernelGGL((k_narrow<W, X, CT, BACK>), dim3((uint32_t)((a.n_tiles + 3) / 4)),
+                           dim3(256), 0, stream, a);
         return hipGetLastError();
     }
-    // few tiles: several blocks a tile, which share its columns (and all take its h)
-    const int64_t most = (a.m + 128 * NW - 1) / (128 * NW);
-    b.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, 512 / a.n_tiles));
-    const dim3 grid((uint32_t)(a.n_tiles * b.splits));
+    constexpr int kThreads = kWideWaves * kWave;
+    const dim3 parts((uint32_t)(a.n_tiles * a.splits));
     if (a.tiles)
-        hipLaunchKernelGGL((k_pass<W, X, CT, 2, NW, BACK>), grid, dim3(NW * kWave), 0, stream, b);
+        hipLaunchKernelGGL((k_shrink<W, X, CT, 2, BACK>), parts, dim3(kThreads), 0, stream, a);
     else
-        hipLaunchKernelGGL((k_pass<W, X, CT, 1, NW, BACK>), grid, dim3(NW * kWave), 0, stream, b);
+        hipLaunchKernelGGL((k_shrink<W, X, CT, 1, BACK>), parts, dim3(kThreads), 0, stream, a);
+    if (hipError_t err = hipGetLastError(); err != hipSuccess)
+        return err;
+    if (!a.out && a.hidden == a.partial)
+        return hipSuccess;
+    // columns by blocks of 512, as far as that makes fewer than 2^14 blocks
+    const int64_t want = std::max<int64_t>(1, (1 << 14) / a.n_tiles);
+    const int32_t blocks = (int32_t)std::min<int64_t>(a.out ? (a.m + 511) / 512 : 1, want);
+    const dim3 grid((uint32_t)(a.n_tiles * blocks));
+    if (a.tiles)
+        hipLaunchKernelGGL((k_expand<W, CT, 2, BACK>), grid, dim3(kThreads), 0, stream, a, blocks);
+    else
+        hipLaunchKernelGGL((k_expand<W, CT, 1, BACK>), grid, dim3(kThreads), 0, stream, a, blocks);
     return hipGetLastError();
 }
 
@@ -558,15 +693,19 @@ hipError_t pass_by_rank(const PassArgs &a, hipStream_t stream)
 }
 
 // ---- gradients of the weights ----
-// D [rank][cols] = sum over a chunk's rows of h[row][rank] y[row][col]: a wave has 16 E
-// columns, 32 rows (16 in float32) a step; a lane loads E columns of 8 (4) rows and turns
-// them by byte permutes into the terms of E products, whose columns are t, E + t, ...
-// h and, where they are no bfloat16, y are taken as sums of two bfloat16, as above.
+// D [rank][cols] = sum over a chunk's rows of h[row][rank] y[row][col]: a block has 16 E
+// columns, and its waves share the rows, 32 (16 in float32) a step; a lane loads E columns of
+// 8 (4) rows and turns them by byte permutes into the terms of E products, whose columns are
+// t, E + t, ...  h is taken as the sum of two bfloat16 as above, float16 y too, since h may be
+// past float16's range and its rows are summed here, so that they have no scale of their own.
+constexpr int kGradWaves = 4;
 
 template <int W, int CT>
-__global__ __launch_bounds__(256) void k_grads(GradArgs a)
+__global__ __launch_bounds__(kGradWaves * kWave) void k_grads(GradArgs a)
 {
     constexpr int E = kEls<W>, S = kSize<W>, kRows = S == 4 ? 4 : 8;   // rows a lane and step
+    constexpr int NW = kGradWaves, kStep = 4 * kRows;
+    __shared__ float joined[NW * E * 4 * kWave];
     const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int32_t blocks = a.job[0].blocks + a.job[1].blocks;
@@ -578,32 +717,49 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a)
     const Piece4 p = a.chunks[chunk];
     if (p.group < 0 || p.group >= a.groups)
         return;
-    const int32_t c0 = (block * 4 + wave) * 16 * E;
-    if (c0 >= j.cols)
-        return;
-    const int32_t at = c0 + col * E, left = max(j.cols - at, 0);
+    const int32_t c0 = block * 16 * E, at = c0 + col * E, left = max(j.cols - at, 0);
+    const bool whole_block = c0 + 16 * E <= j.cols;
     f32x4 sum[CT][E];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int t = 0; t < E; ++t)
-            sum[ct][t] = f32x4{0, 0, 0, 0};
+    clear(sum);
     const char *y = j.y + (left > 0 ? (int64_t)at * S : 0);
-    for (int32_t s = 0; s < p.count; s += 4 * kRows) {
+    const int32_t *order = a.order + p.first;
+    for (int32_t s = wave * kStep; s < p.count; s += NW * kStep) {
+        const bool whole_step = s + kStep <= p.count;
         Frag f[kRows];
         float hv[CT][kRows];
+        int32_t row[kRows];
+        if (whole_step) {
+            __builtin_memcpy(row, order + s + quad * kRows, sizeof row);
+        } else {
 #pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            const int32_t place = s + quad * kRows + u;
-            const bool there = place < p.count;
-            const int64_t row = a.order[p.first + (there ? place : 0)];
-            f[u] = load_frag<W>(y + row * j.y_stride, there ? left : 0);
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const int32_t r = ct * 16 + col;
-                hv[ct][u] = there && r < a.rank ? j.h[row * a.rank + r] : 0.0f;
-            }
+            for (int u = 0; u < kRows; ++u)
+                row[u] = order[min(s + quad * kRows + u, p.count - 1)];
         }
+        if (whole_block) {
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                __builtin_memcpy(f[u].w, y + row[u] * j.y_stride, 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                f[u] = load_frag<W>(y + row[u] * j.y_stride, left);
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const int32_t r = min(ct * 16 + col, a.rank - 1);   // (past the rank: not stored)
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                hv[ct][u] = j.h[(int64_t)row[u] * a.rank + r];
+        }
+        if (!whole_step)                                  // rows past the chunk's last
+#pragma unroll
+            for (int u = 0; u < kRows; ++u)
+                if (s + quad * kRows + u >= p.count) {
+                    f[u] = {{0, 0, 0, 0}};
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+                        hv[ct][u] = 0.0f;
+                }
         if constexpr (S == 4) {
             if (j.y_i32)
 #pragma unroll
@@ -659,34 +815,54 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a)
             }
         }
     }
-    // a group of one chunk is done; others leave a part of the sum
-    const bool whole = a.chunk_starts[p.group + 1] - a.chunk_starts[p.group] == 1;
+    // The waves' sums, added in order, 16 ranks at a time; wave w has ranks 4 quad + w of them.
+    // A group of one chunk is done, others leave a part of the sum.
+    static_assert(NW == 4, "a wave an i");
+    const bool done = a.chunk_starts[p.group + 1] - a.chunk_starts[p.group] == 1;
     const float scale = a.scales ? a.scales[p.group] : a.scale;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
+    for (int ct = 0; ct < CT; ++ct) {
+        if (ct > 0)
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int32_t r = ct * 16 + quad * 4 + i;
-            if (r >= a.rank)
-                continue;
+        for (int t = 0; t < E; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                joined[((i * NW + wave) * E + t) * kWave + lane] = sum[ct][t][i];
+        __syncthreads();
+        const int32_t r = ct * 16 + quad * 4 + wave;
+        float v[E];
+#pragma unroll
+        for (int t = 0; t < E; ++t) {
+            v[t] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                v[t] += joined[((wave * NW + w) * E + t) * kWave + lane];
+        }
+        if (r >= a.rank)
+            continue;
+        if (!done) {
+            float *to = j.partial + ((int64_t)p.slot * a.rank + r) * j.cols + at;
+#pragma unroll
+            for (int t = 0; t < E; ++t)
+                if (t < left)
+                    to[t] = v[t];
+        } else {
+            const int64_t base = (int64_t)p.group * a.rank * j.cols;
 #pragma unroll
             for (int t = 0; t < E; ++t) {
-                if (t >= left)
-                    continue;
-                const float v = sum[ct][t][i];
-                if (!whole) {
-                    j.partial[((int64_t)p.slot * a.rank + r) * j.cols + at + t] = v;
-                } else {
-                    const int64_t to = (int64_t)p.group * a.rank * j.cols +
-                                       (j.transposed ? (int64_t)(at + t) * a.rank + r
-                                                     : (int64_t)r * j.cols + at + t);
+                const int64_t to = base + (j.transposed ? (int64_t)(at + t) * a.rank + r
+                                                        : (int64_t)r * j.cols + at + t);
+                if (t < left) {
                     if constexpr (S == 4)
-                        reinterpret_cast<uint32_t *>(j.out)[to] = el_bits<W>(scale * v);
+                        reinterpret_cast<uint32_t *>(j.out)[to] = el_bits<W>(scale * v[t]);
                     else
-                        reinterpret_cast<uint16_t *>(j.out)[to] = (uint16_t)el_bits<W>(scale * v);
+                        reinterpret_cast<uint16_t *>(j.out)[to] =
+                            (uint16_t)el_bits<W>(scale * v[t]);
                 }
             }
         }
+    }
 }
 
 // Gradients of groups with no rows (zero) and of those with several chunks, whose parts are
@@ -708,6 +884,7 @@ __global__ __launch_bounds__(256) void k_join_grads(GradArgs a, int32_t per_grou
         for (int64_t e = (int64_t)(blockIdx.x - g * per_group) * 256 + threadIdx.x; e < all;
              e += (int64_t)per_group * 256) {
             float v = 0.0f;
+#pragma unroll 8
             for (int32_t c = first; c < last; ++c)
                 v += j.partial[c * all + e];
             const int64_t r = e / j.cols, at = e - r * j.cols;
@@ -731,7 +908,7 @@ hipError_t grads_of(const GradArgs &a, hipStream_t stream)
     }
     const int64_t els = (int64_t)a.rank * std::max(a.job[0].out ? a.job[0].cols : 0,
                                                    a.job[1].out ? a.job[1].cols : 0);
-    const int32_t per_group = (int32_t)std::min<int64_t>(64, (els + 1023) / 1024);
+    const int32_t per_group = (int32_t)std::min<int64_t>(1024, (els + 255) / 256);
     hipLaunchKernelGGL(k_join_grads<W>, dim3((uint32_t)((int64_t)a.groups * per_group)),
                        dim3(256), 0, stream, a, per_group);
     return hipGetLastError();
@@ -753,7 +930,7 @@ hipError_t launch_pass(const PassArgs &a, bool x_i32, bool back, hipStream_t str
 template <int W>
 int32_t grad_block()
 {
-    return 4 * 16 * kEls<W>;
+    return 16 * kEls<W>;
 }
 
 template <int W>

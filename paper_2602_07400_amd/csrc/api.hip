@@ -375,6 +375,7 @@ int take_rows(const char *who, bl::adapt::PassArgs &a, int64_t n_rows, int32_t g
     if (!plan && n_rows > kMaxLoneRows)
         return fail(BITLOGIC_ERR_SHAPE, "%s: more than 2^20 rows need a plan", who);
     a.groups = groups;
+    a.n_rows = n_rows;
     if (plan) {
         const auto l = bl::adapt::group_layout(n_rows, groups);
         const char *p = static_cast<const char *>(plan);
@@ -385,6 +386,26 @@ int take_rows(const char *who, bl::adapt::PassArgs &a, int64_t n_rows, int32_t g
         a.ids = ids;
         a.n_tiles = n_rows;
     }
+    return BITLOGIC_OK;
+}
+
+// A pass's form, and its workspace.
+int take_parts(const char *who, bl::adapt::PassArgs &a, int32_t el, void *workspace,
+               size_t workspace_bytes)
+{
+    const auto l = bl::adapt::pass_layout(a.n_rows, a.groups, a.rank, a.k, a.m, el,
+                                          a.tiles != nullptr);
+    a.splits = l.splits;
+    if (l.splits == 1 && a.hidden) {
+        a.partial = a.hidden;
+        return BITLOGIC_OK;
+    }
+    if (l.bytes > 0 && (!workspace || workspace_bytes < l.bytes))
+        return fail(BITLOGIC_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who,
+                    workspace_bytes, l.bytes);
+    if (l.bytes > 0 && !aligned(workspace, 16))
+        return fail(BITLOGIC_ERR_ALIGN, "%s: workspace not 16-byte aligned", who);
+    a.partial = static_cast<float *>(workspace);
     return BITLOGIC_OK;
 }
 
@@ -399,17 +420,31 @@ hipError_t by_weight(int32_t type, F f)
 }
 
 struct BackwardLayout {
-    size_t back, partial_down, partial_up, bytes;
+    size_t back, parts, parts_bytes, partial_down, partial_up, bytes;
+    int cut;                            // of the plan's two
 };
 
 BackwardLayout backward_layout(const bitlogic_adapter_set &s, int64_t n_rows)
 {
     const auto l = bl::adapt::group_layout(n_rows, s.n_adapters);
+    const int32_t el = (int32_t)logit_bytes(s.weight_type);
     BackwardLayout b;
+    // the small cut's chunks, unless the large one's make blocks enough
+    const int64_t columns = ((int64_t)s.n_in + s.n_out) * el / 256 + 1;
+    b.cut = (n_rows / l.cut[1].rows + 1) * columns >= 768;
     b.back = 0;
-    b.partial_down = round_up((size_t)n_rows * s.rank * 4);
-    b.partial_up = b.partial_down + round_up((size_t)l.n_slots * s.rank * s.n_in * 4);
-    b.bytes = b.partial_up + round_up((size_t)l.n_slots * s.rank * s.n_out * 4);
+    b.parts = round_up((size_t)n_rows * s.rank * 4);
+    // a pass by plan or by ids, whichever takes more
+    b.parts_bytes = 0;
+    for (bool planned : {true, false})
+        if (planned || n_rows <= kMaxLoneRows)
+            b.parts_bytes = std::max(b.parts_bytes,
+                                     bl::adapt::pass_layout(n_rows, s.n_adapters, s.rank, s.n_out,
+                                                            s.n_in, el, planned).bytes);
+    b.partial_down = b.parts + round_up(b.parts_bytes);
+    const size_t slots = (size_t)l.cut[b.cut].n_slots * s.rank * 4;
+    b.partial_up = b.partial_down + round_up(slots * s.n_in);
+    b.bytes = b.partial_up + round_up(slots * s.n_out);
     return b;
 }
 
@@ -1277,7 +1312,7 @@ int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_s
                       const bitlogic_adapter_set *set, const int32_t *ids, const void *plan,
                       const void *base, int32_t base_type, int64_t base_stride,
                       float base_scale, void *out, int64_t out_stride, float *hidden,
-                      void *stream)
+                      void *workspace, size_t workspace_bytes, void *stream)
 {
     const char *who = "adapters";
     if (int rc = check_set(who, set, n_rows))
@@ -1336,10 +1371,21 @@ int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_s
     a.out = static_cast<char *>(out);
     a.out_stride = out_stride * (int64_t)el;
     a.hidden = hidden;
+    if (int rc = take_parts(who, a, (int32_t)el, workspace, workspace_bytes))
+        return rc;
     return hip_status(by_weight(s.weight_type, [&](auto W) {
         return bl::adapt::launch_pass<decltype(W)::value>(a, x_type == BITLOGIC_LOGITS_I32, false,
                                                           (hipStream_t)stream);
     }), "adapters launch");
+}
+
+size_t bitlogic_adapters_workspace_bytes(const bitlogic_adapter_set *set, int64_t n_rows,
+                                         int32_t planned)
+{
+    if (check_set("adapters", set, n_rows) != BITLOGIC_OK || (!planned && n_rows > kMaxLoneRows))
+        return 0;
+    return bl::adapt::pass_layout(n_rows, set->n_adapters, set->rank, set->n_in, set->n_out,
+                                  (int32_t)logit_bytes(set->weight_type), planned != 0).bytes;
 }
 
 size_t bitlogic_adapters_backward_workspace_bytes(const bitlogic_adapter_set *set,
@@ -1415,11 +1461,12 @@ int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_st
         g.job[1].out = static_cast<char *>(grad_up);
         g.job[1].transposed = 1;
         if (n_rows > 0) {
-            g.chunks = reinterpret_cast<const bl::adapt::Piece4 *>(p + l.chunks);
+            const auto &cut = l.cut[b.cut];
+            g.chunks = reinterpret_cast<const bl::adapt::Piece4 *>(p + cut.chunks);
             g.order = reinterpret_cast<const int32_t *>(p + l.order);
-            g.chunk_starts = reinterpret_cast<const int32_t *>(p + l.chunk_starts);
-            g.slot_starts = reinterpret_cast<const int32_t *>(p + l.slot_starts);
-            g.n_chunks = l.n_chunks;
+            g.chunk_starts = reinterpret_cast<const int32_t *>(p + cut.starts);
+            g.slot_starts = reinterpret_cast<const int32_t *>(p + cut.slots);
+            g.n_chunks = cut.n;
             g.job[0].y = static_cast<const char *>(x);
             g.job[0].y_stride = x_stride * (int64_t)el;
             g.job[0].y_i32 = x_type == BITLOGIC_LOGITS_I32;
@@ -1451,6 +1498,8 @@ int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_st
         a.out = static_cast<char *>(grad_x);
         a.out_stride = grad_x_stride * (int64_t)el;
         a.hidden = grad_down ? back : nullptr;
+        if (int rc = take_parts(who, a, (int32_t)el, ws + b.parts, b.parts_bytes))
+            return rc;
         const hipError_t err = by_weight(s.weight_type, [&](auto W) {
             return bl::adapt::launch_pass<decltype(W)::value>(a, false, true,
                                                               (hipStream_t)stream);

@@ -15,22 +15,18 @@ namespace {
 using namespace adapt;
 
 // The place of this lane's row among the step's rows of its group, and how many those are:
-// one ballot a group that is present.
-__device__ __forceinline__ void match(int32_t group, bool valid, uint32_t &before,
+// lanes of one group agree in every bit of its number, one ballot a bit (a ballot a group
+// instead, 25 of them present: 32 us for 2^18 rows in runs of 1024, these 9).
+__device__ __forceinline__ void match(uint32_t group, bool valid, int bits, uint32_t &before,
                                       uint32_t &count)
 {
-    uint64_t left = __ballot(valid);
-    const uint64_t mine = 1ull << (threadIdx.x % kWave);
-    before = count = 0;
-    while (left) {
-        const int32_t one = __shfl(group, __builtin_ctzll(left));
-        const uint64_t same = __ballot(valid && group == one);
-        if (valid && group == one) {
-            before = __popcll(same & (mine - 1));
-            count = __popcll(same);
-        }
-        left &= ~same;
+    uint64_t same = __ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(group >> b & 1);
+        same &= group >> b & 1 ? set : ~set;
     }
+    before = __popcll(same & ((1ull << (threadIdx.x % kWave)) - 1));
+    count = __popcll(same);
 }
 
 __device__ __forceinline__ int32_t group_of_row(const int32_t *ids, int64_t row, int32_t groups)
@@ -72,24 +68,29 @@ __device__ __forceinline__ void write_pieces(Piece4 *table, int64_t entries, int
     }
 }
 
-// Exclusive sums over the groups' totals: rows, tiles, chunks and slots.  A block of
-// 64 * WAVES; part: 4 * WAVES words of LDS.
+// Exclusive sums over the groups' totals: rows, tiles, and the chunks and slots of both cuts.
+// A block of 64 * WAVES; part: kSums * WAVES words of LDS.
+constexpr int kSums = 6;
 template <int WAVES>
 __device__ void sum_groups(const GroupArgs &a, int32_t *part)
 {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int32_t groups = a.groups + 1;
-    int32_t *const to[4] = {a.starts, a.tile_starts, a.chunk_starts, a.slot_starts};
-    int32_t base[4] = {0, 0, 0, 0};
+    int32_t *const to[kSums] = {a.starts,         a.tile_starts,  a.cut[0].starts,
+                                a.cut[0].slots, a.cut[1].starts, a.cut[1].slots};
+    int32_t base[kSums] = {};
     for (int32_t g0 = 0; g0 < groups; g0 += kWave * WAVES) {
         const int32_t g = g0 + threadIdx.x;
         const int32_t rows = g < groups ? (int32_t)a.totals[g] : 0;
-        const int32_t chunks = rows / a.chunk + (rows % a.chunk > 0);
-        const int32_t v[4] = {rows, rows / kTile + (rows % kTile > 0), chunks,
-                              chunks > 1 && g < a.groups ? chunks : 0};
-        int32_t in[4];
+        int32_t v[kSums] = {rows, rows / kTile + (rows % kTile > 0)}, in[kSums];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int c = 0; c < 2; ++c) {
+            const int32_t chunks = rows / a.cut[c].rows + (rows % a.cut[c].rows > 0);
+            v[2 + 2 * c] = chunks;
+            v[3 + 2 * c] = chunks > 1 && g < a.groups ? chunks : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) {
             in[k] = v[k];
             for (int d = 1; d < kWave; d *= 2) {
                 const int32_t o = __shfl_up(in[k], d);
@@ -101,7 +102,7 @@ __device__ void sum_groups(const GroupArgs &a, int32_t *part)
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kSums; ++k) {
             int32_t all = 0, before = 0;
             for (int w = 0; w < WAVES; ++w) {
                 before += w < wave ? part[k * WAVES + w] : 0;
@@ -115,33 +116,44 @@ __device__ void sum_groups(const GroupArgs &a, int32_t *part)
     }
     if (threadIdx.x == 0)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < kSums; ++k)
             to[k][groups] = base[k];
     __syncthreads();
 }
 
 // A run's rows [lo, hi) to their places; next: the places of the run's next row of each group.
+// The ids of kAhead steps are loaded together.
+constexpr int kAhead = 4;
 template <class P>
 __device__ __forceinline__ void place_rows(const int32_t *ids, int64_t lo, int64_t hi,
                                            int32_t groups, P next, int32_t *order)
 {
-    for (int64_t at = lo; at < hi; at += kWave) {
-        const int64_t row = at + threadIdx.x % kWave;
-        const bool valid = row < hi;
-        const int32_t g = valid ? group_of_row(ids, row, groups) : 0;
-        uint32_t before, count;
-        match(g, valid, before, count);
-        uint32_t to = 0;
-        if (valid)
-            to = next[g];
-        __builtin_amdgcn_wave_barrier();
-        if (valid) {
-            order[to + before] = (int32_t)row;
-            if (before == 0)
-                next[g] = to + count;
+    const int bits = 32 - __builtin_clz(groups);          // (the number `groups` occurs too)
+    for (int64_t at = lo; at < hi; at += kAhead * kWave) {
+        uint32_t g[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t row = at + k * kWave + threadIdx.x % kWave;
+            g[k] = row < hi ? (uint32_t)group_of_row(ids, row, groups) : 0;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t row = at + k * kWave + threadIdx.x % kWave;
+            const bool valid = row < hi;
+            uint32_t before, count;
+            match(g[k], valid, bits, before, count);
+            uint32_t to = 0;
+            if (valid)
+                to = next[g[k]];
+            __builtin_amdgcn_wave_barrier();
+            if (valid) {
+                order[to + before] = (int32_t)row;
+                if (before == 0)
+                    next[g[k]] = to + count;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
     }
 }
 
@@ -150,7 +162,7 @@ template <int WAVES>
 __global__ __launch_bounds__(kWave * WAVES) void k_group_few(GroupArgs a)
 {
     extern __shared__ uint32_t counts[];                  // [WAVES][all groups]
-    __shared__ int32_t part[4 * WAVES];
+    __shared__ int32_t part[kSums * WAVES];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int32_t all = a.groups + 1;
     uint32_t *mine = counts + wave * all;
@@ -159,6 +171,7 @@ __global__ __launch_bounds__(kWave * WAVES) void k_group_few(GroupArgs a)
     __syncthreads();
     const int64_t run = (a.rows + kWave * WAVES - 1) / (kWave * WAVES) * kWave;
     const int64_t lo = min(a.rows, wave * run), hi = min(a.rows, lo + run);
+#pragma unroll 4
     for (int64_t row = lo + lane; row < hi; row += kWave)
         atomicAdd(&mine[group_of_row(a.ids, row, a.groups)], 1u);
     __syncthreads();
@@ -177,10 +190,11 @@ __global__ __launch_bounds__(kWave * WAVES) void k_group_few(GroupArgs a)
         counts[i] += (uint32_t)a.starts[i % all];
     __syncthreads();
     place_rows(a.ids, lo, hi, a.groups, mine, a.order);
-    write_pieces(a.tiles, a.n_tiles, kTile, a.tile_starts, a.starts, a.slot_starts, all, threadIdx.x,
+    write_pieces(a.tiles, a.n_tiles, kTile, a.tile_starts, a.starts, a.starts, all, threadIdx.x,
                  kWave * WAVES);
-    write_pieces(a.chunks, a.n_chunks, a.chunk, a.chunk_starts, a.starts, a.slot_starts, all, threadIdx.x,
-                 kWave * WAVES);
+    for (int c = 0; c < 2; ++c)
+        write_pieces(a.cut[c].chunks, a.cut[c].n, a.cut[c].rows, a.cut[c].starts, a.starts,
+                     a.cut[c].slots, all, threadIdx.x, kWave * WAVES);
 }
 
 // ---- many rows ----
@@ -192,6 +206,7 @@ __global__ __launch_bounds__(kWave) void k_group_count(GroupArgs a)
         counts[g] = 0;
     __syncthreads();
     const int64_t lo = blockIdx.x * a.run, hi = min(a.rows, lo + a.run);
+#pragma unroll 4
     for (int64_t row = lo + threadIdx.x; row < hi; row += kWave)
         atomicAdd(&counts[group_of_row(a.ids, row, a.groups)], 1u);
     __syncthreads();
@@ -202,7 +217,7 @@ __global__ __launch_bounds__(kWave) void k_group_count(GroupArgs a)
 constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(kWave * kSumWaves) void k_group_sum(GroupArgs a)
 {
-    __shared__ int32_t part[4 * kSumWaves];
+    __shared__ int32_t part[kSums * kSumWaves];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int32_t all = a.groups + 1;
     for (int32_t g = wave; g < all; g += kSumWaves) {     // a wave sums up a group's runs
@@ -239,12 +254,14 @@ __global__ __launch_bounds__(kWave) void k_group_place(GroupArgs a)
     place_rows(a.ids, lo, hi, a.groups, next, a.order);
     const int64_t first = (int64_t)blockIdx.x * kWave + threadIdx.x,
                   step = (int64_t)gridDim.x * kWave;
-    write_pieces(a.tiles, a.n_tiles, kTile, a.tile_starts, a.starts, a.slot_starts, all, first, step);
-    write_pieces(a.chunks, a.n_chunks, a.chunk, a.chunk_starts, a.starts, a.slot_starts, all, first, step);
+    write_pieces(a.tiles, a.n_tiles, kTile, a.tile_starts, a.starts, a.starts, all, first, step);
+    for (int c = 0; c < 2; ++c)
+        write_pieces(a.cut[c].chunks, a.cut[c].n, a.cut[c].rows, a.cut[c].starts, a.starts,
+                     a.cut[c].slots, all, first, step);
 }
 
-// One block up to here: a wave's steps of 64 rows are a chain of about 0.3 us each.
-constexpr int64_t kFewRows = 8192;
+// One block up to here.
+constexpr int64_t kFewRows = 16384;
 
 }  // namespace
 
@@ -260,15 +277,14 @@ hipError_t launch_group_rows(const int32_t *ids, int64_t rows, int32_t groups, v
     a.order = reinterpret_cast<int32_t *>(p + l.order);
     a.starts = reinterpret_cast<int32_t *>(p + l.starts);
     a.tile_starts = reinterpret_cast<int32_t *>(p + l.tile_starts);
-    a.chunk_starts = reinterpret_cast<int32_t *>(p + l.chunk_starts);
-    a.slot_starts = reinterpret_cast<int32_t *>(p + l.slot_starts);
     a.tiles = reinterpret_cast<Piece4 *>(p + l.tiles);
-    a.chunks = reinterpret_cast<Piece4 *>(p + l.chunks);
+    for (int c = 0; c < 2; ++c)
+        a.cut[c] = {reinterpret_cast<Piece4 *>(p + l.cut[c].chunks),
+                    reinterpret_cast<int32_t *>(p + l.cut[c].starts),
+                    reinterpret_cast<int32_t *>(p + l.cut[c].slots), l.cut[c].n, l.cut[c].rows};
     a.totals = reinterpret_cast<uint32_t *>(p + l.totals);
     a.counts = reinterpret_cast<uint32_t *>(p + l.counts);
     a.n_tiles = l.n_tiles;
-    a.n_chunks = l.n_chunks;
-    a.chunk = l.chunk;
     a.run = l.run;
     a.runs = l.runs;
     const size_t all = (size_t)groups + 1;

@@ -30,12 +30,12 @@ def _set(**fields):
 
 
 def _forward(lib, x=FAKE, x_type=F32, rows=5, stride=10, ids=FAKE, plan=FAKE, base=FAKE,
-             base_type=F32, base_stride=12, out=FAR, out_stride=12, hidden=FAKE, set_=True,
-             **fields):
+             base_type=F32, base_stride=12, out=FAR, out_stride=12, hidden=FAKE,
+             workspace=FAKE, ws_bytes=1 << 40, set_=True, **fields):
     s = _set(**fields)
     return lib.bitlogic_adapters(x, x_type, rows, stride, ctypes.addressof(s) if set_ else None,
                                  ids, plan, base, base_type, base_stride, 1.0, out, out_stride,
-                                 hidden, None)
+                                 hidden, workspace, ws_bytes, None)
 
 
 def _backward(lib, grad=FAKE, rows=5, grad_stride=12, x=FAKE, x_type=F32, stride=10, hidden=FAKE,
@@ -81,6 +81,15 @@ def test_forward_validation(lib):
                 {"base": FAR, "out": FAR, "base_stride": 13}, {"base": FAR + 4},
                 {"base": FAR, "base_type": I32}):
         assert _forward(lib, **bad) == ESHAPE, bad
+    need = lib.bitlogic_adapters_workspace_bytes
+    s = _set(n_in=5000)
+    size = need(ctypes.addressof(s), 5, 1)
+    assert size >= 5 * 4 * 4 and need(ctypes.addressof(s), (1 << 20) + 1, 0) == 0
+    assert need(None, 5, 1) == 0 and need(ctypes.addressof(_set()), 5, 1) == 0
+    wide = dict(n_in=5000, stride=5000, hidden=None)
+    assert _forward(lib, **wide, ws_bytes=size - 1) == EWS
+    assert _forward(lib, **wide, workspace=None) == EWS
+    assert _forward(lib, **wide, workspace=FAKE + 8) == EALIGN
     assert _forward(lib, rows=0, x=None, out=None, hidden=None, plan=None, ids=None) == OK
 
 
