@@ -127,12 +127,13 @@ inline bool is_narrow(bool planned, int32_t k, int32_t m, int32_t el_bytes)
     return planned && k <= 1024 / el_bytes && m <= 1024 / el_bytes;
 }
 
-// Parts of the k terms of wide adapters: for about 2048 blocks of 4 waves, each wave with a unit
-// of 128 bytes or more.
-inline int32_t split_terms(int64_t n_tiles, int32_t k, int32_t el_bytes)
+// Parts of the k terms of wide adapters: for about 1024 blocks, whose waves (8 or, above rank
+// 32, 4) have a unit of 128 bytes or more each.
+inline int32_t split_terms(int64_t n_tiles, int32_t k, int32_t rank, int32_t el_bytes)
 {
-    const int64_t most = ((int64_t)k * el_bytes + 511) / 512;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({most, 16, 2048 / n_tiles}));
+    const int64_t share = (rank <= 32 ? 8 : 4) * 128;
+    const int64_t most = ((int64_t)k * el_bytes + share - 1) / share;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({most, 8, 1024 / n_tiles}));
 }
 
 struct PassLayout {
@@ -147,7 +148,7 @@ inline PassLayout pass_layout(int64_t n_rows, int32_t groups, int32_t rank, int3
     PassLayout l;
     l.n_tiles = planned ? group_layout(n_rows, groups).n_tiles : n_rows;
     l.narrow = is_narrow(planned, k, m, el_bytes);
-    l.splits = l.narrow || n_rows == 0 ? 0 : split_terms(l.n_tiles, k, el_bytes);
+    l.splits = l.narrow || n_rows == 0 ? 0 : split_terms(l.n_tiles, k, rank, el_bytes);
     l.bytes = (size_t)l.splits * n_rows * rank * 4;
     return l;
 }

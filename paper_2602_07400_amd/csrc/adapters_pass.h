@@ -200,7 +200,7 @@ __device__ __forceinline__ f32x4 mma_h(const uint32_t (&w)[kSize<W>], Frag h, f3
         return mma<W>({w[0], w[1], w[0], w[1]}, h, c);
 }
 
-// base and out of one row: out columns [m, m + kEls) from their sums, as many as there are.
+// base and out of one row: out columns [col, col + kEls) from their sums, as many as there are.
 template <int W>
 struct Output {
     const char *base;                   // the row's, or NULL
@@ -209,32 +209,30 @@ struct Output {
     float base_scale, scale;
     int32_t m;
 
-    __device__ __forceinline__ Frag load_base(int32_t col) const
-    {
-        if (!base || !there)
-            return {{0, 0, 0, 0}};
-        return load_frag<W>(base + (int64_t)col * kSize<W>, m - col);
-    }
-    __device__ __forceinline__ void store(int32_t col, const float (&sum)[kEls<W>],
+    __device__ __forceinline__ void store(int32_t col, bool whole, const float (&sum)[kEls<W>],
                                           const Frag &b) const
     {
-        if (!there || col >= m)
+        if (!there)
             return;
         uint32_t bits[kEls<W>];
 #pragma unroll
         for (int u = 0; u < kEls<W>; ++u) {
-            float from;
-            if constexpr (W == kF32)
-                from = base_i32 ? (float)(int32_t)b.w[u] : __uint_as_float(b.w[u]);
-            else if constexpr (W == kBf16)
-                from = __uint_as_float(u & 1 ? b.w[u / 2] & 0xFFFF0000u : b.w[u / 2] << 16);
-            else
-                from = (float)__builtin_bit_cast(_Float16,
-                                                 (uint16_t)(b.w[u / 2] >> (16 * (u & 1))));
-            bits[u] = el_bits<W>(base_scale * from + scale * sum[u]);
+            float v = scale * sum[u];
+            if (base) {
+                float from;
+                if constexpr (W == kF32)
+                    from = base_i32 ? (float)(int32_t)b.w[u] : __uint_as_float(b.w[u]);
+                else if constexpr (W == kBf16)
+                    from = __uint_as_float(u & 1 ? b.w[u / 2] & 0xFFFF0000u : b.w[u / 2] << 16);
+                else
+                    from = (float)__builtin_bit_cast(_Float16,
+                                                     (uint16_t)(b.w[u / 2] >> (16 * (u & 1))));
+                v += base_scale * from;
+            }
+            bits[u] = el_bits<W>(v);
         }
         char *to = out + (int64_t)col * kSize<W>;
-        if (col + kEls<W> <= m) {
+        if (whole) {
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -282,8 +280,67 @@ struct Tile {
     }
 };
 
+// Which of the E terms from k on a lane takes at the end of a row of n: it loads the row's last
+// E instead, which start `back` terms earlier, and keeps those that are its own.
+template <int W>
+struct End {
+    int32_t at;                         // where it loads
+    uint32_t keep[4];                   // of the words there
+
+    __device__ __forceinline__ End(int32_t k, int32_t n)
+    {
+        constexpr int E = kEls<W>;
+        at = min(k, n - E);
+        const int32_t back = k - at;    // (E or more: none is its own)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kSize<W> == 4)
+                keep[i] = i >= back ? 0xFFFFFFFFu : 0u;
+            else
+                keep[i] = (2 * i >= back ? 0x0000FFFFu : 0u) |
+                          (2 * i + 1 >= back ? 0xFFFF0000u : 0u);
+        }
+    }
+    __device__ __forceinline__ Frag take(Frag f) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f.w[i] &= keep[i];
+        return f;
+    }
+};
+
+__device__ __forceinline__ Frag load_16(const char *p)
+{
+    Frag f;
+    __builtin_memcpy(f.w, p, 16);
+    return f;
+}
+
+// E terms of a column of a matrix with `step` bytes from term to term.
+template <int W>
+__device__ __forceinline__ Frag load_across(const char *p, int64_t step)
+{
+    Frag f;
+    if constexpr (kSize<W> == 4) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            f.w[u] = *reinterpret_cast<const uint32_t *>(p + u * step);
+    } else {
+        uint32_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = *reinterpret_cast<const uint16_t *>(p + u * step);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f.w[i] = v[2 * i] | v[2 * i + 1] << 16;
+    }
+    return f;
+}
+
 // h += w1 x over terms [from, to): units of 128 bytes of a row, every `deal`-th from the
-// `turn`-th on; `to` is k or a multiple of the unit.
+// `turn`-th on; `to` is k or a multiple of the unit.  A unit's loads are issued before the
+// products of the one before.
 template <int W, int X, int CT, int RT, bool BACK>
 __device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, int col, int quad,
                                        int32_t from, int32_t to, int turn, int deal,
@@ -295,64 +352,95 @@ __device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, 
     for (int rt = 0; rt < RT; ++rt)
         x[rt] = a.x + tile.row[rt] * a.x_stride;
     const char *first = a.w1 + tile.p.group * a.w1_step;
+    const int64_t across = (int64_t)a.rank * S;           // BACK: from term to term
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         // ranks behind the last one read its weights: what comes of it is cleared afterwards
         const int32_t r = min(ct * 16 + col, a.rank - 1);
         w1[ct] = first + (BACK ? (int64_t)r : (int64_t)r * a.k) * S;
     }
-    const auto load_w1 = [&](int ct, int32_t k, int32_t left) __attribute__((always_inline)) {
-        if constexpr (!BACK) {
-            return load_frag<W>(w1[ct] + (int64_t)k * S, left);
-        } else {
-            Frag f;
-            const char *at = w1[ct] + (int64_t)k * a.rank * S;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                f.w[i] = 0;
-#pragma unroll
-            for (int u = 0; u < E; ++u)
-                if (u < left) {
-                    const char *el = at + (int64_t)u * a.rank * S;
-                    if constexpr (S == 4)
-                        f.w[u] = *reinterpret_cast<const uint32_t *>(el);
-                    else
-                        f.w[u / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(el)
-                                      << (16 * (u & 1));
-                }
-            return f;
-        }
+    struct Unit {
+        Frag x[2][RT], w[2][CT];
     };
-    const auto step = [&](int32_t k0, bool whole) __attribute__((always_inline)) {
-        Frag fx[2][RT], fw[2][CT];
+    const auto load = [&](Unit &u, int32_t k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int32_t k = k0 + half * 4 * E + quad * E;
-            const int32_t left = whole ? E : a.k - k;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
-                fx[half][rt] = load_frag<W>(x[rt] + (int64_t)k * S, left);
+                u.x[half][rt] = load_16(x[rt] + (int64_t)k * S);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
-                fw[half][ct] = load_w1(ct, k, left);
+                u.w[half][ct] = BACK ? load_across<W>(w1[ct] + k * across, across)
+                                     : load_16(w1[ct] + (int64_t)k * S);
         }
+    };
+    const auto products = [&](const Unit &u) __attribute__((always_inline)) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const Frag t = to_terms<X>(fx[half][rt]);
+                const Frag t = to_terms<X>(u.x[half][rt]);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
-                    h[rt][ct] = mma<W>(fw[half][ct], t, h[rt][ct]);
+                    h[rt][ct] = mma<W>(u.w[half][ct], t, h[rt][ct]);
             }
     };
-    const int32_t whole = min(to, a.k / kUnit * kUnit);
+    const int32_t whole = min(to, a.k / kUnit * kUnit), step = deal * kUnit;
     int32_t k0 = from + turn * kUnit;
-#pragma unroll(CT <= 2 ? 2 : 1)
-    for (; k0 < whole; k0 += deal * kUnit)
-        step(k0, true);
-    if (k0 < to)
-        step(k0, false);
+    if (k0 < whole) {
+        Unit now, next;
+        load(now, k0);
+        for (;;) {
+            k0 += step;
+            if (k0 >= whole)
+                break;
+            load(next, k0);
+            products(now);
+            now = next;
+        }
+        products(now);
+    }
+    if (k0 < to) {                                        // the row's last terms
+        Unit u;
+        if (a.k >= E) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const End<W> end(k0 + half * 4 * E + quad * E, a.k);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    u.x[half][rt] = end.take(load_16(x[rt] + (int64_t)end.at * S));
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    u.w[half][ct] = end.take(
+                        BACK ? load_across<W>(w1[ct] + end.at * across, across)
+                             : load_16(w1[ct] + (int64_t)end.at * S));
+            }
+        } else {                                          // fewer than one load's
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int32_t left = half == 0 && quad == 0 ? a.k : 0;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    u.x[half][rt] = load_frag<W>(x[rt], left);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    Frag f = {{0, 0, 0, 0}};
+                    for (int32_t i = 0; i < left; ++i) {  // (a run-time index of few)
+                        const char *el = w1[ct] + i * (BACK ? across : S);
+                        const uint32_t v = S == 4 ? *reinterpret_cast<const uint32_t *>(el)
+                                                  : *reinterpret_cast<const uint16_t *>(el);
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (e == i)
+                                f.w[e * S / 4] |= S == 4 ? v : v << (16 * (e & 1));
+                    }
+                    u.w[half][ct] = f;
+                }
+            }
+        }
+        products(u);
+    }
 }
 
 template <int RT, int CT>
@@ -400,133 +488,211 @@ __device__ __forceinline__ void store_hidden(float *to, int32_t rank, const Tile
             }
 }
 
-// out = base + scale w2 h: units of columns, every `deal`-th from the `turn`-th on.
-template <int W, int CT, int RT, bool BACK>
-__device__ __forceinline__ void expand(const PassArgs &a, const Tile<RT> &tile, int col, int quad,
-                                       int turn, int deal, const f32x4 (&h)[RT][CT])
+// Four ranks of a row of `rank` from r on; zeros past the last one.
+template <int W>
+__device__ __forceinline__ void load_ranks(const char *row, int32_t r, int32_t rank,
+                                           uint32_t (&w)[kSize<W>])
 {
-    constexpr int E = kEls<W>, S = kSize<W>;
-    const bool adapted = tile.p.group < a.groups;
-    Frag terms[RT][CT];
-    float factor[RT];
-    make_terms<W>(h, terms, factor);
-    Output<W> o[RT];
-    const float scale = !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        o[rt].base = a.base ? a.base + tile.row[rt] * a.base_stride : nullptr;
-        o[rt].out = a.out + tile.row[rt] * a.out_stride;
-        o[rt].base_i32 = a.base_i32;
-        o[rt].there = tile.there[rt];
-        o[rt].base_scale = a.base_scale;
-        o[rt].scale = scale * factor[rt];
-        o[rt].m = a.m;
+    constexpr int S = kSize<W>;
+    if (r + 4 <= rank) {
+        __builtin_memcpy(w, row + r * S, 4 * S);
+        return;
     }
-    const char *w2 = a.w2 + (adapted ? tile.p.group * a.w2_step : 0);
-    if constexpr (!BACK) {
-        // a unit: two tiles of 16 columns.  16-bit types give a lane 8 neighbours of them.
-        constexpr int kCols = 32, kPieces = S == 2 ? 1 : 2;
-        const bool fours = a.rank % 4 == 0;
-        const auto column = [&](int t, int place) __attribute__((always_inline)) {
-            return S == 2 ? place / 4 * 8 + t * 4 + place % 4 : t * 16 + place;
-        };
-        for (int32_t m0 = turn * kCols; m0 < a.m; m0 += deal * kCols) {
-            Frag b[RT][kPieces];
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+        w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (r + i < rank) {
+            if constexpr (S == 4)
+                w[i] = reinterpret_cast<const uint32_t *>(row)[r + i];
+            else
+                w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[r + i]
+                            << (16 * (i & 1));
+        }
+}
+
+// out = base + scale w2 h: units of columns, every `deal`-th from the `turn`-th on.  The next
+// unit's base is loaded, and the next weights where registers allow, before this one's products.
+template <int W, int CT, int RT, bool BACK>
+struct Expand {
+    static constexpr int E = kEls<W>, S = kSize<W>;
+    static constexpr int kCols = BACK ? 16 * E : 32;      // of a unit
+    static constexpr int kPieces = S == 2 ? 1 : 2;        // forward: loads of base a row
+    static constexpr bool kAhead = (BACK ? 16 : 2 * S) * CT <= 32;
+    struct Weights {
+        uint32_t w[BACK ? 1 : 2][CT][S];                  // forward: 4 ranks of two tiles' rows
+        Frag f[BACK ? CT : 1][4];                         // back: 4 ranks of E columns
+    };
+    struct Base {
+        Frag f[RT][kPieces];
+    };
+    const PassArgs &a;
+    const char *w2;
+    Output<W> o[RT];
+    int col, quad;
+    bool adapted;
+
+    __device__ __forceinline__ Expand(const PassArgs &args, const Tile<RT> &tile, int c, int q)
+        : a(args), col(c), quad(q), adapted(tile.p.group < args.groups)
+    {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            o[rt].base = BACK || !a.base ? nullptr : a.base + tile.row[rt] * a.base_stride;
+            o[rt].out = a.out + tile.row[rt] * a.out_stride;
+            o[rt].base_i32 = a.base_i32;
+            o[rt].there = tile.there[rt];
+            o[rt].base_scale = a.base_scale;
+            o[rt].m = a.m;
+            o[rt].scale = !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
+        }
+        w2 = a.w2 + (adapted ? tile.p.group * a.w2_step : 0);
+    }
+    __device__ __forceinline__ void load_base(Base &b, int32_t m0) const
+    {
+        if constexpr (!BACK) {
+            if (!a.base)
+                return;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i)
-                    b[rt][i] = o[rt].load_base(m0 + i * 16 + quad * E);
-            f32x4 sum[2][RT];
-            clear(sum);
-            if (adapted)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int32_t m = min(m0 + column(t, col), a.m - 1);
-                    const char *from = w2 + (int64_t)m * a.rank * S;
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        const int32_t r = ct * 16 + quad * 4;
-                        uint32_t w[S] = {};
-                        if (fours) {
-                            if (r < a.rank)
-                                __builtin_memcpy(w, from + r * S, 4 * S);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (r + i < a.rank) {
-                                    if constexpr (S == 4)
-                                        w[i] = reinterpret_cast<const uint32_t *>(from)[r + i];
-                                    else
-                                        w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(
-                                                        from)[r + i] << (16 * (i & 1));
-                                }
-                        }
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt)
-                            sum[t][rt] = mma_h<W>(w, terms[rt][ct], sum[t][rt]);
-                    }
+                for (int i = 0; i < kPieces; ++i) {
+                    const int32_t m = m0 + i * 16 + quad * E;
+                    if (m0 + kCols <= a.m)                // (rows that are not there: the first)
+                        b.f[rt][i] = load_16(o[rt].base + (int64_t)m * S);
+                    else
+                        b.f[rt][i] = load_frag<W>(o[rt].base + (int64_t)m * S, a.m - m);
                 }
+        }
+    }
+    // forward: the tiles' rows of w2; 16-bit types give a lane 8 neighbours of them
+    __device__ __forceinline__ int32_t column(int t) const
+    {
+        return S == 2 ? col / 4 * 8 + t * 4 + col % 4 : t * 16 + col;
+    }
+    __device__ __forceinline__ void load_weights(Weights &w, int32_t m0) const
+    {
+        if (!adapted)
+            return;
+        if constexpr (!BACK) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int t = 0; t < 2; ++t) {
+                const char *row = w2 + (int64_t)min(m0 + column(t), a.m - 1) * a.rank * S;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    load_ranks<W>(row, ct * 16 + quad * 4, a.rank, w.w[t][ct]);
+            }
+        } else {
+            const int32_t m = m0 + col * E;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t r = ct * 16 + quad * 4 + i;
+                    const char *from = w2 + ((int64_t)min(r, a.rank - 1) * a.m + m) * S;
+                    Frag f;
+                    if (m0 + kCols <= a.m)
+                        f = load_16(from);
+                    else
+                        f = load_frag<W>(from, a.m - m);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)           // (their h is zero, they may be NaNs)
+                        f.w[e] = r < a.rank ? f.w[e] : 0;
+                    w.f[ct][i] = f;
+                }
+        }
+    }
+    __device__ __forceinline__ void unit(int32_t m0, const Weights &w, const Base &b,
+                                         const Frag (&terms)[RT][CT]) const
+    {
+        constexpr int T = BACK ? E : 2;
+        f32x4 sum[T][RT];
+        clear(sum);
+        if (adapted)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    uint32_t v[S];
+                    if constexpr (!BACK) {
+#pragma unroll
+                        for (int i = 0; i < S; ++i)
+                            v[i] = w.w[t][ct][i];
+                    } else if constexpr (S == 4) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[i] = w.f[ct][i].w[t];
+                    } else {
+                        const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            v[i] = __builtin_amdgcn_perm(w.f[ct][2 * i + 1].w[t / 2],
+                                                         w.f[ct][2 * i].w[t / 2], pick);
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+                        sum[t][rt] = mma_h<W>(v, terms[rt][ct], sum[t][rt]);
+                }
+        const bool whole = m0 + kCols <= a.m;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if constexpr (!BACK) {
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) {
                     float v[E];
 #pragma unroll
                     for (int u = 0; u < E; ++u)
                         v[u] = sum[S == 2 ? u / 4 : i][rt][u % 4];
-                    o[rt].store(m0 + i * 16 + quad * E, v, b[rt][i]);
+                    o[rt].store(m0 + i * 16 + quad * E, whole, v, b.f[rt][i]);
                 }
-        }
-    } else {
-        // a unit: E tiles of 16 columns; tile t has columns t, E + t, 2 E + t, ...
-        constexpr int kCols = 16 * E;
-        for (int32_t m0 = turn * kCols; m0 < a.m; m0 += deal * kCols) {
-            f32x4 sum[E][RT];
-            clear(sum);
-            if (adapted)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    Frag f[4];                            // 4 ranks of E columns
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int32_t r = ct * 16 + quad * 4 + i, m = m0 + col * E;
-                        f[i] = load_frag<W>(w2 + ((int64_t)min(r, a.rank - 1) * a.m + m) * S,
-                                            r < a.rank ? a.m - m : 0);
-                    }
-#pragma unroll
-                    for (int t = 0; t < E; ++t) {
-                        uint32_t w[S];
-                        if constexpr (S == 4) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                w[i] = f[i].w[t];
-                        } else {
-                            const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-                            for (int i = 0; i < 2; ++i)
-                                w[i] = __builtin_amdgcn_perm(f[2 * i + 1].w[t / 2],
-                                                             f[2 * i].w[t / 2], pick);
-                        }
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt)
-                            sum[t][rt] = mma_h<W>(w, terms[rt][ct], sum[t][rt]);
-                    }
-                }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            } else {
+                // tile t has columns t, E + t, 2 E + t, ...
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v[E];
 #pragma unroll
                     for (int t = 0; t < E; ++t)
                         v[t] = sum[t][rt][i];
-                    const int32_t at = m0 + (quad * 4 + i) * E;
-                    o[rt].store(at, v, o[rt].load_base(at));
+                    o[rt].store(m0 + (quad * 4 + i) * E, whole, v, {{0, 0, 0, 0}});
                 }
+            }
         }
     }
-}
+    __device__ __forceinline__ void run(int turn, int deal, Base &b, const f32x4 (&h)[RT][CT])
+    {
+        Weights w;
+        int32_t m0 = turn * kCols;
+        if (m0 >= a.m)
+            return;
+        if constexpr (kAhead)
+            load_weights(w, m0);
+        Frag terms[RT][CT];
+        float factor[RT];
+        make_terms<W>(h, terms, factor);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+            o[rt].scale *= factor[rt];
+        for (;;) {
+            const int32_t next = m0 + deal * kCols;
+            Weights w_next;
+            Base b_next;
+            if constexpr (!kAhead)
+                load_weights(w, m0);
+            if (next < a.m) {
+                load_base(b_next, next);
+                if constexpr (kAhead)
+                    load_weights(w_next, next);
+            }
+            unit(m0, w, b, terms);
+            if (next >= a.m)
+                return;
+            m0 = next;
+            b = b_next;
+            if constexpr (kAhead)
+                w = w_next;
+        }
+    }
+};
 
 // ---- narrow adapters: a wave a tile ----
 template <int W, int X, int CT, bool BACK>
@@ -541,6 +707,10 @@ __global__ __launch_bounds__(256) void k_narrow(PassArgs a)
         return;
     f32x4 h[RT][CT];
     clear(h);
+    Expand<W, CT, RT, BACK> expand(a, tile, col, quad);
+    typename Expand<W, CT, RT, BACK>::Base b;
+    if (a.out)
+        expand.load_base(b, 0);
     if (tile.p.group < a.groups) {
         shrink<W, X, CT, RT, BACK>(a, tile, col, quad, 0, a.k, 0, 1, h);
         clear_past_rank(a.rank, quad, h);
@@ -548,17 +718,19 @@ __global__ __launch_bounds__(256) void k_narrow(PassArgs a)
     if (a.hidden)
         store_hidden(a.hidden, a.rank, tile, quad, h);
     if (a.out)
-        expand<W, CT, RT, BACK>(a, tile, col, quad, 0, 1, h);
+        expand.run(0, 1, b, h);
 }
 
 // ---- wide adapters ----
 constexpr int kWideWaves = 4;
+// waves that share a block's terms: as many as a rank's sums leave LDS for
+template <int CT> constexpr int kTermWaves = CT <= 2 ? 8 : 4;
 
 // Part `blockIdx % splits` of a tile's h, to [part][row][rank].
 template <int W, int X, int CT, int RT, bool BACK>
-__global__ __launch_bounds__(kWideWaves * kWave) void k_shrink(PassArgs a)
+__global__ __launch_bounds__(kTermWaves<CT> * kWave) void k_shrink(PassArgs a)
 {
-    constexpr int NW = kWideWaves, kAcc = CT * RT * 4, kUnit = 8 * kEls<W>;
+    constexpr int NW = kTermWaves<CT>, kAcc = CT * RT * 4, kUnit = 8 * kEls<W>;
     __shared__ float joined[NW * kAcc * kWave];
     const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -623,32 +795,32 @@ __global__ __launch_bounds__(kWideWaves * kWave) void k_expand(PassArgs a, int32
     Tile<RT> tile;
     if (!tile.take(a, at, col))
         return;
+    Expand<W, CT, RT, BACK> expand(a, tile, col, quad);
+    typename Expand<W, CT, RT, BACK>::Base b;
+    const int turn = block * kWideWaves + wave;
+    if (a.out && turn * expand.kCols < a.m)
+        expand.load_base(b, turn * expand.kCols);
     f32x4 h[RT][CT];
     clear(h);
+#pragma unroll(CT <= 2 ? 2 : 1)
+    for (int32_t p = 0; p < a.splits; ++p)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+        for (int rt = 0; rt < RT; ++rt) {
+            const float *from = a.partial + (p * a.n_rows + tile.row[rt]) * a.rank;
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const int32_t r = ct * 16 + quad * 4;
-            const float *from = a.partial + (int64_t)tile.row[rt] * a.rank + r;
-            for (int32_t p = 0; p < a.splits; ++p, from += a.n_rows * a.rank) {
-                f32x4 one = {0, 0, 0, 0};
-                if (r + 4 <= a.rank) {
-                    __builtin_memcpy(&one, from, 16);
-                } else {
+            for (int ct = 0; ct < CT; ++ct) {
+                uint32_t w[4];
+                load_ranks<kF32>(reinterpret_cast<const char *>(from), ct * 16 + quad * 4, a.rank,
+                                 w);
 #pragma unroll
-                    for (int i = 0; i < 3; ++i)
-                        if (r + i < a.rank)
-                            one[i] = from[i];
-                }
-                h[rt][ct] += one;
+                for (int i = 0; i < 4; ++i)
+                    h[rt][ct][i] += __uint_as_float(w[i]);
             }
         }
     if (a.hidden && a.hidden != a.partial && block == 0 && wave == 0)
         store_hidden(a.hidden, a.rank, tile, quad, h);
     if (a.out)
-        expand<W, CT, RT, BACK>(a, tile, col, quad, block * kWideWaves + wave,
-                                blocks * kWideWaves, h);
+        expand.run(turn, blocks * kWideWaves, b, h);
 }
 
 template <int W, int X, int CT, bool BACK>
@@ -659,24 +831,25 @@ hipError_t pass_of(const PassArgs &a, hipStream_t stream)
                            dim3(256), 0, stream, a);
         return hipGetLastError();
     }
-    constexpr int kThreads = kWideWaves * kWave;
-    const dim3 parts((uint32_t)(a.n_tiles * a.splits));
+    const dim3 parts((uint32_t)(a.n_tiles * a.splits)), term_waves(kTermWaves<CT> * kWave);
     if (a.tiles)
-        hipLaunchKernelGGL((k_shrink<W, X, CT, 2, BACK>), parts, dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((k_shrink<W, X, CT, 2, BACK>), parts, term_waves, 0, stream, a);
     else
-        hipLaunchKernelGGL((k_shrink<W, X, CT, 1, BACK>), parts, dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((k_shrink<W, X, CT, 1, BACK>), parts, term_waves, 0, stream, a);
     if (hipError_t err = hipGetLastError(); err != hipSuccess)
         return err;
     if (!a.out && a.hidden == a.partial)
         return hipSuccess;
-    // columns by blocks of 512, as far as that makes fewer than 2^14 blocks
-    const int64_t want = std::max<int64_t>(1, (1 << 14) / a.n_tiles);
-    const int32_t blocks = (int32_t)std::min<int64_t>(a.out ? (a.m + 511) / 512 : 1, want);
-    const dim3 grid((uint32_t)(a.n_tiles * blocks));
+    // about 2048 blocks, of 512 columns at most and a unit a wave at least
+    constexpr int kLeast = kWideWaves * Expand<W, CT, 2, BACK>::kCols;
+    const int64_t least = (a.m + kLeast - 1) / kLeast, most = (a.m + 511) / 512;
+    const int32_t blocks = !a.out ? 1 : (int32_t)std::min<int64_t>(
+        least, std::max<int64_t>(most, 2048 / a.n_tiles));
+    const dim3 grid((uint32_t)(a.n_tiles * blocks)), waves(kWideWaves * kWave);
     if (a.tiles)
-        hipLaunchKernelGGL((k_expand<W, CT, 2, BACK>), grid, dim3(kThreads), 0, stream, a, blocks);
+        hipLaunchKernelGGL((k_expand<W, CT, 2, BACK>), grid, waves, 0, stream, a, blocks);
     else
-        hipLaunchKernelGGL((k_expand<W, CT, 1, BACK>), grid, dim3(kThreads), 0, stream, a, blocks);
+        hipLaunchKernelGGL((k_expand<W, CT, 1, BACK>), grid, waves, 0, stream, a, blocks);
     return hipGetLastError();
 }
 
