@@ -20,10 +20,14 @@
 // rows of h are scaled by powers of two, since h may be past its range.  One term alone would
 // round h to 2^-9 or 2^-12.
 //
-// Operands come from memory in the lanes' own layout, 16 bytes a load, without LDS: a row's
-// 128 bytes by 8 loads of 16 lanes each.  Where a matrix lies the other way round (the
-// gradient of x takes up^T and down^T), a lane loads 4 rows of 8 columns and picks its terms
-// by byte permutes; its output columns are then 8 neighbours.
+// Memory is read and written by 8 lanes to 128 bytes of a row, which is where the matrix cores'
+// layouts (16 lanes, 16 rows) touch four times the cache lines a byte: with those, the L1's tags
+// were busy all the time (12289 x 5003 bfloat16 beside rank 24: 7.3e7 accesses, 1.1 a clock and
+// CU, 109 us for 246 MB).  A wave turns its pieces in LDS of its own, without barriers; 16-byte
+// slots are swizzled by the row.  A matrix whose rows are the ranks of one term (up, and
+// its transpose in the gradient) is contiguous over a unit of terms and is copied as it lies.
+// Where the gradient of x takes down^T, a lane loads 4 rows of 8 columns and picks its terms by
+// byte permutes; its output columns are then 8 neighbours.
 //
 // What bounds it: memory; x, base and out once, an adapter once a tile (from the L2 but for
 // the first).
@@ -200,115 +204,9 @@ __device__ __forceinline__ f32x4 mma_h(const uint32_t (&w)[kSize<W>], Frag h, f3
         return mma<W>({w[0], w[1], w[0], w[1]}, h, c);
 }
 
-// base and out of one row: out columns [col, col + kEls) from their sums, as many as there are.
-template <int W>
-struct Output {
-    const char *base;                   // the row's, or NULL
-    char *out;
-    bool base_i32, there;
-    float base_scale, scale;
-    int32_t m;
-
-    __device__ __forceinline__ void store(int32_t col, bool whole, const float (&sum)[kEls<W>],
-                                          const Frag &b) const
-    {
-        if (!there)
-            return;
-        uint32_t bits[kEls<W>];
-#pragma unroll
-        for (int u = 0; u < kEls<W>; ++u) {
-            float v = scale * sum[u];
-            if (base) {
-                float from;
-                if constexpr (W == kF32)
-                    from = base_i32 ? (float)(int32_t)b.w[u] : __uint_as_float(b.w[u]);
-                else if constexpr (W == kBf16)
-                    from = __uint_as_float(u & 1 ? b.w[u / 2] & 0xFFFF0000u : b.w[u / 2] << 16);
-                else
-                    from = (float)__builtin_bit_cast(_Float16,
-                                                     (uint16_t)(b.w[u / 2] >> (16 * (u & 1))));
-                v += base_scale * from;
-            }
-            bits[u] = el_bits<W>(v);
-        }
-        char *to = out + (int64_t)col * kSize<W>;
-        if (whole) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = kSize<W> == 4 ? bits[i] : bits[2 * i] | bits[2 * i + 1] << 16;
-            __builtin_memcpy(to, w, 16);
-        } else {
-#pragma unroll
-            for (int u = 0; u < kEls<W>; ++u)
-                if (col + u < m) {
-                    if constexpr (kSize<W> == 4)
-                        reinterpret_cast<uint32_t *>(to)[u] = bits[u];
-                    else
-                        reinterpret_cast<uint16_t *>(to)[u] = (uint16_t)bits[u];
-                }
-        }
-    }
-};
-
-// A tile and the lane's rows in it: 16 rt + l % 16.
-template <int RT>
-struct Tile {
-    Piece4 p;
-    int32_t row[RT];
-    bool there[RT];
-
-    // false: no tile
-    __device__ __forceinline__ bool take(const PassArgs &a, int64_t tile, int col)
-    {
-        if (a.tiles) {
-            p = a.tiles[tile];
-            if (p.group < 0)
-                return false;
-        } else {
-            const int32_t id = a.ids[tile];
-            p = {id >= 0 && id < a.groups ? id : a.groups, (int32_t)tile, 1, 0};
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int32_t at = rt * 16 + col;
-            there[rt] = at < p.count;
-            const int32_t place = p.first + (there[rt] ? at : 0);
-            row[rt] = a.order ? a.order[place] : place;
-        }
-        return true;
-    }
-};
-
-// Which of the E terms from k on a lane takes at the end of a row of n: it loads the row's last
-// E instead, which start `back` terms earlier, and keeps those that are its own.
-template <int W>
-struct End {
-    int32_t at;                         // where it loads
-    uint32_t keep[4];                   // of the words there
-
-    __device__ __forceinline__ End(int32_t k, int32_t n)
-    {
-        constexpr int E = kEls<W>;
-        at = min(k, n - E);
-        const int32_t back = k - at;    // (E or more: none is its own)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (kSize<W> == 4)
-                keep[i] = i >= back ? 0xFFFFFFFFu : 0u;
-            else
-                keep[i] = (2 * i >= back ? 0x0000FFFFu : 0u) |
-                          (2 * i + 1 >= back ? 0xFFFF0000u : 0u);
-        }
-    }
-    __device__ __forceinline__ Frag take(Frag f) const
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f.w[i] &= keep[i];
-        return f;
-    }
-};
+// ---- a wave's LDS ----
+// Rows of 128 bytes in 16-byte slots; slot p of row r is at place p ^ (r % 8).
+__device__ __forceinline__ int slot_at(int row, int p) { return row * 128 + ((p ^ (row & 7)) * 16); }
 
 __device__ __forceinline__ Frag load_16(const char *p)
 {
@@ -316,130 +214,201 @@ __device__ __forceinline__ Frag load_16(const char *p)
     __builtin_memcpy(f.w, p, 16);
     return f;
 }
+__device__ __forceinline__ Frag lds_frag(const char *p) { return *reinterpret_cast<const Frag *>(p); }
+__device__ __forceinline__ void lds_put(char *p, Frag f) { *reinterpret_cast<Frag *>(p) = f; }
 
-// E terms of a column of a matrix with `step` bytes from term to term.
-template <int W>
-__device__ __forceinline__ Frag load_across(const char *p, int64_t step)
-{
-    Frag f;
-    if constexpr (kSize<W> == 4) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            f.w[u] = *reinterpret_cast<const uint32_t *>(p + u * step);
-    } else {
-        uint32_t v[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            v[u] = *reinterpret_cast<const uint16_t *>(p + u * step);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f.w[i] = v[2 * i] | v[2 * i + 1] << 16;
+template <int W, int CT, int RT, bool BACK>
+struct Room {
+    static constexpr int E = kEls<W>;
+    static constexpr int kCols = BACK ? 16 * E : 8 * E;   // out columns of a unit
+    static constexpr int kX = RT * 16 * 128, kWeights = CT * 16 * 128;
+    static constexpr int kPitch = kCols + 4;              // floats of a row of sums
+    static constexpr int kSums = 16 * kPitch * 4;
+    static constexpr int kShrink = kX + kWeights, kExpand = kSums + (BACK ? 0 : kWeights);
+    static constexpr int kBytes = kShrink > kExpand ? kShrink : kExpand;
+};
+
+// A tile, the wave's place in it, and the lane's rows: 8 j + l / 8.
+template <int RT>
+struct Tile {
+    static constexpr int J = 2 * RT;
+    Piece4 p;
+    int32_t row[J];
+    bool there[J];
+    int lane, col, quad, eighth, piece;
+
+    __device__ __forceinline__ Tile()
+        : lane(threadIdx.x % kWave), col(lane % 16), quad(lane / 16), eighth(lane / 8),
+          piece(lane % 8)
+    {
     }
-    return f;
-}
+    // rows from the tile's `skip`-th on; false: there are none
+    __device__ __forceinline__ bool take(const PassArgs &a, int64_t tile, int skip = 0)
+    {
+        if (a.tiles) {
+            p = a.tiles[tile];
+            p.first += skip;
+            p.count -= skip;
+            if (p.group < 0 || p.count <= 0)
+                return false;
+        } else {
+            const int32_t id = a.ids[tile];
+            p = {id >= 0 && id < a.groups ? id : a.groups, (int32_t)tile, 1, 0};
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int32_t at = j * 8 + eighth;
+            there[j] = at < p.count;                      // (others read the tile's first row)
+            const int32_t place = p.first + (there[j] ? at : 0);
+            row[j] = a.order ? a.order[place] : place;
+        }
+        return true;
+    }
+    // of row 16 rt + l % 16
+    __device__ __forceinline__ int32_t sample(int rt) const
+    {
+        const int from = col % 8 * 8;
+        const int32_t low = __shfl(row[2 * rt], from), high = __shfl(row[2 * rt + 1], from);
+        return col < 8 ? low : high;
+    }
+    __device__ __forceinline__ bool sample_there(int rt) const { return rt * 16 + col < p.count; }
+};
 
 // h += w1 x over terms [from, to): units of 128 bytes of a row, every `deal`-th from the
 // `turn`-th on; `to` is k or a multiple of the unit.  A unit's loads are issued before the
 // products of the one before.
 template <int W, int X, int CT, int RT, bool BACK>
-__device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, int col, int quad,
+__device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, char *lds,
                                        int32_t from, int32_t to, int turn, int deal,
                                        f32x4 (&h)[RT][CT])
 {
-    constexpr int E = kEls<W>, S = kSize<W>, kUnit = 8 * E;
-    const char *x[RT], *w1[CT];
+    constexpr int E = kEls<W>, S = kSize<W>, kUnit = 8 * E, J = 2 * RT, C = 2 * CT;
+    char *lds_w = lds + RT * 16 * 128;
+    const char *x[J], *w[BACK ? 1 : C];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-        x[rt] = a.x + tile.row[rt] * a.x_stride;
+    for (int j = 0; j < J; ++j)
+        x[j] = a.x + tile.row[j] * a.x_stride + tile.piece * 16;
     const char *first = a.w1 + tile.p.group * a.w1_step;
-    const int64_t across = (int64_t)a.rank * S;           // BACK: from term to term
+    if constexpr (!BACK) {
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        // ranks behind the last one read its weights: what comes of it is cleared afterwards
-        const int32_t r = min(ct * 16 + col, a.rank - 1);
-        w1[ct] = first + (BACK ? (int64_t)r : (int64_t)r * a.k) * S;
+        for (int c = 0; c < C; ++c) {
+            // ranks behind the last one read its weights: what comes of it is cleared afterwards
+            const int32_t r = min(c * 8 + tile.eighth, a.rank - 1);
+            w[c] = first + (int64_t)r * a.k * S + tile.piece * 16;
+        }
     }
+    const int32_t pieces = 8 * a.rank;                    // BACK: of a unit's weights
+    const int64_t across = (int64_t)a.rank * S;
     struct Unit {
-        Frag x[2][RT], w[2][CT];
+        Frag x[J], w[C];
     };
     const auto load = [&](Unit &u, int32_t k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int32_t k = k0 + half * 4 * E + quad * E;
+        for (int j = 0; j < J; ++j)
+            u.x[j] = load_16(x[j] + (int64_t)k0 * S);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-                u.x[half][rt] = load_16(x[rt] + (int64_t)k * S);
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-                u.w[half][ct] = BACK ? load_across<W>(w1[ct] + k * across, across)
-                                     : load_16(w1[ct] + (int64_t)k * S);
+        for (int c = 0; c < C; ++c) {
+            if constexpr (!BACK) {
+                u.w[c] = load_16(w[c] + (int64_t)k0 * S);
+            } else {
+                const int at = c * kWave + tile.lane;
+                if (at < pieces)
+                    u.w[c] = load_16(first + k0 * across + at * 16);
+            }
         }
     };
-    const auto products = [&](const Unit &u) __attribute__((always_inline)) {
+    const auto put = [&](const Unit &u) __attribute__((always_inline)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int j = 0; j < J; ++j)
+            lds_put(lds + slot_at(j * 8 + tile.eighth, tile.piece), to_terms<X>(u.x[j]));
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const Frag t = to_terms<X>(u.x[half][rt]);
+        for (int c = 0; c < C; ++c) {
+            if constexpr (!BACK) {
+                lds_put(lds_w + slot_at(c * 8 + tile.eighth, tile.piece), u.w[c]);
+            } else {
+                const int at = c * kWave + tile.lane;
+                if (at < pieces)
+                    lds_put(lds_w + at * 16, u.w[c]);
+            }
+        }
+    };
+    const auto products = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            Frag fx[RT], fw[CT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                fx[rt] = lds_frag(lds + slot_at(rt * 16 + tile.col, half * 4 + tile.quad));
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if constexpr (!BACK) {
+                    fw[ct] = lds_frag(lds_w + slot_at(ct * 16 + tile.col, half * 4 + tile.quad));
+                } else {
+                    const int32_t r = min(ct * 16 + tile.col, a.rank - 1);
+                    const int at = (half * 4 + tile.quad) * E * a.rank + r;
+                    if constexpr (S == 4) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            fw[ct].w[e] = reinterpret_cast<uint32_t *>(lds_w)[at + e * a.rank];
+                    } else {
+                        uint32_t v[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            v[e] = reinterpret_cast<uint16_t *>(lds_w)[at + e * a.rank];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            fw[ct].w[i] = v[2 * i] | v[2 * i + 1] << 16;
+                    }
+                }
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
-                    h[rt][ct] = mma<W>(u.w[half][ct], t, h[rt][ct]);
-            }
+                    h[rt][ct] = mma<W>(fw[ct], fx[rt], h[rt][ct]);
+        }
     };
     const int32_t whole = min(to, a.k / kUnit * kUnit), step = deal * kUnit;
     int32_t k0 = from + turn * kUnit;
     if (k0 < whole) {
-        Unit now, next;
-        load(now, k0);
-        for (;;) {
-            k0 += step;
-            if (k0 >= whole)
-                break;
-            load(next, k0);
-            products(now);
-            now = next;
-        }
-        products(now);
-    }
-    if (k0 < to) {                                        // the row's last terms
         Unit u;
-        if (a.k >= E) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const End<W> end(k0 + half * 4 * E + quad * E, a.k);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    u.x[half][rt] = end.take(load_16(x[rt] + (int64_t)end.at * S));
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-                    u.w[half][ct] = end.take(
-                        BACK ? load_across<W>(w1[ct] + end.at * across, across)
-                             : load_16(w1[ct] + (int64_t)end.at * S));
-            }
-        } else {                                          // fewer than one load's
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int32_t left = half == 0 && quad == 0 ? a.k : 0;
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    u.x[half][rt] = load_frag<W>(x[rt], left);
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    Frag f = {{0, 0, 0, 0}};
-                    for (int32_t i = 0; i < left; ++i) {  // (a run-time index of few)
-                        const char *el = w1[ct] + i * (BACK ? across : S);
-                        const uint32_t v = S == 4 ? *reinterpret_cast<const uint32_t *>(el)
-                                                  : *reinterpret_cast<const uint16_t *>(el);
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (e == i)
-                                f.w[e * S / 4] |= S == 4 ? v : v << (16 * (e & 1));
-                    }
-                    u.w[half][ct] = f;
-                }
-            }
+        load(u, k0);
+        for (;;) {
+            put(u);
+            rows::wave_sync();
+            k0 += step;
+            const bool more = k0 < whole;
+            if (more)
+                load(u, k0);
+            products();
+            rows::wave_sync();
+            if (!more)
+                break;
         }
-        products(u);
+    }
+    if (k0 < to) {                                        // the row's last terms, zeros after them
+        const int32_t left = a.k - k0 - tile.piece * E;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            lds_put(lds + slot_at(j * 8 + tile.eighth, tile.piece),
+                    to_terms<X>(load_frag<W>(x[j] + (int64_t)k0 * S, left)));
+        if constexpr (!BACK) {
+#pragma unroll 1
+            for (int c = 0; c < C; ++c) {
+                const int32_t r = min(c * 8 + tile.eighth, a.rank - 1);
+                lds_put(lds_w + slot_at(c * 8 + tile.eighth, tile.piece),
+                        load_frag<W>(first + ((int64_t)r * a.k + k0) * S + tile.piece * 16, left));
+            }
+        } else {
+            const int32_t there = (a.k - k0) * a.rank;
+#pragma unroll 1
+            for (int at = tile.lane; at < pieces; at += kWave)
+                lds_put(lds_w + at * 16, load_frag<W>(first + k0 * across + at * 16,
+                                                      there - at * E));
+        }
+        rows::wave_sync();
+        products();
+        rows::wave_sync();
     }
 }
 
@@ -466,86 +435,73 @@ __device__ __forceinline__ void clear_past_rank(int32_t rank, int quad, f32x4 (&
                     h[rt][ct][i] = 0.0f;
 }
 
-template <int RT, int CT>
-__device__ __forceinline__ void store_hidden(float *to, int32_t rank, const Tile<RT> &tile,
-                                             int quad, const f32x4 (&h)[RT][CT])
+// Ranks r .. r + 3 of a row of h, as many as there are.
+__device__ __forceinline__ void store_ranks(float *row, int32_t r, int32_t rank, f32x4 v)
 {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-        if (tile.there[rt])
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const int32_t r = ct * 16 + quad * 4;
-                float *at = to + (int64_t)tile.row[rt] * rank + r;
-                if (r + 4 <= rank) {
-                    __builtin_memcpy(at, &h[rt][ct], 16);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 3; ++i)
-                        if (r + i < rank)
-                            at[i] = h[rt][ct][i];
-                }
-            }
-}
-
-// Four ranks of a row of `rank` from r on; zeros past the last one.
-template <int W>
-__device__ __forceinline__ void load_ranks(const char *row, int32_t r, int32_t rank,
-                                           uint32_t (&w)[kSize<W>])
-{
-    constexpr int S = kSize<W>;
     if (r + 4 <= rank) {
-        __builtin_memcpy(w, row + r * S, 4 * S);
+        __builtin_memcpy(row + r, &v, 16);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < S; ++i)
-        w[i] = 0;
+    for (int i = 0; i < 3; ++i)
+        if (r + i < rank)
+            row[r + i] = v[i];
+}
+__device__ __forceinline__ f32x4 load_ranks(const float *row, int32_t r, int32_t rank)
+{
+    f32x4 v = {0, 0, 0, 0};
+    if (r + 4 <= rank) {
+        __builtin_memcpy(&v, row + r, 16);
+        return v;
+    }
 #pragma unroll
     for (int i = 0; i < 3; ++i)
-        if (r + i < rank) {
-            if constexpr (S == 4)
-                w[i] = reinterpret_cast<const uint32_t *>(row)[r + i];
-            else
-                w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[r + i]
-                            << (16 * (i & 1));
-        }
+        if (r + i < rank)
+            v[i] = row[r + i];
+    return v;
+}
+
+template <int RT, int CT>
+__device__ __forceinline__ void store_hidden(float *to, int32_t rank, const Tile<RT> &tile,
+                                             const f32x4 (&h)[RT][CT])
+{
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int32_t row = tile.sample(rt);
+        if (tile.sample_there(rt))
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+                store_ranks(to + (int64_t)row * rank, ct * 16 + tile.quad * 4, rank, h[rt][ct]);
+    }
 }
 
 // out = base + scale w2 h: units of columns, every `deal`-th from the `turn`-th on.  The next
 // unit's base is loaded, and the next weights where registers allow, before this one's products.
 template <int W, int CT, int RT, bool BACK>
 struct Expand {
-    static constexpr int E = kEls<W>, S = kSize<W>;
-    static constexpr int kCols = BACK ? 16 * E : 32;      // of a unit
-    static constexpr int kPieces = S == 2 ? 1 : 2;        // forward: loads of base a row
-    static constexpr bool kAhead = (BACK ? 16 : 2 * S) * CT <= 32;
+    typedef Room<W, CT, RT, BACK> R;
+    static constexpr int E = kEls<W>, S = kSize<W>, J = 2 * RT, C = 2 * CT;
+    static constexpr int kCols = R::kCols, T = kCols / 16;
+    static constexpr bool kAhead = BACK ? CT == 1 : CT <= 2;   // the next weights in registers
     struct Weights {
-        uint32_t w[BACK ? 1 : 2][CT][S];                  // forward: 4 ranks of two tiles' rows
-        Frag f[BACK ? CT : 1][4];                         // back: 4 ranks of E columns
+        Frag f[BACK ? CT * 4 : C];      // back: 4 ranks of E columns, forward: pieces as they lie
     };
     struct Base {
-        Frag f[RT][kPieces];
+        Frag f[J];
     };
     const PassArgs &a;
+    const Tile<RT> &tile;
     const char *w2;
-    Output<W> o[RT];
-    int col, quad;
+    char *lds_w;
+    float *sums;
+    float scale;
     bool adapted;
 
-    __device__ __forceinline__ Expand(const PassArgs &args, const Tile<RT> &tile, int c, int q)
-        : a(args), col(c), quad(q), adapted(tile.p.group < args.groups)
+    __device__ __forceinline__ Expand(const PassArgs &args, const Tile<RT> &t, char *lds)
+        : a(args), tile(t), lds_w(lds + R::kSums), sums(reinterpret_cast<float *>(lds)),
+          adapted(t.p.group < args.groups)
     {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            o[rt].base = BACK || !a.base ? nullptr : a.base + tile.row[rt] * a.base_stride;
-            o[rt].out = a.out + tile.row[rt] * a.out_stride;
-            o[rt].base_i32 = a.base_i32;
-            o[rt].there = tile.there[rt];
-            o[rt].base_scale = a.base_scale;
-            o[rt].m = a.m;
-            o[rt].scale = !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
-        }
+        scale = !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
         w2 = a.w2 + (adapted ? tile.p.group * a.w2_step : 0);
     }
     __device__ __forceinline__ void load_base(Base &b, int32_t m0) const
@@ -553,59 +509,169 @@ struct Expand {
         if constexpr (!BACK) {
             if (!a.base)
                 return;
+            const int32_t m = m0 + tile.piece * E;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int32_t m = m0 + i * 16 + quad * E;
-                    if (m0 + kCols <= a.m)                // (rows that are not there: the first)
-                        b.f[rt][i] = load_16(o[rt].base + (int64_t)m * S);
-                    else
-                        b.f[rt][i] = load_frag<W>(o[rt].base + (int64_t)m * S, a.m - m);
-                }
+            for (int j = 0; j < J; ++j) {
+                const char *from = a.base + tile.row[j] * a.base_stride + (int64_t)m * S;
+                if (m0 + kCols <= a.m)
+                    b.f[j] = load_16(from);
+                else
+                    b.f[j] = load_frag<W>(from, a.m - m);
+            }
         }
-    }
-    // forward: the tiles' rows of w2; 16-bit types give a lane 8 neighbours of them
-    __device__ __forceinline__ int32_t column(int t) const
-    {
-        return S == 2 ? col / 4 * 8 + t * 4 + col % 4 : t * 16 + col;
     }
     __device__ __forceinline__ void load_weights(Weights &w, int32_t m0) const
     {
         if (!adapted)
             return;
         if constexpr (!BACK) {
+            if (!by_pieces(m0))
+                return;                                   // (put() loads them)
+            const char *from = w2 + (int64_t)m0 * a.rank * S;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const char *row = w2 + (int64_t)min(m0 + column(t), a.m - 1) * a.rank * S;
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-                    load_ranks<W>(row, ct * 16 + quad * 4, a.rank, w.w[t][ct]);
+            for (int c = 0; c < C; ++c) {
+                const int at = c * kWave + tile.lane;
+                if (at < 8 * a.rank)
+                    w.f[c] = load_16(from + at * 16);
             }
         } else {
-            const int32_t m = m0 + col * E;
+            const int32_t m = m0 + tile.col * E;
+            const bool whole = m0 + kCols <= a.m;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int32_t r = ct * 16 + quad * 4 + i;
+                    const int32_t r = ct * 16 + tile.quad * 4 + i;
                     const char *from = w2 + ((int64_t)min(r, a.rank - 1) * a.m + m) * S;
                     Frag f;
-                    if (m0 + kCols <= a.m)
+                    if (whole)
                         f = load_16(from);
                     else
                         f = load_frag<W>(from, a.m - m);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)           // (their h is zero, they may be NaNs)
                         f.w[e] = r < a.rank ? f.w[e] : 0;
-                    w.f[ct][i] = f;
+                    w.f[ct * 4 + i] = f;
+                }
+        }
+    }
+    // forward: the weights into LDS, [columns][ranks up to a multiple of 4, zeros past the last]
+    __device__ __forceinline__ void put(const Weights &w, int32_t m0) const
+    {
+        if constexpr (!BACK) {
+            if (!adapted)
+                return;
+            if (by_pieces(m0)) {
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int at = c * kWave + tile.lane;
+                    if (at < 8 * a.rank)
+                        lds_put(lds_w + at * 16, w.f[c]);
+                }
+            } else {                                      // four ranks of a column at a time
+                const int fours = (a.rank + 3) / 4, there = min(a.m - m0, kCols) * fours;
+                const char *from = w2 + (int64_t)m0 * a.rank * S;
+#pragma unroll 1
+                for (int at = tile.lane; at < there; at += kWave) {
+                    const int m = at / fours, r = (at - m * fours) * 4;
+                    const char *row = from + (m * a.rank + r) * S;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (S == 4)
+                            reinterpret_cast<uint32_t *>(lds_w)[at * 4 + i] =
+                                r + i < a.rank ? reinterpret_cast<const uint32_t *>(row)[i] : 0;
+                        else
+                            reinterpret_cast<uint16_t *>(lds_w)[at * 4 + i] =
+                                r + i < a.rank ? reinterpret_cast<const uint16_t *>(row)[i] : 0;
+                    }
+                }
+            }
+            rows::wave_sync();
+        }
+    }
+    __device__ __forceinline__ bool by_pieces(int32_t m0) const
+    {
+        return a.rank % 4 == 0 && m0 + kCols <= a.m;
+    }
+    // 4 ranks of column t 16 + l % 16 (forward) or t + E (l % 16) (back), zeros past the last
+    __device__ __forceinline__ void terms_of(const Weights &w, int t, int ct,
+                                             uint32_t (&v)[S]) const
+    {
+        if constexpr (!BACK) {
+            const int32_t pitch = (a.rank + 3) & ~3, r = ct * 16 + tile.quad * 4;
+            const int at = ((t * 16 + tile.col) * pitch + r) * S;
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+                v[i] = 0;
+            if (r < pitch) {
+                if constexpr (S == 4) {
+                    const Frag f = lds_frag(lds_w + at);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        v[i] = f.w[i];
+                } else {
+                    const uint64_t f = *reinterpret_cast<const uint64_t *>(lds_w + at);
+                    v[0] = (uint32_t)f;
+                    v[1] = (uint32_t)(f >> 32);
+                }
+            }
+        } else if constexpr (S == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = w.f[ct * 4 + i].w[t];
+        } else {
+            const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                v[i] = __builtin_amdgcn_perm(w.f[ct * 4 + 2 * i + 1].w[t / 2],
+                                             w.f[ct * 4 + 2 * i].w[t / 2], pick);
+        }
+    }
+    // E columns from m on of the lane's row j
+    __device__ __forceinline__ void store(int j, int32_t m, const float *from, const Frag &b,
+                                          bool whole) const
+    {
+        float v[E];
+        __builtin_memcpy(v, from, sizeof v);
+        if (!BACK && a.base) {
+#pragma unroll
+            for (int u = 0; u < E; ++u) {
+                float c;
+                if constexpr (W == kF32)
+                    c = a.base_i32 ? (float)(int32_t)b.w[u] : __uint_as_float(b.w[u]);
+                else if constexpr (W == kBf16)
+                    c = __uint_as_float(u & 1 ? b.w[u / 2] & 0xFFFF0000u : b.w[u / 2] << 16);
+                else
+                    c = (float)__builtin_bit_cast(_Float16,
+                                                  (uint16_t)(b.w[u / 2] >> (16 * (u & 1))));
+                v[u] += a.base_scale * c;
+            }
+        }
+        if (!tile.there[j])
+            return;
+        char *to = a.out + tile.row[j] * a.out_stride + (int64_t)m * S;
+        if (whole) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = S == 4 ? el_bits<W>(v[i])
+                              : el_bits<W>(v[2 * i % E]) | el_bits<W>(v[(2 * i + 1) % E]) << 16;
+            __builtin_memcpy(to, w, 16);
+        } else {
+#pragma unroll
+            for (int u = 0; u < E; ++u)
+                if (m + u < a.m) {
+                    if constexpr (S == 4)
+                        reinterpret_cast<uint32_t *>(to)[u] = el_bits<W>(v[u]);
+                    else
+                        reinterpret_cast<uint16_t *>(to)[u] = (uint16_t)el_bits<W>(v[u]);
                 }
         }
     }
     __device__ __forceinline__ void unit(int32_t m0, const Weights &w, const Base &b,
-                                         const Frag (&terms)[RT][CT]) const
+                                         const Frag (&terms)[RT][CT],
+                                         const float (&factor)[RT]) const
     {
-        constexpr int T = BACK ? E : 2;
         f32x4 sum[T][RT];
         clear(sum);
         if (adapted)
@@ -614,21 +680,7 @@ struct Expand {
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
                     uint32_t v[S];
-                    if constexpr (!BACK) {
-#pragma unroll
-                        for (int i = 0; i < S; ++i)
-                            v[i] = w.w[t][ct][i];
-                    } else if constexpr (S == 4) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            v[i] = w.f[ct][i].w[t];
-                    } else {
-                        const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            v[i] = __builtin_amdgcn_perm(w.f[ct][2 * i + 1].w[t / 2],
-                                                         w.f[ct][2 * i].w[t / 2], pick);
-                    }
+                    terms_of(w, t, ct, v);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
                         sum[t][rt] = mma_h<W>(v, terms[rt][ct], sum[t][rt]);
@@ -636,26 +688,34 @@ struct Expand {
         const bool whole = m0 + kCols <= a.m;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+            float *own = sums + tile.col * R::kPitch;     // the lane's row of sums
             if constexpr (!BACK) {
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    float v[E];
-#pragma unroll
-                    for (int u = 0; u < E; ++u)
-                        v[u] = sum[S == 2 ? u / 4 : i][rt][u % 4];
-                    o[rt].store(m0 + i * 16 + quad * E, whole, v, b.f[rt][i]);
-                }
+                for (int t = 0; t < T; ++t)
+                    *reinterpret_cast<f32x4 *>(own + t * 16 + tile.quad * 4) =
+                        sum[t][rt] * factor[rt];
             } else {
-                // tile t has columns t, E + t, 2 E + t, ...
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v[E];
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int t = 0; t < E; ++t)
-                        v[t] = sum[t][rt][i];
-                    o[rt].store(m0 + (quad * 4 + i) * E, whole, v, {{0, 0, 0, 0}});
-                }
+                    for (int q = 0; q < E / 4; ++q) {
+                        f32x4 v;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            v[u] = sum[q * 4 + u][rt][i] * factor[rt];
+                        *reinterpret_cast<f32x4 *>(own + (tile.quad * 4 + i) * E + q * 4) = v;
+                    }
             }
+            rows::wave_sync();
+#pragma unroll
+            for (int j = 2 * rt; j < 2 * rt + 2; ++j)
+#pragma unroll
+                for (int q = 0; q < (BACK ? 2 : 1); ++q) {
+                    const int at = (tile.piece + q * 8) * E;
+                    store(j, m0 + at, sums + ((j & 1) * 8 + tile.eighth) * R::kPitch + at, b.f[j],
+                          whole);
+                }
+            rows::wave_sync();
         }
     }
     __device__ __forceinline__ void run(int turn, int deal, Base &b, const f32x4 (&h)[RT][CT])
@@ -671,154 +731,156 @@ struct Expand {
         make_terms<W>(h, terms, factor);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
-            o[rt].scale *= factor[rt];
+            factor[rt] *= scale;
         for (;;) {
             const int32_t next = m0 + deal * kCols;
-            Weights w_next;
             Base b_next;
+            Weights w_back;
             if constexpr (!kAhead)
                 load_weights(w, m0);
+            put(w, m0);
             if (next < a.m) {
                 load_base(b_next, next);
-                if constexpr (kAhead)
-                    load_weights(w_next, next);
+                if constexpr (kAhead && !BACK)
+                    load_weights(w, next);                // (this unit's are in LDS)
+                else if constexpr (kAhead)
+                    load_weights(w_back, next);
             }
-            unit(m0, w, b, terms);
+            unit(m0, w, b, terms, factor);
             if (next >= a.m)
                 return;
             m0 = next;
             b = b_next;
-            if constexpr (kAhead)
-                w = w_next;
+            if constexpr (kAhead && BACK)
+                w = w_back;
         }
     }
 };
 
-// ---- narrow adapters: a wave a tile ----
+// ---- narrow adapters: a wave half a tile ----
+constexpr int kNarrowWaves = 4;
+// waves a SIMD to compile for
+template <int CT> constexpr int kWavesPerSimd = CT <= 2 ? 4 : CT == 4 ? 3 : 2;
+
 template <int W, int X, int CT, bool BACK>
-__global__ __launch_bounds__(256) void k_narrow(PassArgs a)
+__global__ __launch_bounds__(kNarrowWaves * kWave, kWavesPerSimd<CT>) void k_narrow(PassArgs a)
 {
-    constexpr int RT = kTile / 16;
-    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
-    const int64_t at = (int64_t)blockIdx.x * 4 +
-                       __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    Tile<RT> tile;
-    if (at >= a.n_tiles || !tile.take(a, at, col))
+    typedef Room<W, CT, 1, BACK> R;
+    __shared__ __align__(16) char lds[kNarrowWaves][R::kBytes];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t at = (int64_t)blockIdx.x * kNarrowWaves + wave;
+    Tile<1> tile;
+    if (at / 2 >= a.n_tiles || !tile.take(a, at / 2, (int)(at % 2) * 16))
         return;
-    f32x4 h[RT][CT];
+    f32x4 h[1][CT];
     clear(h);
-    Expand<W, CT, RT, BACK> expand(a, tile, col, quad);
-    typename Expand<W, CT, RT, BACK>::Base b;
+    Expand<W, CT, 1, BACK> expand(a, tile, lds[wave]);
+    typename Expand<W, CT, 1, BACK>::Base b;
     if (a.out)
         expand.load_base(b, 0);
     if (tile.p.group < a.groups) {
-        shrink<W, X, CT, RT, BACK>(a, tile, col, quad, 0, a.k, 0, 1, h);
-        clear_past_rank(a.rank, quad, h);
+        shrink<W, X, CT, 1, BACK>(a, tile, lds[wave], 0, a.k, 0, 1, h);
+        clear_past_rank(a.rank, tile.quad, h);
     }
     if (a.hidden)
-        store_hidden(a.hidden, a.rank, tile, quad, h);
+        store_hidden(a.hidden, a.rank, tile, h);
     if (a.out)
         expand.run(0, 1, b, h);
 }
 
 // ---- wide adapters ----
 constexpr int kWideWaves = 4;
-// waves that share a block's terms: as many as a rank's sums leave LDS for
+// waves that share a block's terms: as many as a rank's weights leave LDS for
 template <int CT> constexpr int kTermWaves = CT <= 2 ? 8 : 4;
 
 // Part `blockIdx % splits` of a tile's h, to [part][row][rank].
 template <int W, int X, int CT, int RT, bool BACK>
-__global__ __launch_bounds__(kTermWaves<CT> * kWave) void k_shrink(PassArgs a)
+__global__ __launch_bounds__(kTermWaves<CT> * kWave, kWavesPerSimd<CT>) void k_shrink(PassArgs a)
 {
     constexpr int NW = kTermWaves<CT>, kAcc = CT * RT * 4, kUnit = 8 * kEls<W>;
-    __shared__ float joined[NW * kAcc * kWave];
-    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
+    constexpr int kWaveBytes = Room<W, CT, RT, BACK>::kShrink;
+    static_assert(kAcc * kWave * 4 <= kWaveBytes, "sums fit where the terms were");
+    __shared__ __align__(16) char lds[NW * kWaveBytes];
+    float *joined = reinterpret_cast<float *>(lds);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int64_t at = blockIdx.x / a.splits;
     const int part = (int)(blockIdx.x - at * a.splits);
     Tile<RT> tile;
-    if (!tile.take(a, at, col))
+    if (!tile.take(a, at))
         return;
-    f32x4 h[RT][CT];
-    clear(h);
-    if (tile.p.group < a.groups) {
+    const bool adapted = tile.p.group < a.groups;
+    if (adapted) {
+        f32x4 h[RT][CT];
+        clear(h);
         const int32_t units = (a.k + kUnit - 1) / kUnit;
         const int32_t each = (units + a.splits - 1) / a.splits;
         const int32_t from = min(part * each, units) * kUnit;
         const int32_t to = min(min((part + 1) * each, units) * kUnit, a.k);
-        shrink<W, X, CT, RT, BACK>(a, tile, col, quad, from, to, wave, NW, h);
-        clear_past_rank(a.rank, quad, h);
+        shrink<W, X, CT, RT, BACK>(a, tile, lds + wave * kWaveBytes, from, to, wave, NW, h);
+        clear_past_rank(a.rank, tile.quad, h);
         // the waves' sums, added in order; each wave adds up some of them
+        __syncthreads();
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    joined[(wave * kAcc + (rt * CT + ct) * 4 + i) * kWave + lane] = h[rt][ct][i];
+                    joined[(wave * kAcc + (rt * CT + ct) * 4 + i) * kWave + tile.lane] =
+                        h[rt][ct][i];
         __syncthreads();
     }
     // wave w stores fragments w, w + NW, ... of the tile's RT * CT
 #pragma unroll
-    for (int f = 0; f < RT * CT; ++f) {
-        if (f % NW != wave)
-            continue;
-        f32x4 sum = {0, 0, 0, 0};
-        if (tile.p.group < a.groups)
+    for (int rt = 0; rt < RT; ++rt) {
+        const int32_t row = tile.sample(rt);
 #pragma unroll
-            for (int w = 0; w < NW; ++w)
+        for (int ct = 0; ct < CT; ++ct) {
+            const int f = rt * CT + ct;
+            if (f % NW != wave)
+                continue;
+            f32x4 sum = {0, 0, 0, 0};
+            if (adapted)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    sum[i] += joined[(w * kAcc + f * 4 + i) * kWave + lane];
-        const int rt = f / CT, r = f % CT * 16 + quad * 4;
-        if (!tile.there[rt] || r >= a.rank)
-            continue;
-        float *to = a.partial + ((int64_t)part * a.n_rows + tile.row[rt]) * a.rank + r;
-        if (r + 4 <= a.rank) {
-            __builtin_memcpy(to, &sum, 16);
-        } else {
+                for (int w = 0; w < NW; ++w)
 #pragma unroll
-            for (int i = 0; i < 3; ++i)
-                if (r + i < a.rank)
-                    to[i] = sum[i];
+                    for (int i = 0; i < 4; ++i)
+                        sum[i] += joined[(w * kAcc + f * 4 + i) * kWave + tile.lane];
+            if (tile.sample_there(rt))
+                store_ranks(a.partial + ((int64_t)part * a.n_rows + row) * a.rank,
+                            ct * 16 + tile.quad * 4, a.rank, sum);
         }
     }
 }
 
-template <int W, int CT, int RT, bool BACK>
-__global__ __launch_bounds__(kWideWaves * kWave) void k_expand(PassArgs a, int32_t blocks)
+// 16 rows a wave: block (tile, half of its rows, columns).
+template <int W, int CT, bool BACK>
+__global__ __launch_bounds__(kWideWaves * kWave, kWavesPerSimd<CT>) void k_expand(PassArgs a,
+                                                                                int32_t blocks)
 {
-    const int lane = threadIdx.x % kWave, col = lane % 16, quad = lane / 16;
+    __shared__ __align__(16) char lds[kWideWaves][Room<W, CT, 1, BACK>::kExpand];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int64_t at = blockIdx.x / blocks;
     const int block = (int)(blockIdx.x - at * blocks);
-    Tile<RT> tile;
-    if (!tile.take(a, at, col))
+    Tile<1> tile;
+    if (a.tiles ? !tile.take(a, at / 2, (int)(at % 2) * 16) : !tile.take(a, at))
         return;
-    Expand<W, CT, RT, BACK> expand(a, tile, col, quad);
-    typename Expand<W, CT, RT, BACK>::Base b;
+    Expand<W, CT, 1, BACK> expand(a, tile, lds[wave]);
+    typename Expand<W, CT, 1, BACK>::Base b;
     const int turn = block * kWideWaves + wave;
     if (a.out && turn * expand.kCols < a.m)
         expand.load_base(b, turn * expand.kCols);
-    f32x4 h[RT][CT];
+    f32x4 h[1][CT];
     clear(h);
-#pragma unroll(CT <= 2 ? 2 : 1)
+    const int64_t row = tile.sample(0);
+#pragma unroll(CT <= 2 ? 4 : 2)
     for (int32_t p = 0; p < a.splits; ++p)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const float *from = a.partial + (p * a.n_rows + tile.row[rt]) * a.rank;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                uint32_t w[4];
-                load_ranks<kF32>(reinterpret_cast<const char *>(from), ct * 16 + quad * 4, a.rank,
-                                 w);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    h[rt][ct][i] += __uint_as_float(w[i]);
-            }
-        }
+        for (int ct = 0; ct < CT; ++ct)
+            h[0][ct] += load_ranks(a.partial + (p * a.n_rows + row) * a.rank,
+                                   ct * 16 + tile.quad * 4, a.rank);
     if (a.hidden && a.hidden != a.partial && block == 0 && wave == 0)
-        store_hidden(a.hidden, a.rank, tile, quad, h);
+        store_hidden(a.hidden, a.rank, tile, h);
     if (a.out)
         expand.run(turn, blocks * kWideWaves, b, h);
 }
@@ -827,8 +889,8 @@ template <int W, int X, int CT, bool BACK>
 hipError_t pass_of(const PassArgs &a, hipStream_t stream)
 {
     if (a.splits == 0) {
-        hipLaunchKernelGGL((k_narrow<W, X, CT, BACK>), dim3((uint32_t)((a.n_tiles + 3) / 4)),
-                           dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((k_narrow<W, X, CT, BACK>), dim3((uint32_t)((2 * a.n_tiles + kNarrowWaves - 1) / kNarrowWaves)),
+                           dim3(kNarrowWaves * kWave), 0, stream, a);
         return hipGetLastError();
     }
     const dim3 parts((uint32_t)(a.n_tiles * a.splits)), term_waves(kTermWaves<CT> * kWave);
@@ -841,15 +903,13 @@ hipError_t pass_of(const PassArgs &a, hipStream_t stream)
     if (!a.out && a.hidden == a.partial)
         return hipSuccess;
     // about 2048 blocks, of 512 columns at most and a unit a wave at least
-    constexpr int kLeast = kWideWaves * Expand<W, CT, 2, BACK>::kCols;
+    constexpr int kLeast = kWideWaves * Expand<W, CT, 1, BACK>::kCols;
+    const int64_t units = a.tiles ? 2 * a.n_tiles : a.n_tiles;
     const int64_t least = (a.m + kLeast - 1) / kLeast, most = (a.m + 511) / 512;
     const int32_t blocks = !a.out ? 1 : (int32_t)std::min<int64_t>(
-        least, std::max<int64_t>(most, 2048 / a.n_tiles));
-    const dim3 grid((uint32_t)(a.n_tiles * blocks)), waves(kWideWaves * kWave);
-    if (a.tiles)
-        hipLaunchKernelGGL((k_expand<W, CT, 2, BACK>), grid, waves, 0, stream, a, blocks);
-    else
-        hipLaunchKernelGGL((k_expand<W, CT, 1, BACK>), grid, waves, 0, stream, a, blocks);
+        least, std::max<int64_t>(most, 2048 / units));
+    hipLaunchKernelGGL((k_expand<W, CT, BACK>), dim3((uint32_t)(units * blocks)),
+                       dim3(kWideWaves * kWave), 0, stream, a, blocks);
     return hipGetLastError();
 }
 
