@@ -14,7 +14,7 @@ using rows::kF16;
 using rows::kF32;
 using rows::kI32;
 
-constexpr int kTile = 32;               // rows of a tile, all of one group
+constexpr int kTile = 64;               // rows of a tile, all of one group
 constexpr int32_t kMaxGroups = 4096;    // (a wave's counters in LDS)
 constexpr int32_t kMaxRank = 128;
 constexpr int32_t kMaxRuns = 1024;
@@ -120,12 +120,9 @@ struct PassArgs {
     int32_t splits;
 };
 
-// One kernel, a wave a tile, where rows come by a plan and a row of x and one of out are a few
-// units of 128 bytes each.
-inline bool is_narrow(bool planned, int32_t k, int32_t m, int32_t el_bytes)
-{
-    return planned && k <= 1024 / el_bytes && m <= 1024 / el_bytes;
-}
+// Whether a plan's rows go through one kernel, a tile and its adapter a block: rows of x and of
+// out of at most 512 bytes each, and 64 KB of LDS.
+template <int W> bool fits_narrow(int32_t k, int32_t m, int32_t rank, bool back);
 
 // Parts of the k terms of wide adapters: for about 1024 blocks, whose waves (8 or, above rank
 // 32, 4) have a unit of 128 bytes or more each.
@@ -142,13 +139,15 @@ struct PassLayout {
     int32_t splits;
     size_t bytes;                       // of partial
 };
-inline PassLayout pass_layout(int64_t n_rows, int32_t groups, int32_t rank, int32_t k, int32_t m,
-                              int32_t el_bytes, bool planned)
+inline PassLayout pass_layout(int64_t n_rows, int32_t groups, int32_t rank, int32_t k,
+                              int32_t el_bytes, bool planned, bool narrow)
 {
     PassLayout l;
     l.n_tiles = planned ? group_layout(n_rows, groups).n_tiles : n_rows;
-    l.narrow = is_narrow(planned, k, m, el_bytes);
-    l.splits = l.narrow || n_rows == 0 ? 0 : split_terms(l.n_tiles, k, rank, el_bytes);
+    l.narrow = planned && narrow;
+    l.splits = l.narrow || n_rows == 0
+                   ? 0 : split_terms(planned ? l.n_tiles * (kTile / 32) : n_rows, k, rank,
+                                     el_bytes);
     l.bytes = (size_t)l.splits * n_rows * rank * 4;
     return l;
 }

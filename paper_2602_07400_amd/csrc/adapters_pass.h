@@ -217,17 +217,6 @@ __device__ __forceinline__ Frag load_16(const char *p)
 __device__ __forceinline__ Frag lds_frag(const char *p) { return *reinterpret_cast<const Frag *>(p); }
 __device__ __forceinline__ void lds_put(char *p, Frag f) { *reinterpret_cast<Frag *>(p) = f; }
 
-template <int W, int CT, int RT, bool BACK>
-struct Room {
-    static constexpr int E = kEls<W>;
-    static constexpr int kCols = BACK ? 16 * E : 8 * E;   // out columns of a unit
-    static constexpr int kX = RT * 16 * 128, kWeights = CT * 16 * 128;
-    static constexpr int kPitch = kCols + 4;              // floats of a row of sums
-    static constexpr int kSums = 16 * kPitch * 4;
-    static constexpr int kShrink = kX + kWeights, kExpand = kSums + (BACK ? 0 : kWeights);
-    static constexpr int kBytes = kShrink > kExpand ? kShrink : kExpand;
-};
-
 // A tile, the wave's place in it, and the lane's rows: 8 j + l / 8.
 template <int RT>
 struct Tile {
@@ -264,6 +253,32 @@ struct Tile {
         }
         return true;
     }
+    // rows from the tile's `skip`-th on or, where there are none (false), its first
+    __device__ __forceinline__ bool take_or_first(const PassArgs &a, int64_t tile, int skip)
+    {
+        const bool any = take(a, tile, a.tiles ? skip : 0) && (a.tiles || skip == 0);
+        if (!any && p.group >= 0) {
+            if (a.tiles)
+                take(a, tile);
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                there[j] = false;
+        }
+        return any;
+    }
+    // as take(), of 16 rows: a lane's is l % 16.  Rows may be fewer than none: of tiles alone
+    // is said that there are none
+    __device__ __forceinline__ bool take_lanes(const PassArgs &a, int64_t tile, int skip)
+    {
+        p = a.tiles[tile];
+        if (p.group < 0)
+            return false;
+        p.first += skip;
+        p.count -= skip;
+        there[0] = col < p.count;
+        row[0] = there[0] ? a.order[p.first + col] : 0;
+        return true;
+    }
     // of row 16 rt + l % 16
     __device__ __forceinline__ int32_t sample(int rt) const
     {
@@ -274,13 +289,34 @@ struct Tile {
     __device__ __forceinline__ bool sample_there(int rt) const { return rt * 16 + col < p.count; }
 };
 
-// h += w1 x over terms [from, to): units of 128 bytes of a row, every `deal`-th from the
-// `turn`-th on; `to` is k or a multiple of the unit.  A unit's loads are issued before the
-// products of the one before.
+// E terms, `step` elements apart, of a matrix in LDS.
+template <int W>
+__device__ __forceinline__ Frag lds_across(const char *p, int at, int step)
+{
+    Frag f;
+    if constexpr (kSize<W> == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            f.w[e] = reinterpret_cast<const uint32_t *>(p)[at + e * step];
+    } else {
+        uint32_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = reinterpret_cast<const uint16_t *>(p)[at + e * step];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f.w[i] = v[2 * i] | v[2 * i + 1] << 16;
+    }
+    return f;
+}
+
+// h += w1 x over terms [from, to): units of 128 bytes of a row; `to` is k or a multiple of the
+// unit.  A unit's loads are issued before the products of the one before.  A wave's units are
+// neighbours: rows need not start at a cache line, and a line that two waves ask for at a time
+// stalls the L1 until it is there.
 template <int W, int X, int CT, int RT, bool BACK>
 __device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, char *lds,
-                                       int32_t from, int32_t to, int turn, int deal,
-                                       f32x4 (&h)[RT][CT])
+                                       int32_t from, int32_t to, f32x4 (&h)[RT][CT])
 {
     constexpr int E = kEls<W>, S = kSize<W>, kUnit = 8 * E, J = 2 * RT, C = 2 * CT;
     char *lds_w = lds + RT * 16 * 128;
@@ -345,20 +381,7 @@ __device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, 
                     fw[ct] = lds_frag(lds_w + slot_at(ct * 16 + tile.col, half * 4 + tile.quad));
                 } else {
                     const int32_t r = min(ct * 16 + tile.col, a.rank - 1);
-                    const int at = (half * 4 + tile.quad) * E * a.rank + r;
-                    if constexpr (S == 4) {
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            fw[ct].w[e] = reinterpret_cast<uint32_t *>(lds_w)[at + e * a.rank];
-                    } else {
-                        uint32_t v[E];
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            v[e] = reinterpret_cast<uint16_t *>(lds_w)[at + e * a.rank];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            fw[ct].w[i] = v[2 * i] | v[2 * i + 1] << 16;
-                    }
+                    fw[ct] = lds_across<W>(lds_w, (half * 4 + tile.quad) * E * a.rank + r, a.rank);
                 }
             }
 #pragma unroll
@@ -368,15 +391,15 @@ __device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, 
                     h[rt][ct] = mma<W>(fw[ct], fx[rt], h[rt][ct]);
         }
     };
-    const int32_t whole = min(to, a.k / kUnit * kUnit), step = deal * kUnit;
-    int32_t k0 = from + turn * kUnit;
+    const int32_t whole = min(to, a.k / kUnit * kUnit);
+    int32_t k0 = from;
     if (k0 < whole) {
         Unit u;
         load(u, k0);
         for (;;) {
             put(u);
             rows::wave_sync();
-            k0 += step;
+            k0 += kUnit;
             const bool more = k0 < whole;
             if (more)
                 load(u, k0);
@@ -475,348 +498,404 @@ __device__ __forceinline__ void store_hidden(float *to, int32_t rank, const Tile
     }
 }
 
-// out = base + scale w2 h: units of columns, every `deal`-th from the `turn`-th on.  The next
-// unit's base is loaded, and the next weights where registers allow, before this one's products.
-template <int W, int CT, int RT, bool BACK>
-struct Expand {
-    typedef Room<W, CT, RT, BACK> R;
-    static constexpr int E = kEls<W>, S = kSize<W>, J = 2 * RT, C = 2 * CT;
-    static constexpr int kCols = R::kCols, T = kCols / 16;
-    static constexpr bool kAhead = BACK ? CT == 1 : CT <= 2;   // the next weights in registers
-    struct Weights {
-        Frag f[BACK ? CT * 4 : C];      // back: 4 ranks of E columns, forward: pieces as they lie
-    };
-    struct Base {
-        Frag f[J];
-    };
-    const PassArgs &a;
-    const Tile<RT> &tile;
-    const char *w2;
-    char *lds_w;
-    float *sums;
-    float scale;
-    bool adapted;
+// ---- the second product, by 16 rows a wave ----
+// Its weights in LDS.  Forward: a column's ranks, a multiple of four (zeros past the last), in an
+// odd number of 16-byte slots, so that 16 columns are in different banks; back: a rank's columns.
+template <int W, int CT, bool BACK>
+struct Second {
+    static constexpr int E = kEls<W>, S = kSize<W>;
+    static constexpr int kCols = BACK ? 16 * E : 8 * E;   // a unit: columns whose sums a wave holds
+    static constexpr int T = kCols / 16;
+    static constexpr int kPitch = kCols + 4;              // floats of a row of a unit's sums
+    const char *lds;
+    int pitch, rank, col, quad;                           // pitch: bytes
 
-    __device__ __forceinline__ Expand(const PassArgs &args, const Tile<RT> &t, char *lds)
-        : a(args), tile(t), lds_w(lds + R::kSums), sums(reinterpret_cast<float *>(lds)),
-          adapted(t.p.group < args.groups)
+    // 4 ranks of column m + t 16 + l % 16 (forward) or m + t + E (l % 16) (back), zeros past the
+    // last rank
+    __device__ __forceinline__ void terms_of(int m, int ct, uint32_t (&v)[T][S]) const
     {
-        scale = !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
-        w2 = a.w2 + (adapted ? tile.p.group * a.w2_step : 0);
-    }
-    __device__ __forceinline__ void load_base(Base &b, int32_t m0) const
-    {
+        const int r = ct * 16 + quad * 4;
         if constexpr (!BACK) {
-            if (!a.base)
-                return;
-            const int32_t m = m0 + tile.piece * E;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const char *from = a.base + tile.row[j] * a.base_stride + (int64_t)m * S;
-                if (m0 + kCols <= a.m)
-                    b.f[j] = load_16(from);
-                else
-                    b.f[j] = load_frag<W>(from, a.m - m);
-            }
-        }
-    }
-    __device__ __forceinline__ void load_weights(Weights &w, int32_t m0) const
-    {
-        if (!adapted)
-            return;
-        if constexpr (!BACK) {
-            if (!by_pieces(m0))
-                return;                                   // (put() loads them)
-            const char *from = w2 + (int64_t)m0 * a.rank * S;
+            for (int t = 0; t < T; ++t) {
+                const char *at = lds + (m + t * 16 + col) * pitch + r * S;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int at = c * kWave + tile.lane;
-                if (at < 8 * a.rank)
-                    w.f[c] = load_16(from + at * 16);
+                for (int i = 0; i < S; ++i)
+                    v[t][i] = 0;
+                if (r < rank)
+                    __builtin_memcpy(v[t], __builtin_assume_aligned(at, 4 * S), 4 * S);
             }
         } else {
-            const int32_t m = m0 + tile.col * E;
-            const bool whole = m0 + kCols <= a.m;
+            Frag f[4];
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
+            for (int i = 0; i < 4; ++i) {
+                f[i] = lds_frag(lds + min(r + i, rank - 1) * pitch + (m + col * E) * S);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int32_t r = ct * 16 + tile.quad * 4 + i;
-                    const char *from = w2 + ((int64_t)min(r, a.rank - 1) * a.m + m) * S;
-                    Frag f;
-                    if (whole)
-                        f = load_16(from);
-                    else
-                        f = load_frag<W>(from, a.m - m);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)           // (their h is zero, they may be NaNs)
-                        f.w[e] = r < a.rank ? f.w[e] : 0;
-                    w.f[ct * 4 + i] = f;
-                }
-        }
-    }
-    // forward: the weights into LDS, [columns][ranks up to a multiple of 4, zeros past the last]
-    __device__ __forceinline__ void put(const Weights &w, int32_t m0) const
-    {
-        if constexpr (!BACK) {
-            if (!adapted)
-                return;
-            if (by_pieces(m0)) {
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const int at = c * kWave + tile.lane;
-                    if (at < 8 * a.rank)
-                        lds_put(lds_w + at * 16, w.f[c]);
-                }
-            } else {                                      // four ranks of a column at a time
-                const int fours = (a.rank + 3) / 4, there = min(a.m - m0, kCols) * fours;
-                const char *from = w2 + (int64_t)m0 * a.rank * S;
-#pragma unroll 1
-                for (int at = tile.lane; at < there; at += kWave) {
-                    const int m = at / fours, r = (at - m * fours) * 4;
-                    const char *row = from + (m * a.rank + r) * S;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (S == 4)
-                            reinterpret_cast<uint32_t *>(lds_w)[at * 4 + i] =
-                                r + i < a.rank ? reinterpret_cast<const uint32_t *>(row)[i] : 0;
-                        else
-                            reinterpret_cast<uint16_t *>(lds_w)[at * 4 + i] =
-                                r + i < a.rank ? reinterpret_cast<const uint16_t *>(row)[i] : 0;
-                    }
-                }
+                for (int e = 0; e < 4; ++e)
+                    f[i].w[e] = r + i < rank ? f[i].w[e] : 0;
             }
-            rows::wave_sync();
-        }
-    }
-    __device__ __forceinline__ bool by_pieces(int32_t m0) const
-    {
-        return a.rank % 4 == 0 && m0 + kCols <= a.m;
-    }
-    // 4 ranks of column t 16 + l % 16 (forward) or t + E (l % 16) (back), zeros past the last
-    __device__ __forceinline__ void terms_of(const Weights &w, int t, int ct,
-                                             uint32_t (&v)[S]) const
-    {
-        if constexpr (!BACK) {
-            const int32_t pitch = (a.rank + 3) & ~3, r = ct * 16 + tile.quad * 4;
-            const int at = ((t * 16 + tile.col) * pitch + r) * S;
 #pragma unroll
-            for (int i = 0; i < S; ++i)
-                v[i] = 0;
-            if (r < pitch) {
+            for (int t = 0; t < T; ++t) {
                 if constexpr (S == 4) {
-                    const Frag f = lds_frag(lds_w + at);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        v[i] = f.w[i];
+                        v[t][i] = f[i].w[t];
                 } else {
-                    const uint64_t f = *reinterpret_cast<const uint64_t *>(lds_w + at);
-                    v[0] = (uint32_t)f;
-                    v[1] = (uint32_t)(f >> 32);
+                    const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        v[t][i] = __builtin_amdgcn_perm(f[2 * i + 1].w[t / 2],
+                                                        f[2 * i].w[t / 2], pick);
                 }
             }
-        } else if constexpr (S == 4) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[i] = w.f[ct * 4 + i].w[t];
-        } else {
-            const uint32_t pick = t & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                v[i] = __builtin_amdgcn_perm(w.f[ct * 4 + 2 * i + 1].w[t / 2],
-                                             w.f[ct * 4 + 2 * i].w[t / 2], pick);
         }
     }
-    // E columns from m on of the lane's row j
-    __device__ __forceinline__ void store(int j, int32_t m, const float *from, const Frag &b,
-                                          bool whole) const
+    // factor w2 h of columns [m, m + kCols) to sums [16 rows][pitch floats], from column 0 on
+    __device__ __forceinline__ void unit(int m, const Frag (&terms)[CT], float factor, float *sums,
+                                         int sums_pitch) const
     {
-        float v[E];
-        __builtin_memcpy(v, from, sizeof v);
-        if (!BACK && a.base) {
+        f32x4 sum[T];
 #pragma unroll
-            for (int u = 0; u < E; ++u) {
-                float c;
-                if constexpr (W == kF32)
-                    c = a.base_i32 ? (float)(int32_t)b.w[u] : __uint_as_float(b.w[u]);
-                else if constexpr (W == kBf16)
-                    c = __uint_as_float(u & 1 ? b.w[u / 2] & 0xFFFF0000u : b.w[u / 2] << 16);
-                else
-                    c = (float)__builtin_bit_cast(_Float16,
-                                                  (uint16_t)(b.w[u / 2] >> (16 * (u & 1))));
-                v[u] += a.base_scale * c;
-            }
+        for (int t = 0; t < T; ++t)
+            sum[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            uint32_t v[T][S];
+            terms_of(m, ct, v);
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+                sum[t] = mma_h<W>(v[t], terms[ct], sum[t]);
         }
-        if (!tile.there[j])
-            return;
-        char *to = a.out + tile.row[j] * a.out_stride + (int64_t)m * S;
-        if (whole) {
-            uint32_t w[4];
+        float *own = sums + col * sums_pitch;             // the lane's row
+        if constexpr (!BACK) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = S == 4 ? el_bits<W>(v[i])
-                              : el_bits<W>(v[2 * i % E]) | el_bits<W>(v[(2 * i + 1) % E]) << 16;
-            __builtin_memcpy(to, w, 16);
+            for (int t = 0; t < T; ++t)
+                *reinterpret_cast<f32x4 *>(own + t * 16 + quad * 4) = sum[t] * factor;
         } else {
 #pragma unroll
-            for (int u = 0; u < E; ++u)
-                if (m + u < a.m) {
-                    if constexpr (S == 4)
-                        reinterpret_cast<uint32_t *>(to)[u] = el_bits<W>(v[u]);
-                    else
-                        reinterpret_cast<uint16_t *>(to)[u] = (uint16_t)el_bits<W>(v[u]);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < E / 4; ++q) {
+                    f32x4 v;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        v[u] = sum[q * 4 + u][i] * factor;
+                    *reinterpret_cast<f32x4 *>(own + (quad * 4 + i) * E + q * 4) = v;
                 }
-        }
-    }
-    __device__ __forceinline__ void unit(int32_t m0, const Weights &w, const Base &b,
-                                         const Frag (&terms)[RT][CT],
-                                         const float (&factor)[RT]) const
-    {
-        f32x4 sum[T][RT];
-        clear(sum);
-        if (adapted)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int t = 0; t < T; ++t) {
-                    uint32_t v[S];
-                    terms_of(w, t, ct, v);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-                        sum[t][rt] = mma_h<W>(v, terms[rt][ct], sum[t][rt]);
-                }
-        const bool whole = m0 + kCols <= a.m;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float *own = sums + tile.col * R::kPitch;     // the lane's row of sums
-            if constexpr (!BACK) {
-#pragma unroll
-                for (int t = 0; t < T; ++t)
-                    *reinterpret_cast<f32x4 *>(own + t * 16 + tile.quad * 4) =
-                        sum[t][rt] * factor[rt];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int q = 0; q < E / 4; ++q) {
-                        f32x4 v;
-#pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            v[u] = sum[q * 4 + u][rt][i] * factor[rt];
-                        *reinterpret_cast<f32x4 *>(own + (tile.quad * 4 + i) * E + q * 4) = v;
-                    }
-            }
-            rows::wave_sync();
-#pragma unroll
-            for (int j = 2 * rt; j < 2 * rt + 2; ++j)
-#pragma unroll
-                for (int q = 0; q < (BACK ? 2 : 1); ++q) {
-                    const int at = (tile.piece + q * 8) * E;
-                    store(j, m0 + at, sums + ((j & 1) * 8 + tile.eighth) * R::kPitch + at, b.f[j],
-                          whole);
-                }
-            rows::wave_sync();
-        }
-    }
-    __device__ __forceinline__ void run(int turn, int deal, Base &b, const f32x4 (&h)[RT][CT])
-    {
-        Weights w;
-        int32_t m0 = turn * kCols;
-        if (m0 >= a.m)
-            return;
-        if constexpr (kAhead)
-            load_weights(w, m0);
-        Frag terms[RT][CT];
-        float factor[RT];
-        make_terms<W>(h, terms, factor);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-            factor[rt] *= scale;
-        for (;;) {
-            const int32_t next = m0 + deal * kCols;
-            Base b_next;
-            Weights w_back;
-            if constexpr (!kAhead)
-                load_weights(w, m0);
-            put(w, m0);
-            if (next < a.m) {
-                load_base(b_next, next);
-                if constexpr (kAhead && !BACK)
-                    load_weights(w, next);                // (this unit's are in LDS)
-                else if constexpr (kAhead)
-                    load_weights(w_back, next);
-            }
-            unit(m0, w, b, terms, factor);
-            if (next >= a.m)
-                return;
-            m0 = next;
-            b = b_next;
-            if constexpr (kAhead && BACK)
-                w = w_back;
         }
     }
 };
 
-// ---- narrow adapters: a wave half a tile ----
-constexpr int kNarrowWaves = 4;
-// waves a SIMD to compile for
-template <int CT> constexpr int kWavesPerSimd = CT <= 2 ? 4 : CT == 4 ? 3 : 2;
+__device__ __forceinline__ int odd_slots(int bytes) { return (((bytes + 15) / 16) | 1) * 16; }
+
+// v += base_scale * base, E columns of it; b: its bits.
+template <int W>
+__device__ __forceinline__ void add_base(const PassArgs &a, float (&v)[kEls<W>], const Frag &b)
+{
+#pragma unroll
+    for (int u = 0; u < kEls<W>; ++u) {
+        float c;
+        if constexpr (W == kF32)
+            c = a.base_i32 ? (float)(int32_t)b.w[u] : __uint_as_float(b.w[u]);
+        else if constexpr (W == kBf16)
+            c = __uint_as_float(u & 1 ? b.w[u / 2] & 0xFFFF0000u : b.w[u / 2] << 16);
+        else
+            c = (float)__builtin_bit_cast(_Float16, (uint16_t)(b.w[u / 2] >> (16 * (u & 1))));
+        v[u] += a.base_scale * c;
+    }
+}
+
+// E results to memory, or as many as there are.
+template <int W>
+__device__ __forceinline__ void store_row(char *to, const float (&v)[kEls<W>], int32_t left)
+{
+    constexpr int E = kEls<W>, S = kSize<W>;
+    if (left >= E) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = S == 4 ? el_bits<W>(v[i])
+                          : el_bits<W>(v[2 * i % E]) | el_bits<W>(v[(2 * i + 1) % E]) << 16;
+        __builtin_memcpy(to, w, 16);
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < E; ++u)
+        if (u < left) {
+            if constexpr (S == 4)
+                reinterpret_cast<uint32_t *>(to)[u] = el_bits<W>(v[u]);
+            else
+                reinterpret_cast<uint16_t *>(to)[u] = (uint16_t)el_bits<W>(v[u]);
+        }
+}
+
+// Four ranks of a column of up [m][rank], zeros past the last.
+template <int W>
+__device__ __forceinline__ void load_four(const char *p, int left, uint32_t (&v)[kSize<W>])
+{
+    constexpr int S = kSize<W>;
+    if (left >= 4) {
+        __builtin_memcpy(v, p, 4 * S);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+        v[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (i < left) {
+            if constexpr (S == 4)
+                v[i] = reinterpret_cast<const uint32_t *>(p)[i];
+            else
+                v[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i & 1));
+        }
+}
+
+// ---- narrow adapters: 16 rows a wave, whole rows at a time ----
+// A block has a tile, and its adapter in LDS.  A wave copies its 16 rows of x there, and holds
+// those of base in registers meanwhile, by 16-byte pieces in the order of memory: of the lines at
+// the ends of rows, none is asked for twice.
+constexpr int kTileWaves = kTile / 16;
+
+// e / d for e < 2^13, d <= 2^7.
+struct Divide {
+    uint32_t magic;
+    __device__ __forceinline__ explicit Divide(int d) : magic(((1u << 20) + d - 1) / d) {}
+    __device__ __forceinline__ int operator()(int e) const { return (int)(e * magic >> 20); }
+};
+
+// `rows` rows of n elements, `stride` bytes apart, to LDS rows of `pitch` bytes, zeros to the end
+// of their last pieces; by all of a block.
+template <int W>
+__device__ __forceinline__ void stage_rows(char *to, int pitch, const char *from, int64_t stride,
+                                           int rows, int n)
+{
+    constexpr int E = kEls<W>;
+    const int pieces = n / E;
+    if (pieces > 0) {
+        const Divide row_of(pieces);
+#pragma unroll 4
+        for (int at = threadIdx.x; at < rows * pieces; at += kTileWaves * kWave) {
+            const int r = row_of(at), p = at - r * pieces;
+            lds_put(to + r * pitch + p * 16, load_16(from + r * stride + p * 16));
+        }
+    }
+    if (n % E)
+#pragma unroll 1
+        for (int r = threadIdx.x; r < rows; r += kTileWaves * kWave)
+            lds_put(to + r * pitch + pieces * 16,
+                    load_frag<W>(from + r * stride + pieces * 16, n % E));
+}
+
+// up [m][rank] of `cols` columns to LDS, a column in `pitch` bytes; by all of a block.
+template <int W>
+__device__ __forceinline__ void stage_up(char *to, int pitch, const char *from, int rank, int cols)
+{
+    constexpr int S = kSize<W>;
+    if (rank * S % 16 == 0) {
+        stage_rows<W>(to, pitch, from, (int64_t)rank * S, cols, rank);
+        return;
+    }
+    const int fours = (rank + 3) / 4;
+    const Divide col_of(fours);
+#pragma unroll 2
+    for (int at = threadIdx.x; at < cols * fours; at += kTileWaves * kWave) {
+        const int m = col_of(at), r = (at - m * fours) * 4;
+        uint32_t v[S];
+        load_four<W>(from + (m * rank + r) * S, rank - r, v);
+        __builtin_memcpy(__builtin_assume_aligned(to + m * pitch + r * S, 4 * S), v, 4 * S);
+    }
+}
+
+// LDS of a block: the first product's weights, the second's, and a wave's rows of x, later its
+// sums.
+template <int W, bool BACK>
+struct NarrowRoom {
+    int w1_pitch, w2_pitch, x_pitch, sums_pitch;          // bytes; sums_pitch floats
+    int w1, w2, wave;                                     // bytes
+
+    __host__ __device__ NarrowRoom(int k, int m, int rank)
+    {
+        constexpr int E = kEls<W>, S = kSize<W>, kCols = BACK ? 16 * E : 8 * E;
+        const auto odd = [](int bytes) { return (((bytes + 15) / 16) | 1) * 16; };
+        const int cols = (m + kCols - 1) / kCols * kCols; // whole units
+        x_pitch = odd(k * S);
+        sums_pitch = cols + 4;
+        w1_pitch = odd(k * S);
+        w2_pitch = BACK ? odd(cols * S) : odd(rank * S);
+        w1 = BACK ? ((k + E - 1) / E * E * rank * S + 15) / 16 * 16 : rank * w1_pitch;
+        w2 = BACK ? rank * w2_pitch : cols * w2_pitch;
+        const int sums = 16 * sums_pitch * 4, x = 16 * x_pitch;
+        wave = sums > x ? sums : x;
+    }
+    __host__ __device__ int bytes() const { return w1 + w2 + kTileWaves * wave; }
+};
 
 template <int W, int X, int CT, bool BACK>
-__global__ __launch_bounds__(kNarrowWaves * kWave, kWavesPerSimd<CT>) void k_narrow(PassArgs a)
+__global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(PassArgs a)
 {
-    typedef Room<W, CT, 1, BACK> R;
-    __shared__ __align__(16) char lds[kNarrowWaves][R::kBytes];
+    constexpr int E = kEls<W>, S = kSize<W>, F = 8;       // pieces of 16 rows: 512 at most
+    extern __shared__ __align__(16) char lds[];
+    const NarrowRoom<W, BACK> room(a.k, a.m, a.rank);
+    char *w1 = lds, *w2 = lds + room.w1;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int64_t at = (int64_t)blockIdx.x * kNarrowWaves + wave;
+    char *own = lds + room.w1 + room.w2 + wave * room.wave;
     Tile<1> tile;
-    if (at / 2 >= a.n_tiles || !tile.take(a, at / 2, (int)(at % 2) * 16))
-        return;
+    if (!tile.take_lanes(a, blockIdx.x, wave * 16))
+        return;                                           // (the whole block)
+    const bool adapted = tile.p.group < a.groups;
+    const int x_pieces = a.k / E, m_pieces = a.m / E;
+    const Divide x_row(max(x_pieces, 1)), m_row(max(m_pieces, 1));
+    Frag b[F], b_end = {{0, 0, 0, 0}};
+    const bool end_lane = tile.lane < tile.p.count && tile.lane < 16;
+    if (!BACK && a.base && a.out) {
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int at = i * kWave + tile.lane, r = m_row(at), p = at - r * m_pieces;
+            const int32_t row = __shfl(tile.row[0], r);
+            if (r < tile.p.count && at < 16 * m_pieces)
+                b[i] = load_16(a.base + row * a.base_stride + p * 16);
+        }
+        if (end_lane && a.m % E)
+            b_end = load_frag<W>(a.base + tile.row[0] * a.base_stride + m_pieces * 16, a.m % E);
+    }
     f32x4 h[1][CT];
     clear(h);
-    Expand<W, CT, 1, BACK> expand(a, tile, lds[wave]);
-    typename Expand<W, CT, 1, BACK>::Base b;
-    if (a.out)
-        expand.load_base(b, 0);
-    if (tile.p.group < a.groups) {
-        shrink<W, X, CT, 1, BACK>(a, tile, lds[wave], 0, a.k, 0, 1, h);
+    if (adapted) {
+        const char *down = a.w1 + tile.p.group * a.w1_step, *up = a.w2 + tile.p.group * a.w2_step;
+        Frag x[F];
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int at = i * kWave + tile.lane, r = x_row(at), p = at - r * x_pieces;
+            const int32_t row = __shfl(tile.row[0], r);
+            if (r < tile.p.count && at < 16 * x_pieces)
+                x[i] = load_16(a.x + row * a.x_stride + p * 16);
+        }
+        if constexpr (!BACK) {
+            stage_rows<W>(w1, room.w1_pitch, down, (int64_t)a.k * S, a.rank, a.k);
+            if (a.out)
+                stage_up<W>(w2, room.w2_pitch, up, a.rank, a.m);
+        } else {
+            const int there = a.k * a.rank;               // [k][rank] as it lies, zeros behind
+#pragma unroll 2
+            for (int at = threadIdx.x; at * 16 < room.w1; at += kTileWaves * kWave)
+                lds_put(w1 + at * 16, load_frag<W>(down + at * 16, there - at * E));
+            if (a.out)
+                stage_rows<W>(w2, room.w2_pitch, up, (int64_t)a.m * S, a.rank, a.m);
+        }
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const int at = i * kWave + tile.lane, r = x_row(at), p = at - r * x_pieces;
+            if (r < tile.p.count && at < 16 * x_pieces)
+                lds_put(own + r * room.x_pitch + p * 16, to_terms<X>(x[i]));
+        }
+        if (end_lane && a.k % E)
+            lds_put(own + tile.lane * room.x_pitch + x_pieces * 16,
+                    to_terms<X>(load_frag<W>(a.x + tile.row[0] * a.x_stride + x_pieces * 16,
+                                             a.k % E)));
+        __syncthreads();
+        // (rows that are not there: whatever is in LDS, in columns of their own)
+        const int pieces = (a.k + E - 1) / E;
+        for (int p0 = 0; p0 < pieces; p0 += 4) {
+            const int p = p0 + tile.quad;
+            Frag fx = {{0, 0, 0, 0}}, fw[CT];
+            if (p < pieces)
+                fx = lds_frag(own + tile.col * room.x_pitch + p * 16);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const int r = min(ct * 16 + tile.col, a.rank - 1);
+                fw[ct] = {{0, 0, 0, 0}};
+                if (p < pieces) {
+                    if constexpr (!BACK)
+                        fw[ct] = lds_frag(w1 + r * room.w1_pitch + p * 16);
+                    else
+                        fw[ct] = lds_across<W>(w1, p * E * a.rank + r, a.rank);
+                }
+                h[0][ct] = mma<W>(fw[ct], fx, h[0][ct]);
+            }
+        }
         clear_past_rank(a.rank, tile.quad, h);
+        rows::wave_sync();
     }
-    if (a.hidden)
-        store_hidden(a.hidden, a.rank, tile, h);
-    if (a.out)
-        expand.run(0, 1, b, h);
+    if (a.hidden && tile.col < tile.p.count)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+            store_ranks(a.hidden + (int64_t)tile.row[0] * a.rank, ct * 16 + tile.quad * 4, a.rank,
+                        h[0][ct]);
+    if (!a.out)
+        return;
+    float *sums = reinterpret_cast<float *>(own);
+    if (adapted) {
+        typedef Second<W, CT, BACK> Product;
+        const Product second = {w2, room.w2_pitch, a.rank, tile.col, tile.quad};
+        Frag terms[1][CT];
+        float factor[1];
+        make_terms<W>(h, terms, factor);
+        factor[0] *= a.scales ? a.scales[tile.p.group] : a.scale;
+#pragma unroll 1
+        for (int m = 0; m < a.m; m += Product::kCols)
+            second.unit(m, terms[0], factor[0], sums + m, room.sums_pitch);
+        rows::wave_sync();
+    }
+    const auto result = [&](int r, int p, const Frag &base, float (&v)[E]) __attribute__((always_inline)) {
+        if (adapted) {
+            __builtin_memcpy(v, sums + r * room.sums_pitch + p * E, sizeof v);
+        } else {
+#pragma unroll
+            for (int u = 0; u < E; ++u)
+                v[u] = 0.0f;
+        }
+        if (!BACK && a.base)
+            add_base<W>(a, v, base);
+    };
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        const int at = i * kWave + tile.lane, r = m_row(at), p = at - r * m_pieces;
+        const int32_t row = __shfl(tile.row[0], r);
+        if (r < tile.p.count && at < 16 * m_pieces) {
+            float v[E];
+            result(r, p, b[i], v);
+            store_row<W>(a.out + row * a.out_stride + p * 16, v, E);
+        }
+    }
+    if (end_lane && a.m % E) {
+        float v[E];
+        result(tile.lane, m_pieces, b_end, v);
+        store_row<W>(a.out + tile.row[0] * a.out_stride + m_pieces * 16, v, a.m % E);
+    }
 }
 
 // ---- wide adapters ----
-constexpr int kWideWaves = 4;
 // waves that share a block's terms: as many as a rank's weights leave LDS for
 template <int CT> constexpr int kTermWaves = CT <= 2 ? 8 : 4;
+// waves a SIMD to compile for
+template <int CT> constexpr int kWavesPerSimd = CT <= 2 ? 4 : CT == 4 ? 3 : 2;
 
-// Part `blockIdx % splits` of a tile's h, to [part][row][rank].
+// Part `blockIdx % splits` of the h of 32 rows of a tile, to [part][row][rank].
 template <int W, int X, int CT, int RT, bool BACK>
 __global__ __launch_bounds__(kTermWaves<CT> * kWave, kWavesPerSimd<CT>) void k_shrink(PassArgs a)
 {
     constexpr int NW = kTermWaves<CT>, kAcc = CT * RT * 4, kUnit = 8 * kEls<W>;
-    constexpr int kWaveBytes = Room<W, CT, RT, BACK>::kShrink;
+    constexpr int kWaveBytes = (RT + CT) * 16 * 128;
     static_assert(kAcc * kWave * 4 <= kWaveBytes, "sums fit where the terms were");
     __shared__ __align__(16) char lds[NW * kWaveBytes];
     float *joined = reinterpret_cast<float *>(lds);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int64_t at = blockIdx.x / a.splits;
     const int part = (int)(blockIdx.x - at * a.splits);
+    constexpr int kParts = RT == 2 ? kTile / 32 : 1;
     Tile<RT> tile;
-    if (!tile.take(a, at))
+    if (!tile.take(a, at / kParts, (int)(at % kParts) * 32))
         return;
     const bool adapted = tile.p.group < a.groups;
     if (adapted) {
         f32x4 h[RT][CT];
         clear(h);
-        const int32_t units = (a.k + kUnit - 1) / kUnit;
-        const int32_t each = (units + a.splits - 1) / a.splits;
-        const int32_t from = min(part * each, units) * kUnit;
-        const int32_t to = min(min((part + 1) * each, units) * kUnit, a.k);
-        shrink<W, X, CT, RT, BACK>(a, tile, lds + wave * kWaveBytes, from, to, wave, NW, h);
+        const int32_t units = (a.k + kUnit - 1) / kUnit, shares = a.splits * NW;
+        const int32_t each = (units + shares - 1) / shares, share = part * NW + wave;
+        const int32_t from = min(share * each, units) * kUnit;
+        const int32_t to = min(min((share + 1) * each, units) * kUnit, a.k);
+        shrink<W, X, CT, RT, BACK>(a, tile, lds + wave * kWaveBytes, from, to, h);
         clear_past_rank(a.rank, tile.quad, h);
         // the waves' sums, added in order; each wave adds up some of them
         __syncthreads();
@@ -853,23 +932,84 @@ __global__ __launch_bounds__(kTermWaves<CT> * kWave, kWavesPerSimd<CT>) void k_s
     }
 }
 
-// 16 rows a wave: block (tile, half of its rows, columns).
+// Units of columns of a tile, 16 rows a wave; a unit's weights are in LDS for all of them, the
+// next unit's on their way.
 template <int W, int CT, bool BACK>
-__global__ __launch_bounds__(kWideWaves * kWave, kWavesPerSimd<CT>) void k_expand(PassArgs a,
+__global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expand(PassArgs a,
                                                                                 int32_t blocks)
 {
-    __shared__ __align__(16) char lds[kWideWaves][Room<W, CT, 1, BACK>::kExpand];
+    typedef Second<W, CT, BACK> Product;
+    constexpr int E = kEls<W>, S = kSize<W>, kCols = Product::kCols, J = 2;
+    constexpr int kWeights = BACK ? CT * 16 * (kCols * S + 16)
+                                  : kCols * ((CT * 16 * S / 16) | 1) * 16;
+    constexpr int kPieces = (CT * 16 * kCols * S / 16 + 255) / 256;   // of the weights, a lane
+    __shared__ __align__(16) char weights[2][kWeights];
+    __shared__ __align__(16) float sums[kTileWaves][16 * Product::kPitch];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const int64_t at = blockIdx.x / blocks;
     const int block = (int)(blockIdx.x - at * blocks);
     Tile<1> tile;
-    if (a.tiles ? !tile.take(a, at / 2, (int)(at % 2) * 16) : !tile.take(a, at))
+    // (a wave without rows takes the tile's first one, and stores nothing)
+    const bool any = tile.take_or_first(a, at, wave * 16);
+    if (tile.p.group < 0)
         return;
-    Expand<W, CT, 1, BACK> expand(a, tile, lds[wave]);
-    typename Expand<W, CT, 1, BACK>::Base b;
-    const int turn = block * kWideWaves + wave;
-    if (a.out && turn * expand.kCols < a.m)
-        expand.load_base(b, turn * expand.kCols);
+    const bool adapted = tile.p.group < a.groups;
+    const int32_t units = (a.m + kCols - 1) / kCols, each = (units + blocks - 1) / blocks * kCols;
+    const int32_t from = block * each, to = a.out ? min(from + each, a.m) : 0;
+    Frag b[J], b_next[J];
+    const auto load_base = [&](Frag (&f)[J], int32_t m0) __attribute__((always_inline)) {
+        if constexpr (!BACK) {
+            if (!a.base || !any)
+                return;
+            const int32_t m = m0 + tile.piece * E;
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                f[j] = load_frag<W>(a.base + tile.row[j] * a.base_stride + (int64_t)m * S,
+                                    a.m - m);
+        }
+    };
+    if (from < to)
+        load_base(b, from);
+    // the weights of a unit: pieces to registers, and from there to LDS
+    const char *w2 = a.w2 + (adapted ? tile.p.group * a.w2_step : 0);
+    const int pitch = BACK ? kCols * S + 16 : odd_slots(a.rank * S);
+    const bool by_pieces = BACK || a.rank * S % 16 == 0;
+    const int per = BACK ? kCols * S / 16 : max(a.rank * S / 16, 1);  // pieces of an LDS row
+    const Divide row_of(per);
+    Frag w[kPieces];
+    const auto load_weights = [&](int32_t m0) __attribute__((always_inline)) {
+        if (!adapted || !by_pieces)
+            return;
+        const int all = BACK ? a.rank * per : min(a.m - m0, kCols) * per;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int e = i * kTileWaves * kWave + threadIdx.x, r = row_of(e), p = e - r * per;
+            if (e < all) {
+                if constexpr (BACK)
+                    w[i] = load_frag<W>(w2 + ((int64_t)r * a.m + m0) * S + p * 16,
+                                        a.m - m0 - p * E);
+                else
+                    w[i] = load_16(w2 + (int64_t)m0 * a.rank * S + e * 16);
+            }
+        }
+    };
+    const auto put_weights = [&](int32_t m0, char *to_lds) __attribute__((always_inline)) {
+        if (!adapted)
+            return;
+        if (!BACK && !by_pieces) {
+            stage_up<W>(to_lds, pitch, w2 + (int64_t)m0 * a.rank * S, a.rank, min(a.m - m0, kCols));
+            return;
+        }
+        const int all = BACK ? a.rank * per : min(a.m - m0, kCols) * per;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int e = i * kTileWaves * kWave + threadIdx.x, r = row_of(e), p = e - r * per;
+            if (e < all)
+                lds_put(to_lds + r * pitch + p * 16, w[i]);
+        }
+    };
+    if (from < to)
+        load_weights(from);
     f32x4 h[1][CT];
     clear(h);
     const int64_t row = tile.sample(0);
@@ -879,37 +1019,90 @@ __global__ __launch_bounds__(kWideWaves * kWave, kWavesPerSimd<CT>) void k_expan
         for (int ct = 0; ct < CT; ++ct)
             h[0][ct] += load_ranks(a.partial + (p * a.n_rows + row) * a.rank,
                                    ct * 16 + tile.quad * 4, a.rank);
-    if (a.hidden && a.hidden != a.partial && block == 0 && wave == 0)
+    if (a.hidden && a.hidden != a.partial && block == 0 && any)
         store_hidden(a.hidden, a.rank, tile, h);
-    if (a.out)
-        expand.run(turn, blocks * kWideWaves, b, h);
+    if (from >= to)
+        return;
+    Frag terms[1][CT];
+    float factor[1];
+    make_terms<W>(h, terms, factor);
+    factor[0] *= !adapted ? 0.0f : a.scales ? a.scales[tile.p.group] : a.scale;
+    put_weights(from, weights[0]);
+    int turn = 0;
+    for (int32_t m0 = from; m0 < to; m0 += kCols, turn ^= 1) {
+        // this unit's weights are there, and nobody reads those of the one before
+        __syncthreads();
+        const int32_t next = m0 + kCols;
+        if (next < to) {
+            load_weights(next);
+            load_base(b_next, next);
+        }
+        if (any) {
+            float *own = sums[wave];
+            if (adapted) {
+                const Product second = {weights[turn], pitch, a.rank, tile.col, tile.quad};
+                second.unit(0, terms[0], factor[0], own, Product::kPitch);
+            }
+            rows::wave_sync();
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int q = 0; q < (BACK ? 2 : 1); ++q) {
+                    const int c = (tile.piece + q * 8) * E;
+                    float v[E];
+                    if (adapted) {
+                        __builtin_memcpy(v, own + (j * 8 + tile.eighth) * Product::kPitch + c,
+                                         sizeof v);
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < E; ++u)
+                            v[u] = 0.0f;
+                    }
+                    if (!BACK && a.base)
+                        add_base<W>(a, v, b[j]);
+                    if (tile.there[j])
+                        store_row<W>(a.out + tile.row[j] * a.out_stride + (int64_t)(m0 + c) * S, v,
+                                     a.m - m0 - c);
+                }
+            rows::wave_sync();
+        }
+        if (next < to) {
+            put_weights(next, weights[turn ^ 1]);
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                b[j] = b_next[j];
+        }
+    }
 }
 
 template <int W, int X, int CT, bool BACK>
 hipError_t pass_of(const PassArgs &a, hipStream_t stream)
 {
     if (a.splits == 0) {
-        hipLaunchKernelGGL((k_narrow<W, X, CT, BACK>), dim3((uint32_t)((2 * a.n_tiles + kNarrowWaves - 1) / kNarrowWaves)),
-                           dim3(kNarrowWaves * kWave), 0, stream, a);
+        const NarrowRoom<W, BACK> room(a.k, a.m, a.rank);
+        hipLaunchKernelGGL((k_narrow<W, X, CT, BACK>), dim3((uint32_t)a.n_tiles),
+                           dim3(kTileWaves * kWave), room.bytes(), stream, a);
         return hipGetLastError();
     }
-    const dim3 parts((uint32_t)(a.n_tiles * a.splits)), term_waves(kTermWaves<CT> * kWave);
+    const dim3 term_waves(kTermWaves<CT> * kWave);
     if (a.tiles)
-        hipLaunchKernelGGL((k_shrink<W, X, CT, 2, BACK>), parts, term_waves, 0, stream, a);
+        hipLaunchKernelGGL((k_shrink<W, X, CT, 2, BACK>),
+                           dim3((uint32_t)(a.n_tiles * (kTile / 32) * a.splits)), term_waves, 0,
+                           stream, a);
     else
-        hipLaunchKernelGGL((k_shrink<W, X, CT, 1, BACK>), parts, term_waves, 0, stream, a);
+        hipLaunchKernelGGL((k_shrink<W, X, CT, 1, BACK>), dim3((uint32_t)(a.n_tiles * a.splits)),
+                           term_waves, 0, stream, a);
     if (hipError_t err = hipGetLastError(); err != hipSuccess)
         return err;
     if (!a.out && a.hidden == a.partial)
         return hipSuccess;
-    // about 2048 blocks, of 512 columns at most and a unit a wave at least
-    constexpr int kLeast = kWideWaves * Expand<W, CT, 1, BACK>::kCols;
-    const int64_t units = a.tiles ? 2 * a.n_tiles : a.n_tiles;
-    const int64_t least = (a.m + kLeast - 1) / kLeast, most = (a.m + 511) / 512;
-    const int32_t blocks = !a.out ? 1 : (int32_t)std::min<int64_t>(
-        least, std::max<int64_t>(most, 2048 / units));
-    hipLaunchKernelGGL((k_expand<W, CT, BACK>), dim3((uint32_t)(units * blocks)),
-                       dim3(kWideWaves * kWave), 0, stream, a, blocks);
+    // about 1024 blocks, with at most eight units each
+    constexpr int kCols = Second<W, CT, BACK>::kCols;
+    const int64_t units = a.out ? (a.m + kCols - 1) / kCols : 1;
+    const int32_t blocks = (int32_t)std::min<int64_t>(
+        units, std::max<int64_t>((units + 7) / 8, 1024 / a.n_tiles));
+    hipLaunchKernelGGL((k_expand<W, CT, BACK>), dim3((uint32_t)(a.n_tiles * blocks)),
+                       dim3(kTileWaves * kWave), 0, stream, a, blocks);
     return hipGetLastError();
 }
 
@@ -1158,6 +1351,14 @@ hipError_t launch_pass(const PassArgs &a, bool x_i32, bool back, hipStream_t str
         if (x_i32)
             return pass_by_rank<W, kI32, false>(a, stream);
     return pass_by_rank<W, W, false>(a, stream);
+}
+
+template <int W>
+bool fits_narrow(int32_t k, int32_t m, int32_t rank, bool back)
+{
+    const int64_t row = (int64_t)std::max(k, m) * kSize<W>;
+    return row <= 512 && (back ? NarrowRoom<W, true>(k, m, rank).bytes()
+                               : NarrowRoom<W, false>(k, m, rank).bytes()) <= 64 << 10;
 }
 
 template <int W>

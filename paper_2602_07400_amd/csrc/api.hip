@@ -389,12 +389,31 @@ int take_rows(const char *who, bl::adapt::PassArgs &a, int64_t n_rows, int32_t g
     return BITLOGIC_OK;
 }
 
+template <class F>
+auto by_weight(int32_t type, F f)
+{
+    switch (type) {
+    case BITLOGIC_LOGITS_F32: return f(std::integral_constant<int, bl::rows::kF32>());
+    case BITLOGIC_LOGITS_F16: return f(std::integral_constant<int, bl::rows::kF16>());
+    default: return f(std::integral_constant<int, bl::rows::kBf16>());
+    }
+}
+
+bl::adapt::PassLayout layout_of(int32_t type, int64_t n_rows, int32_t groups, int32_t rank,
+                                int32_t k, int32_t m, bool planned, bool back)
+{
+    const bool narrow = by_weight(type, [&](auto W) {
+        return bl::adapt::fits_narrow<decltype(W)::value>(k, m, rank, back);
+    });
+    return bl::adapt::pass_layout(n_rows, groups, rank, k, (int32_t)logit_bytes(type), planned,
+                                  narrow);
+}
+
 // A pass's form, and its workspace.
-int take_parts(const char *who, bl::adapt::PassArgs &a, int32_t el, void *workspace,
+int take_parts(const char *who, bl::adapt::PassArgs &a, int32_t type, bool back, void *workspace,
                size_t workspace_bytes)
 {
-    const auto l = bl::adapt::pass_layout(a.n_rows, a.groups, a.rank, a.k, a.m, el,
-                                          a.tiles != nullptr);
+    const auto l = layout_of(type, a.n_rows, a.groups, a.rank, a.k, a.m, a.tiles != nullptr, back);
     a.splits = l.splits;
     if (l.splits == 1 && a.hidden) {
         a.partial = a.hidden;
@@ -407,16 +426,6 @@ int take_parts(const char *who, bl::adapt::PassArgs &a, int32_t el, void *worksp
         return fail(BITLOGIC_ERR_ALIGN, "%s: workspace not 16-byte aligned", who);
     a.partial = static_cast<float *>(workspace);
     return BITLOGIC_OK;
-}
-
-template <class F>
-hipError_t by_weight(int32_t type, F f)
-{
-    switch (type) {
-    case BITLOGIC_LOGITS_F32: return f(std::integral_constant<int, bl::rows::kF32>());
-    case BITLOGIC_LOGITS_F16: return f(std::integral_constant<int, bl::rows::kF16>());
-    default: return f(std::integral_constant<int, bl::rows::kBf16>());
-    }
 }
 
 struct BackwardLayout {
@@ -439,8 +448,8 @@ BackwardLayout backward_layout(const bitlogic_adapter_set &s, int64_t n_rows)
     for (bool planned : {true, false})
         if (planned || n_rows <= kMaxLoneRows)
             b.parts_bytes = std::max(b.parts_bytes,
-                                     bl::adapt::pass_layout(n_rows, s.n_adapters, s.rank, s.n_out,
-                                                            s.n_in, el, planned).bytes);
+                                     layout_of(s.weight_type, n_rows, s.n_adapters, s.rank,
+                                               s.n_out, s.n_in, planned, true).bytes);
     b.partial_down = b.parts + round_up(b.parts_bytes);
     const size_t slots = (size_t)l.cut[b.cut].n_slots * s.rank * 4;
     b.partial_up = b.partial_down + round_up(slots * s.n_in);
@@ -1371,7 +1380,7 @@ int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_s
     a.out = static_cast<char *>(out);
     a.out_stride = out_stride * (int64_t)el;
     a.hidden = hidden;
-    if (int rc = take_parts(who, a, (int32_t)el, workspace, workspace_bytes))
+    if (int rc = take_parts(who, a, s.weight_type, false, workspace, workspace_bytes))
         return rc;
     return hip_status(by_weight(s.weight_type, [&](auto W) {
         return bl::adapt::launch_pass<decltype(W)::value>(a, x_type == BITLOGIC_LOGITS_I32, false,
@@ -1384,8 +1393,8 @@ size_t bitlogic_adapters_workspace_bytes(const bitlogic_adapter_set *set, int64_
 {
     if (check_set("adapters", set, n_rows) != BITLOGIC_OK || (!planned && n_rows > kMaxLoneRows))
         return 0;
-    return bl::adapt::pass_layout(n_rows, set->n_adapters, set->rank, set->n_in, set->n_out,
-                                  (int32_t)logit_bytes(set->weight_type), planned != 0).bytes;
+    return layout_of(set->weight_type, n_rows, set->n_adapters, set->rank, set->n_in, set->n_out,
+                     planned != 0, false).bytes;
 }
 
 size_t bitlogic_adapters_backward_workspace_bytes(const bitlogic_adapter_set *set,
@@ -1444,10 +1453,8 @@ int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_st
     char *ws = static_cast<char *>(workspace);
     float *back = reinterpret_cast<float *>(ws + b.back);
     bl::adapt::GradArgs g = {};
-    int32_t block = 0;
-    by_weight(s.weight_type, [&](auto W) {
-        block = bl::adapt::grad_block<decltype(W)::value>();
-        return hipSuccess;
+    const int32_t block = by_weight(s.weight_type, [](auto W) {
+        return bl::adapt::grad_block<decltype(W)::value>();
     });
     if (weights) {
         const char *p = static_cast<const char *>(plan);
@@ -1498,7 +1505,7 @@ int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_st
         a.out = static_cast<char *>(grad_x);
         a.out_stride = grad_x_stride * (int64_t)el;
         a.hidden = grad_down ? back : nullptr;
-        if (int rc = take_parts(who, a, (int32_t)el, ws + b.parts, b.parts_bytes))
+        if (int rc = take_parts(who, a, s.weight_type, true, ws + b.parts, b.parts_bytes))
             return rc;
         const hipError_t err = by_weight(s.weight_type, [&](auto W) {
             return bl::adapt::launch_pass<decltype(W)::value>(a, false, true,
