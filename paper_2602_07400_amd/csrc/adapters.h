@@ -18,6 +18,7 @@ constexpr int kTile = 64;               // rows of a tile, all of one group
 constexpr int32_t kMaxGroups = 4096;    // (a wave's counters in LDS)
 constexpr int32_t kMaxRank = 128;
 constexpr int32_t kMaxRuns = 1024;
+constexpr int64_t kLeastRun = 1024;     // rows that a block sorts at a time
 
 // Rows [first, first + count) of the order, of one group (-1: no piece).  slot: of a group of
 // several chunks, the chunk's partial sums in the workspace.
@@ -35,7 +36,7 @@ struct CutLayout {
     int32_t rows;
 };
 struct GroupLayout {
-    size_t order, starts, tile_starts, tiles, totals, counts, bytes;
+    size_t order, starts, tile_starts, tiles, counts, bytes;
     CutLayout cut[2];
     int64_t n_tiles, run;
     int32_t runs;
@@ -46,8 +47,8 @@ inline GroupLayout group_layout(int64_t n_rows, int32_t groups)
     GroupLayout l;
     const int64_t small = std::max<int64_t>(256, n_rows / 1024 / kTile * kTile);
     l.n_tiles = n_rows / kTile + groups + 1;              // at most a partial one a group
-    l.run = std::max<int64_t>(256, (n_rows + kMaxRuns - 1) / kMaxRuns);
-    l.run = (l.run + 63) / 64 * 64;
+    l.run = std::max<int64_t>(1, (n_rows + kMaxRuns * kLeastRun - 1) / (kMaxRuns * kLeastRun)) *
+            kLeastRun;
     l.runs = (int32_t)((n_rows + l.run - 1) / l.run);
     size_t at = 0;
     const auto take = [&](size_t bytes) {
@@ -69,7 +70,6 @@ inline GroupLayout group_layout(int64_t n_rows, int32_t groups)
         k.starts = take(all * 4);
         k.slots = take(all * 4);
     }
-    l.totals = take(all * 4);
     l.counts = take((size_t)l.runs * (groups + 1) * 4);
     l.bytes = at;
     return l;
@@ -88,7 +88,7 @@ struct GroupArgs {
     int32_t *order, *starts, *tile_starts;
     Piece4 *tiles;
     Cut cut[2];
-    uint32_t *totals, *counts;
+    uint32_t *counts;
 };
 
 // ---- a pass through adapters ----

@@ -214,6 +214,11 @@ __device__ __forceinline__ Frag load_16(const char *p)
     __builtin_memcpy(f.w, p, 16);
     return f;
 }
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ Frag load_nt(const char *p)
+{
+    return __builtin_bit_cast(Frag, __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2 *>(p)));
+}
 __device__ __forceinline__ Frag lds_frag(const char *p) { return *reinterpret_cast<const Frag *>(p); }
 __device__ __forceinline__ void lds_put(char *p, Frag f) { *reinterpret_cast<Frag *>(p) = f; }
 
@@ -754,7 +759,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
             const int at = i * kWave + tile.lane, r = m_row(at), p = at - r * m_pieces;
             const int32_t row = __shfl(tile.row[0], r);
             if (r < tile.p.count && at < 16 * m_pieces)
-                b[i] = load_16(a.base + row * a.base_stride + p * 16);
+                b[i] = load_nt(a.base + row * a.base_stride + p * 16);
         }
         if (end_lane && a.m % E)
             b_end = load_frag<W>(a.base + tile.row[0] * a.base_stride + m_pieces * 16, a.m % E);
@@ -769,7 +774,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
             const int at = i * kWave + tile.lane, r = x_row(at), p = at - r * x_pieces;
             const int32_t row = __shfl(tile.row[0], r);
             if (r < tile.p.count && at < 16 * x_pieces)
-                x[i] = load_16(a.x + row * a.x_stride + p * 16);
+                x[i] = load_nt(a.x + row * a.x_stride + p * 16);
         }
         if constexpr (!BACK) {
             stage_rows<W>(w1, room.w1_pitch, down, (int64_t)a.k * S, a.rank, a.k);
@@ -1013,7 +1018,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expan
     f32x4 h[1][CT];
     clear(h);
     const int64_t row = tile.sample(0);
-#pragma unroll(CT <= 2 ? 4 : 2)
+#pragma unroll CT <= 2 ? 4 : 2
     for (int32_t p = 0; p < a.splits; ++p)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
