@@ -53,13 +53,13 @@ struct Side {
     }
 };
 
-// A row's (or a part's) largest logit, as its bits, the first class that has it (of greedy
-// rows) and the sum of exponentials relative to it.
+// A row's (or a part's) largest logit (-inf: none; every type's values are exact in 64 bits), the
+// first class that has it (of greedy rows) and the sum of exponentials relative to it.
 struct Stat {
-    uint32_t m;
+    double m, s;
     int32_t first;
-    double s;
 };
+constexpr double kInf = __builtin_inf();
 
 // The best class of a part of a draw, by how much its score may be off, and the most that
 // any other class's may be.
@@ -105,59 +105,74 @@ __device__ __forceinline__ auto by_type(int type, F f)
     }
 }
 
-template <int TYPE>
-__device__ __forceinline__ typename Elem<TYPE>::Cmp cmp_of(uint32_t bits)
+// An element's value, -inf where it is masked.  (Types are told apart here and in the loops over
+// rows alone: what is behind them is there once.)
+__device__ __forceinline__ double value_at(const char *row, int type, int64_t i)
 {
-    typename Elem<TYPE>::Cmp v;
-    __builtin_memcpy(&v, &bits, 4);
-    return v;
-}
-template <class T>
-__device__ __forceinline__ uint32_t bits_of(T v)
-{
-    uint32_t b;
-    __builtin_memcpy(&b, &v, 4);
-    return b;
-}
-
-// v - m in 64 bits, m the row's largest: 0 at it, -inf for masked classes and, beside a
-// +inf, for all others.
-template <int TYPE>
-__device__ __forceinline__ double below(typename Elem<TYPE>::Cmp v, typename Elem<TYPE>::Cmp m)
-{
-    return !(v > Elem<TYPE>::lowest()) ? -__builtin_inf() : v == m ? 0.0 : (double)v - (double)m;
-}
-
-__device__ __forceinline__ double below_at(const char *row, int type, int64_t i, uint32_t m)
-{
-    return by_type(type, [&](auto T) {
+    return by_type(type, [&](auto T) __attribute__((always_inline)) {
         constexpr int TYPE = decltype(T)::value;
-        return below<TYPE>(load_one<TYPE>(row, i), cmp_of<TYPE>(m));
+        const auto v = load_one<TYPE>(row, i);
+        return v > Elem<TYPE>::lowest() ? (double)v : -kInf;
     });
 }
+// v - m, m the row's largest: 0 at it, -inf for masked values and, beside a +inf, for all others.
+__device__ __forceinline__ double below(double v, double m) { return v == m ? 0.0 : v - m; }
 
-// f(class, piece) over [lo, hi) of a row, kFlight pieces in flight a lane.
-template <int TYPE, int G, int VEC, int FLIGHT, class F>
-__device__ __forceinline__ void over(const char *row, int32_t lo, int32_t hi, int t, F f)
+// Elements from class i on of a row of n, those of [i, hi) and the rest masked; returns the class
+// of the first.  Near the row's end it loads the last VEC of it instead, without a branch a
+// lane: such branches, unrolled, took the registers of all that follows.
+template <int TYPE, int VEC>
+__device__ __forceinline__ int32_t load_end(Piece<TYPE, VEC> &p, const char *row, int32_t i,
+                                            int32_t hi, int32_t n)
 {
-    for (int32_t i = lo; i < hi; i += FLIGHT * G * VEC) {
-        Piece<TYPE, VEC> p[FLIGHT];
+    constexpr int B = Elem<TYPE>::kBytes;
+    if (n < VEC) {                                        // (in the whole wave)
+        p.fill_masked();
+        if (i == 0)
+            p.load(row, 0, 0, hi);
+        return i;
+    }
+    const int32_t at = min(i, n - VEC);
+    __builtin_memcpy(p.w, row + (int64_t)at * B, sizeof p.w);
+#pragma unroll
+    for (int u = 0; u < VEC; ++u)
+        if (at + u < i || at + u >= hi)
+            p.mask(u);
+    return at;
+}
+
+// f(first class, piece) over [lo, hi) of a row of n, FLIGHT pieces in flight a lane.
+template <int TYPE, int G, int VEC, int FLIGHT, class F>
+__device__ __forceinline__ void over(const char *row, int32_t lo, int32_t hi, int32_t n, int t, F f)
+{
+    typedef Piece<TYPE, VEC> P;
+    int32_t i = lo;
+    for (; i + FLIGHT * G * VEC <= hi; i += FLIGHT * G * VEC) {
+        P p[FLIGHT];
         static_for<FLIGHT>([&](auto j) __attribute__((always_inline)) {
-            p[j].load(row, i + j * (G * VEC), t * VEC, hi);
+            __builtin_memcpy(p[j].w, row + (int64_t)(i + j * G * VEC) * Elem<TYPE>::kBytes
+                                         + (uint32_t)(t * VEC * Elem<TYPE>::kBytes), sizeof p[j].w);
         });
         static_for<FLIGHT>([&](auto j) __attribute__((always_inline)) {
             f(i + j * (G * VEC) + t * VEC, p[j]);
         });
     }
+#pragma unroll 2
+    for (; i < hi; i += G * VEC) {
+        P p;
+        const int32_t at = load_end(p, row, i + t * VEC, hi, n);
+        f(at, p);
+    }
 }
 
 // The first class of [lo, hi) whose logit is m.
-template <int TYPE, class Grp, int G>
-__device__ int32_t first_at(Grp &g, const char *row, int32_t lo, int32_t hi,
-                            typename Elem<TYPE>::Cmp m)
+template <int TYPE, int G>
+__device__ __forceinline__ int32_t first_at(Group<G> &g, const char *row, int32_t lo, int32_t hi,
+                                            int32_t n, typename Elem<TYPE>::Cmp m)
 {
     uint32_t first = 0;                                   // ~class
-    over<TYPE, G, 4, 1>(row, lo, hi, g.t, [&](int32_t i, const Piece<TYPE, 4> &p) {
+    over<TYPE, G, 4, 1>(row, lo, hi, n, g.t, [&](int32_t i, const Piece<TYPE, 4> &p)
+                                                 __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
             if (p.get(u) == m)
@@ -166,10 +181,10 @@ __device__ int32_t first_at(Grp &g, const char *row, int32_t lo, int32_t hi,
     return (int32_t)~g.reduce(first, Max());
 }
 
-// Stat of [lo, hi) of a row at 1 / T (0: greedy).
+// Stat of [lo, hi) of a row of n at 1 / T (0: greedy).
 template <int TYPE, int G>
 __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo, int32_t hi,
-                                        double inverse)
+                                        int32_t n, double inverse)
 {
     typedef Elem<TYPE> E;
     typedef typename E::Cmp Cmp;
@@ -177,7 +192,8 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo
     const float c = (float)(inverse * 1.4426950408889634);
     Cmp m = E::lowest();
     double s = 0.0;
-    over<TYPE, G, VEC, 4>(row, lo, hi, g.t, [&](int32_t, const Piece<TYPE, VEC> &p) {
+    over<TYPE, G, VEC, 4>(row, lo, hi, n, g.t, [&](int32_t, const Piece<TYPE, VEC> &p)
+                                                   __attribute__((always_inline)) {
         Cmp vm = E::lowest();
 #pragma unroll
         for (int u = 0; u < VEC; ++u) {
@@ -199,16 +215,17 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo
         s += (double)part;
     });
     const Cmp most = g.reduce(m, Max());
-    Stat out = {bits_of(most), 0, 0.0};
     if (!(most > E::lowest()))
-        return out;
+        return {-kInf, 0.0, 0};
+    Stat out = {(double)most, 0.0, 0};
     if (inverse == 0.0) {
-        out.first = first_at<TYPE, Group<G>, G>(g, row, lo, hi, most);
+        out.first = first_at<TYPE, G>(g, row, lo, hi, n, most);
         return out;
     }
     if (E::to_float(most) == __builtin_inff()) {          // shared by those that have it
         s = 0.0;
-        over<TYPE, G, VEC, 1>(row, lo, hi, g.t, [&](int32_t, const Piece<TYPE, VEC> &p) {
+        over<TYPE, G, VEC, 1>(row, lo, hi, n, g.t, [&](int32_t, const Piece<TYPE, VEC> &p)
+                                                       __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < VEC; ++u)
                 s += p.get(u) == most ? 1.0 : 0.0;
@@ -222,54 +239,31 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo
 
 template <int G>
 __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int type, int32_t lo,
-                                        int32_t hi, double inverse)
+                                        int32_t hi, int32_t n, double inverse)
 {
-    return by_type(type, [&](auto T) {
-        return stat_of<decltype(T)::value, G>(g, row, lo, hi, inverse);
+    return by_type(type, [&](auto T) __attribute__((always_inline)) {
+        return stat_of<decltype(T)::value, G>(g, row, lo, hi, n, inverse);
     });
 }
 
-// The sum of a row's exponentials in 64 bits.  (Rare: a call, which takes its own copy of
-// the group and ends with a barrier, so that the caller's next reduction finds free slots.)
-template <int G>
-__device__ __attribute__((noinline)) double exact_sum(Group<G> g, const char *row, int type,
-                                                      int32_t n, uint32_t m, double inverse)
+// Sums of parts, relative to the largest of them, by 16 lanes; each gets it.
+constexpr int kJoin = 16;
+__device__ __forceinline__ Stat join(const Stat *parts, int32_t count, double inverse)
 {
-    double s = 0.0;
-    for (int32_t i = g.t; i < n; i += G)
-        s += exp(below_at(row, type, i, m) * inverse);
-    s = g.reduce(s, Add());
-    g.barrier();
-    return s;
-}
-
-// Sums of parts, relative to the largest of them.
-__device__ __forceinline__ Stat join(const Stat *parts, int32_t count, int type, double inverse)
-{
-    Stat all = parts[0];
-    for (int32_t k = 1; k < count; ++k) {
-        const Stat one = parts[k];
-        by_type(type, [&](auto T) {
-            constexpr int TYPE = decltype(T)::value;
-            const auto a = cmp_of<TYPE>(all.m), b = cmp_of<TYPE>(one.m);
-            if (b > a) {
-                all.s = (all.s > 0.0 ? all.s * exp(below<TYPE>(a, b) * inverse) : 0.0) + one.s;
-                all.m = one.m;
-                all.first = one.first;
-            } else if (one.s > 0.0) {
-                all.s += one.s * exp(below<TYPE>(b, a) * inverse);
-            }
-        });
-    }
-    return all;
-}
-
-__device__ __forceinline__ bool is_masked(const Stat &s, int type)
-{
-    return by_type(type, [&](auto T) {
-        constexpr int TYPE = decltype(T)::value;
-        return !(cmp_of<TYPE>(s.m) > Elem<TYPE>::lowest());
-    });
+    const int lane = threadIdx.x % kJoin;
+    double m = -kInf, s = 0.0;
+    int32_t first = 0;
+    for (int32_t k = lane; k < count; k += kJoin)
+        if (parts[k].m > m) {                             // (the lane's parts ascend)
+            m = parts[k].m;
+            first = parts[k].first;
+        }
+    const double most = wave_reduce<kJoin>(m, Max());
+    const uint32_t no = m == most && most > -kInf ? ~(uint32_t)first : 0u;
+    for (int32_t k = lane; k < count; k += kJoin)
+        if (parts[k].s > 0.0)
+            s += parts[k].s * exp(below(parts[k].m, most) * inverse);
+    return {most, wave_reduce<kJoin>(s, Add()), (int32_t)~wave_reduce<kJoin>(no, Max())};
 }
 
 enum : int { kRejected = 0, kAccepted = 1, kOpen = 2 };
@@ -288,35 +282,46 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, int64_t r, int32_t i,
 {
     const int64_t at = r * a.drafts + i;
     const int32_t t = a.drafted[at];
-    if (t < 0 || t >= a.n || is_masked(p, a.target.type))
+    if (t < 0 || t >= a.n || p.m == -kInf)
         return kRejected;
     if (inverse_p == 0.0)
         return t == p.first ? kAccepted : kRejected;
-    const double x = below_at(a.target.row(r, i), a.target.type, t, p.m);
-    if (x == -__builtin_inf())
+    const double x = below(value_at(a.target.row(r, i), a.target.type, t), p.m);
+    if (x == -kInf)
         return kRejected;
     double log_ratio = x * inverse_p - log(p.s);
     if (has_row(a, inverse_q)) {
-        const double y = below_at(a.draft.row(r, i), a.draft.type, t, q.m);
-        log_ratio = y == -__builtin_inf() ? __builtin_inf()
-                                          : log_ratio - (y * inverse_q - log(q.s));
+        const double v = value_at(a.draft.row(r, i), a.draft.type, t);
+        log_ratio = v == -kInf || below(v, q.m) == -kInf
+                        ? kInf : log_ratio - (below(v, q.m) * inverse_q - log(q.s));
     }
     const double ratio = exp(log_ratio), u = a.uniform[at];
-    if (fabs(u - ratio) <= loose * ratio && ratio < __builtin_inf())
+    if (fabs(u - ratio) <= loose * ratio && ratio < kInf)
         return kOpen;
     return u < ratio ? kAccepted : kRejected;
 }
 
-// decide() with sums in 64 bits, by a group.
-template <int G>
-__device__ __forceinline__ int decide_exactly(const Group<G> &g, const VerifyArgs &a, int64_t r,
-                                              int32_t i, double inverse_p, double inverse_q,
-                                              Stat p, Stat q)
+// Whether decide() will certainly reject, in 32 bits with a thousandth to spare.
+__device__ __forceinline__ bool surely_rejected(const VerifyArgs &a, int64_t r, int32_t i,
+                                                double inverse_p, double inverse_q, const Stat &p,
+                                                const Stat &q)
 {
-    p.s = exact_sum(g, a.target.row(r, i), a.target.type, a.n, p.m, inverse_p);
-    if (has_row(a, inverse_q) && !is_masked(q, a.draft.type))
-        q.s = exact_sum(g, a.draft.row(r, i), a.draft.type, a.n, q.m, inverse_q);
-    return decide(a, r, i, inverse_p, inverse_q, p, q, -1.0);
+    const int64_t at = r * a.drafts + i;
+    const int32_t t = a.drafted[at];
+    if (t < 0 || t >= a.n || p.m == -kInf)
+        return true;
+    if (inverse_p == 0.0)
+        return t != p.first;
+    const auto log2_share = [&](const Side &of, const Stat &s,
+                                double inverse) __attribute__((always_inline)) {
+        const float x = (float)(below(value_at(of.row(r, i), of.type, t), s.m) * inverse);
+        return x * kLog2e - __builtin_amdgcn_logf((float)s.s);
+    };
+    float log_ratio = log2_share(a.target, p, inverse_p);
+    if (has_row(a, inverse_q))
+        log_ratio -= log2_share(a.draft, q, inverse_q);
+    // (a NaN, of two masked logits, is not sure)
+    return a.uniform[at] > __builtin_amdgcn_exp2f(log_ratio) * 1.001f + 1e-30f;
 }
 
 // What the next class is drawn from: the target's row, less the drafter's (kRow), less the
@@ -327,8 +332,7 @@ struct Draw {
     const float *noise;
     int p_type, q_type, less;
     int32_t n, drafted;
-    uint32_t pm, qm;
-    double inverse_p, inverse_q, log_p, log_q;            // logs of the sums
+    double pm, qm, inverse_p, inverse_q, log_p, log_q;    // logs of the sums
 };
 
 __device__ __forceinline__ void merge(Best &a, const Best &b)
@@ -339,14 +343,14 @@ __device__ __forceinline__ void merge(Best &a, const Best &b)
         a = {b.score, b.off, fmax(a.other, b.other), b.cls};
     else
         a.other = fmax(a.other, b.other);
-    if (low.score > -__builtin_inf())
+    if (low.score > -kInf)
         a.other = fmax(a.other, low.score + low.off);
 }
 
 constexpr int64_t kNoClass = INT64_MAX;
 __device__ __forceinline__ Best nothing()
 {
-    return {-__builtin_inf(), 0.0, -__builtin_inf(), kNoClass};
+    return {-kInf, 0.0, -kInf, kNoClass};
 }
 
 // The best of the group's lanes; every lane gets it.
@@ -360,7 +364,7 @@ __device__ __forceinline__ Best join(Group<G> &g, const Best &mine)
     const bool won = mine.score == b.score && mine.cls == b.cls;
     b.off = g.reduce(won ? mine.off : 0.0, Max());
     double other = mine.other;
-    if (!won && mine.score > -__builtin_inf())
+    if (!won && mine.score > -kInf)
         other = fmax(other, mine.score + mine.off);
     b.other = g.reduce(other, Max());
     return b;
@@ -370,10 +374,10 @@ __device__ __forceinline__ Best join(Group<G> &g, const Best &mine)
 __device__ __forceinline__ void offer(Best &best, const Draw &d, int32_t cls, double x, double y,
                                       double number)
 {
-    Best one = {x + number, 0.0, -__builtin_inf(), cls};
+    Best one = {x + number, 0.0, -kInf, cls};
     if (d.less == kOne && cls == d.drafted)
         return;
-    if (d.less == kRow && y > -__builtin_inf()) {
+    if (d.less == kRow && y > -kInf) {
         const double delta = (y - d.log_q) - (x - d.log_p);
         if (!(delta < 2 * kLoose))
             return;
@@ -387,133 +391,87 @@ __device__ __forceinline__ void offer(Best &best, const Draw &d, int32_t cls, do
         one.score += (double)logf(w);
         one.off = kLoose / (double)w;
     }
-    if (one.score > -__builtin_inf())                     // (no NaN either)
+    if (one.score > -kInf)                     // (no NaN either)
         merge(best, one);
 }
 
-// The group's best of classes [lo, hi).
+// The group's best of classes [lo, hi).  A lane bounds 8 classes by x + number, which no mass
+// below p changes upwards, and evaluates its best of them, all lanes at once, while any is above
+// what the wave has: two or three times for the first 512 classes, then seldom.  The values are
+// loaded again for that (p's are in the L1), which is what keeps the loop small.
 template <int G>
 __device__ __forceinline__ Best draw_part(Group<G> &g, const Draw &d, int32_t lo, int32_t hi)
 {
-    constexpr int V = 4, kFlight = 2;
-    struct Raw {
-        uint32_t w[V];
-    };
-    const auto load = [&](Raw &to, const char *row, int type, int32_t i, int32_t base) {
-        by_type(type, [&](auto T) {
-            Piece<decltype(T)::value, V> p;
-            p.load(row, base, i, hi);
-            __builtin_memcpy(to.w, p.w, sizeof p.w);
-        });
-    };
-    Best best = nothing();
+    constexpr int V = 4, kFlight = 2, N = kFlight * V;
     const float inv = (float)d.inverse_p;
+    Best best = nothing();
     float bound = -__builtin_inff();                      // the wave's best, less what it is off
-    for (int32_t base = lo; base < hi; base += kFlight * G * V) {
-        Raw p[kFlight], q[kFlight];
-        float number[kFlight][V];
+    for (int32_t base = lo; base < hi; base += N * G) {
+        float most[N];
+        int32_t at[kFlight];
+        uint32_t open = 0;                                // not evaluated, and not below the bound
+        by_type(d.p_type, [&](auto T) __attribute__((always_inline)) {
+            constexpr int TYPE = decltype(T)::value;
+            typedef Elem<TYPE> E;
+            const auto m = (typename E::Cmp)d.pm;
+            Piece<TYPE, V> p[kFlight];
+            Piece<kF32, V> z[kFlight];
+            const char *numbers = reinterpret_cast<const char *>(d.noise);
+            if (base + N * G <= hi) {
 #pragma unroll
-        for (int j = 0; j < kFlight; ++j) {
-            const int32_t from = base + j * G * V, i = g.t * V;
-            load(p[j], d.p, d.p_type, i, from);
-            if (d.less == kRow)
-                load(q[j], d.q, d.q_type, i, from);
-            Piece<kF32, V> z;
-            z.load(reinterpret_cast<const char *>(d.noise), from, i, hi);
-#pragma unroll
-            for (int u = 0; u < V; ++u)
-                number[j][u] = z.get(u);
-        }
-#pragma unroll
-        for (int j = 0; j < kFlight; ++j) {
-            uint32_t in = 0;
-            by_type(d.p_type, [&](auto T) {
-                constexpr int TYPE = decltype(T)::value;
-                Piece<TYPE, V> piece;
-                __builtin_memcpy(piece.w, p[j].w, sizeof piece.w);
-                const auto m = cmp_of<TYPE>(d.pm);
-#pragma unroll
-                for (int u = 0; u < V; ++u) {
-                    const auto v = piece.get(u);
-                    const float x = v == m ? 0.0f : Elem<TYPE>::minus(v, m) * inv;
-                    // (rounded: a millionth of what it is made of)
-                    const float most = x + number[j][u]
-                                       + (fabsf(x) + fabsf(number[j][u])) * 1e-6f;
-                    in |= (uint32_t)(v > Elem<TYPE>::lowest() && !(most < bound)) << u;
+                for (int j = 0; j < kFlight; ++j) {
+                    at[j] = base + j * G * V + g.t * V;
+                    __builtin_memcpy(p[j].w, d.p + (int64_t)at[j] * E::kBytes, sizeof p[j].w);
+                    __builtin_memcpy(z[j].w, numbers + (int64_t)at[j] * 4, sizeof z[j].w);
                 }
-            });
-            if (!__any(in))
-                continue;
-            const int32_t i = base + j * G * V + g.t * V;
-            for (int u = 0; u < V; ++u) {
-                if (!(in >> u & 1))
-                    continue;
-                const auto at = [&](const Raw &raw, int type, uint32_t m) {
-                    return by_type(type, [&](auto T) {
-                        constexpr int TYPE = decltype(T)::value;
-                        Piece<TYPE, V> piece;
-                        __builtin_memcpy(piece.w, raw.w, sizeof piece.w);
-                        typename Elem<TYPE>::Cmp v = piece.get(0);
+            } else {
 #pragma unroll
-                        for (int k = 1; k < V; ++k)
-                            if (k == u)
-                                v = piece.get(k);
-                        return below<TYPE>(v, cmp_of<TYPE>(m));
-                    });
-                };
-                float own = number[j][0];
+                for (int j = 0; j < kFlight; ++j) {
+                    at[j] = load_end(p[j], d.p, base + j * G * V + g.t * V, hi, d.n);
+                    load_end(z[j], numbers, base + j * G * V + g.t * V, hi, d.n);
+                }
+            }
 #pragma unroll
-                for (int k = 1; k < V; ++k)
-                    if (k == u)
-                        own = number[j][k];
-                const double x = at(p[j], d.p_type, d.pm) * d.inverse_p;
-                const double y = d.less == kRow ? at(q[j], d.q_type, d.qm) * d.inverse_q : 0.0;
-                offer(best, d, i + u, x, y, (double)own);
+            for (int k = 0; k < N; ++k) {
+                const auto v = p[k / V].get(k % V);
+                const float number = z[k / V].get(k % V);
+                const float x = v == m ? 0.0f : E::minus(v, m) * inv;
+                // (rounded: a millionth of what it is made of)
+                most[k] = x + number + (fabsf(x) + fabsf(number)) * 1e-6f;
+                open |= (uint32_t)(v > E::lowest() && !(most[k] < bound)) << k;
+            }
+        });
+#pragma unroll 1
+        while (__any(open)) {
+            float top = -__builtin_inff();
+            int32_t i = -1;
+            uint32_t own = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {                 // (NaNs too: x or number infinite)
+                const bool more = (open >> k & 1) && (i < 0 || !(most[k] <= top));
+                top = more ? most[k] : top;
+                i = more ? at[k / V] + k % V : i;
+                own = more ? 1u << k : own;
+            }
+            if (i >= 0) {
+                open &= ~own;
+                const double x = below(value_at(d.p, d.p_type, i), d.pm) * d.inverse_p;
+                double y = 0.0;
+                if (d.less == kRow) {
+                    const double v = value_at(d.q, d.q_type, i);
+                    y = v == -kInf ? v : below(v, d.qm) * d.inverse_q;
+                }
+                offer(best, d, i, x, y, (double)d.noise[i]);
             }
             float low = (float)(best.score - best.off);
             low -= fabsf(low) * 1e-6f;
             bound = wave_reduce<(G < kWave ? G : kWave)>(fmaxf(low, bound), Max());
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                open &= ~((uint32_t)(most[k] < bound) << k);
         }
     }
     return join(g, best);
-}
-
-// The draw in 64 bits throughout, by a group.
-template <int G>
-__device__ __attribute__((noinline)) Best draw_exactly(Group<G> g, Draw d)
-{
-    d.log_p = log(exact_sum(g, d.p, d.p_type, d.n, d.pm, d.inverse_p));
-    d.log_q = log(exact_sum(g, d.q, d.q_type, d.n, d.qm, d.inverse_q));
-    Best best = nothing();
-    for (int32_t i = g.t; i < d.n; i += G) {
-        const double p = exp(below_at(d.p, d.p_type, i, d.pm) * d.inverse_p - d.log_p);
-        const double q = exp(below_at(d.q, d.q_type, i, d.qm) * d.inverse_q - d.log_q);
-        const Best one = {log(p - q) + (double)d.noise[i], 0.0, -__builtin_inf(), i};
-        if (p > q && one.score > -__builtin_inf())
-            merge(best, one);
-    }
-    best = join(g, best);
-    g.barrier();
-    return best;
-}
-
-// The class of a draw from the best of all its parts, with what is seldom needed: the draw
-// again in 64 bits, from the target's row alone, or the first class of its order.
-template <int G>
-__device__ __forceinline__ int32_t settle(Group<G> &g, Draw d, Best best)
-{
-    if (d.less == kRow && best.other > -__builtin_inf() && best.other >= best.score - best.off)
-        best = draw_exactly(g, d);
-    if (best.cls == kNoClass && d.less != kWhole) {
-        d.less = kWhole;
-        best = draw_part(g, d, 0, d.n);
-    }
-    if (best.cls != kNoClass)
-        return (int32_t)best.cls;
-    return by_type(d.p_type, [&](auto T) {
-        constexpr int TYPE = decltype(T)::value;
-        return first_at<TYPE, Group<G>, G>(g, d.p, 0, d.n, cmp_of<TYPE>(d.pm));
-    });
 }
 
 // The draw at row j of request r, of which `length` drafts were given.
@@ -540,7 +498,7 @@ __device__ __forceinline__ Draw draw_of(const VerifyArgs &a, int64_t r, int32_t 
         if (!has_row(a, inverse_q)) {
             d.less = kOne;
             d.drafted = a.drafted[r * a.drafts + j];
-        } else if (!is_masked(q, a.draft.type)) {
+        } else if (q.m > -kInf) {
             d.less = kRow;
             d.q = a.draft.row(r, j);
             d.log_q = log(q.s);
@@ -558,54 +516,197 @@ __device__ __forceinline__ void answer(const VerifyArgs &a, int64_t r, int32_t j
     if (a.log_prob) {
         float value = token < 0 ? -__builtin_inff() : 0.0f;
         if (token >= 0 && inverse_p > 0.0)
-            value = (float)(below_at(a.target.row(r, j), a.target.type, token, p.m) * inverse_p
-                            - log(p.s));
+            value = (float)(below(value_at(a.target.row(r, j), a.target.type, token), p.m)
+                            * inverse_p - log(p.s));
         a.log_prob[r] = value;
     }
 }
 
-// ---- short rows: a wave a request ----
-constexpr int kShortBlock = 256;
-
-__global__ __launch_bounds__(kShortBlock) void k_verify_short(VerifyArgs a)
+// ---- the walk ----
+// The first of drafts [base, base + 64), below `length`, that does not stand, or kNone; kLeftOpen
+// where 32 bits do not tell.  stats: p and q of each in turn.  The same in every wave of a group.
+constexpr int32_t kNone = -1, kLeftOpen = -2;
+__device__ __forceinline__ int32_t walk(const VerifyArgs &a, int64_t r, int32_t base,
+                                        int32_t length, double inverse_p, double inverse_q,
+                                        const Stat *stats)
 {
-    constexpr int G = kWave, kGroups = kShortBlock / G;
-    const int gi = group_of<G>();
-    Group<G> g(threadIdx.x - gi * G, nullptr);
+    const int lane = threadIdx.x % kWave;
+    int how = kAccepted;
+    if (base + lane < length)
+        how = decide(a, r, base + lane, inverse_p, inverse_q, stats[2 * lane], stats[2 * lane + 1],
+                     kLoose);
+    const uint64_t ends = __ballot(how != kAccepted);
+    if (!ends)
+        return kNone;
+    const int k = __builtin_ctzll(ends);
+    return __shfl(how, k) == kOpen ? kLeftOpen : base + k;
+}
+
+// The class of a draw, or kLeftOpen: it takes 64 bits, or there is none in what is left of p.
+__device__ __forceinline__ int32_t settle(const Draw &d, const Best &best)
+{
+    const bool open = best.cls == kNoClass ||
+                      (d.less == kRow && best.other > -kInf &&
+                       best.other >= best.score - best.off);
+    return open ? kLeftOpen : (int32_t)best.cls;
+}
+
+// A request from the start in 64 bits throughout, by a group: what 32 bits left open, and draws
+// without a class.  Rare (a draft or draw in 10^4 or so), and behind everything else, so that
+// it takes no registers from what always runs.
+template <int G>
+__device__ __forceinline__ void redo(Group<G> &g, const VerifyArgs &a, int64_t r)
+{
+    struct Row {
+        const char *p;
+        int type;
+        double inverse, m, log_s;
+        int32_t first;
+        __device__ __forceinline__ double value(int64_t i) const          // -inf: masked
+        {
+            return value_at(p, type, i);
+        }
+        // log of a class's share
+        __device__ __forceinline__ double log_share(int64_t i) const
+        {
+            const double v = value(i);
+            return v == -kInf ? v : (v == m ? 0.0 : v - m) * inverse - log_s;
+        }
+        __device__ __forceinline__ void take(Group<G> &g, const Side &of, int64_t r, int32_t i, int32_t n)
+        {
+            p = of.row(r, i);
+            type = of.type;
+            inverse = of.inverse_of(r);
+            m = -kInf;
+            uint32_t at = 0;
+            for (int32_t k = g.t; k < n; k += G) {
+                const double v = value(k);
+                if (v > m) {
+                    m = v;
+                    at = ~(uint32_t)k;
+                }
+            }
+            const double most = g.reduce(m, Max());
+            first = (int32_t)~g.reduce(m == most ? at : 0u, Max());
+            m = most;
+            log_s = 0.0;
+            double s = 0.0;
+            for (int32_t k = g.t; k < n; k += G)
+                s += exp(log_share(k));
+            log_s = log(g.reduce(s, Add()));
+        }
+    };
+    const int32_t length = a.length(r);
+    Row p, q;
+    int32_t j = 0, t = -1;
+    bool row_q = false;
+    for (;; ++j) {
+        p.take(g, a.target, r, j, a.n);
+        if (j == length)
+            break;
+        t = a.drafted[r * a.drafts + j];
+        row_q = has_row(a, a.draft.inverse_of(r));
+        if (row_q)
+            q.take(g, a.draft, r, j, a.n);
+        if (t < 0 || t >= a.n)
+            break;
+        const double log_p = p.log_share(t), log_q = row_q ? q.log_share(t) : 0.0;
+        if (!(log_p > -kInf) ||
+            !((double)a.uniform[r * a.drafts + j] <
+              (log_q == -kInf ? kInf : exp(log_p - log_q))))
+            break;
+    }
+    // from what is left of p or, where no class has more in it, from p
+    Best best = nothing();
+    const bool masked = p.m == -kInf;
+    for (int turn = j < length ? 0 : 1; turn < 2 && !masked; ++turn) {
+        const bool rest = turn == 0;
+        bool mass = false;
+        for (int32_t i = g.t; i < a.n; i += G) {
+            const double share = exp(p.log_share(i));
+            const double less = !rest ? 0.0 : row_q ? exp(q.log_share(i)) : i == t ? 1.0 : 0.0;
+            if (!(share > less))                          // (a NaN: a row of masked logits)
+                if (!(rest && row_q && q.m == -kInf && share > 0.0))
+                    continue;
+            mass = true;
+            const double left = rest && !(row_q && q.m == -kInf) ? share - less : share;
+            const double score = log(left) + (double)a.noise[r * a.noise_stride + i];
+            if (score > -kInf)
+                merge(best, {score, 0.0, -kInf, i});
+        }
+        if (g.reduce((uint32_t)mass, Max()))
+            break;
+    }
+    best = join(g, best);
+    if (g.t == 0) {
+        const int32_t token = masked ? -1 : best.cls == kNoClass ? p.first : (int32_t)best.cls;
+        a.accepted[r] = j;
+        a.token[r] = token;
+        if (a.log_prob)
+            a.log_prob[r] = token < 0 ? -__builtin_inff() : (float)p.log_share(token);
+    }
+}
+
+// ---- short rows: a wave a request ----
+// Rows of up to kManyRows classes: 16 lanes a row, the rows of 32 drafts together, since a wait
+// for memory costs more than rows behind a rejection.  Longer ones: a draft's rows at a time.
+constexpr int kShortBlock = 256;
+constexpr int32_t kManyRows = 512;
+
+template <int G>
+__global__ __launch_bounds__(kShortBlock, 4) void k_verify_short(VerifyArgs a)
+{
+    constexpr int kGroups = kShortBlock / kWave, kDrafts = G < kWave ? 32 : 1;
+    __shared__ Stat all[kGroups][2 * kDrafts];
+    const int gi = group_of<kWave>(), lane = threadIdx.x % kWave;
+    Group<kWave> g(lane, nullptr);
+    Group<G> own(lane % G, nullptr);
+    Stat *stats = all[gi];
     for (int64_t r = (int64_t)blockIdx.x * kGroups + gi; r < a.n_requests;
          r += (int64_t)gridDim.x * kGroups) {
         const double inverse_p = uniform(a.target.inverse_of(r));
         const double inverse_q = uniform(a.draft.inverse_of(r));
         const int32_t length = uniform(a.length(r));
-        int32_t j = 0;
-        Stat p, q = {0, 0, 0.0};
-        for (;; ++j) {
-            const bool both = j < length && has_row(a, inverse_q) && inverse_p > 0.0;
-            for (int side = 0; side <= (int)both; ++side) {
-                const Side &of = side ? a.draft : a.target;
-                const Stat one = stat_of(g, of.row(r, j), of.type, 0, a.n,
-                                         side ? inverse_q : inverse_p);
-                (side ? q : p) = one;
+        const bool both = has_row(a, inverse_q) && inverse_p > 0.0;
+        int32_t j = -1, base = 0;
+        for (;; base += kDrafts) {
+            const int32_t count = min(kDrafts, length + 1 - base);     // (of the target's rows)
+            for (int32_t u = lane / G; u < 2 * count; u += kWave / G) {
+                const int32_t i = base + u / 2;
+                const bool q = u & 1;
+                if (q && (!both || i == length))
+                    continue;
+                const Stat one = stat_of(own, q ? a.draft.row(r, i) : a.target.row(r, i),
+                                         q ? a.draft.type : a.target.type, 0, a.n, a.n,
+                                         q ? inverse_q : inverse_p);
+                if (own.t == 0)
+                    stats[u] = one;
             }
-            if (j == length)
+            wave_sync();
+            j = walk(a, r, base, min(length, base + kDrafts), inverse_p, inverse_q, stats);
+            if (j == kNone && length < base + kDrafts)
+                j = length;
+            if (j != kNone)
                 break;
-            int how = decide(a, r, j, inverse_p, inverse_q, p, q, kLoose);
-            if (how == kOpen)
-                how = decide_exactly(g, a, r, j, inverse_p, inverse_q, p, q);
-            if (how == kRejected)
-                break;
+            wave_sync();
         }
-        int32_t token = -1;
-        if (!is_masked(p, a.target.type)) {
-            if (inverse_p > 0.0) {
-                const Draw d = draw_of(a, r, j, length, inverse_p, inverse_q, p, q);
-                token = settle(g, d, draw_part(g, d, 0, a.n));
-            } else {
-                token = p.first;
+        int32_t token = j == kLeftOpen ? kLeftOpen : -1;
+        if (j >= 0) {
+            const Stat p = stats[2 * (j - base)], q = stats[2 * (j - base) + 1];
+            wave_sync();
+            if (p.m > -kInf) {
+                if (inverse_p > 0.0) {
+                    const Draw d = draw_of(a, r, j, length, inverse_p, inverse_q, p, q);
+                    token = settle(d, draw_part(g, d, 0, a.n));
+                } else {
+                    token = p.first;
+                }
             }
+            if (lane == 0 && token != kLeftOpen)
+                answer(a, r, j, token, inverse_p, p);
         }
-        if (g.t == 0)
-            answer(a, r, j, token, inverse_p, p);
+        if (token == kLeftOpen)
+            redo(g, a, r);
     }
 }
 
@@ -624,7 +725,7 @@ __global__ __launch_bounds__(256) void k_verify_clear(VerifyArgs a)
 // (WHOLE): rows i of all requests before rows i + 1 of any, and a row behind a draft that is
 // known to be rejected by then is left out: nobody asks for it.
 template <int G, bool WHOLE>
-__global__ __launch_bounds__(G) void k_verify_rows(VerifyArgs a)
+__global__ __launch_bounds__(G, 8) void k_verify_rows(VerifyArgs a)
 {
     __shared__ Scratch scratch;
     __shared__ int32_t known;
@@ -653,19 +754,18 @@ __global__ __launch_bounds__(G) void k_verify_rows(VerifyArgs a)
         }
         const int32_t lo = part * a.part, hi = min(a.n, lo + a.part);
         const double inverse_p = a.target.inverse_of(r), inverse_q = a.draft.inverse_of(r);
-        Stat p, q = {0, 0, 0.0};
+        Stat p, q = {-kInf, 0.0, 0};
         const bool both = i < length && has_row(a, inverse_q) && inverse_p > 0.0;
         for (int side = 0; side <= (int)both; ++side) {
-            const Side &of = side ? a.draft : a.target;
-            const Stat one = stat_of(g, of.row(r, i), of.type, lo, hi,
+            const Stat one = stat_of(g, side ? a.draft.row(r, i) : a.target.row(r, i),
+                                     side ? a.draft.type : a.target.type, lo, hi, a.n,
                                      side ? inverse_q : inverse_p);
             (side ? q : p) = one;
         }
         if (g.t == 0) {
             a.stat(r, i, 0)[part] = p;
             a.stat(r, i, 1)[part] = q;
-            if (WHOLE && i < length &&
-                decide(a, r, i, inverse_p, inverse_q, p, q, kLoose) == kRejected)
+            if (WHOLE && i < length && surely_rejected(a, r, i, inverse_p, inverse_q, p, q))
                 atomicMin(&a.rejected[r], i);
         }
     }
@@ -673,56 +773,55 @@ __global__ __launch_bounds__(G) void k_verify_rows(VerifyArgs a)
 
 constexpr int kDrawBlock = 256;
 
-__global__ __launch_bounds__(kDrawBlock) void k_verify_draw(VerifyArgs a)
+__global__ __launch_bounds__(kDrawBlock, 4) void k_verify_draw(VerifyArgs a)
 {
-    constexpr int G = kDrawBlock;
+    constexpr int G = kDrawBlock, kDrafts = 64;
     __shared__ Scratch scratch;
     __shared__ uint32_t place;
+    __shared__ Stat stats[2 * kDrafts];
     Group<G> g(threadIdx.x, &scratch);
-    const int lane = threadIdx.x % kWave;
     const int64_t units = a.n_requests * a.draw_parts;
     for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const int64_t r = unit / a.draw_parts;
         const int32_t part = (int32_t)(unit - r * a.draw_parts);
         const double inverse_p = a.target.inverse_of(r), inverse_q = a.draft.inverse_of(r);
         const int32_t length = a.length(r);
-        // the walk, 64 drafts at a time and the same in every wave of the block
-        int32_t j = length;
-        for (int32_t base = 0; base < length && j == length; base += kWave) {
-            const int32_t i = base + lane;
-            int how = kAccepted;
-            Stat p = {0, 0, 0.0}, q = p;
-            if (i < length) {
-                p = join(a.stat(r, i, 0), a.parts, a.target.type, inverse_p);
-                if (has_row(a, inverse_q) && inverse_p > 0.0)
-                    q = join(a.stat(r, i, 1), a.parts, a.draft.type, inverse_q);
-                how = decide(a, r, i, inverse_p, inverse_q, p, q, kLoose);
+        // the walk, kDrafts at a time: their rows' parts joined by 16 lanes each, then the same
+        // decisions in every wave of the block
+        const bool both = has_row(a, inverse_q) && inverse_p > 0.0;
+        int32_t j = -1, base = 0;
+        for (;; base += kDrafts) {
+            const int32_t count = min(kDrafts, length + 1 - base);
+            for (int32_t u = threadIdx.x / kJoin; u < 2 * count; u += G / kJoin) {
+                const int32_t i = base + u / 2;
+                const bool q = u & 1;
+                if (q && (!both || i == length))
+                    continue;
+                const Stat one = join(a.stat(r, i, q), a.parts, q ? inverse_q : inverse_p);
+                if (threadIdx.x % kJoin == 0)
+                    stats[u] = one;
             }
-            uint64_t ends = __ballot(how != kAccepted);
-            while (ends) {
-                const int k = __builtin_ctzll(ends);
-                ends &= ends - 1;
-                int one = __shfl(how, k);
-                if (one == kOpen) {
-                    Stat pk = {(uint32_t)__shfl((int)p.m, k), 0, 0.0}, qk = pk;
-                    qk.m = (uint32_t)__shfl((int)q.m, k);
-                    one = decide_exactly(g, a, r, base + k, inverse_p, inverse_q, pk, qk);
-                }
-                if (one == kRejected) {
-                    j = base + k;
-                    break;
-                }
-            }
+            __syncthreads();
+            j = walk(a, r, base, min(length, base + kDrafts), inverse_p, inverse_q, stats);
+            if (j == kNone && length < base + kDrafts)
+                j = length;
+            if (j != kNone)
+                break;
+            __syncthreads();
         }
-        const Stat p = join(a.stat(r, j, 0), a.parts, a.target.type, inverse_p);
-        if (inverse_p == 0.0 || is_masked(p, a.target.type)) {
-            if (part == 0 && g.t == 0)
-                answer(a, r, j, is_masked(p, a.target.type) ? -1 : p.first, inverse_p, p);
+        if (j == kLeftOpen) {                             // (all of the request's blocks see it)
+            if (part == 0)
+                redo(g, a, r);
+            __syncthreads();
             continue;
         }
-        Stat q = {0, 0, 0.0};
-        if (j < length && has_row(a, inverse_q))
-            q = join(a.stat(r, j, 1), a.parts, a.draft.type, inverse_q);
+        const Stat p = stats[2 * (j - base)], q = stats[2 * (j - base) + 1];
+        __syncthreads();                                  // (the next unit writes them)
+        if (inverse_p == 0.0 || p.m == -kInf) {
+            if (part == 0 && g.t == 0)
+                answer(a, r, j, p.m == -kInf ? -1 : p.first, inverse_p, p);
+            continue;
+        }
         const Draw d = draw_of(a, r, j, length, inverse_p, inverse_q, p, q);
         const int32_t lo = part * a.draw_part;
         Best best = draw_part(g, d, lo, min(a.n, lo + a.draw_part));
@@ -755,8 +854,10 @@ __global__ __launch_bounds__(kDrawBlock) void k_verify_draw(VerifyArgs a)
             }
             best = join(g, best);
         }
-        const int32_t token = settle(g, d, best);
-        if (g.t == 0)
+        const int32_t token = settle(d, best);
+        if (token == kLeftOpen)
+            redo(g, a, r);
+        else if (g.t == 0)
             answer(a, r, j, token, inverse_p, p);
     }
 }
@@ -837,8 +938,12 @@ hipError_t launch_verify(const VerifySide &target, const VerifySide &draft, int6
     const Plan p = plan_of(n_requests, drafts, n);
     if (p.is_short) {
         constexpr int kGroups = kShortBlock / kWave;
-        hipLaunchKernelGGL(k_verify_short, grid((n_requests + kGroups - 1) / kGroups),
-                           dim3(kShortBlock), 0, stream, a);
+        if (n <= kManyRows)
+            hipLaunchKernelGGL(k_verify_short<16>, grid((n_requests + kGroups - 1) / kGroups),
+                               dim3(kShortBlock), 0, stream, a);
+        else
+            hipLaunchKernelGGL(k_verify_short<64>, grid((n_requests + kGroups - 1) / kGroups),
+                               dim3(kShortBlock), 0, stream, a);
         return hipGetLastError();
     }
     char *ws = static_cast<char *>(workspace);
