@@ -20,7 +20,7 @@
 // Short rows: a wave walks its request alone, and reads nothing behind the first rejection.
 // Long rows: k_verify_rows takes the sums of all rows, in parts where there are few, and
 // k_verify_draw has a request's blocks each decide its walk from the sums and draw from their
-// part of the last row; the last of them joins the parts.
+// part of the last row, and k_verify_pick joins the parts.
 #include <float.h>
 
 #include <algorithm>
@@ -45,11 +45,11 @@ struct Side {
     {
         return rows + r * request_stride + i * row_stride;
     }
-    // 1 / T in 64 bits; 0 where T <= 0 (or is a NaN)
+    // 1 / T in 64 bits, within what keeps masked terms zero; 0 where T <= 0 (or is a NaN)
     __device__ double inverse_of(int64_t r) const
     {
         const float t = temperatures ? temperatures[r] : temperature;
-        return t > 0.0f ? fmin(1.0 / (double)fminf(t, FLT_MAX), 0x1p126) : 0.0;
+        return t > 0.0f ? fmin(1.0 / (double)fminf(t, 0x1p120f), 0x1p126) : 0.0;
     }
 };
 
@@ -68,6 +68,12 @@ struct Best {
     int64_t cls;
 };
 
+// Where a request's walk ended (or kLeftOpen), the target's row there, and what is drawn from.
+struct Walk {
+    Stat p;
+    int32_t j, less;
+};
+
 struct VerifyArgs {
     Side target, draft;
     int64_t n_requests;
@@ -80,7 +86,7 @@ struct VerifyArgs {
     // long rows
     Stat *stats;                        // [request][drafts + 1][2][parts]
     int32_t *rejected;                  // [request]: a draft known to be rejected
-    uint32_t *done;                     // [request]: finished parts of the draw
+    struct Walk *walks;                 // [request]
     Best *bests;                        // [request][draw_parts]
     int32_t parts, part, draw_parts, draw_part;
 
@@ -209,8 +215,8 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo
 #pragma unroll
         for (int u = 0; u < VEC; ++u) {
             const Cmp v = p.get(u);
-            const float e = __builtin_amdgcn_exp2f(E::minus(v, m) * c);
-            part += v > E::lowest() ? e : 0.0f;
+            // (masked: -inf or, of two of them or a NaN, no number, which the maximum drops)
+            part += __builtin_amdgcn_exp2f(fmaxf(E::minus(v, m), -FLT_MAX) * c);
         }
         s += (double)part;
     });
@@ -250,6 +256,8 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int type, 
 constexpr int kJoin = 16;
 __device__ __forceinline__ Stat join(const Stat *parts, int32_t count, double inverse)
 {
+    if (count == 1)
+        return parts[0];
     const int lane = threadIdx.x % kJoin;
     double m = -kInf, s = 0.0;
     int32_t first = 0;
@@ -289,13 +297,16 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, int64_t r, int32_t i,
     const double x = below(value_at(a.target.row(r, i), a.target.type, t), p.m);
     if (x == -kInf)
         return kRejected;
-    double log_ratio = x * inverse_p - log(p.s);
+    // p / q = e^(x - y) s_q / s_p
+    double ratio = x * inverse_p, sums = 1.0 / p.s;
     if (has_row(a, inverse_q)) {
         const double v = value_at(a.draft.row(r, i), a.draft.type, t);
-        log_ratio = v == -kInf || below(v, q.m) == -kInf
-                        ? kInf : log_ratio - (below(v, q.m) * inverse_q - log(q.s));
+        const double y = v == -kInf ? v : below(v, q.m) * inverse_q;
+        ratio = y == -kInf ? kInf : ratio - y;
+        sums = q.s / p.s;
     }
-    const double ratio = exp(log_ratio), u = a.uniform[at];
+    ratio = ratio == kInf ? kInf : exp(ratio) * sums;     // (no mass in q at all: s_q is 0)
+    const double u = a.uniform[at];
     if (fabs(u - ratio) <= loose * ratio && ratio < kInf)
         return kOpen;
     return u < ratio ? kAccepted : kRejected;
@@ -332,7 +343,7 @@ struct Draw {
     const float *noise;
     int p_type, q_type, less;
     int32_t n, drafted;
-    double pm, qm, inverse_p, inverse_q, log_p, log_q;    // logs of the sums
+    double pm, qm, inverse_p, inverse_q, log_sums;        // log(s_p / s_q)
 };
 
 __device__ __forceinline__ void merge(Best &a, const Best &b)
@@ -378,7 +389,7 @@ __device__ __forceinline__ void offer(Best &best, const Draw &d, int32_t cls, do
     if (d.less == kOne && cls == d.drafted)
         return;
     if (d.less == kRow && y > -kInf) {
-        const double delta = (y - d.log_q) - (x - d.log_p);
+        const double delta = y - x + d.log_sums;          // log(q / p)
         if (!(delta < 2 * kLoose))
             return;
         if (delta > -2 * kLoose) {                        // p > q, or not, by less than 4 kLoose
@@ -491,8 +502,7 @@ __device__ __forceinline__ Draw draw_of(const VerifyArgs &a, int64_t r, int32_t 
     d.qm = q.m;
     d.inverse_p = inverse_p;
     d.inverse_q = inverse_q;
-    d.log_p = log(p.s);
-    d.log_q = 0.0;
+    d.log_sums = 0.0;
     d.less = kWhole;
     if (j < length) {
         if (!has_row(a, inverse_q)) {
@@ -501,7 +511,7 @@ __device__ __forceinline__ Draw draw_of(const VerifyArgs &a, int64_t r, int32_t 
         } else if (q.m > -kInf) {
             d.less = kRow;
             d.q = a.draft.row(r, j);
-            d.log_q = log(q.s);
+            d.log_sums = log(p.s / q.s);
         }
     }
     return d;
@@ -524,7 +534,7 @@ __device__ __forceinline__ void answer(const VerifyArgs &a, int64_t r, int32_t j
 
 // ---- the walk ----
 // The first of drafts [base, base + 64), below `length`, that does not stand, or kNone; kLeftOpen
-// where 32 bits do not tell.  stats: p and q of each in turn.  The same in every wave of a group.
+// where 32 bits do not tell.  stats: p and q of each in turn.  By a wave.
 constexpr int32_t kNone = -1, kLeftOpen = -2;
 __device__ __forceinline__ int32_t walk(const VerifyArgs &a, int64_t r, int32_t base,
                                         int32_t length, double inverse_p, double inverse_q,
@@ -543,10 +553,10 @@ __device__ __forceinline__ int32_t walk(const VerifyArgs &a, int64_t r, int32_t 
 }
 
 // The class of a draw, or kLeftOpen: it takes 64 bits, or there is none in what is left of p.
-__device__ __forceinline__ int32_t settle(const Draw &d, const Best &best)
+__device__ __forceinline__ int32_t settle(int less, const Best &best)
 {
     const bool open = best.cls == kNoClass ||
-                      (d.less == kRow && best.other > -kInf &&
+                      (less == kRow && best.other > -kInf &&
                        best.other >= best.score - best.off);
     return open ? kLeftOpen : (int32_t)best.cls;
 }
@@ -697,7 +707,7 @@ __global__ __launch_bounds__(kShortBlock, 4) void k_verify_short(VerifyArgs a)
             if (p.m > -kInf) {
                 if (inverse_p > 0.0) {
                     const Draw d = draw_of(a, r, j, length, inverse_p, inverse_q, p, q);
-                    token = settle(d, draw_part(g, d, 0, a.n));
+                    token = settle(d.less, draw_part(g, d, 0, a.n));
                 } else {
                     token = p.first;
                 }
@@ -715,10 +725,8 @@ __global__ __launch_bounds__(kShortBlock, 4) void k_verify_short(VerifyArgs a)
 __global__ __launch_bounds__(256) void k_verify_clear(VerifyArgs a)
 {
     for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.n_requests;
-         r += (int64_t)gridDim.x * 256) {
+         r += (int64_t)gridDim.x * 256)
         a.rejected[r] = INT32_MAX;
-        a.done[r] = 0;
-    }
 }
 
 // The stats of row i of request r, target's and drafter's, or of a part of them.  Whole rows
@@ -736,8 +744,6 @@ __global__ __launch_bounds__(G, 8) void k_verify_rows(VerifyArgs a)
         const int32_t part = WHOLE ? 0 : (int32_t)(unit - row * a.parts);
         const int32_t i = (int32_t)(row / a.n_requests);
         const int64_t r = row - i * a.n_requests;
-        if (!WHOLE && i == 0 && part == 0 && g.t == 0)
-            a.done[r] = 0;
         const int32_t length = a.length(r);
         if (i > length)
             continue;
@@ -777,7 +783,7 @@ __global__ __launch_bounds__(kDrawBlock, 4) void k_verify_draw(VerifyArgs a)
 {
     constexpr int G = kDrawBlock, kDrafts = 64;
     __shared__ Scratch scratch;
-    __shared__ uint32_t place;
+    __shared__ int32_t found;
     __shared__ Stat stats[2 * kDrafts];
     Group<G> g(threadIdx.x, &scratch);
     const int64_t units = a.n_requests * a.draw_parts;
@@ -786,8 +792,8 @@ __global__ __launch_bounds__(kDrawBlock, 4) void k_verify_draw(VerifyArgs a)
         const int32_t part = (int32_t)(unit - r * a.draw_parts);
         const double inverse_p = a.target.inverse_of(r), inverse_q = a.draft.inverse_of(r);
         const int32_t length = a.length(r);
-        // the walk, kDrafts at a time: their rows' parts joined by 16 lanes each, then the same
-        // decisions in every wave of the block
+        // the walk, kDrafts at a time: their rows' parts joined by 16 lanes each, then the
+        // decisions, which one wave takes (64-bit exponentials in all four: 30 us of 109)
         const bool both = has_row(a, inverse_q) && inverse_p > 0.0;
         int32_t j = -1, base = 0;
         for (;; base += kDrafts) {
@@ -802,63 +808,59 @@ __global__ __launch_bounds__(kDrawBlock, 4) void k_verify_draw(VerifyArgs a)
                     stats[u] = one;
             }
             __syncthreads();
-            j = walk(a, r, base, min(length, base + kDrafts), inverse_p, inverse_q, stats);
-            if (j == kNone && length < base + kDrafts)
-                j = length;
+            if (threadIdx.x < kWave) {
+                j = walk(a, r, base, min(length, base + kDrafts), inverse_p, inverse_q, stats);
+                if (j == kNone && length < base + kDrafts)
+                    j = length;
+                if (threadIdx.x == 0)
+                    found = j;
+            }
+            __syncthreads();
+            j = found;
             if (j != kNone)
                 break;
-            __syncthreads();
         }
-        if (j == kLeftOpen) {                             // (all of the request's blocks see it)
-            if (part == 0)
-                redo(g, a, r);
-            __syncthreads();
-            continue;
+        const bool open = j == kLeftOpen;                 // (all of the request's blocks see it)
+        Stat p = {-kInf, 0.0, 0}, q = p;
+        if (!open) {
+            p = stats[2 * (j - base)];
+            q = stats[2 * (j - base) + 1];
         }
-        const Stat p = stats[2 * (j - base)], q = stats[2 * (j - base) + 1];
         __syncthreads();                                  // (the next unit writes them)
-        if (inverse_p == 0.0 || p.m == -kInf) {
-            if (part == 0 && g.t == 0)
-                answer(a, r, j, p.m == -kInf ? -1 : p.first, inverse_p, p);
-            continue;
+        const bool drawn = !open && inverse_p > 0.0 && p.m > -kInf;
+        int32_t less = kWhole;
+        if (drawn) {
+            const Draw d = draw_of(a, r, j, length, inverse_p, inverse_q, p, q);
+            const int32_t lo = part * a.draw_part;
+            const Best best = draw_part(g, d, lo, min(a.n, lo + a.draw_part));
+            if (g.t == 0)
+                a.bests[r * a.draw_parts + part] = best;
+            less = d.less;
         }
-        const Draw d = draw_of(a, r, j, length, inverse_p, inverse_q, p, q);
-        const int32_t lo = part * a.draw_part;
-        Best best = draw_part(g, d, lo, min(a.n, lo + a.draw_part));
-        if (a.draw_parts > 1) {
-            Best *of = a.bests + r * a.draw_parts;
-            if (g.t == 0) {
-                // past this die's caches, before the count says that it is there
-                uint64_t w[4];
-                __builtin_memcpy(w, &best, sizeof w);
-                for (int k = 0; k < 4; ++k)
-                    __hip_atomic_store(reinterpret_cast<uint64_t *>(of + part) + k, w[k],
-                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                place = __hip_atomic_fetch_add(&a.done[r], 1u, __ATOMIC_ACQ_REL,
-                                               __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            const bool last = place == (uint32_t)a.draw_parts - 1;
-            __syncthreads();
-            if (!last)
-                continue;
-            best = nothing();
-            for (int32_t k = g.t; k < a.draw_parts; k += G) {
-                uint64_t w[4];
-                for (int e = 0; e < 4; ++e)
-                    w[e] = __hip_atomic_load(reinterpret_cast<uint64_t *>(of + k) + e,
-                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                Best one;
-                __builtin_memcpy(&one, w, sizeof one);
-                merge(best, one);
-            }
-            best = join(g, best);
+        if (part == 0 && g.t == 0)
+            a.walks[r] = {p, j, less};
+    }
+}
+
+// The parts of a request's draw joined, by a wave.  (A last block that joins them instead needs
+// fences between the dies' L2s, one a block: 192 x 131072, 16 blocks a request, 195 us, without 74.)
+__global__ __launch_bounds__(kWave) void k_verify_pick(VerifyArgs a)
+{
+    Group<kWave> g(threadIdx.x, nullptr);
+    for (int64_t r = blockIdx.x; r < a.n_requests; r += gridDim.x) {
+        const Walk w = a.walks[r];
+        const double inverse_p = a.target.inverse_of(r);
+        int32_t token = w.j == kLeftOpen ? kLeftOpen : w.p.m == -kInf ? -1 : w.p.first;
+        if (token >= 0 && inverse_p > 0.0) {
+            Best best = nothing();
+            for (int32_t k = g.t; k < a.draw_parts; k += kWave)
+                merge(best, a.bests[r * a.draw_parts + k]);
+            token = settle(w.less, join(g, best));
         }
-        const int32_t token = settle(d, best);
         if (token == kLeftOpen)
             redo(g, a, r);
         else if (g.t == 0)
-            answer(a, r, j, token, inverse_p, p);
+            answer(a, r, w.j, token, inverse_p, w.p);
     }
 }
 
@@ -869,7 +871,7 @@ constexpr int kWholeBlock = 1024;
 struct Plan {
     bool is_short, whole;
     int32_t parts, part, draw_parts, draw_part;
-    size_t stats, rejected, done, bests, bytes;
+    size_t rejected, walks, bests, bytes;
 };
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
@@ -892,11 +894,13 @@ Plan plan_of(int64_t n_requests, int32_t drafts, int32_t n)
     const int64_t rows = n_requests * (drafts + 1);
     p.whole = rows >= 512;
     split(rows, n, p.whole ? 1 : 1024, 4096, p.parts, p.part);
-    split(n_requests, n, 1024, 4096, p.draw_parts, p.draw_part);
+    // (192 rows of 131072, all kernels: 169 us at 1024 blocks, 158 at 2048, 154 at 4096; one
+    // row: 23.8, 24.3 and 25.1)
+    split(n_requests, n, 2048, 4096, p.draw_parts, p.draw_part);
     p.rejected = up((size_t)rows * 2 * p.parts * sizeof(Stat));
-    p.done = p.rejected + up((size_t)n_requests * 4);
-    p.bests = p.done + up((size_t)n_requests * 4);
-    p.bytes = p.bests + (p.draw_parts > 1 ? (size_t)n_requests * p.draw_parts * sizeof(Best) : 0);
+    p.walks = p.rejected + up((size_t)n_requests * 4);
+    p.bests = p.walks + up((size_t)n_requests * sizeof(Walk));
+    p.bytes = p.bests + (size_t)n_requests * p.draw_parts * sizeof(Best);
     return p;
 }
 
@@ -949,7 +953,7 @@ hipError_t launch_verify(const VerifySide &target, const VerifySide &draft, int6
     char *ws = static_cast<char *>(workspace);
     a.stats = reinterpret_cast<Stat *>(ws);
     a.rejected = reinterpret_cast<int32_t *>(ws + p.rejected);
-    a.done = reinterpret_cast<uint32_t *>(ws + p.done);
+    a.walks = reinterpret_cast<Walk *>(ws + p.walks);
     a.bests = reinterpret_cast<Best *>(ws + p.bests);
     a.parts = p.parts;
     a.part = p.part;
@@ -968,6 +972,9 @@ hipError_t launch_verify(const VerifySide &target, const VerifySide &draft, int6
         return err;
     hipLaunchKernelGGL(k_verify_draw, grid(n_requests * p.draw_parts), dim3(kDrawBlock), 0,
                        stream, a);
+    if (hipError_t err = hipGetLastError(); err != hipSuccess)
+        return err;
+    hipLaunchKernelGGL(k_verify_pick, grid(n_requests), dim3(kWave), 0, stream, a);
     return hipGetLastError();
 }
 
