@@ -7,6 +7,11 @@
 // number is at least round(p 2^16).  Sixteen bits a number halve the generator's work a
 // byte; what they cost is that p is one of 2^16 + 1 values, and the factor of the elements
 // that stay is the exact reciprocal of that value's complement, so the mean is unbiased.
+//
+// Memory bounds it: a copy's bytes.  16384 x 8192 in bf16 takes 95 us where torch's copy of
+// it takes 101, 2^18 x 100 counts 35 us where their copy as float takes 47; with one round
+// for ten 88 and 33 us, so the products hide behind the loads.  Lanes of eight elements load
+// and store 16 or 32 bytes.
 #include "logit_rows.h"
 
 namespace bl {
@@ -64,6 +69,55 @@ __device__ __forceinline__ uint32_t to_bits(float v)
     }
 }
 
+// The first of N words moved down by `by` elements of `bytes` bytes, a bit of it at a time.
+template <int N>
+__device__ __forceinline__ void move_down(uint32_t (&w)[N], int by, int bytes)
+{
+    const int words = by * bytes / 4;
+#pragma unroll
+    for (int step = 1; step < N; step *= 2)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            w[k] = words & step ? (k + step < N ? w[k + step] : 0u) : w[k];
+    if (bytes == 2 && (by & 1)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            w[k] = w[k] >> 16 | (k + 1 < N ? w[k + 1] << 16 : 0u);
+    }
+}
+
+// The last eight elements of a row, moved down to those from i on: one load, where a loop
+// over them, each waiting for the one before, took 133 us for 16381 x 8191 in bf16, not 107.
+// (In place, a neighbour may have stored some of them already: those are moved out.)
+template <int TYPE>
+__device__ __forceinline__ void load_row(Piece<TYPE, kEight> &p, const char *row, int32_t i,
+                                         int32_t n)
+{
+    constexpr int B = Elem<TYPE>::kBytes;
+    if (n < kEight) {                                     // (in the whole wave)
+        p.load(row, 0, i, n);
+        return;
+    }
+    const int32_t at = min(i, n - kEight);
+    __builtin_memcpy(p.w, row + (int64_t)at * B, sizeof p.w);
+    if (at < i)
+        move_down(p.w, i - at, B);
+}
+
+// The first `count` (below eight) of eight elements stored, four, two and one at a time.
+template <int N>
+__device__ __forceinline__ void store_end(char *dst, uint32_t (&w)[N], int count)
+{
+    constexpr int B = N / 2;                              // bytes of an element: 2, 4
+#pragma unroll
+    for (int some = 4; some; some /= 2)
+        if (count & some) {
+            __builtin_memcpy(dst, w, (size_t)some * B);
+            dst += some * B;
+            move_down(w, some, B);
+        }
+}
+
 template <int TYPE>
 __global__ __launch_bounds__(kBlock) void k_dropout(DropoutArgs a, uint64_t tasks)
 {
@@ -85,7 +139,7 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropoutArgs a, uint64_t task
         const char *src = a.x + row * a.stride;
         char *dst = a.out + row * a.out_stride + (int64_t)i * kBytes;
         Piece<TYPE, kEight> p;
-        p.load(src, 0, i, a.n);
+        load_row(p, src, i, a.n);
         uint32_t c[4] = {eight, (uint32_t)row, (uint32_t)offset, (uint32_t)(offset >> 32)};
         philox(c, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
         uint32_t w[kEight];
@@ -100,23 +154,15 @@ __global__ __launch_bounds__(kBlock) void k_dropout(DropoutArgs a, uint64_t task
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 packed[u] = w[2 * u] | w[2 * u + 1] << 16;
-            if (i + kEight <= a.n) {
+            if (i + kEight <= a.n)
                 __builtin_memcpy(dst, packed, sizeof packed);
-            } else {
-#pragma unroll
-                for (int k = 0; k < kEight; ++k)
-                    if (i + k < a.n)
-                        reinterpret_cast<uint16_t *>(dst)[k] = (uint16_t)w[k];
-            }
+            else
+                store_end(dst, packed, a.n - i);
         } else {
-            if (i + kEight <= a.n) {
+            if (i + kEight <= a.n)
                 __builtin_memcpy(dst, w, sizeof w);
-            } else {
-#pragma unroll
-                for (int k = 0; k < kEight; ++k)
-                    if (i + k < a.n)
-                        reinterpret_cast<uint32_t *>(dst)[k] = w[k];
-            }
+            else
+                store_end(dst, w, a.n - i);
         }
     }
 }
