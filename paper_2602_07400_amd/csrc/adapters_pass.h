@@ -517,7 +517,7 @@ struct Second {
 
     // 4 ranks of column m + t 16 + l % 16 (forward) or m + t + E (l % 16) (back), zeros past the
     // last rank
-    __device__ __forceinline__ void terms_of(int m, int ct, uint32_t (&v)[T][S]) const
+    __device__ __forceinline__ void terms_of(int m, int ct, uint32_t (&v)[T][S], int there) const
     {
         const int r = ct * 16 + quad * 4;
         if constexpr (!BACK) {
@@ -527,7 +527,7 @@ struct Second {
 #pragma unroll
                 for (int i = 0; i < S; ++i)
                     v[t][i] = 0;
-                if (r < rank)
+                if (r < rank && t * 16 < there)
                     __builtin_memcpy(v[t], __builtin_assume_aligned(at, 4 * S), 4 * S);
             }
         } else {
@@ -555,9 +555,10 @@ struct Second {
             }
         }
     }
-    // factor w2 h of columns [m, m + kCols) to sums [16 rows][pitch floats], from column 0 on
+    // factor w2 h of columns [m, m + kCols) to sums [16 rows][pitch floats], from column 0 on;
+    // forward, as many 16s of them as the first `there` are in.
     __device__ __forceinline__ void unit(int m, const Frag (&terms)[CT], float factor, float *sums,
-                                         int sums_pitch) const
+                                         int sums_pitch, int there = kCols) const
     {
         f32x4 sum[T];
 #pragma unroll
@@ -566,7 +567,7 @@ struct Second {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             uint32_t v[T][S];
-            terms_of(m, ct, v);
+            terms_of(m, ct, v, there);
 #pragma unroll
             for (int t = 0; t < T; ++t)
                 sum[t] = mma_h<W>(v[t], terms[ct], sum[t]);
@@ -575,7 +576,8 @@ struct Second {
         if constexpr (!BACK) {
 #pragma unroll
             for (int t = 0; t < T; ++t)
-                *reinterpret_cast<f32x4 *>(own + t * 16 + quad * 4) = sum[t] * factor;
+                if (t * 16 < there)
+                    *reinterpret_cast<f32x4 *>(own + t * 16 + quad * 4) = sum[t] * factor;
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -721,9 +723,10 @@ struct NarrowRoom {
 
     __host__ __device__ NarrowRoom(int k, int m, int rank)
     {
-        constexpr int E = kEls<W>, S = kSize<W>, kCols = BACK ? 16 * E : 8 * E;
+        // (in whole units, 100 floats take 43 KB and 3 blocks a CU fit)
+        constexpr int E = kEls<W>, S = kSize<W>, kCols = BACK ? 16 * E : 16;
         const auto odd = [](int bytes) { return (((bytes + 15) / 16) | 1) * 16; };
-        const int cols = (m + kCols - 1) / kCols * kCols; // whole units
+        const int cols = (m + kCols - 1) / kCols * kCols;
         x_pitch = odd(k * S);
         sums_pitch = cols + 4;
         w1_pitch = odd(k * S);
@@ -839,7 +842,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
         factor[0] *= a.scales ? a.scales[tile.p.group] : a.scale;
 #pragma unroll 1
         for (int m = 0; m < a.m; m += Product::kCols)
-            second.unit(m, terms[0], factor[0], sums + m, room.sums_pitch);
+            second.unit(m, terms[0], factor[0], sums + m, room.sums_pitch, a.m - m);
         rows::wave_sync();
     }
     const auto result = [&](int r, int p, const Frag &base, float (&v)[E]) __attribute__((always_inline)) {
