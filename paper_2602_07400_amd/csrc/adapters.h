@@ -124,13 +124,13 @@ struct PassArgs {
 // out of at most 512 bytes each, and 64 KB of LDS.
 template <int W> bool fits_narrow(int32_t k, int32_t m, int32_t rank, bool back);
 
-// Parts of the k terms of wide adapters: for about 1024 blocks, whose waves (8 or, above rank
+// Parts of the k terms of wide adapters: for about 768 blocks, whose waves (8 or, above rank
 // 32, 4) have a unit of 128 bytes or more each.
 inline int32_t split_terms(int64_t n_tiles, int32_t k, int32_t rank, int32_t el_bytes)
 {
     const int64_t share = (rank <= 32 ? 8 : 4) * 128;
     const int64_t most = ((int64_t)k * el_bytes + share - 1) / share;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({most, 8, 1024 / n_tiles}));
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({most, 8, 768 / n_tiles}));
 }
 
 struct PassLayout {

@@ -107,22 +107,40 @@ __device__ __forceinline__ uint32_t el_bits(float v)
         return __float_as_uint(v);
 }
 
-// kEls elements from p, of which `left` are there; the others are zero.
+// kEls elements from p, of which `left` are there; the others are zero.  p is in a row of n
+// elements that ends with them: if those are enough, its last ones are loaded and moved down.
+// (An element at a time, each lane's loads are waited for one by one: the last block of 5003
+// columns kept the gradients of 12289 rows waiting, 57 us for 48.)
 template <int T>
-__device__ __forceinline__ Frag load_frag(const char *p, int left)
+__device__ __forceinline__ Frag load_frag(const char *p, int left, int64_t n)
 {
+    constexpr int E = kEls<T>, S = kSize<T>;
     Frag f;
-    if (left >= kEls<T>) {
-        __builtin_memcpy(f.w, p, 16);
+    if (n >= E) {
+        const int past = max(E - left, 0);
+        __builtin_memcpy(f.w, p - (int64_t)past * S, 16);
+        if (past > 0) {
+            const int words = past * S / 4;
+#pragma unroll
+            for (int step = 1; step <= 4; step *= 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    f.w[i] = words >= 4 ? 0 : words & step ? (i + step < 4 ? f.w[i + step] : 0)
+                                                           : f.w[i];
+            if (S == 2 && (past & 1))
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    f.w[i] = f.w[i] >> 16 | (i < 3 ? f.w[i + 1] << 16 : 0);
+        }
         return f;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         f.w[i] = 0;
 #pragma unroll
-    for (int u = 0; u < kEls<T>; ++u)
+    for (int u = 0; u < E; ++u)
         if (u < left) {
-            if constexpr (kSize<T> == 4)
+            if constexpr (S == 4)
                 f.w[u] = reinterpret_cast<const uint32_t *>(p)[u];
             else
                 f.w[u / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[u]
@@ -419,20 +437,21 @@ __device__ __forceinline__ void shrink(const PassArgs &a, const Tile<RT> &tile, 
 #pragma unroll
         for (int j = 0; j < J; ++j)
             lds_put(lds + slot_at(j * 8 + tile.eighth, tile.piece),
-                    to_terms<X>(load_frag<W>(x[j] + (int64_t)k0 * S, left)));
+                    to_terms<X>(load_frag<W>(x[j] + (int64_t)k0 * S, left, a.k)));
         if constexpr (!BACK) {
 #pragma unroll 1
             for (int c = 0; c < C; ++c) {
                 const int32_t r = min(c * 8 + tile.eighth, a.rank - 1);
                 lds_put(lds_w + slot_at(c * 8 + tile.eighth, tile.piece),
-                        load_frag<W>(first + ((int64_t)r * a.k + k0) * S + tile.piece * 16, left));
+                        load_frag<W>(first + ((int64_t)r * a.k + k0) * S + tile.piece * 16, left,
+                                     a.k));
             }
         } else {
             const int32_t there = (a.k - k0) * a.rank;
 #pragma unroll 1
             for (int at = tile.lane; at < pieces; at += kWave)
                 lds_put(lds_w + at * 16, load_frag<W>(first + k0 * across + at * 16,
-                                                      there - at * E));
+                                                      there - at * E, (int64_t)a.k * a.rank));
         }
         rows::wave_sync();
         products();
@@ -691,7 +710,7 @@ __device__ __forceinline__ void stage_rows(char *to, int pitch, const char *from
 #pragma unroll 1
         for (int r = threadIdx.x; r < rows; r += kTileWaves * kWave)
             lds_put(to + r * pitch + pieces * 16,
-                    load_frag<W>(from + r * stride + pieces * 16, n % E));
+                    load_frag<W>(from + r * stride + pieces * 16, n % E, n));
 }
 
 // up [m][rank] of `cols` columns to LDS, a column in `pitch` bytes; by all of a block.
@@ -765,7 +784,8 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
                 b[i] = load_nt(a.base + row * a.base_stride + p * 16);
         }
         if (end_lane && a.m % E)
-            b_end = load_frag<W>(a.base + tile.row[0] * a.base_stride + m_pieces * 16, a.m % E);
+            b_end = load_frag<W>(a.base + tile.row[0] * a.base_stride + m_pieces * 16, a.m % E,
+                                 a.m);
     }
     f32x4 h[1][CT];
     clear(h);
@@ -787,7 +807,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
             const int there = a.k * a.rank;               // [k][rank] as it lies, zeros behind
 #pragma unroll 2
             for (int at = threadIdx.x; at * 16 < room.w1; at += kTileWaves * kWave)
-                lds_put(w1 + at * 16, load_frag<W>(down + at * 16, there - at * E));
+                lds_put(w1 + at * 16, load_frag<W>(down + at * 16, there - at * E, there));
             if (a.out)
                 stage_rows<W>(w2, room.w2_pitch, up, (int64_t)a.m * S, a.rank, a.m);
         }
@@ -800,7 +820,7 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
         if (end_lane && a.k % E)
             lds_put(own + tile.lane * room.x_pitch + x_pieces * 16,
                     to_terms<X>(load_frag<W>(a.x + tile.row[0] * a.x_stride + x_pieces * 16,
-                                             a.k % E)));
+                                             a.k % E, a.k)));
         __syncthreads();
         // (rows that are not there: whatever is in LDS, in columns of their own)
         const int pieces = (a.k + E - 1) / E;
@@ -942,12 +962,15 @@ __global__ __launch_bounds__(kTermWaves<CT> * kWave, kWavesPerSimd<CT>) void k_s
 
 // Units of columns of a tile, 16 rows a wave; a unit's weights are in LDS for all of them, the
 // next unit's on their way.
+template <int CT, bool BACK> constexpr int kUnits = BACK || CT > 2 ? 1 : 2;
+
 template <int W, int CT, bool BACK>
 __global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expand(PassArgs a,
                                                                                 int32_t blocks)
 {
     typedef Second<W, CT, BACK> Product;
-    constexpr int E = kEls<W>, S = kSize<W>, kCols = Product::kCols, J = 2;
+    constexpr int E = kEls<W>, S = kSize<W>, kUnit = Product::kCols, J = 2, U = kUnits<CT, BACK>;
+    constexpr int kCols = U * kUnit;
     constexpr int kWeights = BACK ? CT * 16 * (kCols * S + 16)
                                   : kCols * ((CT * 16 * S / 16) | 1) * 16;
     constexpr int kPieces = (CT * 16 * kCols * S / 16 + 255) / 256;   // of the weights, a lane
@@ -962,18 +985,27 @@ __global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expan
     if (tile.p.group < 0)
         return;
     const bool adapted = tile.p.group < a.groups;
-    const int32_t units = (a.m + kCols - 1) / kCols, each = (units + blocks - 1) / blocks * kCols;
+    const int32_t units = (a.m + kUnit - 1) / kUnit, each = (units + blocks - 1) / blocks * kUnit;
     const int32_t from = block * each, to = a.out ? min(from + each, a.m) : 0;
-    Frag b[J], b_next[J];
-    const auto load_base = [&](Frag (&f)[J], int32_t m0) __attribute__((always_inline)) {
+    Frag b[U][J], b_next[U][J];
+    const auto load_base = [&](Frag (&f)[U][J], int32_t m0) __attribute__((always_inline)) {
         if constexpr (!BACK) {
             if (!a.base || !any)
                 return;
-            const int32_t m = m0 + tile.piece * E;
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-                f[j] = load_frag<W>(a.base + tile.row[j] * a.base_stride + (int64_t)m * S,
-                                    a.m - m);
+            for (int u = 0; u < U; ++u) {
+                const int32_t m = m0 + u * kUnit + tile.piece * E;
+                const char *at = a.base + (int64_t)m * S;
+                if (m0 + (u + 1) * kUnit <= a.m) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        f[u][j] = load_16(at + tile.row[j] * a.base_stride);
+                } else if (m0 + u * kUnit < to) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        f[u][j] = load_frag<W>(at + tile.row[j] * a.base_stride, a.m - m, a.m);
+                }
+            }
         }
     };
     if (from < to)
@@ -988,14 +1020,14 @@ __global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expan
     const auto load_weights = [&](int32_t m0) __attribute__((always_inline)) {
         if (!adapted || !by_pieces)
             return;
-        const int all = BACK ? a.rank * per : min(a.m - m0, kCols) * per;
+        const int all = BACK ? a.rank * per : min(to - m0, kCols) * per;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int e = i * kTileWaves * kWave + threadIdx.x, r = row_of(e), p = e - r * per;
             if (e < all) {
                 if constexpr (BACK)
                     w[i] = load_frag<W>(w2 + ((int64_t)r * a.m + m0) * S + p * 16,
-                                        a.m - m0 - p * E);
+                                        a.m - m0 - p * E, a.m);
                 else
                     w[i] = load_16(w2 + (int64_t)m0 * a.rank * S + e * 16);
             }
@@ -1005,10 +1037,10 @@ __global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expan
         if (!adapted)
             return;
         if (!BACK && !by_pieces) {
-            stage_up<W>(to_lds, pitch, w2 + (int64_t)m0 * a.rank * S, a.rank, min(a.m - m0, kCols));
+            stage_up<W>(to_lds, pitch, w2 + (int64_t)m0 * a.rank * S, a.rank, min(to - m0, kCols));
             return;
         }
-        const int all = BACK ? a.rank * per : min(a.m - m0, kCols) * per;
+        const int all = BACK ? a.rank * per : min(to - m0, kCols) * per;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int e = i * kTileWaves * kWave + threadIdx.x, r = row_of(e), p = e - r * per;
@@ -1047,38 +1079,46 @@ __global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expan
         }
         if (any) {
             float *own = sums[wave];
-            if (adapted) {
-                const Product second = {weights[turn], pitch, a.rank, tile.col, tile.quad};
-                second.unit(0, terms[0], factor[0], own, Product::kPitch);
-            }
-            rows::wave_sync();
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int q = 0; q < (BACK ? 2 : 1); ++q) {
-                    const int c = (tile.piece + q * 8) * E;
-                    float v[E];
-                    if (adapted) {
-                        __builtin_memcpy(v, own + (j * 8 + tile.eighth) * Product::kPitch + c,
-                                         sizeof v);
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < E; ++u)
-                            v[u] = 0.0f;
-                    }
-                    if (!BACK && a.base)
-                        add_base<W>(a, v, b[j]);
-                    if (tile.there[j])
-                        store_row<W>(a.out + tile.row[j] * a.out_stride + (int64_t)(m0 + c) * S, v,
-                                     a.m - m0 - c);
+            for (int u = 0; u < U; ++u) {
+                const int32_t mu = m0 + u * kUnit;
+                if (mu >= to)
+                    break;
+                if (adapted) {
+                    const Product second = {weights[turn], pitch, a.rank, tile.col, tile.quad};
+                    second.unit(u * kUnit, terms[0], factor[0], own, Product::kPitch);
                 }
-            rows::wave_sync();
+                rows::wave_sync();
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int q = 0; q < (BACK ? 2 : 1); ++q) {
+                        const int c = (tile.piece + q * 8) * E;
+                        float v[E];
+                        if (adapted) {
+                            __builtin_memcpy(v, own + (j * 8 + tile.eighth) * Product::kPitch + c,
+                                             sizeof v);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < E; ++i)
+                                v[i] = 0.0f;
+                        }
+                        if (!BACK && a.base)
+                            add_base<W>(a, v, b[u][j]);
+                        if (tile.there[j])
+                            store_row<W>(a.out + tile.row[j] * a.out_stride +
+                                         (int64_t)(mu + c) * S, v, a.m - mu - c);
+                    }
+                rows::wave_sync();
+            }
         }
         if (next < to) {
             put_weights(next, weights[turn ^ 1]);
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-                b[j] = b_next[j];
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    b[u][j] = b_next[u][j];
         }
     }
 }
@@ -1151,24 +1191,31 @@ __global__ __launch_bounds__(kGradWaves * kWave) void k_grads(GradArgs a)
     const Piece4 p = a.chunks[chunk];
     if (p.group < 0 || p.group >= a.groups)
         return;
-    const int32_t c0 = block * 16 * E, at = c0 + col * E, left = max(j.cols - at, 0);
+    const int32_t c0 = block * 16 * E, at = c0 + col * E, left = j.cols - at;
     const bool whole_block = c0 + 16 * E <= j.cols;
     f32x4 sum[CT][E];
     clear(sum);
-    const char *y = j.y + (left > 0 ? (int64_t)at * S : 0);
+    const char *y = j.y + (int64_t)at * S;
     const int32_t *order = a.order + p.first;
-    for (int32_t s = wave * kStep; s < p.count; s += NW * kStep) {
-        const bool whole_step = s + kStep <= p.count;
-        Frag f[kRows];
-        float hv[CT][kRows];
-        int32_t row[kRows];
-        if (whole_step) {
+    const auto rows_of = [&](int32_t s, int32_t (&row)[kRows]) __attribute__((always_inline)) {
+        if (s + kStep <= p.count) {
             __builtin_memcpy(row, order + s + quad * kRows, sizeof row);
         } else {
 #pragma unroll
             for (int u = 0; u < kRows; ++u)
                 row[u] = order[min(s + quad * kRows + u, p.count - 1)];
         }
+    };
+    int32_t next[kRows];
+    rows_of(wave * kStep, next);
+    for (int32_t s = wave * kStep; s < p.count; s += NW * kStep) {
+        const bool whole_step = s + kStep <= p.count;
+        Frag f[kRows];
+        float hv[CT][kRows];
+        int32_t row[kRows];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+            row[u] = next[u];
         if (whole_block) {
 #pragma unroll
             for (int u = 0; u < kRows; ++u)
@@ -1176,7 +1223,7 @@ __global__ __launch_bounds__(kGradWaves * kWave) void k_grads(GradArgs a)
         } else {
 #pragma unroll
             for (int u = 0; u < kRows; ++u)
-                f[u] = load_frag<W>(y + row[u] * j.y_stride, left);
+                f[u] = load_frag<W>(y + row[u] * j.y_stride, left, j.cols);
         }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
@@ -1185,6 +1232,7 @@ __global__ __launch_bounds__(kGradWaves * kWave) void k_grads(GradArgs a)
             for (int u = 0; u < kRows; ++u)
                 hv[ct][u] = j.h[(int64_t)row[u] * a.rank + r];
         }
+        rows_of(s + NW * kStep, next);                    // the next step's, meanwhile
         if (!whole_step)                                  // rows past the chunk's last
 #pragma unroll
             for (int u = 0; u < kRows; ++u)
@@ -1277,6 +1325,10 @@ __global__ __launch_bounds__(kGradWaves * kWave) void k_grads(GradArgs a)
             continue;
         if (!done) {
             float *to = j.partial + ((int64_t)p.slot * a.rank + r) * j.cols + at;
+            if (left >= E) {
+                __builtin_memcpy(to, v, sizeof v);
+                continue;
+            }
 #pragma unroll
             for (int t = 0; t < E; ++t)
                 if (t < left)
