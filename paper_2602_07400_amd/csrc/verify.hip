@@ -323,14 +323,14 @@ __device__ __forceinline__ bool surely_rejected(const VerifyArgs &a, int64_t r, 
         return true;
     if (inverse_p == 0.0)
         return t != p.first;
-    const auto log2_share = [&](const Side &of, const Stat &s,
-                                double inverse) __attribute__((always_inline)) {
-        const float x = (float)(below(value_at(of.row(r, i), of.type, t), s.m) * inverse);
-        return x * kLog2e - __builtin_amdgcn_logf((float)s.s);
-    };
-    float log_ratio = log2_share(a.target, p, inverse_p);
-    if (has_row(a, inverse_q))
-        log_ratio -= log2_share(a.draft, q, inverse_q);
+    // (exponents of 10^5 cancel: their difference comes before its rounding)
+    double e = below(value_at(a.target.row(r, i), a.target.type, t), p.m) * inverse_p;
+    float sums = -__builtin_amdgcn_logf((float)p.s);
+    if (has_row(a, inverse_q)) {
+        e -= below(value_at(a.draft.row(r, i), a.draft.type, t), q.m) * inverse_q;
+        sums += __builtin_amdgcn_logf((float)q.s);
+    }
+    const float log_ratio = (float)e * kLog2e + sums;
     // (a NaN, of two masked logits, is not sure)
     return a.uniform[at] > __builtin_amdgcn_exp2f(log_ratio) * 1.001f + 1e-30f;
 }

@@ -342,3 +342,22 @@ def test_streams_and_graphs(r, c):
             torch.cuda.synchronize()
             case.check(out)
             other.run(workspace=workspace)
+
+
+def test_shares_far_below_the_largest():
+    """Drafts whose shares are e^-100000 in both rows: their exponents cancel, and what 32 bits
+    would leave of the difference must not reject a draft and have the rows behind it left out."""
+    rng = np.random.default_rng(12)
+    r, d, c, t = 300, 2, 5003, 0.01
+    x, y = np.zeros((r, d + 1, c), np.float32), np.zeros((r, d, c), np.float32)
+    drafted = rng.integers(1, c, (r, d)).astype(np.int32)
+    at = np.arange(r)[:, None], np.arange(d)[None], drafted
+    x[at] = -rng.uniform(900, 1100, (r, d))
+    y[at] = x[at] + rng.uniform(0, 0.02, (r, d)).astype(np.float32)
+    # the sums are the same classes in both rows: p / q = e^((x - y) / T)
+    ratio = np.exp((x[at].astype(np.float64) - y[at]) / float(np.float32(t)))
+    uniform = (ratio * 0.9995).astype(np.float32)
+    dev = lambda a: torch.from_numpy(a).to(DEV)           # noqa: E731
+    accepted, token, _ = bl.bitlogic_verify(dev(x), dev(drafted), dev(y), dev(uniform),
+                                            _gumbel(rng, r, c).to(DEV), temperature=t)
+    assert (accepted == d).all() and ((token >= 0) & (token < c)).all()
