@@ -625,7 +625,7 @@ int bitlogic_group_rows(const int32_t *ids, int64_t n_rows, int32_t n_groups, vo
  *   x       [n_rows][n_in] of the weights' type or, with float32 weights, int32 counts;
  *           x_stride >= 0 elements from row to row
  *   ids     int32 [n_rows], read where plan is NULL: each row by itself then, which suits
- *           few rows (at most 2^20)
+ *           few rows (at most 2^20; rows times columns past a launch's 2^32 lanes are refused)
  *   plan    of n_rows ids and n_adapters groups, or NULL.  A plan of other sizes, or one that
  *           bitlogic_group_rows did not write, is the caller's error, which is not detected
  *   base    [n_rows][n_out] of the weights' type or, with float32 weights, int32 logits

@@ -152,6 +152,22 @@ inline PassLayout pass_layout(int64_t n_rows, int32_t groups, int32_t rank, int3
     return l;
 }
 
+// Blocks of a tile in the second product of wide adapters: about 1024 in all, with at most eight
+// units of columns each (128 bytes, back 256).
+inline int32_t expand_blocks(const PassArgs &a, int32_t el_bytes, bool back)
+{
+    const int64_t unit = back ? 256 : 128;
+    const int64_t units = a.out ? ((int64_t)a.m * el_bytes + unit - 1) / unit : 1;
+    return (int32_t)std::min<int64_t>(units,
+                                      std::max<int64_t>((units + 7) / 8, 1024 / a.n_tiles));
+}
+
+// Whether each launch of a pass stays below 2^32 lanes.
+inline bool fits_launches(const PassArgs &a, int32_t el_bytes, bool back)
+{
+    return a.n_tiles * std::max(expand_blocks(a, el_bytes, back), 4 * a.splits) < 1 << 24;
+}
+
 // Gradients: d down [groups][rank][n_in] = sum scale back x^T, d up [groups][n_out][rank] =
 // sum scale grad hidden^T, over a group's rows.
 struct GradJob {

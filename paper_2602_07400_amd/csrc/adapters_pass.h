@@ -1144,11 +1144,8 @@ hipError_t pass_of(const PassArgs &a, hipStream_t stream)
         return err;
     if (!a.out && a.hidden == a.partial)
         return hipSuccess;
-    // about 1024 blocks, with at most eight units each
-    constexpr int kCols = Second<W, CT, BACK>::kCols;
-    const int64_t units = a.out ? (a.m + kCols - 1) / kCols : 1;
-    const int32_t blocks = (int32_t)std::min<int64_t>(
-        units, std::max<int64_t>((units + 7) / 8, 1024 / a.n_tiles));
+    static_assert(Second<W, CT, BACK>::kCols * kSize<W> == (BACK ? 256 : 128), "expand_blocks()");
+    const int32_t blocks = expand_blocks(a, kSize<W>, BACK);
     hipLaunchKernelGGL((k_expand<W, CT, BACK>), dim3((uint32_t)(a.n_tiles * blocks)),
                        dim3(kTileWaves * kWave), 0, stream, a, blocks);
     return hipGetLastError();

@@ -415,6 +415,9 @@ int take_parts(const char *who, bl::adapt::PassArgs &a, int32_t type, bool back,
 {
     const auto l = layout_of(type, a.n_rows, a.groups, a.rank, a.k, a.m, a.tiles != nullptr, back);
     a.splits = l.splits;
+    if (!bl::adapt::fits_launches(a, (int32_t)logit_bytes(type), back))
+        return fail(BITLOGIC_ERR_UNSUPPORTED, "%s: rows (or adapters) times columns too large for "
+                    "one launch", who);
     if (l.splits == 1 && a.hidden) {
         a.partial = a.hidden;
         return BITLOGIC_OK;

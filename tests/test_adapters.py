@@ -171,3 +171,11 @@ def test_oracle_gradients_are_the_slopes():
             low = value()
             leaf[at] = kept
             assert abs(high - low - grad[at]) < 1e-12 * (1 + abs(high) + abs(low))
+
+
+def test_launches_past_2_32_lanes_are_refused(lib):
+    """A row without a plan is a tile of its own: 2^20 of them by 256 blocks of columns."""
+    wide = dict(rows=1 << 20, stride=10, n_out=1 << 18, base=None, out=1 << 45,
+                out_stride=1 << 18)
+    assert _forward(lib, plan=None, **wide) == EUNSUP
+    assert b"one launch" in lib.bitlogic_last_error()
