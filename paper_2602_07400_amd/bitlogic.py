@@ -1029,7 +1029,9 @@ def bitlogic_dropout(x: torch.Tensor, p: float, seed: int, offset=0,
 
 MAX_ADAPTERS, MAX_RANK = 4096, 128    # BITLOGIC_MAX_ADAPTERS, BITLOGIC_MAX_RANK
 # Up to as many rows go through adapters without a plan: a row reads its adapter by itself
-_LONE_ROWS = 16
+# (4096 -> 4096, rank 16: 15 us, 21 with a plan; 1024 -> 8192, rank 64, float32: 32 rows 26 and 27,
+# 64 rows 47 and 29)
+_LONE_ROWS = 32
 
 
 @dataclass

@@ -660,8 +660,9 @@ __device__ __forceinline__ void redo(Group<G> &g, const VerifyArgs &a, int64_t r
 // ---- short rows: a wave a request ----
 // Rows of up to kManyRows classes: 16 lanes a row, the rows of 32 drafts together, since a wait
 // for memory costs more than rows behind a rejection.  Longer ones: a draft's rows at a time.
+// (1024 requests of 1024 classes 22 us and 29, of 2048 35 and 37, of 4096 57 and 54.)
 constexpr int kShortBlock = 256;
-constexpr int32_t kManyRows = 512;
+constexpr int32_t kManyRows = 2048;
 
 template <int G>
 __global__ __launch_bounds__(kShortBlock, 4) void k_verify_short(VerifyArgs a)
@@ -844,28 +845,47 @@ __global__ __launch_bounds__(kDrawBlock, 4) void k_verify_draw(VerifyArgs a)
 
 // The parts of a request's draw joined, by a wave.  (A last block that joins them instead needs
 // fences between the dies' L2s, one a block: 192 x 131072, 16 blocks a request, 195 us, without 74.)
-__global__ __launch_bounds__(kWave) void k_verify_pick(VerifyArgs a)
+// A whole block, for what 32 bits left open: 64 lanes took 4 ms more for a row of 131072.
+constexpr int kPickBlock = 1024;
+
+__global__ __launch_bounds__(kPickBlock) void k_verify_pick(VerifyArgs a)
 {
-    Group<kWave> g(threadIdx.x, nullptr);
+    __shared__ Scratch scratch;
+    __shared__ int32_t picked;
+    Group<kPickBlock> g(threadIdx.x, &scratch);
     for (int64_t r = blockIdx.x; r < a.n_requests; r += gridDim.x) {
-        const Walk w = a.walks[r];
-        const double inverse_p = a.target.inverse_of(r);
-        int32_t token = w.j == kLeftOpen ? kLeftOpen : w.p.m == -kInf ? -1 : w.p.first;
-        if (token >= 0 && inverse_p > 0.0) {
-            Best best = nothing();
-            for (int32_t k = g.t; k < a.draw_parts; k += kWave)
-                merge(best, a.bests[r * a.draw_parts + k]);
-            token = settle(w.less, join(g, best));
+        if (threadIdx.x < kWave) {
+            Group<kWave> wave(threadIdx.x, nullptr);
+            const Walk w = a.walks[r];
+            const double inverse_p = a.target.inverse_of(r);
+            int32_t token = w.j == kLeftOpen ? kLeftOpen : w.p.m == -kInf ? -1 : w.p.first;
+            if (token >= 0 && inverse_p > 0.0) {
+                Best best = nothing();
+                for (int32_t k = wave.t; k < a.draw_parts; k += kWave)
+                    merge(best, a.bests[r * a.draw_parts + k]);
+                token = settle(w.less, join(wave, best));
+            }
+            if (threadIdx.x == 0) {
+                picked = token;
+                if (token != kLeftOpen)
+                    answer(a, r, w.j, token, inverse_p, w.p);
+            }
         }
-        if (token == kLeftOpen)
+        __syncthreads();
+        const bool open = picked == kLeftOpen;
+        __syncthreads();                                  // (the next request writes it)
+        if (open)
             redo(g, a, r);
-        else if (g.t == 0)
-            answer(a, r, w.j, token, inverse_p, w.p);
     }
 }
 
 // ---- which form, and its workspace ----
-constexpr int32_t kShortClasses = 4096;
+// A wave a request: always up to kShortClasses, and up to kMostShort where requests are enough to
+// fill the card; else k_verify_rows and what follows (us, 4 drafts of bfloat16, 1 / 64 / 1024
+// requests: 1024 classes 15 / 19 / 22 and 22 / 22 / 101; 4096 29 / 44 / 54 and 22 / 23 / 107; 8192
+// 54 / 71 / 86 and 21 / 26 / 121).  Above 4096 what a wave alone may have to redo in 64 bits (500 us
+// for 8192 classes, in about one call of 25 with 1024 requests) costs what is won.
+constexpr int32_t kShortClasses = 1024, kMostShort = 4096;
 constexpr int kWholeBlock = 1024;
 
 struct Plan {
@@ -888,11 +908,14 @@ void split(int64_t rows, int32_t n, int64_t want, int32_t unit, int32_t &parts, 
 Plan plan_of(int64_t n_requests, int32_t drafts, int32_t n)
 {
     Plan p = {};
-    p.is_short = n <= kShortClasses;
+    p.is_short = n <= kShortClasses || (n <= kMostShort && n_requests >= n / 16 + 192);
     if (p.is_short || n_requests == 0)
         return p;
     const int64_t rows = n_requests * (drafts + 1);
-    p.whole = rows >= 512;
+    // A block of 1024 a row, which skips rows behind a rejection, or blocks of 256 (us, all
+    // kernels): 2000 rows of 8192 59 and 39, 5000 87 and 85; 1000 of 65536 94 and 90, 2000 163
+    // and 166; 1152 of 131072, four drafts in five standing, 160 and 182.
+    p.whole = rows >= 1024 && rows * n >= 1 << 26;
     split(rows, n, p.whole ? 1 : 1024, 4096, p.parts, p.part);
     // (192 rows of 131072, all kernels: 169 us at 1024 blocks, 158 at 2048, 154 at 4096; one
     // row: 23.8, 24.3 and 25.1)
@@ -974,7 +997,7 @@ hipError_t launch_verify(const VerifySide &target, const VerifySide &draft, int6
                        stream, a);
     if (hipError_t err = hipGetLastError(); err != hipSuccess)
         return err;
-    hipLaunchKernelGGL(k_verify_pick, grid(n_requests), dim3(kWave), 0, stream, a);
+    hipLaunchKernelGGL(k_verify_pick, grid(n_requests), dim3(kPickBlock), 0, stream, a);
     return hipGetLastError();
 }
 
