@@ -344,11 +344,12 @@ def test_streams_and_graphs(r, c):
             other.run(workspace=workspace)
 
 
-def test_shares_far_below_the_largest():
+@pytest.mark.parametrize("r,d,c", [(300, 2, 5003), (350, 2, 64001)])
+def test_shares_far_below_the_largest(r, d, c):
     """Drafts whose shares are e^-100000 in both rows: their exponents cancel, and what 32 bits
     would leave of the difference must not reject a draft and have the rows behind it left out."""
     rng = np.random.default_rng(12)
-    r, d, c, t = 300, 2, 5003, 0.01
+    t = 0.01
     x, y = np.zeros((r, d + 1, c), np.float32), np.zeros((r, d, c), np.float32)
     drafted = rng.integers(1, c, (r, d)).astype(np.int32)
     at = np.arange(r)[:, None], np.arange(d)[None], drafted
@@ -361,3 +362,25 @@ def test_shares_far_below_the_largest():
     accepted, token, _ = bl.bitlogic_verify(dev(x), dev(drafted), dev(y), dev(uniform),
                                             _gumbel(rng, r, c).to(DEV), temperature=t)
     assert (accepted == d).all() and ((token >= 0) & (token < c)).all()
+
+
+@pytest.mark.parametrize("near", [0.3, 2.0])
+@pytest.mark.parametrize("r,d,c", [(330, 3, 1500), (460, 2, 4000), (460, 2, 4096), (256, 3, 8193),
+                                   (350, 2, 64001)])
+def test_many_requests(r, d, c, near):
+    """Requests enough for a wave each, or a block a row; drafts that stand and that do not."""
+    rng = _rng(13, r, c, 10 * near)
+    lengths = torch.from_numpy(rng.integers(0, d + 1, r).astype(np.int32))
+    case = Case(rng, r, d, c, torch.bfloat16, torch.bfloat16, lengths=lengths, near=near)
+    # rows of masks, masked drafts, requests without randomness
+    case.x[5, 0] = float("-inf")
+    case.y[6, 0] = float("-inf")
+    case.x[torch.arange(7, 30), 0, case.drafted[7:30, 0].long()] = float("-inf")
+    case.t = torch.from_numpy(np.where(np.arange(r) % 9 == 4, 0, 0.8).astype(np.float32))
+    want = case.check()
+    assert len({w[0] for w in want}) > 1
+
+
+@pytest.mark.parametrize("c,r", [(1500, 330), (4000, 460)])
+def test_many_numbers_next_to_a_border(c, r):
+    test_numbers_next_to_a_border(c, r)
