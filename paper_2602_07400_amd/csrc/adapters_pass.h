@@ -1349,34 +1349,35 @@ __global__ __launch_bounds__(kGradWaves * kWave) void k_grads(GradArgs a)
 }
 
 // Gradients of groups with no rows (zero) and of those with several chunks, whose parts are
-// added in order.
+// added in order; those of down and of up by blocks of their own.
 template <int W>
 __global__ __launch_bounds__(256) void k_join_grads(GradArgs a, int32_t per_group)
 {
-    const int32_t g = (int32_t)(blockIdx.x / per_group);
-    if (a.chunk_starts && a.chunk_starts[g + 1] - a.chunk_starts[g] == 1)
+    const int32_t k = (int32_t)(blockIdx.x / ((uint32_t)a.groups * per_group));
+    const int32_t block = (int32_t)(blockIdx.x - (uint32_t)k * a.groups * per_group);
+    const int32_t g = block / per_group;
+    const GradJob &j = a.job[k];
+    if (!j.out || (a.chunk_starts && a.chunk_starts[g + 1] - a.chunk_starts[g] == 1))
         return;
     const int32_t first = a.chunk_starts ? a.slot_starts[g] : 0,
                   last = a.chunk_starts ? a.slot_starts[g + 1] : 0;
     const float scale = a.scales ? a.scales[g] : a.scale;
-    for (int k = 0; k < 2; ++k) {
-        const GradJob &j = a.job[k];
-        if (!j.out)
-            continue;
-        const int64_t all = (int64_t)a.rank * j.cols;
-        for (int64_t e = (int64_t)(blockIdx.x - g * per_group) * 256 + threadIdx.x; e < all;
-             e += (int64_t)per_group * 256) {
-            float v = 0.0f;
+    const int64_t all = (int64_t)a.rank * j.cols;
+    for (int64_t e = (int64_t)(block - g * per_group) * 256 + threadIdx.x; e < all;
+         e += (int64_t)per_group * 256) {
+        float v = 0.0f;
 #pragma unroll 8
-            for (int32_t c = first; c < last; ++c)
-                v += j.partial[c * all + e];
+        for (int32_t c = first; c < last; ++c)
+            v += j.partial[c * all + e];
+        int64_t to = g * all + e;
+        if (j.transposed) {
             const int64_t r = e / j.cols, at = e - r * j.cols;
-            const int64_t to = g * all + (j.transposed ? at * a.rank + r : e);
-            if constexpr (kSize<W> == 4)
-                reinterpret_cast<uint32_t *>(j.out)[to] = el_bits<W>(scale * v);
-            else
-                reinterpret_cast<uint16_t *>(j.out)[to] = (uint16_t)el_bits<W>(scale * v);
+            to = g * all + at * a.rank + r;
         }
+        if constexpr (kSize<W> == 4)
+            reinterpret_cast<uint32_t *>(j.out)[to] = el_bits<W>(scale * v);
+        else
+            reinterpret_cast<uint16_t *>(j.out)[to] = (uint16_t)el_bits<W>(scale * v);
     }
 }
 
@@ -1392,7 +1393,7 @@ hipError_t grads_of(const GradArgs &a, hipStream_t stream)
     const int64_t els = (int64_t)a.rank * std::max(a.job[0].out ? a.job[0].cols : 0,
                                                    a.job[1].out ? a.job[1].cols : 0);
     const int32_t per_group = (int32_t)std::min<int64_t>(1024, (els + 255) / 256);
-    hipLaunchKernelGGL(k_join_grads<W>, dim3((uint32_t)((int64_t)a.groups * per_group)),
+    hipLaunchKernelGGL(k_join_grads<W>, dim3((uint32_t)(2 * (int64_t)a.groups * per_group)),
                        dim3(256), 0, stream, a, per_group);
     return hipGetLastError();
 }
