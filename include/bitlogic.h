@@ -543,7 +543,8 @@ int bitlogic_sample(const void *logits, int32_t type, int64_t n_rows, int32_t n_
  *   temperature, draft_temperature  of all requests or, where the array [n_requests]
  *                 (device memory) is not NULL, of each.  T <= 0: greedy, p_i is one at the
  *                 first class of the row's order, and uniform and noise are not read;
- *                 T_draft <= 0: q_i is one at t_i, and the draft's row is not read
+ *                 T_draft <= 0: q_i is one at t_i, and the draft's row is not read.  NaNs in an
+ *                 array are <= 0; values in (0, 2^-126) and above 2^120 count as those bounds
  *   accepted      int32 [n_requests]: drafts that stand
  *   token         int32 [n_requests]: the class after them; -1 where the target's row is
  *                 masked altogether

@@ -678,6 +678,9 @@ __device__ __forceinline__ void load_four(const char *p, int left, uint32_t (&v)
 }
 
 // ---- narrow adapters: 16 rows a wave, whole rows at a time ----
+// (2^18 rows of 100 int32 counts and logits in the order of 24 adapters, rank 8: 93 us for 316 MB;
+// a block's loads, products and stores take turns, and LDS and registers leave room for four.
+// Loads that pass by the L1: 85 us, 109 without, inputs warm.)
 // A block has a tile, and its adapter in LDS.  A wave copies its 16 rows of x there, and holds
 // those of base in registers meanwhile, by 16-byte pieces in the order of memory: of the lines at
 // the ends of rows, none is asked for twice.
@@ -896,10 +899,17 @@ __global__ __launch_bounds__(kTileWaves * kWave, CT <= 2 ? 4 : 2) void k_narrow(
 // ---- wide adapters ----
 // waves that share a block's terms: as many as a rank's weights leave LDS for
 template <int CT> constexpr int kTermWaves = CT <= 2 ? 8 : 4;
-// waves a SIMD to compile for
+// waves a SIMD to compile for; k_expand's: what its LDS leaves room for
 template <int CT> constexpr int kWavesPerSimd = CT <= 2 ? 4 : CT == 4 ? 3 : 2;
+template <int W, int CT, bool BACK>
+constexpr int kExpandWaves = !BACK || (kSize<W> == 4 && CT < 8) ? kWavesPerSimd<CT>
+                             : CT <= 2 ? 3 : CT == 4 ? 2 : 1;
 
 // Part `blockIdx % splits` of the h of 32 rows of a tile, to [part][row][rank].
+//
+// Bound by the memory's answers to 128-byte pieces of many rows: 20 us for 50 MB (12289 x 2048
+// bfloat16, rank 24), 47 us for 123 MB of odd rows (back; the loads alone take 26).  64 rows a wave,
+// loads two units ahead and other numbers of blocks were within 3% or slower.
 template <int W, int X, int CT, int RT, bool BACK>
 __global__ __launch_bounds__(kTermWaves<CT> * kWave, kWavesPerSimd<CT>) void k_shrink(PassArgs a)
 {
@@ -962,11 +972,17 @@ __global__ __launch_bounds__(kTermWaves<CT> * kWave, kWavesPerSimd<CT>) void k_s
 
 // Units of columns of a tile, 16 rows a wave; a unit's weights are in LDS for all of them, the
 // next unit's on their way.
+//
+// Bound by memory in this pattern: 71 us for 246 MB (12289 x 5003 bfloat16, rank 24) and 46 us for
+// 134 MB (8192 x 4096 float16, rank 64), where loads and stores alone take 75 and 35 us (by units)
+// and a copy of whole rows 48 and 26.
+// Units at a time: two where their registers leave four waves a SIMD (12289 rows, 5003 columns,
+// rank 24: 71 us, by one 87; rank 64, 8192 rows of 4096: 58 us, by one 49).
 template <int CT, bool BACK> constexpr int kUnits = BACK || CT > 2 ? 1 : 2;
 
 template <int W, int CT, bool BACK>
-__global__ __launch_bounds__(kTileWaves * kWave, kWavesPerSimd<CT>) void k_expand(PassArgs a,
-                                                                                int32_t blocks)
+__global__ __launch_bounds__(kTileWaves * kWave, (kExpandWaves<W, CT, BACK>))
+void k_expand(PassArgs a, int32_t blocks)
 {
     typedef Second<W, CT, BACK> Product;
     constexpr int E = kEls<W>, S = kSize<W>, kUnit = Product::kCols, J = 2, U = kUnits<CT, BACK>;
@@ -1169,6 +1185,10 @@ hipError_t pass_by_rank(const PassArgs &a, hipStream_t stream)
 // 8 (4) rows and turns them by byte permutes into the terms of E products, whose columns are
 // t, E + t, ...  h is taken as the sum of two bfloat16 as above, float16 y too, since h may be
 // past float16's range and its rows are summed here, so that they have no scale of their own.
+//
+// Bound by the waves' chains of loads: 50 us for 173 MB (12289 rows of 2048 and 5003 bfloat16 columns,
+// rank 24), 58 without the next step's row numbers ahead and with odd rows' ends element by
+// element; h through LDS instead 69.
 constexpr int kGradWaves = 4;
 
 template <int W, int CT>

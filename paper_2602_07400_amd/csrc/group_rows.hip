@@ -9,7 +9,7 @@
 //
 // What bounds it: chains of loads and LDS accesses, and fetching code that runs once: with 16
 // steps of a wave unrolled, one block took 29 us for 12289 rows, in a loop 21.  2^18 rows of 24
-// groups: 5, 11 and 9 us.
+// groups: 5, 8 and 9 us.
 #include "adapters.h"
 
 namespace bl {
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(kRunThreads) void k_group_count(GroupArgs a)
         a.counts[(int64_t)g * a.runs + blockIdx.x] = lds[g];
 }
 
-constexpr int kSumWaves = 16;
+constexpr int kSumWaves = 16, kAhead = 4;                 // runs by the wave, loaded together
 __global__ __launch_bounds__(kWave * kSumWaves) void k_group_sum(GroupArgs a)
 {
     extern __shared__ uint32_t totals[];
@@ -281,20 +281,29 @@ __global__ __launch_bounds__(kWave * kSumWaves) void k_group_sum(GroupArgs a)
 #pragma unroll 1
     for (int32_t g = wave; g < all; g += kSumWaves) {     // a wave sums up a group's runs
         uint32_t base = 0;
-#pragma unroll 4
-        for (int32_t r0 = 0; r0 < a.runs; r0 += kWave) {
-            const int32_t r = r0 + lane;
-            uint32_t *at = a.counts + (int64_t)g * a.runs + r;
-            const uint32_t own = r < a.runs ? *at : 0;
-            uint32_t in = own;
+        uint32_t *counts = a.counts + (int64_t)g * a.runs;
 #pragma unroll 1
-            for (int d = 1; d < kWave; d *= 2) {
-                const uint32_t o = __shfl_up(in, d);
-                in += lane >= d ? o : 0;
+        for (int32_t r0 = 0; r0 < a.runs; r0 += kAhead * kWave) {
+            uint32_t own[kAhead], in[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int32_t r = r0 + k * kWave + lane;
+                in[k] = own[k] = r < a.runs ? counts[r] : 0;
             }
-            if (r < a.runs)
-                *at = base + in - own;
-            base += __shfl(in, kWave - 1);
+#pragma unroll 1
+            for (int d = 1; d < kWave; d *= 2)
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const uint32_t o = __shfl_up(in[k], d);
+                    in[k] += lane >= d ? o : 0;
+                }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int32_t r = r0 + k * kWave + lane;
+                if (r < a.runs)
+                    counts[r] = base + in[k] - own[k];
+                base += __shfl(in[k], kWave - 1);
+            }
         }
         if (lane == 0)
             totals[g] = base;
