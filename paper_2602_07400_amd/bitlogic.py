@@ -1226,7 +1226,9 @@ def bitlogic_adapt(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
                    base: Optional[torch.Tensor] = None, base_scale: float = 1.0,
                    plan: Optional[RowGroups] = None) -> torch.Tensor:
     """bitlogic_adapters' out as a differentiable function of x, down, up and base (scales
-    have no gradient).  Both passes run on the current stream."""
+    have no gradient).  Both passes run on the current stream.  For a training step in a
+    captured graph call bitlogic_adapters and bitlogic_adapters_backward: autograd ends the
+    process where a backward pass is captured while an eager graph of the same leaves lives."""
     return _Adapt.apply(x, down, up, base, ids, scales, base_scale, plan)
 
 
