@@ -456,3 +456,52 @@ def test_more_rows_than_a_run_a_wave():
         want_d = scales[a].double() * back[a] * rows.sum(0)
         size = float((scales[a].double() * back[a].abs() * rows.abs().sum(0)).max())
         assert ((grads[1][a].double() - want_d).abs() <= size * 2.0 ** -24 * 8192).all()
+
+
+def _far(n, c, dtype, step):
+    """Rows [n][c], `step` elements apart, in memory that holds anything between them."""
+    return torch.empty((n - 1) * step + c, dtype=dtype, device=DEV).as_strided((n, c), (step, 1))
+
+
+@pytest.mark.parametrize("f,c,rank", [(100, 120, 8), (301, 403, 24)])
+def test_rows_past_32_bit_offsets(f, c, rank):
+    """Rows 2^26 elements apart, narrow and wide, both passes: the same as of rows together."""
+    rng = np.random.default_rng(f)
+    n, g, dtype, step = 70, 3, torch.bfloat16, 1 << 26    # 9.4 GB a tensor
+    of = lambda *s: torch.from_numpy(rng.normal(0, 0.3, s).astype(np.float32)).to(DEV, dtype)  # noqa: E731,E501
+    x, base, grad, down, up = of(n, f), of(n, c), of(n, c), of(g, rank, f), of(g, c, rank)
+    ids = torch.from_numpy(rng.integers(-1, g, n).astype(np.int32)).to(DEV)
+    plan = bl.bitlogic_group_rows(ids, g)
+    want, hidden = bl.bitlogic_adapters(x, down, up, ids, 0.5, base, 1.0, plan, want_hidden=True)
+    want_grads = bl.bitlogic_adapters_backward(grad, x, hidden, down, up, ids, 0.5, plan)
+    far_x, far_out, far_grad = (_far(n, t.shape[1], dtype, step) for t in (x, base, grad))
+    for far, near in ((far_x, x), (far_out, base), (far_grad, grad)):
+        far.copy_(near)
+    got, far_hidden = bl.bitlogic_adapters(far_x, down, up, ids, 0.5, far_out, 1.0, plan,
+                                           out=far_out, want_hidden=True)
+    assert torch.equal(got, want) and torch.equal(far_hidden, hidden)
+    grads = bl.bitlogic_adapters_backward(far_grad, far_x, far_hidden, down, up, ids, 0.5, plan,
+                                          grad_x=_far(n, f, dtype, step))
+    for a, b in zip(grads, want_grads):
+        assert torch.equal(a, b)
+
+
+def test_adapters_past_32_bit_offsets():
+    """The last of nine adapters of 512 MB each."""
+    rng = np.random.default_rng(8)
+    g, rank, f, c = 9, 128, 1 << 20, 10
+    down = torch.zeros(g, rank, f, device=DEV)
+    at = torch.from_numpy(np.sort(rng.choice(f, 5, replace=False))).to(DEV)
+    down[8, :, at] = torch.from_numpy(rng.normal(size=(rank, 5)).astype(np.float32)).to(DEV)
+    up = torch.from_numpy(rng.normal(size=(g, c, rank)).astype(np.float32)).to(DEV)
+    x = torch.zeros(40, f, device=DEV)
+    x[:, at] = torch.from_numpy(rng.normal(size=(40, 5)).astype(np.float32)).to(DEV)
+    ids = torch.full((40,), 8, dtype=torch.int32, device=DEV)
+    d5, x5, u = (t.double().cpu() for t in (down[8][:, at], x[:, at], up[8]))
+    want = x5 @ d5.t() @ u.t()
+    size = x5.abs() @ d5.abs().t() @ u.abs().t()
+    for plan in (bl.bitlogic_group_rows(ids, g), None):
+        rows = slice(None) if plan else slice(0, 20)
+        got, _ = bl.bitlogic_adapters(x[rows], down, up, ids[rows], 1.0, plan=plan)
+        # five terms that are not zero, then 128: a rounding each, in 32 bits
+        assert ((got.double().cpu() - want[rows]).abs() <= 140 * 2.0 ** -24 * size[rows]).all()

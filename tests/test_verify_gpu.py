@@ -384,3 +384,22 @@ def test_many_requests(r, d, c, near):
 @pytest.mark.parametrize("c,r", [(1500, 330), (4000, 460)])
 def test_many_numbers_next_to_a_border(c, r):
     test_numbers_next_to_a_border(c, r)
+
+
+@pytest.mark.parametrize("c", [100, 5003])
+def test_requests_past_32_bit_offsets(c):
+    """Requests 2^30 elements apart, on both sides, and numbers 2^28: as of requests together."""
+    rng = _rng(14, c)
+    r, d = 5, 2
+    case = Case(rng, r, d, c, torch.bfloat16, torch.bfloat16)
+
+    def far(t, step):                                     # up to 8.6 GB a tensor
+        size = (r - 1) * step + t[0].numel()
+        strides = (step, c, 1) if t.dim() == 3 else (step, 1)
+        out = torch.empty(size, dtype=t.dtype, device=DEV).as_strided(t.shape, strides)
+        return out.copy_(t)
+
+    got = bl.bitlogic_verify(far(case.x, 1 << 30), case.drafted.to(DEV), far(case.y, 1 << 30),
+                             case.uniform.to(DEV), far(case.noise, 1 << 28),
+                             temperature=case.t, draft_temperature=case.tq)
+    case.check(got)
