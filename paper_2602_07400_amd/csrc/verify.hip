@@ -312,7 +312,9 @@ __device__ __forceinline__ int decide(const VerifyArgs &a, int64_t r, int32_t i,
     return u < ratio ? kAccepted : kRejected;
 }
 
-// Whether decide() will certainly reject, in 32 bits with a thousandth to spare.
+// Whether decide() will certainly reject, in 32 bits with a thousandth to spare.  Never where the
+// drafter's row has no mass at the draft: p / q is infinite then, while of a row without any (its
+// largest -inf, its sum zero) the steps below would make zero.
 __device__ __forceinline__ bool surely_rejected(const VerifyArgs &a, int64_t r, int32_t i,
                                                 double inverse_p, double inverse_q, const Stat &p,
                                                 const Stat &q)
@@ -327,11 +329,14 @@ __device__ __forceinline__ bool surely_rejected(const VerifyArgs &a, int64_t r, 
     double e = below(value_at(a.target.row(r, i), a.target.type, t), p.m) * inverse_p;
     float sums = -__builtin_amdgcn_logf((float)p.s);
     if (has_row(a, inverse_q)) {
-        e -= below(value_at(a.draft.row(r, i), a.draft.type, t), q.m) * inverse_q;
+        const double v = value_at(a.draft.row(r, i), a.draft.type, t);
+        if (v == -kInf)
+            return false;
+        e -= below(v, q.m) * inverse_q;
         sums += __builtin_amdgcn_logf((float)q.s);
     }
     const float log_ratio = (float)e * kLog2e + sums;
-    // (a NaN, of two masked logits, is not sure)
+    // (a NaN, of drafts beside +inf in both rows, is not sure)
     return a.uniform[at] > __builtin_amdgcn_exp2f(log_ratio) * 1.001f + 1e-30f;
 }
 

@@ -403,3 +403,33 @@ def test_requests_past_32_bit_offsets(c):
                              case.uniform.to(DEV), far(case.noise, 1 << 28),
                              temperature=case.t, draft_temperature=case.tq)
     case.check(got)
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("r,d,c", [(350, 2, 64001), (600, 1, 60001)])
+def test_drafters_rows_without_mass_among_many_long_ones(r, d, c, dtype):
+    """A draft that the drafter itself rules out with its whole row has p / q = infinity and
+    stands: the rows behind it count, whatever the workspace held before."""
+    rng = _rng(15, r, c, TYPES.index(dtype))
+    case = Case(rng, r, d, c, dtype, dtype)
+    low = torch.iinfo(dtype).min if dtype == torch.int32 else -np.inf
+    case.y[:, 0] = low
+    if dtype != torch.int32:
+        case.y[::2, 0] = np.nan
+    want = case.want()
+    case.want = lambda: want
+    need = bl.load_library().bitlogic_verify_workspace_bytes(r, d, c)
+    for fill in (0, 63):                                  # (63: small positive numbers)
+        workspace = torch.full((need,), fill, dtype=torch.uint8, device=DEV)
+        case.check(case.run(workspace=workspace))
+    assert {w[0] for w in want} >= set(range(1, d + 1))
+
+
+@pytest.mark.parametrize("r,d,c", [(256, 3, 65537), (400, 2, 60003)])
+def test_shares_far_below_the_largest_a_block_a_row(r, d, c):
+    test_shares_far_below_the_largest(r, d, c)
+
+
+@pytest.mark.parametrize("near", [0.3, 2.0])
+def test_many_requests_a_block_a_row(near):
+    test_many_requests(256, 3, 65537, near)
