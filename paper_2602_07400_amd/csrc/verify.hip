@@ -6,9 +6,9 @@
 // after the first that does not, at j, the next class is drawn from max(0, p_j - q_j), or,
 // where all stand, from the target's row behind them: the largest log(mass) + Gumbel number.
 //
-// A row's part in a decision is its largest logit m and the sum s of its exponentials, one
-// pass over the row.  Sums are 32-bit terms in 64-bit totals and good to kLoose of
-// themselves; everything behind them is a handful of values a request and taken in 64 bits.
+// A row's part in a decision is a reference m, at or just above its largest logit, and the sum s
+// of its exponentials relative to it, one pass over the row.  Sums are 32-bit terms in 64-bit totals, and the quotient of two is good to
+// kLoose of itself; everything behind them is a handful of values a request and taken in 64 bits.
 // A decision that kLoose could turn is taken again with sums in 64 bits (about one draft in
 // 10^5), so accepted drafts and classes are those of 64-bit arithmetic.
 //
@@ -32,7 +32,20 @@ namespace {
 
 using namespace rows;
 
-constexpr double kLoose = 1e-5;
+// A lane's reference is set kLead binary orders above its largest logit, and set anew, with its sum
+// multiplied to be relative to it, where a logit is above it: every 2.8 (in powers of e).  With
+// the largest itself as reference, the sum of an ascending row is multiplied with every load,
+// and the roundings of equal steps add up (2^22 ascending classes: a quotient off by more than 3e-5).
+// What a sum is off by, in shares of itself:
+//   exponents: three roundings of 2^-24 of each difference on the way of a term from its logit
+//   to the row's reference, X + 5.6 in powers of e (a reference that is rounded may be twice as far
+//   ahead), X how far the logit is below the largest, whose mean over the terms is at most the
+//   logarithm of the number of classes, 20.8: 4.8e-6
+//   exponentials: 2^-23 each, one for the term, one a change of reference, one behind all of
+//   them, X / 2.8 + 4 of them: 1.4e-6.  32-bit sums of eight terms: 0.5e-6
+// that is 6.7e-6 at 2^30 classes, and twice that for two sums.
+constexpr float kLead = 4.0f;
+constexpr double kLoose = 1.4e-5;
 
 struct Side {
     const char *rows;                   // NULL: drafts without probabilities
@@ -53,8 +66,9 @@ struct Side {
     }
 };
 
-// A row's (or a part's) largest logit (-inf: none; every type's values are exact in 64 bits), the
-// first class that has it (of greedy rows) and the sum of exponentials relative to it.
+// A row's (or a part's) reference (-inf: no logit; in greedy rows and beside +inf, the largest
+// logit itself; every type's values are exact in 64 bits), the first class that has it (of greedy
+// rows) and the sum of exponentials relative to it.
 struct Stat {
     double m, s;
     int32_t first;
@@ -121,7 +135,7 @@ __device__ __forceinline__ double value_at(const char *row, int type, int64_t i)
         return v > Elem<TYPE>::lowest() ? (double)v : -kInf;
     });
 }
-// v - m, m the row's largest: 0 at it, -inf for masked values and, beside a +inf, for all others.
+// v - m, m the row's reference: 0 at it, -inf for masked values and, beside a +inf, for all others.
 __device__ __forceinline__ double below(double v, double m) { return v == m ? 0.0 : v - m; }
 
 // Elements from class i on of a row of n, those of [i, hi) and the rest masked; returns the class
@@ -187,6 +201,19 @@ __device__ __forceinline__ int32_t first_at(Group<G> &g, const char *row, int32_
     return (int32_t)~g.reduce(first, Max());
 }
 
+// A reference `lead` above v (int32: rounded down), at most the type's largest finite value; +inf
+// is its own.
+template <int TYPE>
+__device__ __forceinline__ typename Elem<TYPE>::Cmp ahead(typename Elem<TYPE>::Cmp v, float lead)
+{
+    if constexpr (TYPE == kI32) {
+        const int32_t up = (int32_t)((uint32_t)v + (uint32_t)fminf(lead, 0x1p30f));
+        return up < v ? INT32_MAX : up;
+    } else {
+        return v > FLT_MAX ? v : fminf(v + lead, FLT_MAX);
+    }
+}
+
 // Stat of [lo, hi) of a row of n at 1 / T (0: greedy).
 template <int TYPE, int G>
 __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo, int32_t hi,
@@ -196,6 +223,7 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo
     typedef typename E::Cmp Cmp;
     constexpr int VEC = 16 / E::kBytes;
     const float c = (float)(inverse * 1.4426950408889634);
+    const float lead = inverse > 0.0 ? kLead / c : 0.0f;
     Cmp m = E::lowest();
     double s = 0.0;
     over<TYPE, G, VEC, 4>(row, lo, hi, n, g.t, [&](int32_t, const Piece<TYPE, VEC> &p)
@@ -207,9 +235,10 @@ __device__ __forceinline__ Stat stat_of(Group<G> &g, const char *row, int32_t lo
             vm = v > vm ? v : vm;
         }
         if (vm > m) {
+            const Cmp old = m;
+            m = ahead<TYPE>(vm, lead);
             if (s > 0.0)
-                s *= (double)__builtin_amdgcn_exp2f(E::minus(m, vm) * c);
-            m = vm;
+                s *= (double)__builtin_amdgcn_exp2f(E::minus(old, m) * c);
         }
         float part = 0.0f;
 #pragma unroll
@@ -398,7 +427,7 @@ __device__ __forceinline__ void offer(Best &best, const Draw &d, int32_t cls, do
         if (!(delta < 2 * kLoose))
             return;
         if (delta > -2 * kLoose) {                        // p > q, or not, by less than 4 kLoose
-            const double most = one.score - 10.1;         // log(4 kLoose), rounded up
+            const double most = one.score - 9.7;          // log(4 kLoose), rounded up
             if (most > best.other)
                 best.other = most;
             return;

@@ -433,3 +433,79 @@ def test_shares_far_below_the_largest_a_block_a_row(r, d, c):
 @pytest.mark.parametrize("near", [0.3, 2.0])
 def test_many_requests_a_block_a_row(near):
     test_many_requests(256, 3, 65537, near)
+
+
+def _ramp(c, t, dtype):
+    """A row of c classes that ascends from 0 to 1 (int32: from 0 to c - 1), every value exact, a
+    temperature for it, and log p: each lane's maximum grows with every load."""
+    x = torch.arange(c, dtype=torch.int32)
+    if dtype == torch.float32:
+        x, scale = x.float() / c, 1.0
+    else:
+        scale = float(c)
+    t = float(np.float32(t * scale))
+    y = x.double().numpy() / t
+    return x, t, y - y[-1] - np.log(np.exp(y - y[-1]).sum())
+
+
+RAMP_T = [0.7, 0.9, 1.0, 1.3, 1.4]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.int32])
+@pytest.mark.parametrize("c,r", [(2048, 400), (3900, 480), (1 << 17, 30), (1 << 20, 500),
+                                 (1 << 22, 500), (1 << 22, 600), (1 << 22, 10)])
+def test_ascending_rows(c, r, dtype):
+    """Rows along which a lane's sum is made relative to a larger logit again and again, against
+    a flat drafter: numbers from 4e-5 below p / q to 4e-5 above it."""
+    rng = _rng(16, c, r, TYPES.index(dtype))
+    t_of = torch.empty(r)
+    draft, noise = c // 4, _gumbel(rng, 1, c)
+    z = noise[0].double().numpy()
+    uniform, want = torch.empty(r, 1), []
+    for k, t in enumerate(RAMP_T):
+        x, t_of[k::5], log_p = _ramp(c, t, dtype)
+        t = float(t_of[k])
+        ratio = np.exp(log_p[draft] + np.log(c))
+        stands = int((log_p + z).argmax())
+        with np.errstate(divide="ignore"):
+            drawn = int((np.log(np.maximum(np.exp(log_p) - 1 / c, 0)) + z).argmax())
+        rows = range(k, r, 5)
+        for n, i in enumerate(rows):
+            uniform[i] = ratio * (1 + (2 * (n + 0.5) / len(rows) - 1) * 4e-5)
+            ok = float(uniform[i]) < ratio
+            want.append((i, int(ok), stands if ok else drawn, log_p[stands if ok else drawn]))
+    x = x.to(DEV).expand(r, 2, c)
+    flat = torch.zeros(c, device=DEV).expand(r, 1, c)
+    accepted, token, log_prob = (v.cpu().numpy() for v in bl.bitlogic_verify(
+        x, torch.full((r, 1), draft, dtype=torch.int32, device=DEV), flat, uniform.to(DEV),
+        noise.to(DEV).expand(r, c), temperature=t_of.to(DEV)))
+    at = [w[0] for w in want]
+    assert accepted[at].tolist() == [w[1] for w in want]
+    assert token[at].tolist() == [w[2] for w in want]
+    off = np.abs(log_prob[at] - np.array([w[3] for w in want]))
+    assert (off <= REL + 2.0 ** -22 * 40).all()
+
+
+@pytest.mark.parametrize("c,r", [(1 << 17, 100), (1 << 20, 505), (1 << 22, 505)])
+def test_draws_from_ascending_rows(c, r):
+    """Two classes whose scores are within 2.5e-3 of each other, one of them with a mass that is a
+    fiftieth of its p: what its row's sum is off by counts fifty times."""
+    noise = torch.full((r, c), -1000.0, device=DEV)
+    t_of, want = torch.empty(r), []
+    for k, t in enumerate(RAMP_T):
+        x, t_of[k::5], log_p = _ramp(c, t, torch.float32)
+        t = float(t_of[k])
+        delta = -np.log(c) - log_p                        # log q - log p, falling
+        a, b = int(np.searchsorted(-delta, 0.02)), c - 1
+        score = lambda i: log_p[i] + np.log(-np.expm1(delta[i]))                 # noqa: E731
+        rows = range(k, r, 5)
+        for n, i in enumerate(rows):
+            z = np.float32(score(b) - score(a) + (2 * (n + 0.5) / len(rows) - 1) * 2.5e-3)
+            noise[i, a], noise[i, b] = float(z), 0.0
+            want.append((i, a if score(a) + float(z) > score(b) else b))
+    accepted, token, _ = bl.bitlogic_verify(
+        x.to(DEV).expand(r, 2, c), torch.zeros((r, 1), dtype=torch.int32, device=DEV),
+        torch.zeros(c, device=DEV).expand(r, 1, c), torch.full((r, 1), 0.9999999, device=DEV),
+        noise, temperature=t_of.to(DEV))
+    assert not accepted.any()
+    assert token.cpu()[[w[0] for w in want]].tolist() == [w[1] for w in want]
