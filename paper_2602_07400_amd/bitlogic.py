@@ -18,6 +18,7 @@ from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 __all__ = [
     "BitlogicError", "bitlogic_encode", "bitlogic_lut_layer", "bitlogic_groupsum_head",
@@ -1012,15 +1013,20 @@ class _Dropout(torch.autograd.Function):
         return _dropout(grad.contiguous(), *ctx.mask, offset, None, None), None, None, None
 
 
+def _has_tangent(x: torch.Tensor) -> bool:
+    """Whether x carries a forward-mode derivative, which needs no gradient to be asked for."""
+    return forward_ad._current_level >= 0 and forward_ad.unpack_dual(x).tangent is not None
+
+
 def bitlogic_dropout(x: torch.Tensor, p: float, seed: int, offset=0,
                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Dropout of rows x [N][c] (float32, float16, bfloat16, or int32 counts, which become
     float32; rows may be strided) with probability p, by a mask that (seed, offset) alone
     decide and that is never stored.  offset is a number or an int64 tensor [1] on the GPU,
-    which a captured graph reads at every replay.  Differentiable in a float x where neither
-    out (which may be x) nor stream is given; both passes run on the current stream."""
-    if out is None and stream is None and isinstance(x, torch.Tensor) and x.requires_grad \
-            and torch.is_grad_enabled():
+    which a captured graph reads at every replay.  Differentiable (backward) in a float x where
+    neither out (which may be x) nor stream is given; both passes run on the current stream."""
+    if out is None and stream is None and isinstance(x, torch.Tensor) and (
+            (x.requires_grad and torch.is_grad_enabled()) or _has_tangent(x)):
         return _Dropout.apply(x, p, seed, offset)
     return _dropout(x, p, seed, offset, out, stream)
 

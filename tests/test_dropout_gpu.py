@@ -177,3 +177,19 @@ def test_rows_past_32_bit_offsets():
     assert (out[39999, -8:] != 0).cpu().tolist() == keep
     share = float((out[39000:] != 0).float().mean())
     assert abs(share - 0.5) < 6 * 0.5 / (1000 * 65536) ** 0.5
+
+
+def test_forward_mode_is_refused():
+    """A tangent is not dropped without a word: there is no forward-mode derivative."""
+    x = torch.ones((4, 9), device=DEV)
+    with torch.autograd.forward_ad.dual_level():
+        for leaf in (x, x.clone().requires_grad_()):
+            dual = torch.autograd.forward_ad.make_dual(leaf, torch.ones_like(x))
+            with pytest.raises((RuntimeError, NotImplementedError)):
+                bl.bitlogic_dropout(dual, 0.3, SEED)
+            with torch.no_grad(), pytest.raises((RuntimeError, NotImplementedError)):
+                bl.bitlogic_dropout(dual, 0.3, SEED)
+        y = bl.bitlogic_dropout(x, 0.3, SEED)             # one without a tangent, beside it
+        assert torch.equal(y, bl.bitlogic_dropout(x.clone(), 0.3, SEED))
+    with pytest.raises((RuntimeError, NotImplementedError)):
+        torch.func.jvp(lambda v: bl.bitlogic_dropout(v, 0.3, SEED), (x,), (x,))
