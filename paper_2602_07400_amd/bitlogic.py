@@ -1060,12 +1060,15 @@ def bitlogic_group_rows(ids: torch.Tensor, n_groups: int,
     ptr = _dev(ids, "ids", _I32)
     lib = load_library()
     need = int(lib.bitlogic_group_rows_bytes(n, n_groups))
-    if plan is None:
+    given = plan is not None
+    if not given:
         plan = _empty((max(need, 1),), torch.uint8, dev, stream)
     if plan.device != dev:
         raise ValueError(f"plan is on {plan.device}, expected {dev}")
     _call(dev, lib.bitlogic_group_rows, ptr, n, n_groups, _dev(plan, "plan", (torch.uint8,)),
           plan.numel(), _stream(stream, dev))
+    if given:                       # a backward pass that has kept what it held is refused
+        torch.autograd.graph.increment_version(plan)
     return RowGroups(plan, n, n_groups)
 
 
@@ -1205,15 +1208,18 @@ class _Adapt(torch.autograd.Function):
         out, hidden = bitlogic_adapters(x, down, up, ids, scales, base, base_scale, plan,
                                         want_hidden=need[2])
         ctx.save_for_backward(x, down, up, ids, hidden,
-                              scales if isinstance(scales, torch.Tensor) else None)
-        ctx.rest = (None if isinstance(scales, torch.Tensor) else scales), base_scale, plan
+                              scales if isinstance(scales, torch.Tensor) else None,
+                              None if plan is None else plan.plan)
+        ctx.rest = (None if isinstance(scales, torch.Tensor) else scales), base_scale
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
-        x, down, up, ids, hidden, scales = ctx.saved_tensors
-        number, base_scale, plan = ctx.rest
+        x, down, up, ids, hidden, scales, plan = ctx.saved_tensors
+        number, base_scale = ctx.rest
+        if plan is not None:
+            plan = RowGroups(plan, x.shape[0], down.shape[0])
         need = ctx.needs_input_grad
         grad = grad.contiguous()
         grads = (None, None, None)

@@ -505,3 +505,23 @@ def test_adapters_past_32_bit_offsets():
         got, _ = bl.bitlogic_adapters(x[rows], down, up, ids[rows], 1.0, plan=plan)
         # five terms that are not zero, then 128: a rounding each, in 32 bits
         assert ((got.double().cpu() - want[rows]).abs() <= 140 * 2.0 ** -24 * size[rows]).all()
+
+
+def test_plan_written_again_before_the_backward_pass_is_refused():
+    case = Case((20,), 100, 60, 50, 6, 3, F32)
+    x, down, up, ids, scales, base = case.on()
+    for leaf in (x, down, up):
+        leaf.requires_grad_()
+        plan = bl.bitlogic_group_rows(ids, 3)
+        out = bl.bitlogic_adapt(x, down, up, ids, scales, base, case.base_scale, plan)
+        again = bl.bitlogic_group_rows((ids + 1) % 3, 3, plan=plan.plan)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(out, leaf, case.grad.to(DEV))
+        # the plan written again serves calls from then on
+        case.ids, first = (case.ids + 1) % 3, case.ids
+        out = bl.bitlogic_adapt(x, down, up, (ids + 1) % 3, scales, base, case.base_scale, again)
+        case.check(out)
+        grad, = torch.autograd.grad(out, leaf, case.grad.to(DEV))
+        case.check_grads(*(grad if v is leaf else None for v in (x, down, up)))
+        case.ids = first
+        leaf.requires_grad_(False)
