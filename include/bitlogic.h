@@ -634,7 +634,8 @@ int bitlogic_group_rows(const int32_t *ids, int64_t n_rows, int32_t n_groups, vo
  *   out     [n_rows][n_out] of the weights' type, out_stride >= n_out: base itself with its
  *           own stride (not int32), or memory apart from x and base
  *   hidden  float [n_rows][rank] or NULL: down_a x[s], 0 where there is no adapter; what the
- *           backward pass takes.  out may be NULL if hidden is not
+ *           backward pass takes.  Memory apart from all of the above; out may be NULL if
+ *           hidden is not
  * Sums are held in 32 bits; down_a x goes into the second product to 2^-17 of itself or, with
  * float16 weights, 2^-22 of the row's largest.  Results do not depend on how a launch is
  * scheduled, nor a row's on other rows' values.  The workspace (16-byte aligned) may hold
@@ -654,7 +655,8 @@ int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_s
  *   grad_up_a   = scale_a sum_s g[s] hidden[s]^T          [n_adapters][n_out][rank]
  * over the rows s of adapter a (none: zeros), in the weights' type; each may be NULL, not all.
  * (The gradient of base is base_scale * g.)  x and hidden are read for the weights' gradients
- * alone, which also need a plan.  The outputs may not overlap each other or any input. */
+ * alone, which also need a plan.  The outputs may not overlap each other or an input that is
+ * read (rows of one stride may lie between each other's): BITLOGIC_ERR_SHAPE. */
 size_t bitlogic_adapters_backward_workspace_bytes(const bitlogic_adapter_set *set,
                                                   int64_t n_rows);
 int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_stride,
@@ -764,7 +766,7 @@ const char *bitlogic_last_error(void);
  * and the node-per-wave layer kernel, whose per-node records enlarge the
  * forward workspace of networks that use it; 0.8.0 bitlogic_network_path; 0.9.0
  * bitlogic_top_logits, bitlogic_distill and bitlogic_sample; 0.10.0 bitlogic_verify,
-bitlogic_dropout, bitlogic_group_rows and bitlogic_adapters with its backward pass). */
+ * bitlogic_dropout, bitlogic_group_rows and bitlogic_adapters with its backward pass). */
 #define BITLOGIC_VERSION 1000
 int bitlogic_version(void);
 

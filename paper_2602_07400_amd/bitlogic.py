@@ -1167,7 +1167,8 @@ def bitlogic_adapters_backward(grad: torch.Tensor, x: torch.Tensor,
                                want_x: bool = True, want_down: bool = True,
                                want_up: bool = True):
     """Gradients of bitlogic_adapters for grad [N][c], that of out: (of x [N][f], of down, of
-    up), each None where it is not wanted.  hidden: bitlogic_adapters' (for that of up)."""
+    up), each None where it is not wanted.  hidden: bitlogic_adapters' (for that of up).  Outputs
+    that are given may not overlap each other or what is read, grad among it."""
     ptr, stride = _rows(grad, "grad")
     x_ptr, x_stride = _rows(x, "x")
     s = _adapter_set(x, down, up, scales)

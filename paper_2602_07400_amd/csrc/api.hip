@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 
 #include "bitlogic.h"
@@ -140,6 +141,45 @@ size_t span_bytes(int64_t n_rows, int64_t n_cols, int64_t stride, int32_t type)
 bool overlaps(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
 {
     return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
+// Rows in memory: widths and strides in bytes (p NULL: not there).
+struct Region {
+    const char *name;
+    const void *p;
+    int64_t rows;
+    size_t width, stride;
+};
+
+Region flat(const char *name, const void *p, size_t bytes) { return {name, p, 1, bytes, bytes}; }
+
+// Rows of one stride may lie between each other's; others are apart where their ranges are.
+bool overlaps(const Region &a, const Region &b)
+{
+    if (!a.p || !b.p || a.rows == 0 || b.rows == 0 ||
+        !overlaps(a.p, (a.rows - 1) * a.stride + a.width, b.p, (b.rows - 1) * b.stride + b.width))
+        return false;
+    const size_t stride = a.stride;
+    if (stride != b.stride || a.width > stride || b.width > stride)
+        return true;
+    const uintptr_t ap = (uintptr_t)a.p, bp = (uintptr_t)b.p;
+    const size_t at = bp >= ap ? (bp - ap) % stride : (stride - (ap - bp) % stride) % stride;
+    return at < a.width || at + b.width > stride;
+}
+
+// Outputs apart from each other and from what is read.
+int check_apart(const char *who, std::initializer_list<Region> outputs,
+                std::initializer_list<Region> inputs)
+{
+    for (const Region *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Region *other = outputs.begin(); other != o; ++other)
+            if (overlaps(*o, *other))
+                return fail(BITLOGIC_ERR_SHAPE, "%s: %s overlaps %s", who, o->name, other->name);
+        for (const Region &i : inputs)
+            if (overlaps(*o, i))
+                return fail(BITLOGIC_ERR_SHAPE, "%s: %s overlaps %s", who, o->name, i.name);
+    }
+    return BITLOGIC_OK;
 }
 
 int check_list(const char *who, int32_t k, float temperature)
@@ -1387,6 +1427,19 @@ int bitlogic_adapters(const void *x, int32_t x_type, int64_t n_rows, int64_t x_s
     a.hidden = hidden;
     if (int rc = take_parts(who, a, s.weight_type, false, workspace, workspace_bytes))
         return rc;
+    // (out beside x and base: above; a wide pass writes hidden before it reads base)
+    const size_t rows = n_rows;
+    if (int rc = check_apart(
+            who, {{"hidden", hidden, n_rows, s.rank * 4ul, s.rank * 4ul}},
+            {{"x", x, n_rows, s.n_in * el, x_stride * el},
+             {"base", out ? base : nullptr, n_rows, s.n_out * el, base_stride * el},
+             {"out", out, n_rows, s.n_out * el, out_stride * el},
+             flat("down", s.down, a.w1_step * s.n_adapters),
+             flat("up", out ? s.up : nullptr, a.w2_step * s.n_adapters),
+             flat("ids", plan ? nullptr : ids, rows * 4),
+             flat("plan", plan, bitlogic_group_rows_bytes(n_rows, s.n_adapters)),
+             flat("scales", s.scales, s.n_adapters * 4ul)}))
+        return rc;
     return hip_status(by_weight(s.weight_type, [&](auto W) {
         return bl::adapt::launch_pass<decltype(W)::value>(a, x_type == BITLOGIC_LOGITS_I32, false,
                                                           (hipStream_t)stream);
@@ -1494,6 +1547,23 @@ int bitlogic_adapters_backward(const void *grad, int64_t n_rows, int64_t grad_st
         if (g.n_chunks * ((int64_t)g.job[0].blocks + g.job[1].blocks) >= 1 << 24)
             return fail(BITLOGIC_ERR_UNSUPPORTED, "adapters_backward: n_rows * (n_in + n_out) too "
                         "large for one launch");
+    }
+    if (n_rows > 0) {
+        const size_t down_bytes = (size_t)s.n_adapters * s.rank * s.n_in * el,
+                     up_bytes = (size_t)s.n_adapters * s.rank * s.n_out * el;
+        if (int rc = check_apart(
+                who,
+                {{"grad_x", grad_x, n_rows, s.n_in * el, grad_x_stride * el},
+                 flat("grad_down", grad_down, down_bytes), flat("grad_up", grad_up, up_bytes)},
+                {{"grad", grad, n_rows, s.n_out * el, grad_stride * el},
+                 {"x", grad_down ? x : nullptr, n_rows, s.n_in * el, x_stride * el},
+                 flat("hidden", grad_up ? hidden : nullptr, (size_t)n_rows * s.rank * 4),
+                 flat("down", grad_x ? s.down : nullptr, down_bytes),
+                 flat("up", grad_x || grad_down ? s.up : nullptr, up_bytes),
+                 flat("ids", plan ? nullptr : ids, (size_t)n_rows * 4),
+                 flat("plan", plan, bitlogic_group_rows_bytes(n_rows, s.n_adapters)),
+                 flat("scales", s.scales, s.n_adapters * 4ul)}))
+            return rc;
     }
     if (n_rows > 0 && (grad_x || grad_down)) {
         a.x = static_cast<const char *>(grad);

@@ -179,3 +179,68 @@ def test_launches_past_2_32_lanes_are_refused(lib):
                 out_stride=1 << 18)
     assert _forward(lib, plan=None, **wide) == EUNSUP
     assert b"one launch" in lib.bitlogic_last_error()
+
+
+def _apart(**fields):
+    """Buffers of five rows by 3 adapters 10 -> 12 of rank 4, none of which overlap."""
+    names = ("x", "grad", "base", "out", "hidden", "grad_x", "grad_down", "grad_up", "down", "up",
+             "ids", "plan", "scales", "workspace")
+    out = {name: FAKE + (i << 20) for i, name in enumerate(names)}
+    out.update(fields)
+    return out
+
+
+def _only(call, args):
+    own = {"_forward": ("x", "base", "out", "hidden"),
+           "_backward": ("x", "grad", "hidden", "grad_x", "grad_down", "grad_up")}[call.__name__]
+    return {k: v for k, v in args.items()
+            if k in own + ("down", "up", "ids", "plan", "scales", "workspace")
+            or k not in _apart()}
+
+
+def test_hidden_apart_from_what_is_read_and_written(lib):
+    at = _apart()
+    sizes = {"x": 200, "base": 240, "out": 240, "down": 480, "up": 576}
+    for name, size in sizes.items():
+        for hidden in (at[name], at[name] + size - 4, at[name] - 76):
+            assert _forward(lib, **_only(_forward, _apart(hidden=hidden))) == ESHAPE, name
+            assert b"hidden overlaps" in lib.bitlogic_last_error()
+        for hidden in (at[name] + size, at[name] - 80):
+            assert _forward(lib, **_only(_forward, _apart(hidden=hidden))) == EHIP, name
+    # a base that is not there, an output that is not there
+    assert _forward(lib, **_only(_forward, _apart(base=None, hidden=at["base"]))) == EHIP
+    assert _forward(lib, **_only(_forward, _apart(out=None, hidden=at["out"]))) == EHIP
+    assert _forward(lib, **_only(_forward, _apart(out=None, hidden=at["up"]))) == EHIP
+    assert _forward(lib, **_only(_forward, _apart(ids=at["hidden"], plan=None))) == ESHAPE
+    assert _forward(lib, **_only(_forward, _apart(scales=at["hidden"] + 16))) == ESHAPE
+
+
+def test_gradients_apart_from_what_is_read_and_written(lib):
+    at = _apart()
+    sizes = {"x": 200, "grad": 240, "hidden": 80, "grad_x": 200, "grad_down": 480,
+             "grad_up": 576, "down": 480, "up": 576}
+    for out in ("grad_x", "grad_down", "grad_up"):
+        for name, size in sizes.items():
+            if name == out:
+                continue
+            for where in (at[name], at[name] + size - 4, at[name] - sizes[out] + 4):
+                assert _backward(lib, **_only(_backward, _apart(**{out: where}))) == ESHAPE
+                assert b"overlaps" in lib.bitlogic_last_error()
+            for where in (at[name] + size, at[name] - sizes[out]):
+                assert _backward(lib, **_only(_backward, _apart(**{out: where}))) == EHIP
+        assert _backward(lib, **_only(_backward, _apart(**{out: at["scales"]}))) == ESHAPE
+    # what is not read: x and hidden beside the gradient of x alone
+    for name in ("x", "hidden"):
+        assert _backward(lib, **_only(_backward, _apart(
+            grad_x=at[name], grad_down=None, grad_up=None))) == EHIP
+    assert _backward(lib, **_only(_backward, _apart(
+        grad_up=at["up"], grad_x=None, grad_down=None))) == EHIP
+    # rows between each other's: 10 columns of x's gradient beside 12 of out's
+    wide = dict(grad_stride=30, grad_x_stride=30)
+    for where, want in ((12, EHIP), (20, EHIP), (11, ESHAPE), (21, ESHAPE)):
+        args = _apart(grad_x=at["grad"] + 4 * where, **wide)
+        assert _backward(lib, **_only(_backward, args)) == want, where
+    args = _apart(grad_x=at["grad"] - 4 * 10, **wide)
+    assert _backward(lib, **_only(_backward, args)) == EHIP
+    args = _apart(grad_x=at["grad"] + 4 * 12, grad_stride=30, grad_x_stride=31)
+    assert _backward(lib, **_only(_backward, args)) == ESHAPE

@@ -525,3 +525,27 @@ def test_plan_written_again_before_the_backward_pass_is_refused():
         case.check_grads(*(grad if v is leaf else None for v in (x, down, up)))
         case.ids = first
         leaf.requires_grad_(False)
+
+
+def test_outputs_over_inputs_are_refused():
+    """The gradient of x over the gradient of out, which the weights' gradients still read; or
+    between its rows, where nothing is lost."""
+    for f in (60, 700):
+        case = Case((21,), 50, f, f, 6, 3, F32)
+        x, down, up, ids, scales, base = case.on()
+        _, hidden = bl.bitlogic_adapters(x, down, up, ids, scales, base, case.base_scale,
+                                         want_hidden=True)
+        wide = torch.zeros((50, 2 * f), device=DEV)
+        grad, grad_x = wide[:, :f], wide[:, f:]
+        grad.copy_(case.grad)
+        case.check_grads(*bl.bitlogic_adapters_backward(grad, x, hidden, down, up, ids, scales,
+                                                        grad_x=grad_x))
+        for over in (grad, wide[:, 1:f + 1], x):
+            with pytest.raises(bl.BitlogicError, match="overlaps"):
+                bl.bitlogic_adapters_backward(grad, x, hidden, down, up, ids, scales, grad_x=over)
+        with pytest.raises(bl.BitlogicError, match="grad_down overlaps down"):
+            bl.bitlogic_adapters_backward(grad, x, hidden, down, up, ids, scales, grad_down=down)
+        with pytest.raises(bl.BitlogicError, match="hidden overlaps base"):
+            bl.bitlogic_adapters(x, down, up, ids, scales, base,
+                                 hidden=base.view(-1)[:300].view(50, 6))
+        assert torch.equal(grad, case.grad.to(DEV))
