@@ -1204,7 +1204,8 @@ class _Adapt(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, down, up, base, ids, scales, base_scale, plan):
         need = ctx.needs_input_grad
-        if plan is None and (need[1] or need[2]) and x.shape[0] > 0:
+        n = x.shape[0]
+        if plan is None and n > 0 and (need[1] or need[2] or (need[0] and n > _LONE_ROWS)):
             plan = bitlogic_group_rows(ids, down.shape[0])        # the backward pass's, too
         out, hidden = bitlogic_adapters(x, down, up, ids, scales, base, base_scale, plan,
                                         want_hidden=need[2])

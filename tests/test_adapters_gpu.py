@@ -549,3 +549,35 @@ def test_outputs_over_inputs_are_refused():
             bl.bitlogic_adapters(x, down, up, ids, scales, base,
                                  hidden=base.view(-1)[:300].view(50, 6))
         assert torch.equal(grad, case.grad.to(DEV))
+
+
+@pytest.mark.parametrize("type_", [F32, BF16])
+@pytest.mark.parametrize("n", [20, 33, 300])
+def test_rows_are_grouped_once_for_both_passes(n, type_, monkeypatch):
+    """Whichever gradients are asked for; and the backward pass has the forward pass's rows."""
+    case = Case((22,), n, 60, 50, 6, 3, type_)
+    x, down, up, ids, scales, base = case.on()
+    calls, group = [], bl.bitlogic_group_rows
+    monkeypatch.setattr(bl, "bitlogic_group_rows",
+                        lambda *a, **k: calls.append(1) or group(*a, **k))
+    leaves = (x, down, up)
+    for wanted in ((x,), (down,), (up,), leaves):
+        for leaf in wanted:
+            leaf.requires_grad_()
+        calls.clear()
+        alone = n <= 32 and len(wanted) == 1 and wanted[0] is x
+        own = ids.clone()
+        out = bl.bitlogic_adapt(x, down, up, own, scales, base, case.base_scale)
+        if n > 32:
+            own.data.fill_(1)                             # (no version of it moves)
+        grads = dict(zip(map(id, wanted), torch.autograd.grad(out, wanted, case.grad.to(DEV))))
+        assert len(calls) == (not alone)
+        case.check(out)
+        case.check_grads(*(grads.get(id(v)) for v in leaves))
+        for leaf in wanted:
+            leaf.requires_grad_(False)
+    calls.clear()
+    base.requires_grad_()
+    out = bl.bitlogic_adapt(x, down, up, ids, scales, base, case.base_scale)
+    torch.autograd.grad(out, base, case.grad.to(DEV))
+    assert len(calls) == (n > 32)
