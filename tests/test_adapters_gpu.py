@@ -581,3 +581,31 @@ def test_rows_are_grouped_once_for_both_passes(n, type_, monkeypatch):
     out = bl.bitlogic_adapt(x, down, up, ids, scales, base, case.base_scale)
     torch.autograd.grad(out, base, case.grad.to(DEV))
     assert len(calls) == (n > 32)
+
+
+@pytest.mark.parametrize("f,c,r,rows", [(2, 3, 1, 1024), (70, 60, 3, 4096)])
+def test_gradients_of_more_rows_than_a_run_a_wave(f, c, r, rows):
+    """All three past 2^20 rows, in chunks of either cut.  Every value is positive, so that a
+    chunk that is lost or counted twice is a hundredth of the sum."""
+    n, g = (1 << 20) + 4097, 9
+    gen = torch.Generator(DEV).manual_seed(19)
+    of = lambda *s: 0.5 + torch.rand(s, device=DEV, generator=gen)              # noqa: E731
+    x, grad, down, up, scales = of(n, f), of(n, c), of(g, r, f), of(g, c, r), of(g)
+    ids = torch.randint(-1, g, (n,), device=DEV, generator=gen).int()
+    _, hidden = bl.bitlogic_adapters(x, down, up, ids, scales, want_hidden=True)
+    got = bl.bitlogic_adapters_backward(grad, x, hidden, down, up, ids, scales)
+    x, grad, down, up, scales = (v.double() for v in (x, grad, down, up, scales))
+    # roundings of the terms, of a chunk's sum, and of the sum over a group's chunks
+    own = (f + c + r + 8) * 2.0 ** -24
+    off = own + (rows + n // rows) * 2.0 ** -24
+    assert off < 0.1 * rows / (n / g)                     # a tenth of a chunk
+    assert not got[0][ids < 0].any()
+    for a in range(g):
+        at = (ids == a).nonzero()[:, 0]
+        xa, ga = x[at], grad[at]
+        back, h = ga @ up[a], xa @ down[a].t()
+        for value, want, bound in (
+                (got[0][at], scales[a] * (back @ down[a]), own),
+                (got[1][a], scales[a] * (back.t() @ xa), off),
+                (got[2][a], scales[a] * (ga.t() @ h), off)):
+            assert ((value.double() - want).abs() <= bound * want).all()
