@@ -894,6 +894,14 @@ def _call(device, f, *args) -> None:
             _check(f(*args))
 
 
+def _changed(*given: Optional[torch.Tensor]) -> None:
+    """Count a call's writes to tensors it was given (by address, which autograd does not see) as
+    changes of them: a backward pass that has kept what one held is refused."""
+    for t in given:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 def _rows3(t: torch.Tensor, name: str, shape, device) -> Tuple[int, int, int]:
     """Address, row and request stride of a tensor [requests][rows][classes] on the GPU
     whose rows are contiguous; shape: what it must have, None where any size will do."""
@@ -959,6 +967,7 @@ def bitlogic_verify(logits: torch.Tensor, drafted: torch.Tensor,
         noise_ptr, noise_stride = _rows(noise, "noise", _F32)
         if tuple(noise.shape) != (n, c) or noise.device != dev:
             raise ValueError(f"noise must be [{n}][{c}] on {dev}")
+    given = accepted, token, log_prob
     if accepted is None:
         accepted = _empty((n,), torch.int32, dev, stream)
     if token is None:
@@ -974,6 +983,7 @@ def bitlogic_verify(logits: torch.Tensor, drafted: torch.Tensor,
           _like(token, "token", _I32, (n,), dev),
           _like(log_prob, "log_prob", _F32, (n,), dev) if log_prob is not None else None,
           ws_ptr, ws_bytes, _stream(stream, dev))
+    _changed(*given)
     return accepted, token, log_prob
 
 
@@ -982,6 +992,7 @@ def _dropout(x, p, seed, offset, out, stream):
     n, c = x.shape
     dev = x.device
     dtype = torch.float32 if x.dtype == torch.int32 else x.dtype
+    given = out
     if out is None:
         out = _empty((n, c), dtype, dev, stream)
     out_ptr, out_stride = _rows(out, "out", (dtype,))
@@ -994,6 +1005,7 @@ def _dropout(x, p, seed, offset, out, stream):
         raise ValueError("seed and offset must be in [0, 2^64)")
     _call(dev, load_library().bitlogic_dropout, ptr, _LOGITS[x.dtype], n, c, stride, p, seed,
           number, at, out_ptr, out_stride, _stream(stream, dev))
+    _changed(given)
     return out
 
 
@@ -1060,15 +1072,14 @@ def bitlogic_group_rows(ids: torch.Tensor, n_groups: int,
     ptr = _dev(ids, "ids", _I32)
     lib = load_library()
     need = int(lib.bitlogic_group_rows_bytes(n, n_groups))
-    given = plan is not None
-    if not given:
+    given = plan
+    if plan is None:
         plan = _empty((max(need, 1),), torch.uint8, dev, stream)
     if plan.device != dev:
         raise ValueError(f"plan is on {plan.device}, expected {dev}")
     _call(dev, lib.bitlogic_group_rows, ptr, n, n_groups, _dev(plan, "plan", (torch.uint8,)),
           plan.numel(), _stream(stream, dev))
-    if given:                       # a backward pass that has kept what it held is refused
-        torch.autograd.graph.increment_version(plan)
+    _changed(given)
     return RowGroups(plan, n, n_groups)
 
 
@@ -1137,6 +1148,7 @@ def bitlogic_adapters(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
         base_type = _LOGITS[base.dtype]
         if tuple(base.shape) != (n, c) or base.device != dev:
             raise ValueError(f"base must be [{n}][{c}] on {dev}")
+    given = out, hidden
     if out is None:
         out = _empty((n, c), dtype, dev, stream)
     out_ptr, out_stride = _rows(out, "out", (dtype,))
@@ -1153,6 +1165,7 @@ def bitlogic_adapters(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
           out_ptr, out_stride,
           _like(hidden, "hidden", _F32, (n, s.rank), dev) if hidden is not None else None,
           ws_ptr, ws_bytes, _stream(stream, dev))
+    _changed(*given)
     return out, hidden
 
 
@@ -1175,6 +1188,7 @@ def bitlogic_adapters_backward(grad: torch.Tensor, x: torch.Tensor,
     n, dev, dtype = x.shape[0], x.device, down.dtype
     if tuple(grad.shape) != (n, s.n_out) or grad.device != dev or grad.dtype != dtype:
         raise ValueError(f"grad must be [{n}][{s.n_out}] of {dtype} on {dev}")
+    given = grad_x, grad_down, grad_up
     if grad_x is None and want_x:
         grad_x = _empty((n, s.n_in), dtype, dev, stream)
     if grad_down is None and want_down:
@@ -1197,6 +1211,7 @@ def bitlogic_adapters_backward(grad: torch.Tensor, x: torch.Tensor,
           like(hidden, "hidden", _F32, (n, s.rank)), ctypes.addressof(s), ids_ptr, plan_ptr,
           gx_ptr, gx_stride, like(grad_down, "grad_down", (dtype,), down.shape),
           like(grad_up, "grad_up", (dtype,), up.shape), ws_ptr, ws_bytes, _stream(stream, dev))
+    _changed(*given)
     return grad_x, grad_down, grad_up
 
 

@@ -609,3 +609,32 @@ def test_gradients_of_more_rows_than_a_run_a_wave(f, c, r, rows):
                 (got[1][a], scales[a] * (back.t() @ xa), off),
                 (got[2][a], scales[a] * (ga.t() @ h), off)):
             assert ((value.double() - want).abs() <= bound * want).all()
+
+
+def test_given_outputs_count_as_changed():
+    """What autograd has kept of a tensor that a call then writes is refused, not wrong."""
+    case = Case((23,), 40, 60, 60, 6, 3, F32)
+    x, down, up, ids, scales, base = case.on()
+    leaf = torch.ones((40, 60), device=DEV, requires_grad=True)
+    narrow = torch.ones((40, 6), device=DEV, requires_grad=True)
+    hidden = torch.ones((40, 6), device=DEV)
+
+    def backward(name, shape):
+        kept = torch.ones(shape, device=DEV, requires_grad=True)
+        y = kept.exp()
+        bl.bitlogic_adapters_backward(case.grad.to(DEV), x, hidden, down, up, ids, scales,
+                                      **{name: y.detach()})
+        return kept, y
+
+    y = leaf.exp()                                        # keeps its result
+    bl.bitlogic_adapters(x, down, up, ids, scales, y.detach(), out=y.detach())
+    h = narrow.exp()
+    bl.bitlogic_adapters(x, down, up, ids, scales, hidden=h.detach())
+    d = leaf.exp()
+    bl.bitlogic_dropout(d.detach(), 0.5, 1, out=d.detach())
+    made = [(leaf, y), (narrow, h), (leaf, d)]
+    made += [backward(name, shape) for name, shape in
+             (("grad_x", x.shape), ("grad_down", down.shape), ("grad_up", up.shape))]
+    for kept, value in made:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(value.sum(), kept)

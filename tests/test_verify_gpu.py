@@ -509,3 +509,13 @@ def test_draws_from_ascending_rows(c, r):
         noise, temperature=t_of.to(DEV))
     assert not accepted.any()
     assert token.cpu()[[w[0] for w in want]].tolist() == [w[1] for w in want]
+
+
+def test_given_outputs_count_as_changed():
+    case = Case(_rng(17), 6, 2, 40)
+    outs = dict(accepted=torch.zeros(6, dtype=torch.int32, device=DEV),
+                token=torch.zeros(6, dtype=torch.int32, device=DEV),
+                log_prob=torch.ones(6, device=DEV))
+    before = {name: t._version for name, t in outs.items()}
+    case.check(case.run(**outs))
+    assert all(t._version > before[name] for name, t in outs.items())
