@@ -915,10 +915,12 @@ __global__ __launch_bounds__(kPickBlock) void k_verify_pick(VerifyArgs a)
 
 // ---- which form, and its workspace ----
 // A wave a request: always up to kShortClasses, and up to kMostShort where requests are enough to
-// fill the card; else k_verify_rows and what follows (us, 4 drafts of bfloat16, 1 / 64 / 1024
-// requests: 1024 classes 15 / 19 / 22 and 22 / 22 / 101; 4096 29 / 44 / 54 and 22 / 23 / 107; 8192
-// 54 / 71 / 86 and 21 / 26 / 121).  Above 4096 what a wave alone may have to redo in 64 bits (500 us
-// for 8192 classes, in about one call of 25 with 1024 requests) costs what is won.
+// fill the card; else k_verify_rows and what follows (us, 4 drafts of bfloat16: 1030 classes, 16
+// requests 22 and 24, 1400 46 and 72; 1300 classes, 256 requests 30 and 28, 400 30 and 33; 2048
+// classes, 400 39 and 34, 600 36 and 39; 4096 classes, 512 51 and 42, 850 56 and 62; of 8
+// drafts the border is where it is for 4, of one below: 2048 classes, 256 requests 21 and 24).
+// Above 4096 what a wave alone may have to redo in 64 bits (500 us for 8192 classes, in about one
+// call of 25 with 1024 requests) costs what is won.
 constexpr int32_t kShortClasses = 1024, kMostShort = 4096;
 constexpr int kWholeBlock = 1024;
 
@@ -942,7 +944,7 @@ void split(int64_t rows, int32_t n, int64_t want, int32_t unit, int32_t &parts, 
 Plan plan_of(int64_t n_requests, int32_t drafts, int32_t n)
 {
     Plan p = {};
-    p.is_short = n <= kShortClasses || (n <= kMostShort && n_requests >= n / 16 + 192);
+    p.is_short = n <= kShortClasses || (n <= kMostShort && n_requests >= n / 6 + 160);
     if (p.is_short || n_requests == 0)
         return p;
     const int64_t rows = n_requests * (drafts + 1);

@@ -519,3 +519,14 @@ def test_given_outputs_count_as_changed():
     before = {name: t._version for name, t in outs.items()}
     case.check(case.run(**outs))
     assert all(t._version > before[name] for name, t in outs.items())
+
+
+@pytest.mark.parametrize("near", [0.3, 2.0])
+@pytest.mark.parametrize("r,d,c", [(420, 3, 1500), (500, 2, 2048), (850, 2, 4001), (850, 2, 4096)])
+def test_many_requests_a_wave_each(r, d, c, near):
+    test_many_requests(r, d, c, near)
+
+
+@pytest.mark.parametrize("c,r", [(1500, 420), (4000, 850)])
+def test_numbers_next_to_a_border_a_wave_each(c, r):
+    test_numbers_next_to_a_border(c, r)
