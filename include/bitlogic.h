@@ -637,8 +637,8 @@ int bitlogic_group_rows(const int32_t *ids, int64_t n_rows, int32_t n_groups, vo
  *           backward pass takes.  Memory apart from all of the above; out may be NULL if
  *           hidden is not
  * Sums are held in 32 bits; down_a x goes into the second product to 2^-17 of itself or, with
- * float16 weights, 2^-22 of the row's largest.  Results do not depend on how a launch is
- * scheduled, nor a row's on other rows' values.  The workspace (16-byte aligned) may hold
+ * float16 weights, 2^-22 of the row's largest; what an infinity takes part in is an infinity or
+ * a NaN, whichever the formula has.  Results do not depend on how a launch is scheduled, nor a row's on other rows' values.  The workspace (16-byte aligned) may hold
  * anything, before and after; its bytes: for calls with a plan, or without. */
 size_t bitlogic_adapters_workspace_bytes(const bitlogic_adapter_set *set, int64_t n_rows,
                                          int32_t planned);

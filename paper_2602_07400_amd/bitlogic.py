@@ -834,7 +834,7 @@ def bitlogic_distill_loss(logits: torch.Tensor, top_values: torch.Tensor,
                           top_temperature: float = 1.0) -> torch.Tensor:
     """bitlogic_distill as a differentiable function: loss float32 [N] whose backward
     pass gives the gradient with respect to logits (the teacher's side has none).  Both
-    passes run on the current stream."""
+    passes run on the current stream (captured into a graph: see bitlogic_adapt)."""
     return _DistillLoss.apply(logits, top_values, top_indices, top_log_norm, temperature,
                               top_temperature)
 
@@ -1036,7 +1036,8 @@ def bitlogic_dropout(x: torch.Tensor, p: float, seed: int, offset=0,
     float32; rows may be strided) with probability p, by a mask that (seed, offset) alone
     decide and that is never stored.  offset is a number or an int64 tensor [1] on the GPU,
     which a captured graph reads at every replay.  Differentiable (backward) in a float x where
-    neither out (which may be x) nor stream is given; both passes run on the current stream."""
+    neither out (which may be x) nor stream is given; both passes run on the current stream
+    (captured into a graph: see bitlogic_adapt)."""
     if out is None and stream is None and isinstance(x, torch.Tensor) and (
             (x.requires_grad and torch.is_grad_enabled()) or _has_tangent(x)):
         return _Dropout.apply(x, p, seed, offset)
@@ -1255,9 +1256,14 @@ def bitlogic_adapt(x: torch.Tensor, down: torch.Tensor, up: torch.Tensor,
                    base: Optional[torch.Tensor] = None, base_scale: float = 1.0,
                    plan: Optional[RowGroups] = None) -> torch.Tensor:
     """bitlogic_adapters' out as a differentiable function of x, down, up and base (scales
-    have no gradient).  Both passes run on the current stream.  For a training step in a
-    captured graph call bitlogic_adapters and bitlogic_adapters_backward: autograd ends the
-    process where a backward pass is captured while an eager graph of the same leaves lives."""
+    have no gradient).  Both passes run on the current stream.  A plan must not be written again
+    before the backward pass.
+
+    For a training step in a captured graph call bitlogic_adapters and
+    bitlogic_adapters_backward (bitlogic_distill, bitlogic_dropout on the gradient): autograd,
+    whichever functions the graph is made of, ends the process where a backward pass is captured
+    while an eager graph of the same leaves lives.  Nothing tells here whether one does; leaves
+    that no eager graph has seen, or whose eager graphs are all gone, can be captured."""
     return _Adapt.apply(x, down, up, base, ids, scales, base_scale, plan)
 
 

@@ -8,10 +8,11 @@
 // byte; what they cost is that p is one of 2^16 + 1 values, and the factor of the elements
 // that stay is the exact reciprocal of that value's complement, so the mean is unbiased.
 //
-// Memory bounds it: a copy's bytes.  16384 x 8192 in bf16 takes 95 us where torch's copy of
-// it takes 101, 2^18 x 100 counts 35 us where their copy as float takes 47; with one round
-// for ten 88 and 33 us, so the products hide behind the loads.  Lanes of eight elements load
-// and store 16 or 32 bytes.
+// Memory bounds it: a copy's bytes.  16384 x 8192 in bf16 takes 99 us where torch's copy of
+// it takes 100, 2^18 x 100 counts 49 us where their copy as float takes 67 (42 where they are in
+// the caches); with one round for ten 88 and 49 us, so the products mostly hide behind the
+// loads.  In odd rows, 16381 x 8191, they show: 103 to 145 us, with one round 95 to 101.  Lanes of
+// eight elements load and store 16 or 32 bytes.
 #include "logit_rows.h"
 
 namespace bl {

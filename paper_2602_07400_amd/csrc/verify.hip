@@ -7,10 +7,11 @@
 // where all stand, from the target's row behind them: the largest log(mass) + Gumbel number.
 //
 // A row's part in a decision is a reference m, at or just above its largest logit, and the sum s
-// of its exponentials relative to it, one pass over the row.  Sums are 32-bit terms in 64-bit totals, and the quotient of two is good to
-// kLoose of itself; everything behind them is a handful of values a request and taken in 64 bits.
-// A decision that kLoose could turn is taken again with sums in 64 bits (about one draft in
-// 10^5), so accepted drafts and classes are those of 64-bit arithmetic.
+// of its exponentials relative to it, one pass over the row.  Sums are 32-bit terms in 64-bit
+// totals, and the quotient of two is good to kLoose of itself; everything behind them is a
+// handful of values a request and taken in 64 bits.  A decision that kLoose could turn is taken
+// again with sums in 64 bits (about one draft in 10^5), so accepted drafts and classes are
+// those of 64-bit arithmetic.
 //
 // Draws: p - q = p (1 - e^delta) with delta = log q - log p in 64 bits, since the difference
 // of two roundings would decide where p and q are close.  The mass is at most p, so a class
@@ -34,8 +35,8 @@ using namespace rows;
 
 // A lane's reference is set kLead binary orders above its largest logit, and set anew, with its sum
 // multiplied to be relative to it, where a logit is above it: every 2.8 (in powers of e).  With
-// the largest itself as reference, the sum of an ascending row is multiplied with every load,
-// and the roundings of equal steps add up (2^22 ascending classes: a quotient off by more than 3e-5).
+// the largest itself as reference, the sum of an ascending row is multiplied with every load, and
+// the roundings of equal steps add up (2^22 ascending classes: a quotient off by up to 4e-5).
 // What a sum is off by, in shares of itself:
 //   exponents: three roundings of 2^-24 of each difference on the way of a term from its logit
 //   to the row's reference, X + 5.6 in powers of e (a reference that is rounded may be twice as far
